@@ -50,13 +50,15 @@ extern "C" {
 #endif
 
 typedef struct skv_cache skv_cache; /* opaque host-side handle */
+typedef struct skv_rope skv_rope;   /* opaque host-side description of a rotary embedding */
 
 typedef enum skv_status {
     SKV_OK = 0,
     SKV_ERR_ARG = -1,         /* null pointer, non-positive size, misaligned buffer */
     SKV_ERR_ROUTING = -2,     /* r[0] != 0, r[l] > l, r[l] < 0 or r[r[l]] != r[l] */
     SKV_ERR_UNSUPPORTED = -3, /* shape outside the supported set */
-    SKV_ERR_NOMEM = -4,       /* caller's pool or workspace is too small */
+    SKV_ERR_NOMEM = -4,       /* caller's pool or workspace is too small; device status: skv_plan_step
+                               * refused a request, skv_plan_release found no room */
     SKV_ERR_LAYER = -5,       /* layer index out of range, or an owner is required */
     SKV_ERR_CUDA = -6,        /* a CUDA runtime call failed (no device, bad stream, ...) */
     SKV_ERR_TIMEOUT = -7,     /* device status: a bounded wait inside a kernel ran out */
@@ -187,6 +189,96 @@ int skv_gather(skv_cache *cache, int layer, const int64_t *slot_ids, int64_t n, 
 int skv_gather_fp8(skv_cache *cache, int layer, const int64_t *slot_ids, int64_t n, void *K_codes,
                    void *V_codes, float *K_scales, float *V_scales, void *stream);
 
+/* ---- rotary embedding with the update -------------------------------------- */
+
+/* Describes a rotary position embedding: frequency i (of rotary_dim / 2) turns the
+ * pair (x1, x2) of a head's row by  angle = position * inv_freq[i]:
+ *   x1' = x1 cos - x2 sin,   x2' = x2 cos + x1 sin.
+ *   rotary_dim  the head's leading dims that are turned, a multiple of 16, at most
+ *               the head_dim of the caches it is used with; the others are copied
+ *   inv_freq    host, rotary_dim / 2 values, radians per position (any scaling of
+ *               the frequencies is the caller's), finite and at most 1e6 in size
+ *   axis        host, rotary_dim / 2 entries in [0, n_axes): which position of a
+ *               token turns frequency i (time, height, width of an image or video
+ *               token, in any arrangement); NULL: all frequencies take axis 0
+ *   n_axes      positions per token, 1 to 255
+ *   adjacent_pairs  0: pairs (i, i + rotary_dim / 2); 1: pairs (2i, 2i + 1)
+ * Pure host; the description is copied into each launch.  Errors: SKV_ERR_ARG,
+ * SKV_ERR_UNSUPPORTED (rotary_dim, n_axes), SKV_ERR_NOMEM. */
+int skv_rope_create(skv_rope **out, int rotary_dim, const double *inv_freq, const int32_t *axis, int n_axes,
+                    int adjacent_pairs);
+void skv_rope_destroy(skv_rope *rope);
+
+/* Turns the queries and keys of n_tokens new tokens and stores K,V in `layer`'s
+ * cache, in one launch: Q_out = rope(Q), and what skv_append(rope(K), V) does.  On a
+ * layer that is not an owner only the queries are turned and K, V, slot_map may
+ * be NULL.
+ *   Q, Q_out   device bf16, rows of [q_heads][head_dim], row t at  t * stride
+ *              elements; Q_out may be Q (with the same stride) but must not overlap
+ *              it otherwise.  q_heads 0: no queries (Q, Q_out may be NULL)
+ *   K, V       device bf16, rows of [kv_heads][head_dim], row strides in elements
+ *              (a fused projection's rows can be given as they are); not changed
+ *   positions  device int32 [n_axes][pos_stride], pos_stride >= n_tokens: the
+ *              token's position on every axis.  Any value; the angle is exact to
+ *              2^-31 of a turn at every one of them
+ *   slot_map   as in skv_append (negative: the token's K,V are not stored; its
+ *              query is turned all the same)
+ * Pointers 16-byte aligned, strides multiples of 8 elements and at least a row.
+ * Arithmetic in fp32, rounded once to bf16 (nearest even); V and dims that are not
+ * turned are copied bit for bit.  On FP8 pages the turned fp32 row is quantised
+ * as skv_append quantises (its maximum sets the scale).
+ * Errors: SKV_ERR_ARG, SKV_ERR_LAYER, SKV_ERR_UNSUPPORTED (rotary_dim above
+ * head_dim), SKV_ERR_CUDA; slots out of range as in skv_append. */
+int skv_rope_append(skv_cache *cache, int layer, const skv_rope *rope, const void *Q, int64_t q_stride,
+                    void *Q_out, int64_t q_out_stride, const void *K, int64_t k_stride, const void *V,
+                    int64_t v_stride, const int32_t *positions, int64_t pos_stride,
+                    const int64_t *slot_map, int64_t n_tokens, int q_heads, void *stream);
+
+/* ---- a step's tables, on the device ---------------------------------------- */
+
+/* Page table entries, slot map, positions, row offsets and lengths of a step, from
+ * the requests' lengths, without the host: request b has seq_lens[b] tokens cached
+ * and wants to add new_lens[b] (negative values count as 0).  The pages it needs
+ * beyond those it has, need_b = ceil((n + a) / 16) - ceil(n / 16), come off a stack of
+ * free page ids (top: free_pages[*n_free - 1]), in request order, lowest page first.
+ * A request is ADMITTED if
+ *   - need_b is 0 or the need of requests 0..b together is at most *n_free,
+ *   - the new tokens of requests 0..b together are at most max_tokens, and
+ *   - n + a fits a page-table row (and 31 bits)
+ * (the sums count every request, admitted or not).  One that is not adds no token
+ * in this step, takes no page, and raises SKV_ERR_NOMEM (SKV_ERR_BOUNDS for the last
+ * condition) in the device status; the caller sees it by its unchanged length.
+ *   page_table    device int32 [batch][pt_stride]: entries of new pages are written
+ *   free_pages    device int32 [free_capacity], not changed;  n_free device int32 [1]
+ *   slot_map      device int64 [max_tokens]: the admitted requests' new tokens, in
+ *                 request order (skv_append's slot_map); behind the last one it is
+ *                 left as it was.  A page id out of range gives slot -1 and
+ *                 SKV_ERR_BOUNDS in the device status
+ *   positions     device int32 [max_tokens], or NULL: index of each token in its sequence
+ *   cu_q_lens     device int32 [batch + 1]: prefix sums of the admitted new tokens
+ *                 (skv_prefill_attn's cu_q_lens)
+ *   seq_lens_out  device int32 [batch]: lengths after the step; may be seq_lens
+ *   n_free_out    device int32 [1]: pages left on the stack; may be n_free
+ * Other buffers must not overlap.  One launch.  batch at most 16384
+ * (SKV_ERR_UNSUPPORTED), max_tokens below 2^31.  Errors: SKV_ERR_ARG, SKV_ERR_CUDA. */
+int skv_plan_step(skv_cache *cache, int32_t *page_table, int pt_stride, const int32_t *seq_lens,
+                  const int32_t *new_lens, int batch, const int32_t *free_pages, int free_capacity,
+                  const int32_t *n_free, int64_t max_tokens, int64_t *slot_map, int32_t *positions,
+                  int32_t *cu_q_lens, int32_t *seq_lens_out, int32_t *n_free_out, void *stream);
+
+/* The way back: entries [first_page[b], end_page[b]) of every page-table row (cut to
+ * the row; an empty range leaves it alone) that hold a page are pushed onto the
+ * stack, in row order, and become -1; entries that are negative are skipped, ids
+ * beyond the pool are left and raise SKV_ERR_BOUNDS.  A finished request gives all its
+ * pages back; a request with a sliding window those its window has left.  Pages
+ * beyond free_capacity stay in the table and raise SKV_ERR_NOMEM.
+ *   first_page, end_page  device int32 [batch]
+ *   n_free, n_free_out    device int32 [1]; may be the same
+ * One launch.  Limits and errors as skv_plan_step. */
+int skv_plan_release(skv_cache *cache, int32_t *page_table, int pt_stride, const int32_t *first_page,
+                     const int32_t *end_page, int batch, int32_t *free_pages, int free_capacity,
+                     const int32_t *n_free, int32_t *n_free_out, void *stream);
+
 /* ---- Algorithm 2 "Load + Attn": decode attention -------------------------- */
 
 /* Bytes of device workspace skv_decode_attn needs for this batch / head count
@@ -268,6 +360,21 @@ int skv_decode_attn_static(skv_cache *cache, int layer, const void *Q, const int
                            const int32_t *seq_lens, void *out, int batch, int q_heads, int pt_stride,
                            float scale, void *stream);
 
+/* skv_decode_attn over a sliding window with sinks: of the n = seq_lens[b] cached
+ * tokens, the newest `window` and the first `sinks` are attended,
+ *   t >= n - window   or   t < sinks,
+ * each once (n <= window + sinks: all of them, as skv_decode_attn).  window >= 1, sinks
+ * >= 0.  Pages that hold no such token are not touched and their page-table entries
+ * not read, so they may have been given back (skv_plan_release); other tokens of the
+ * pages that are read contribute nothing, whatever they hold.
+ * Other arguments, workspace, status and errors as skv_decode_attn.  Runs the
+ * CTA-per-range kernel whatever skv_set_decode_worker (mode 1) and
+ * skv_set_decode_variant (FP8: always the mma.sync arithmetic) say. */
+int skv_decode_attn_window(skv_cache *cache, int layer, const void *Q, const int32_t *page_table,
+                           const int32_t *seq_lens, void *out, int batch, int q_heads, int pt_stride,
+                           int window, int sinks, float scale, void *workspace, size_t workspace_bytes,
+                           void *stream);
+
 /* The two launches of skv_decode_attn separately (profiling, sequence-sharded
  * use): the split-K pass fills `workspace` with partials; the merge kernel
  * turns the partials in `workspace` into `out`.  Same arguments and errors. */
@@ -313,6 +420,18 @@ int skv_prefill_attn(skv_cache *cache, int layer, const void *Q, const int32_t *
 int skv_prefill_attn_src(skv_cache *cache, int src_layer, const void *Q, const int32_t *cu_q_lens,
                          const int32_t *page_table, const int32_t *seq_lens, void *out, int batch,
                          int max_q_len, int q_heads, int pt_stride, float scale, void *stream);
+
+/* skv_prefill_attn over a sliding window with sinks: the row at position pos attends
+ *   t <= pos  and  (t > pos - window  or  t < sinks);
+ * window >= 1 (a row always sees itself), sinks >= 0.  Pages that no row of a sequence
+ * sees are not touched and their page-table entries not read.  A token that no row
+ * of a sequence's call sees contributes nothing, whatever it holds; one that some rows
+ * see should be finite, as its V may be multiplied by the zero weight of another row.
+ * Other arguments, status and errors as skv_prefill_attn. */
+int skv_prefill_attn_window(skv_cache *cache, int layer, const void *Q, const int32_t *cu_q_lens,
+                            const int32_t *page_table, const int32_t *seq_lens, void *out, int batch,
+                            int max_q_len, int q_heads, int pt_stride, int window, int sinks,
+                            float scale, void *stream);
 
 /* Pre-fill on an FP8 cache through the bf16 tensor-core kernel.  Given a scratch
  * area of skv_prefill_scratch_bytes (room for the pages of ONE owner layer as
@@ -377,7 +496,8 @@ int skv_decode_step_host(skv_cache *cache, const void *hQ, const void *hK, const
 /* ---- status, tuning, counters ------------------------------------------- */
 
 /* Synchronises `stream`, reads and clears the device status word.
- * *device_status receives SKV_OK, SKV_ERR_TIMEOUT or SKV_ERR_BOUNDS. */
+ * *device_status receives SKV_OK, SKV_ERR_TIMEOUT, SKV_ERR_BOUNDS or SKV_ERR_NOMEM
+ * (the first of them in this order that was raised). */
 int skv_get_status(skv_cache *cache, void *stream, int *device_status);
 
 /* Split-K kernel variant: 0 = automatic (CUDA-core kernel when

@@ -64,6 +64,14 @@ lib.skv_decode_attn.argtypes = [_vp, _int, _vp, _i32p, _i32p, _vp, _int, _int, _
 lib.skv_decode_attn_static.argtypes = [_vp, _int, _vp, _i32p, _i32p, _vp, _int, _int, _int, _f32, _vp]
 lib.skv_prefill_attn.argtypes = [_vp, _int, _vp, _i32p, _i32p, _i32p, _vp, _int, _int, _int, _int, _f32, _vp]
 lib.skv_prefill_attn_src.argtypes = [_vp, _int, _vp, _i32p, _i32p, _i32p, _vp, _int, _int, _int, _int, _f32, _vp]
+lib.skv_rope_create.argtypes = [ctypes.POINTER(_vp), _int, _vp, _vp, _int, _int]
+lib.skv_rope_destroy.restype = None
+lib.skv_rope_destroy.argtypes = [_vp]
+lib.skv_rope_append.argtypes = [_vp, _int, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i32p, _i64, _i64p, _i64, _int, _vp]
+lib.skv_plan_step.argtypes = [_vp, _i32p, _int, _i32p, _i32p, _int, _i32p, _int, _i32p, _i64, _i64p, _i32p, _i32p, _i32p, _i32p, _vp]
+lib.skv_plan_release.argtypes = [_vp, _i32p, _int, _i32p, _i32p, _int, _i32p, _int, _i32p, _i32p, _vp]
+lib.skv_decode_attn_window.argtypes = [_vp, _int, _vp, _i32p, _i32p, _vp, _int, _int, _int, _int, _int, _f32, _vp, _sz, _vp]
+lib.skv_prefill_attn_window.argtypes = [_vp, _int, _vp, _i32p, _i32p, _i32p, _vp, _int, _int, _int, _int, _int, _int, _f32, _vp]
 lib.skv_decode_splitk.argtypes = [_vp, _int, _vp, _i32p, _i32p, _int, _int, _int, _f32, _vp, _sz, _vp]
 lib.skv_decode_merge.argtypes = [_vp, _vp, _int, _int, _vp, _sz, _vp]
 lib.skv_decode_step.argtypes = [_vp, _vp, _vp, _vp, _i64p, _i32p, _i32p, _vp, _int, _int, _int, _f32, _vp, _sz, _vp]
@@ -206,8 +214,61 @@ def _arg(name: str, t: Optional[torch.Tensor], dtype, shape=None, min_numel: Opt
     return t
 
 
+def _i32(name: str, x: int) -> int:
+    """ctypes cuts an int to its low 32 bits without a word."""
+    if not -(1 << 31) <= x < (1 << 31):
+        raise ValueError(f"{name}: {x} is not a 32-bit integer")
+    return x
+
+
 def _nbytes(t: torch.Tensor) -> int:
     return t.numel() * t.element_size()
+
+
+def _rows(name: str, t: Optional[torch.Tensor], shape) -> Optional[torch.Tensor]:
+    """Checks bf16 rows [n][heads][dim] on the device whose heads are dense and whose rows may be further apart
+    (a slice of a fused projection)."""
+    if t is None:
+        return None
+    if t.dtype != torch.bfloat16:
+        raise TypeError(f"{name}: expected {torch.bfloat16}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: expected a CUDA tensor")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    n, heads, dim = shape
+    if n and heads and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim) or (n > 1 and t.stride(0) < heads * dim)):
+        raise ValueError(f"{name}: the rows' heads must be dense")
+    return t
+
+
+def _row_stride(t: Optional[torch.Tensor]) -> int:
+    """Elements from row to row; a single row's stride says nothing and may not even be a row long."""
+    if t is None:
+        return 0
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+class SkvRope:
+    """Handle of a rotary embedding: ``inv_freq`` radians per position of every frequency (half the rotary dims),
+    ``axis`` which of the ``n_axes`` positions of a token turns it (None: the first)."""
+
+    def __init__(self, inv_freq: Sequence[float], axis: Optional[Sequence[int]] = None, n_axes: int = 1,
+                 adjacent_pairs: bool = False):
+        inv_freq = [float(x) for x in inv_freq]
+        if axis is not None and len(axis) != len(inv_freq):
+            raise ValueError(f"axis: expected {len(inv_freq)} entries, got {len(axis)}")
+        self.rotary_dim, self.n_axes = 2 * len(inv_freq), n_axes
+        self._h = _vp()
+        _check(lib.skv_rope_create(ctypes.byref(self._h), self.rotary_dim, _f64_array(inv_freq),
+                                   None if axis is None else _i32_array(axis), n_axes, int(bool(adjacent_pairs))), "skv_rope_create")
+
+    def close(self):
+        if getattr(self, "_h", None):
+            lib.skv_rope_destroy(self._h)
+            self._h = None
+
+    __del__ = close
 
 
 class SkvCache:
@@ -298,6 +359,89 @@ class SkvCache:
                                 _ptr(K_scales), _ptr(V_scales), _stream_ptr(stream))
         _check(rc, "skv_gather_fp8")
 
+    def skv_rope_append(self, layer: int, rope: SkvRope, Q: Optional[torch.Tensor], Q_out: Optional[torch.Tensor],
+                        K: Optional[torch.Tensor], V: Optional[torch.Tensor], positions: torch.Tensor,
+                        slot_map: Optional[torch.Tensor], stream=None) -> None:
+        """Q, Q_out [n][q_heads][head_dim], K, V [n][kv_heads][head_dim] with any row stride; positions [n] or
+        [n_axes][n] int32; slot_map [n] int64.  On a layer that is not an owner K, V, slot_map are not used."""
+        self._on_current_device(Q, Q_out, K, V, positions, slot_map)
+        n = positions.shape[-1]
+        q_heads = 0 if Q is None else Q.shape[1]
+        _rows("Q", Q, (n, q_heads, self.head_dim))
+        _rows("Q_out", Q_out, (n, q_heads, self.head_dim))
+        if (Q is None) != (Q_out is None):
+            raise ValueError("Q and Q_out go together")
+        if positions.dtype != torch.int32 or not positions.is_cuda:
+            raise TypeError("positions: expected an int32 CUDA tensor")
+        axes = 1 if positions.dim() == 1 else positions.shape[0]
+        if positions.dim() not in (1, 2) or axes != rope.n_axes or (n > 1 and positions.stride(-1) != 1):
+            raise ValueError(f"positions: expected [{rope.n_axes}][n] with dense rows, got {tuple(positions.shape)}")
+        pos_stride = positions.stride(0) if axes > 1 else n
+        if 0 <= layer < self.n_layers and self.r[layer] == layer:
+            _rows("K", K, (n, self.kv_heads, self.head_dim))
+            _rows("V", V, (n, self.kv_heads, self.head_dim))
+            _arg("slot_map", slot_map, torch.int64, (n,))
+        else:
+            K = V = slot_map = None
+        rc = lib.skv_rope_append(self._h, layer, rope._h, _ptr(Q), _row_stride(Q), _ptr(Q_out), _row_stride(Q_out), _ptr(K),
+                                 _row_stride(K), _ptr(V), _row_stride(V), _ptr(positions), pos_stride, _ptr(slot_map), n,
+                                 q_heads, _stream_ptr(stream))
+        _check(rc, "skv_rope_append")
+
+    # -- a step's tables
+    def skv_plan_step(self, page_table: torch.Tensor, seq_lens: torch.Tensor, new_lens: torch.Tensor,
+                      free_pages: torch.Tensor, n_free: torch.Tensor, slot_map: torch.Tensor, cu_q_lens: torch.Tensor,
+                      seq_lens_out: torch.Tensor, n_free_out: torch.Tensor, positions: Optional[torch.Tensor] = None,
+                      stream=None) -> None:
+        """page_table [batch][width], seq_lens, new_lens, seq_lens_out [batch], free_pages [capacity], n_free, n_free_out [1],
+        cu_q_lens [batch+1], positions [max_tokens]: int32; slot_map [max_tokens]: int64."""
+        self._on_current_device(page_table, seq_lens, new_lens, free_pages, n_free, slot_map, cu_q_lens, seq_lens_out, n_free_out, positions)
+        _arg("seq_lens", seq_lens, torch.int32)
+        if seq_lens.dim() != 1:
+            raise ValueError("seq_lens: expected [batch]")
+        batch, i32 = seq_lens.shape[0], torch.int32
+        _arg("page_table", page_table, i32)
+        if page_table.dim() != 2 or page_table.shape[0] != batch:
+            raise ValueError(f"page_table: expected [{batch}][width], got {tuple(page_table.shape)}")
+        _arg("new_lens", new_lens, i32, (batch,))
+        _arg("seq_lens_out", seq_lens_out, i32, (batch,))
+        _arg("cu_q_lens", cu_q_lens, i32, (batch + 1,))
+        _arg("free_pages", free_pages, i32)
+        _arg("n_free", n_free, i32, (1,))
+        _arg("n_free_out", n_free_out, i32, (1,))
+        _arg("slot_map", slot_map, torch.int64)
+        _arg("positions", positions, i32, min_numel=slot_map.numel())
+        rc = lib.skv_plan_step(self._h, _ptr(page_table), page_table.shape[1], _ptr(seq_lens), _ptr(new_lens), batch,
+                               _ptr(free_pages), free_pages.numel(), _ptr(n_free), slot_map.numel(), _ptr(slot_map),
+                               _ptr(positions), _ptr(cu_q_lens), _ptr(seq_lens_out), _ptr(n_free_out), _stream_ptr(stream))
+        _check(rc, "skv_plan_step")
+
+    def skv_plan_release(self, page_table: torch.Tensor, first_page: torch.Tensor, end_page: torch.Tensor,
+                         free_pages: torch.Tensor, n_free: torch.Tensor, n_free_out: torch.Tensor, stream=None) -> None:
+        self._on_current_device(page_table, first_page, end_page, free_pages, n_free, n_free_out)
+        _arg("page_table", page_table, torch.int32)
+        if page_table.dim() != 2:
+            raise ValueError(f"page_table: expected [batch][width], got {tuple(page_table.shape)}")
+        batch = page_table.shape[0]
+        _arg("first_page", first_page, torch.int32, (batch,))
+        _arg("end_page", end_page, torch.int32, (batch,))
+        _arg("free_pages", free_pages, torch.int32)
+        _arg("n_free", n_free, torch.int32, (1,))
+        _arg("n_free_out", n_free_out, torch.int32, (1,))
+        rc = lib.skv_plan_release(self._h, _ptr(page_table), page_table.shape[1], _ptr(first_page), _ptr(end_page), batch,
+                                  _ptr(free_pages), free_pages.numel(), _ptr(n_free), _ptr(n_free_out), _stream_ptr(stream))
+        _check(rc, "skv_plan_release")
+
+    def _on_current_device(self, *tensors: Optional[torch.Tensor]) -> None:
+        """Launches go to the current device: it has to be the pool's, and the tensors' (host tensors are told apart
+        by the checks that follow)."""
+        if self.pool is None:
+            return
+        device = torch.cuda.current_device()
+        for t in (self.pool,) + tensors:
+            if t is not None and t.is_cuda and t.get_device() != device:
+                raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{device}")
+
     # -- Load + Attn
     def _decode_args(self, Q, page_table, seq_lens, out):
         """Shapes of one decode-attention call: Q, out [batch][q_heads][head_dim] bf16; page_table
@@ -328,6 +472,17 @@ class SkvCache:
                                  q_heads, page_table.shape[1], scale, _ptr(workspace), _nbytes(workspace),
                                  _stream_ptr(stream))
         _check(rc, "skv_decode_attn")
+
+    def skv_decode_attn_window(self, layer: int, Q: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor,
+                               out: torch.Tensor, workspace: torch.Tensor, window: int, sinks: int = 0,
+                               scale: float = 0.0, stream=None) -> None:
+        self._on_current_device(Q, page_table, seq_lens, out, workspace)
+        batch, q_heads = self._decode_args(Q, page_table, seq_lens, out)
+        _arg("workspace", workspace, torch.uint8)
+        rc = lib.skv_decode_attn_window(self._h, layer, _ptr(Q), _ptr(page_table), _ptr(seq_lens), _ptr(out), batch,
+                                        q_heads, page_table.shape[1], _i32("window", window), _i32("sinks", sinks), scale,
+                                        _ptr(workspace), _nbytes(workspace), _stream_ptr(stream))
+        _check(rc, "skv_decode_attn_window")
 
     def skv_decode_attn_static(self, layer: int, Q: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor,
                                out: torch.Tensor, scale: float = 0.0, stream=None) -> None:
@@ -360,6 +515,16 @@ class SkvCache:
                                   _ptr(out), batch, max_q_len, q_heads, page_table.shape[1], scale,
                                   _stream_ptr(stream))
         _check(rc, "skv_prefill_attn")
+
+    def skv_prefill_attn_window(self, layer: int, Q: torch.Tensor, cu_q_lens: torch.Tensor, page_table: torch.Tensor,
+                                seq_lens: torch.Tensor, out: torch.Tensor, max_q_len: int, window: int, sinks: int = 0,
+                                scale: float = 0.0, stream=None) -> None:
+        self._on_current_device(Q, cu_q_lens, page_table, seq_lens, out)
+        batch, q_heads = self._prefill_args(Q, cu_q_lens, page_table, seq_lens, out)
+        rc = lib.skv_prefill_attn_window(self._h, layer, _ptr(Q), _ptr(cu_q_lens), _ptr(page_table), _ptr(seq_lens),
+                                         _ptr(out), batch, max_q_len, q_heads, page_table.shape[1], _i32("window", window),
+                                         _i32("sinks", sinks), scale, _stream_ptr(stream))
+        _check(rc, "skv_prefill_attn_window")
 
     def skv_prefill_attn_src(self, src_layer: int, Q: torch.Tensor, cu_q_lens: torch.Tensor, page_table: torch.Tensor,
                              seq_lens: torch.Tensor, out: torch.Tensor, max_q_len: int, scale: float = 0.0,

@@ -92,6 +92,13 @@ struct skv_cache {
     }
 };
 
+struct skv_rope {
+    int rotary_dim = 0, n_axes = 1;
+    bool adjacent = false;
+    uint64_t freq[64] = {};          // fraction of a turn per position, 2^64 = one turn
+    uint8_t axis[64] = {};
+};
+
 namespace {
 
 int check_routing(int n_layers, const int32_t *r)
@@ -542,7 +549,8 @@ struct SplitkPlan {
 // it, the CTA-per-range kernel may run, which finishes the segments that lie inside one range.
 int launch_splitk(skv_cache *c, int layer, const void *Q, const int32_t *page_table, const int32_t *seq_lens,
                   int batch, int q_heads, int pt_stride, float scale, void *workspace, size_t workspace_bytes,
-                  void *stream, SplitkPlan *plan, void *out = nullptr, int buf = 0, bool chained = false)
+                  void *stream, SplitkPlan *plan, void *out = nullptr, int buf = 0, bool chained = false,
+                  int window = 0, int sinks = 0)
 {
     int rc = check_decode_args(c, layer, batch, q_heads);
     if (rc) return rc;
@@ -553,11 +561,12 @@ int launch_splitk(skv_cache *c, int layer, const void *Q, const int32_t *page_ta
     const WorkspaceLayout wl = workspace_layout(c, batch, q_heads, n_workers_max(c));
     if (workspace_bytes < wl.total) return SKV_ERR_NOMEM;
     const bool tensor_core = c->fp8 || c->tune.variant == 2 || (c->tune.variant == 0 && G > 1);
-    const bool umma = fp8_on_umma(c) && decode_fp8_umma_supported(c->head_dim, G);
+    const bool umma = !window && fp8_on_umma(c) && decode_fp8_umma_supported(c->head_dim, G);
     // CTA per range: stand-alone calls whose result buffer is known (not the links of a chain, which overlap
     // by having many small CTAs; not the tcgen05 FP8 kernel, which has its own CTA-wide design)
     const int cta_S = cta_stages_for(c, batch, G);
-    const bool cta = !umma && !chained && out && c->worker_mode != 1 && cta_S > 0;
+    const bool cta = window ? cta_S > 0 : !umma && !chained && out && c->worker_mode != 1 && cta_S > 0;
+    if (window && !cta) return SKV_ERR_UNSUPPORTED;              // (the sliding window lives in the CTA-per-range kernel alone)
     // Default launch shapes of the warp-per-range kernel (8 warps per SM, two 8 KB stages each, many small
     // CTAs so that the CTAs of the next launch can move in one by one): 2 warps x 4 CTAs per SM for the
     // tensor-core kernel, 1 warp x 8 CTAs per SM for the CUDA-core kernel (measured best for each on B200).
@@ -609,6 +618,8 @@ int launch_splitk(skv_cache *c, int layer, const void *Q, const int32_t *page_ta
         if (c->walk_reverse[(size_t)layer]) p.flags |= DECODE_REVERSE;
         if (c->walk_keep[(size_t)layer]) p.keep_pct = c->l2_keep_pct;
     }
+    p.window = window;
+    p.sinks = sinks;
     p.status = c->status_word();
     const size_t trace_need = (size_t)W * (cta ? c->cta_consumers : 1) * 32;
     p.trace = (c->trace && c->trace_bytes >= trace_need) ? c->trace : nullptr;
@@ -697,6 +708,35 @@ int skv_decode_attn(skv_cache *c, int layer, const void *Q, const int32_t *page_
     if (rc) return rc;
     if (plan.merged) return SKV_OK;
     return launch_merge_on(c, out, batch, q_heads, workspace, workspace_bytes, stream, 0, &plan, seq_lens, pt_stride);
+}
+
+int skv_decode_attn_window(skv_cache *c, int layer, const void *Q, const int32_t *page_table, const int32_t *seq_lens,
+                           void *out, int batch, int q_heads, int pt_stride, int window, int sinks, float scale,
+                           void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!out || window < 1 || sinks < 0) return SKV_ERR_ARG;
+    const int rc0 = check_decode_args(c, layer, batch, q_heads);
+    if (rc0) return rc0;
+    if (!Q || !page_table || !seq_lens || !workspace || pt_stride <= 0) return SKV_ERR_ARG;
+    if (!aligned(Q, 16) || !aligned(workspace, 256) || !aligned(out, 8)) return SKV_ERR_ARG;
+    if (workspace_bytes < workspace_layout(c, batch, q_heads, n_workers_max(c)).total) return SKV_ERR_NOMEM;
+    // The kernel keeps two words per sequence in shared memory beside its ring: larger batches go in pieces.
+    constexpr int PIECE = 4096;
+    const size_t row = (size_t)q_heads * c->head_dim * 2;
+    for (int b = 0; b < batch; b += PIECE) {
+        const int n = batch - b < PIECE ? batch - b : PIECE;
+        const uint8_t *q = static_cast<const uint8_t *>(Q) + (size_t)b * row;
+        uint8_t *o = static_cast<uint8_t *>(out) + (size_t)b * row;
+        SplitkPlan plan;
+        int rc = launch_splitk(c, layer, q, page_table + (size_t)b * pt_stride, seq_lens + b, n, q_heads, pt_stride, scale,
+                               workspace, workspace_bytes, stream, &plan, o, 0, false, window, sinks);
+        if (rc) return rc;
+        if (plan.merged) continue;
+        // (the page counts the split-K launch left in the workspace: the lengths alone do not give them here)
+        rc = launch_merge_on(c, o, n, q_heads, workspace, workspace_bytes, stream, 0, &plan);
+        if (rc) return rc;
+    }
+    return SKV_OK;
 }
 
 }  // extern "C"
@@ -810,6 +850,158 @@ int skv_decode_step(skv_cache *c, const void *Q, const void *K, const void *V, c
                        batch, q_heads, pt_stride, scale, workspace, workspace_bytes, stream, batched);
 }
 
+// ---- rotary embedding with the update ------------------------------------------
+int skv_rope_create(skv_rope **out, int rotary_dim, const double *inv_freq, const int32_t *axis, int n_axes, int adjacent_pairs)
+{
+    if (!out) return SKV_ERR_ARG;
+    *out = nullptr;
+    if (!inv_freq || rotary_dim <= 0 || n_axes < 1 || adjacent_pairs < 0 || adjacent_pairs > 1) return SKV_ERR_ARG;
+    if (rotary_dim % 16 != 0 || rotary_dim > 128 || n_axes > 255) return SKV_ERR_UNSUPPORTED;
+    for (int i = 0; i < rotary_dim / 2; ++i) {
+        if (!(fabs(inv_freq[i]) <= 1e6)) return SKV_ERR_ARG;             // (NaN and infinities too)
+        if (axis && (axis[i] < 0 || axis[i] >= n_axes)) return SKV_ERR_ARG;
+    }
+    skv_rope *r = new (std::nothrow) skv_rope;
+    if (!r) return SKV_ERR_NOMEM;
+    r->rotary_dim = rotary_dim;
+    r->n_axes = n_axes;
+    r->adjacent = adjacent_pairs != 0;
+    for (int i = 0; i < rotary_dim / 2; ++i) {
+        // turns per position; only the fraction matters.  An extended-precision quotient is off by under 2^-62 of a
+        // turn, by under 2^-31 at the furthest position.
+        const long double turns = (long double)inv_freq[i] / 6.283185307179586476925286766559L;
+        const long double part = turns - floorl(turns);
+        r->freq[i] = part >= 1.0L ? 0 : (uint64_t)(part * 18446744073709551616.0L);
+        r->axis[i] = (uint8_t)(axis ? axis[i] : 0);
+    }
+    *out = r;
+    return SKV_OK;
+}
+
+void skv_rope_destroy(skv_rope *r) { delete r; }
+
+int skv_rope_append(skv_cache *c, int layer, const skv_rope *rope, const void *Q, int64_t q_stride, void *Q_out,
+                    int64_t q_out_stride, const void *K, int64_t k_stride, const void *V, int64_t v_stride,
+                    const int32_t *positions, int64_t pos_stride, const int64_t *slot_map, int64_t n_tokens,
+                    int q_heads, void *stream)
+{
+    if (!c || !c->pool || !rope) return SKV_ERR_ARG;
+    if (layer < 0 || layer >= c->n_layers) return SKV_ERR_LAYER;
+    if (n_tokens < 0 || q_heads < 0) return SKV_ERR_ARG;
+    if (rope->rotary_dim > c->head_dim) return SKV_ERR_UNSUPPORTED;
+    const bool owner = c->slot[(size_t)layer] >= 0;
+    if (n_tokens == 0 || (q_heads == 0 && !owner)) return SKV_OK;
+    const int64_t q_row = (int64_t)q_heads * c->head_dim, kv_row = (int64_t)c->kv_heads * c->head_dim;
+    if (!positions || pos_stride < n_tokens) return SKV_ERR_ARG;
+    if (q_heads > 0 && (!Q || !Q_out || !aligned(Q, 16) || !aligned(Q_out, 16) || q_stride < q_row || q_out_stride < q_row ||
+                        q_stride % 8 != 0 || q_out_stride % 8 != 0 || (Q == Q_out && q_stride != q_out_stride)))
+        return SKV_ERR_ARG;
+    if (owner && (!K || !V || !slot_map || !aligned(K, 16) || !aligned(V, 16) || k_stride < kv_row || v_stride < kv_row ||
+                  k_stride % 8 != 0 || v_stride % 8 != 0))
+        return SKV_ERR_ARG;
+    RopeParams p;
+    memset(&p, 0, sizeof(p));
+    for (int i = 0; i < rope->rotary_dim / 2; ++i) {
+        p.freq[i] = rope->freq[i];
+        p.axis[i] = rope->axis[i];
+    }
+    p.positions = positions;
+    p.pos_stride = pos_stride;
+    p.Q = static_cast<const uint16_t *>(Q);
+    p.Q_out = static_cast<uint16_t *>(Q_out);
+    p.K = static_cast<const uint16_t *>(K);
+    p.V = static_cast<const uint16_t *>(V);
+    p.q_stride = q_stride;
+    p.qo_stride = q_out_stride;
+    p.k_stride = k_stride;
+    p.v_stride = v_stride;
+    p.layer_base = owner ? c->layer_base(c->slot[(size_t)layer]) : nullptr;
+    p.slot_map = slot_map;
+    p.n_tokens = n_tokens;
+    p.n_slots = c->max_pages * PAGE;
+    p.page_stride = (int64_t)c->page_bytes;
+    p.Hq = q_heads;
+    p.Hkv = owner ? c->kv_heads : 0;
+    p.rotary_dim = rope->rotary_dim;
+    p.status = c->status_word();
+    // few tokens: their heads are dealt to several warps, until there are 8 warps for every SM or 4 heads for a warp
+    const int tok = 32 / (c->head_dim / 16), heads = p.Hq + 2 * p.Hkv;
+    const int64_t groups = (n_tokens + tok - 1) / tok, want = ((int64_t)c->sm_count * 8 + groups - 1) / groups;
+    const int most = (heads + 3) / 4;
+    p.head_parts = want < 1 ? 1 : want > most ? most : (int)want;
+    if (launch_rope_append(p, c->head_dim, c->fp8, rope->adjacent, c->tune.pdl != 0, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return SKV_ERR_CUDA;
+    }
+    c->launches += 1;
+    return SKV_OK;
+}
+
+// ---- a step's tables -------------------------------------------------------------
+int skv_plan_step(skv_cache *c, int32_t *page_table, int pt_stride, const int32_t *seq_lens, const int32_t *new_lens,
+                  int batch, const int32_t *free_pages, int free_capacity, const int32_t *n_free, int64_t max_tokens,
+                  int64_t *slot_map, int32_t *positions, int32_t *cu_q_lens, int32_t *seq_lens_out,
+                  int32_t *n_free_out, void *stream)
+{
+    if (!c || !c->pool) return SKV_ERR_ARG;
+    if (batch <= 0 || pt_stride <= 0 || free_capacity < 0 || max_tokens < 0 || max_tokens > 0x7FFFFFFFll) return SKV_ERR_ARG;
+    if (!page_table || !seq_lens || !new_lens || !n_free || !cu_q_lens || !seq_lens_out || !n_free_out) return SKV_ERR_ARG;
+    if ((max_tokens > 0 && !slot_map) || (free_capacity > 0 && !free_pages)) return SKV_ERR_ARG;
+    if (batch > plan_max_batch()) return SKV_ERR_UNSUPPORTED;
+    PlanParams p;
+    p.page_table = page_table;
+    p.pt_stride = pt_stride;
+    p.seq_lens = seq_lens;
+    p.new_lens = new_lens;
+    p.B = batch;
+    p.free_pages = free_pages;
+    p.free_capacity = free_capacity;
+    p.n_free = n_free;
+    p.max_tokens = max_tokens;
+    p.max_pages = c->max_pages;
+    p.slot_map = slot_map;
+    p.positions = positions;
+    p.cu_q_lens = cu_q_lens;
+    p.seq_lens_out = seq_lens_out;
+    p.n_free_out = n_free_out;
+    p.status = c->status_word();
+    const bool in_place = seq_lens_out == seq_lens || n_free_out == n_free;
+    if (launch_plan_step(p, in_place, c->sm_count, c->tune.pdl != 0, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return SKV_ERR_CUDA;
+    }
+    c->launches += 1;
+    return SKV_OK;
+}
+
+int skv_plan_release(skv_cache *c, int32_t *page_table, int pt_stride, const int32_t *first_page, const int32_t *end_page,
+                     int batch, int32_t *free_pages, int free_capacity, const int32_t *n_free, int32_t *n_free_out,
+                     void *stream)
+{
+    if (!c || !c->pool) return SKV_ERR_ARG;
+    if (batch <= 0 || pt_stride <= 0 || free_capacity < 0) return SKV_ERR_ARG;
+    if (!page_table || !first_page || !end_page || !n_free || !n_free_out || (free_capacity > 0 && !free_pages)) return SKV_ERR_ARG;
+    if (batch > plan_max_batch()) return SKV_ERR_UNSUPPORTED;
+    ReleaseParams p;
+    p.page_table = page_table;
+    p.pt_stride = pt_stride;
+    p.first_page = first_page;
+    p.end_page = end_page;
+    p.B = batch;
+    p.free_pages = free_pages;
+    p.free_capacity = free_capacity;
+    p.n_free = n_free;
+    p.n_free_out = n_free_out;
+    p.max_pages = c->max_pages;
+    p.status = c->status_word();
+    if (launch_plan_release(p, c->tune.pdl != 0, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return SKV_ERR_CUDA;
+    }
+    c->launches += 1;
+    return SKV_OK;
+}
+
 // ---- pre-fill attention -------------------------------------------------------
 }  // extern "C"
 
@@ -817,7 +1009,7 @@ namespace {
 // pre-fill attention over the pages of owner layer `src` (already resolved and checked)
 int prefill_over(skv_cache *c, int src, const void *Q, const int32_t *cu_q_lens, const int32_t *page_table,
                  const int32_t *seq_lens, void *out, int batch, int max_q_len, int q_heads, int pt_stride,
-                 float scale, void *stream);
+                 float scale, void *stream, int window = 0, int sinks = 0);
 }  // namespace
 
 extern "C" {
@@ -843,12 +1035,23 @@ int skv_prefill_attn_src(skv_cache *c, int src_layer, const void *Q, const int32
                         scale, stream);
 }
 
+int skv_prefill_attn_window(skv_cache *c, int layer, const void *Q, const int32_t *cu_q_lens, const int32_t *page_table,
+                            const int32_t *seq_lens, void *out, int batch, int max_q_len, int q_heads, int pt_stride,
+                            int window, int sinks, float scale, void *stream)
+{
+    if (window < 1 || sinks < 0) return SKV_ERR_ARG;
+    const int rc = check_decode_args(c, layer, batch, q_heads);
+    if (rc) return rc;
+    return prefill_over(c, c->r[(size_t)layer], Q, cu_q_lens, page_table, seq_lens, out, batch, max_q_len, q_heads,
+                        pt_stride, scale, stream, window, sinks);
+}
+
 }  // extern "C"
 
 namespace {
 int prefill_over(skv_cache *c, int src, const void *Q, const int32_t *cu_q_lens, const int32_t *page_table,
                  const int32_t *seq_lens, void *out, int batch, int max_q_len, int q_heads, int pt_stride,
-                 float scale, void *stream)
+                 float scale, void *stream, int window, int sinks)
 {
     if (!Q || !cu_q_lens || !page_table || !seq_lens || !out || pt_stride <= 0 || max_q_len <= 0) return SKV_ERR_ARG;
     if (!aligned(Q, 4) || !aligned(out, 4)) return SKV_ERR_ARG;
@@ -859,7 +1062,7 @@ int prefill_over(skv_cache *c, int src, const void *Q, const int32_t *cu_q_lens,
     // the codes on the way in
     const size_t bf16_page = page_bytes_of(c->kv_heads, c->head_dim, false);
     const bool via_scratch = c->fp8 && c->prefill_scratch && c->prefill_scratch_bytes >= (size_t)c->max_pages * bf16_page;
-    const bool can_umma = (!c->fp8 || via_scratch) && prefill_umma_supported(c->head_dim, G) && aligned(Q, 16) && aligned(out, 16) &&
+    const bool can_umma = !window && (!c->fp8 || via_scratch) && prefill_umma_supported(c->head_dim, G) && aligned(Q, 16) && aligned(out, 16) &&
                           prefill_umma_smem_bytes(c->head_dim) <= (size_t)c->max_smem_optin;
     if (c->prefill_variant == 2 && !can_umma) return SKV_ERR_UNSUPPORTED;
     const bool umma = c->prefill_variant == 2 || (c->prefill_variant == 0 && can_umma);
@@ -881,6 +1084,8 @@ int prefill_over(skv_cache *c, int src, const void *Q, const int32_t *cu_q_lens,
     p.pt_stride = pt_stride;
     const float sc = scale > 0.f ? scale : 1.0f / sqrtf((float)c->head_dim);
     p.scale_log2 = sc * 1.4426950408889634f;
+    p.window = window;
+    p.sinks = sinks;
     p.status = c->status_word();
     const int tq = umma ? prefill_umma_tile_tokens(G) : prefill_tile_tokens(G);
     const int q_tiles = (max_q_len + tq - 1) / tq;
@@ -1080,7 +1285,8 @@ int skv_get_status(skv_cache *c, void *stream, int *device_status)
         (void)cudaGetLastError();
         return SKV_ERR_CUDA;
     }
-    *device_status = (word & STATUS_TIMEOUT) ? SKV_ERR_TIMEOUT : (word & STATUS_BOUNDS) ? SKV_ERR_BOUNDS : SKV_OK;
+    *device_status = (word & STATUS_TIMEOUT) ? SKV_ERR_TIMEOUT : (word & STATUS_BOUNDS) ? SKV_ERR_BOUNDS
+                     : (word & STATUS_NOMEM) ? SKV_ERR_NOMEM : SKV_OK;
     return SKV_OK;
 }
 

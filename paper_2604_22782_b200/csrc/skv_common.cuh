@@ -39,6 +39,7 @@ __host__ __device__ constexpr int fp8_block_bytes(int D) { return 2 * PAGE * D +
 // device status bits
 constexpr int STATUS_TIMEOUT = 1;
 constexpr int STATUS_BOUNDS = 2;
+constexpr int STATUS_NOMEM = 4;
 
 struct AppendParams {
     uint8_t *layer_base;        // first page of the (first) owner layer written
@@ -125,6 +126,7 @@ struct DecodeParams {
                                 // normal L2 priority; the rest is loaded evict-first
     int64_t l2_fit_blocks;      // a call with at most this many blocks in all is small enough to stay in L2 for
                                 // the next layer that reads the same owner: all of it is loaded with normal priority
+    int window, sinks;          // sliding-window instances only: tokens t >= n - window or t < sinks are attended
     int *status;
     unsigned long long *trace;  // optional [n_workers][4]: sm id, entry ns, first-page ns, exit ns
     unsigned long long *tags;   // [n_slots]: `epoch` once the partial at that slot is complete (DECODE_MERGE_IN_KERNEL)
@@ -157,6 +159,7 @@ struct PrefillParams {
     const int32_t *seq_lens;    // [B] cached tokens including the new ones
     int B, Hq, Hkv, pt_stride;
     float scale_log2;
+    int window, sinks;          // sliding-window instances only: a row at pos sees t <= pos, t > pos - window or t < sinks
     int *status;
 };
 
@@ -168,6 +171,59 @@ struct DequantParams {
     const int32_t *page_table;  // [B][pt_stride]
     const int32_t *seq_lens;    // [B]
     int B, Hkv, pt_stride;
+};
+
+struct RopeParams {
+    uint64_t freq[64];          // inv_freq[i] as a fraction of a turn per position, 2^64 = one turn
+    uint8_t axis[64];           // which row of `positions` turns frequency i
+    const int32_t *positions;   // [axes][pos_stride]
+    int64_t pos_stride;
+    const uint16_t *Q;          // [n_tokens] rows of [Hq][D] bf16, q_stride elements apart
+    uint16_t *Q_out;
+    const uint16_t *K, *V;      // [n_tokens] rows of [Hkv][D] bf16
+    int64_t q_stride, qo_stride, k_stride, v_stride;
+    uint8_t *layer_base;        // first page of the owner layer that is written
+    const int64_t *slot_map;    // [n_tokens]
+    int64_t n_tokens;
+    int64_t n_slots;            // max_pages * PAGE
+    int64_t page_stride;
+    int Hq, Hkv;                // heads turned / stored by this call (Hkv 0: a layer that keeps no K,V)
+    int rotary_dim;             // leading dims of a head that are turned (a multiple of 16)
+    int head_parts;             // warps that share a group of tokens, each with its part of the heads
+    int *status;
+};
+
+struct PlanParams {
+    int32_t *page_table;        // [B][pt_stride]
+    int pt_stride;
+    const int32_t *seq_lens;    // [B] cached tokens before the step
+    const int32_t *new_lens;    // [B] tokens the step wants to add
+    int B;
+    const int32_t *free_pages;  // a stack: the top is free_pages[*n_free - 1]
+    int free_capacity;
+    const int32_t *n_free;
+    int64_t max_tokens;         // room in slot_map / positions
+    int64_t max_pages;
+    int64_t *slot_map;
+    int32_t *positions;         // may be null
+    int32_t *cu_q_lens;         // [B+1]
+    int32_t *seq_lens_out;      // [B]; may be seq_lens
+    int32_t *n_free_out;        // may be n_free
+    int *status;
+};
+
+struct ReleaseParams {
+    int32_t *page_table;        // [B][pt_stride]
+    int pt_stride;
+    const int32_t *first_page;  // [B] entries [first_page, end_page) of a row go back
+    const int32_t *end_page;
+    int B;
+    int32_t *free_pages;
+    int free_capacity;
+    const int32_t *n_free;
+    int32_t *n_free_out;        // may be n_free
+    int64_t max_pages;
+    int *status;
 };
 
 struct DecodeTuning {
@@ -199,7 +255,13 @@ cudaError_t launch_merge(const MergeParams &p, bool pdl, cudaStream_t s);
 size_t decode_cta_smem_bytes(int D, int B, int G, int consumers, int stages, bool fp8);
 bool decode_cta_can_merge(int D, int kernel);   // the variant (kernel: 0 CUDA cores, 1 tensor cores, 2 FP8 pages) can finish cut segments itself
 cudaError_t launch_decode_cta(const DecodeParams &p, int D, int G, int kernel, int grid, int consumers, int stages,
-                              bool pdl, cudaStream_t s);
+                              bool pdl, cudaStream_t s);   // p.window > 0: the sliding-window instance
+// rotary embedding with the update (skv_rope.cu); adjacent: pairs (2i, 2i+1)
+cudaError_t launch_rope_append(const RopeParams &p, int D, bool fp8, bool adjacent, bool pdl, cudaStream_t s);
+// a step's tables (skv_plan.cu); in_place: an output is the memory of an input
+int plan_max_batch();
+cudaError_t launch_plan_step(const PlanParams &p, bool in_place, int sm_count, bool pdl, cudaStream_t s);
+cudaError_t launch_plan_release(const ReleaseParams &p, bool pdl, cudaStream_t s);
 // FP8 pages of the sequences' pages -> bf16 pages in a scratch area (skv_dequant.cu); grid covers max_pages_per_seq
 cudaError_t launch_dequant_pages(const DequantParams &p, int D, int max_pages_per_seq, cudaStream_t s);
 size_t prefill_smem_bytes(int D);

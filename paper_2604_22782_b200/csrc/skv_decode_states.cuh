@@ -2,6 +2,7 @@
 // that has landed in shared memory, for the three storage / arithmetic variants.  Every State has
 //   begin(p, b, h, G, lane)          load the G query heads of kv head h of sequence b, clear the running state
 //   page(blk, valid, scale_log2, lane)  fold one block (shared address blk, `valid` tokens in use) into it
+//   page_bits(blk, bits, scale_log2, lane)  the same with the tokens in use given as a 16-bit set (not empty)
 //   finish(part_o, part_ml, slot, G, lane)  write the run's partial (running max in log2 units, sum,
 //                                        unnormalised output) to slot `slot` of the given arrays
 //                                        (global or shared memory: generic pointers)
@@ -56,6 +57,15 @@ struct TensorCoreState {
     // one page: blk = shared address of the block (K half, V half), valid = tokens in use (1..16)
     __device__ __forceinline__ void page(uint32_t blk, int valid, float scale_log2, int lane)
     {
+        fold(blk, valid < PAGE, [valid](int t) { return t < valid; }, scale_log2, lane);
+    }
+    __device__ __forceinline__ void page_bits(uint32_t blk, uint32_t bits, float scale_log2, int lane)
+    {
+        fold(blk, bits != 0xFFFFu, [bits](int t) { return ((bits >> t) & 1u) != 0; }, scale_log2, lane);
+    }
+    template <class InUse>
+    __device__ __forceinline__ void fold(uint32_t blk, bool partly, InUse in_use, float scale_log2, int lane)
+    {
         const uint32_t sK = blk, sV = blk + half_bytes(D);
         const int tig = lane & 3;
         float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
@@ -71,16 +81,16 @@ struct TensorCoreState {
         // this thread's four scores: tokens 2tig, 2tig+1, 8+2tig, 9+2tig of head lane>>2
         float v0 = s[0][0] * scale_log2, v1 = s[0][1] * scale_log2;
         float v2 = s[1][0] * scale_log2, v3 = s[1][1] * scale_log2;
-        if (valid < PAGE) {
+        if (partly) {
             const int t0 = 2 * tig;
-            if (t0 >= valid) v0 = -INFINITY;
-            if (t0 + 1 >= valid) v1 = -INFINITY;
-            if (t0 + 8 >= valid) v2 = -INFINITY;
-            if (t0 + 9 >= valid) v3 = -INFINITY;
+            if (!in_use(t0)) v0 = -INFINITY;
+            if (!in_use(t0 + 1)) v1 = -INFINITY;
+            if (!in_use(t0 + 8)) v2 = -INFINITY;
+            if (!in_use(t0 + 9)) v3 = -INFINITY;
             // rows of V past the valid tokens may hold anything: zero them so 0 * x stays 0
             for (int i = lane; i < (D / 8) * PAGE; i += 32) {
                 const int t = i & (PAGE - 1);
-                if (t >= valid) {
+                if (!in_use(t)) {
                     const uint32_t a = sV + (uint32_t)(i * 16);
                     asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(a), "r"(0u) : "memory");
                 }
@@ -169,6 +179,15 @@ struct CudaCoreState {
 
     __device__ __forceinline__ void page(uint32_t blk, int valid, float scale_log2, int lane)
     {
+        fold(blk, (lane & 15) < valid, scale_log2, lane);
+    }
+    __device__ __forceinline__ void page_bits(uint32_t blk, uint32_t bits, float scale_log2, int lane)
+    {
+        fold(blk, ((bits >> (lane & 15)) & 1u) != 0, scale_log2, lane);
+    }
+    // live: this lane's token slot is in use
+    __device__ __forceinline__ void fold(uint32_t blk, bool live, float scale_log2, int lane)
+    {
         const uint32_t sK = blk, sV = blk + half_bytes(D);
         const int t = lane & 15, hf = lane >> 4;
         const uint32_t off = (uint32_t)((hf * HC * PAGE + t) * 16);
@@ -185,7 +204,6 @@ struct CudaCoreState {
         }
         float acc = acc0 + acc1;
         acc += __shfl_xor_sync(FULL, acc, 16);
-        const bool live = t < valid;
         const float v = live ? acc * scale_log2 : -INFINITY;
         const float m_new = fmaxf(m, v);
         const bool grew = m_new > m;
@@ -318,6 +336,22 @@ struct Fp8State {
 
     __device__ __forceinline__ void page(uint32_t blk, int valid, float scale_log2, int lane)
     {
+        fold(blk, valid < PAGE, [valid](int t) { return t < valid; }, [valid](int t0) {
+            const int keep = valid - t0;       // leading bytes to keep
+            return keep >= 4 ? 0xFFFFFFFFu : keep <= 0 ? 0u : (0xFFFFFFFFu >> (8 * (4 - keep)));
+        }, scale_log2, lane);
+    }
+    __device__ __forceinline__ void page_bits(uint32_t blk, uint32_t bits, float scale_log2, int lane)
+    {
+        fold(blk, bits != 0xFFFFu, [bits](int t) { return ((bits >> t) & 1u) != 0; }, [bits](int t0) {
+            const uint32_t b = (bits >> t0) & 0xFu;
+            return ((b & 1u) | ((b & 2u) << 7) | ((b & 4u) << 14) | ((b & 8u) << 21)) * 0xFFu;
+        }, scale_log2, lane);
+    }
+    // byte_mask(t0): the bytes to keep of a V word that holds tokens t0 .. t0+3
+    template <class InUse, class ByteMask>
+    __device__ __forceinline__ void fold(uint32_t blk, bool partly, InUse in_use, ByteMask byte_mask, float scale_log2, int lane)
+    {
         const int g = lane >> 2, tig = lane & 3;
         // ---- scores of tokens 4tig .. 4tig+3 for query head g ----
         float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
@@ -349,13 +383,12 @@ struct Fp8State {
         const int t0 = 4 * tig;
         float v0 = s0[0] * (qs * sk.x), v1 = s0[1] * (qs * sk.y), v2 = s1[0] * (qs * sk.z), v3 = s1[1] * (qs * sk.w);
         uint32_t vmask = 0xFFFFFFFFu;          // bytes of a V word (tokens 4tig..4tig+3) that are in use
-        if (valid < PAGE) {                    // slots past the sequence's end may hold anything
-            if (t0 >= valid) { v0 = -INFINITY; sv.x = 0.f; }
-            if (t0 + 1 >= valid) { v1 = -INFINITY; sv.y = 0.f; }
-            if (t0 + 2 >= valid) { v2 = -INFINITY; sv.z = 0.f; }
-            if (t0 + 3 >= valid) { v3 = -INFINITY; sv.w = 0.f; }
-            const int keep = valid - t0;       // leading bytes to keep
-            vmask = keep >= 4 ? 0xFFFFFFFFu : keep <= 0 ? 0u : (0xFFFFFFFFu >> (8 * (4 - keep)));
+        if (partly) {                          // slots past the sequence's end may hold anything
+            if (!in_use(t0)) { v0 = -INFINITY; sv.x = 0.f; }
+            if (!in_use(t0 + 1)) { v1 = -INFINITY; sv.y = 0.f; }
+            if (!in_use(t0 + 2)) { v2 = -INFINITY; sv.z = 0.f; }
+            if (!in_use(t0 + 3)) { v3 = -INFINITY; sv.w = 0.f; }
+            vmask = byte_mask(t0);
         }
         float mx = fmaxf(fmaxf(v0, v1), fmaxf(v2, v3));
         mx = fmaxf(mx, __shfl_xor_sync(FULL, mx, 1));

@@ -6,6 +6,7 @@
 // copies, and keeps the online-softmax state of its rows in registers (flash attention).
 // No split over the keys and therefore no workspace.
 #include "skv_common.cuh"
+#include "skv_walk.cuh"
 
 #include <math.h>
 
@@ -18,7 +19,10 @@ constexpr int ROWS = 64;        // query rows per CTA: 4 warps x 16
 constexpr int KB = 4;           // pages per key block (64 keys)
 constexpr int NSTAGE = 3;       // key blocks in flight
 
-template <int D>
+// WIN: the sliding-window instance (p.window, p.sinks).  A tile walks only the pages that one of its rows sees
+// (window_pages); the other tokens of those pages are masked row by row, and V rows that no row of the tile sees
+// are zeroed in shared memory, whatever they hold.
+template <int D, bool WIN>
 __global__ void __launch_bounds__(128, 2) prefill_kernel(PrefillParams p, int G)
 {
     extern __shared__ __align__(128) uint8_t smem_raw[];
@@ -51,7 +55,9 @@ __global__ void __launch_bounds__(128, 2) prefill_kernel(PrefillParams p, int G)
     const int q_end = (q0 + TQ < q_len) ? q0 + TQ : q_len;    // tokens [q0, q_end) of the sequence's new ones
     const int pos0 = n_b - q_len;                             // position of the sequence's first new token
     const int n_keys = pos0 + q_end;                          // keys 0 .. n_keys-1 are visible to some row
-    const int n_pages = (n_keys + PAGE - 1) / PAGE;
+    WindowPages win = {};
+    if (WIN) win = window_pages(pos0 + q0, n_keys, p.window, p.sinks);
+    const int n_pages = WIN ? win.count : (n_keys + PAGE - 1) / PAGE;
     const int n_kb = (n_pages + KB - 1) / KB;
 
     // producer (thread 0): key block kb -> stage kb % NSTAGE
@@ -61,7 +67,7 @@ __global__ void __launch_bounds__(128, 2) prefill_kernel(PrefillParams p, int G)
         const int np = (n_pages - pg0) < KB ? (n_pages - pg0) : KB;
         int ids[KB];
 #pragma unroll
-        for (int j = 0; j < KB; ++j) ids[j] = j < np ? __ldg(p.page_table + (int64_t)b * p.pt_stride + pg0 + j) : 0;
+        for (int j = 0; j < KB; ++j) ids[j] = j < np ? __ldg(p.page_table + (int64_t)b * p.pt_stride + (WIN ? win.page(pg0 + j) : pg0 + j)) : 0;
         const uint32_t bar = bars + 8 * s;
         mbar_expect_tx(bar, (uint32_t)(np * BLOCK));
 #pragma unroll
@@ -87,6 +93,10 @@ __global__ void __launch_bounds__(128, 2) prefill_kernel(PrefillParams p, int G)
     const bool ok_lo = qi_lo < TQ && q0 + qi_lo < q_end, ok_hi = qi_hi < TQ && q0 + qi_hi < q_end;
     // rows outside the tile run unmasked on whatever is there; nothing of theirs is stored
     const int pos_lo = ok_lo ? pos0 + q0 + qi_lo : 0x7FFFFFFF, pos_hi = ok_hi ? pos0 + q0 + qi_hi : 0x7FFFFFFF;
+    // first token inside the row's window
+    const int from_lo = WIN && pos_lo >= p.window ? pos_lo - p.window + 1 : 0, from_hi = WIN && pos_hi >= p.window ? pos_hi - p.window + 1 : 0;
+    auto sees_lo = [&](int key) { return key <= pos_lo && (!WIN || key >= from_lo || key < p.sinks); };
+    auto sees_hi = [&](int key) { return key <= pos_hi && (!WIN || key >= from_hi || key < p.sinks); };
     const int64_t row_lo = ((int64_t)(q_begin + q0 + qi_lo) * p.Hq + (int64_t)h * G + g_lo) * D;
     const int64_t row_hi = ((int64_t)(q_begin + q0 + qi_hi) * p.Hq + (int64_t)h * G + g_hi) * D;
 
@@ -122,7 +132,22 @@ __global__ void __launch_bounds__(128, 2) prefill_kernel(PrefillParams p, int G)
         // slots of the sequence's last page that were never written may hold anything: zero their V rows
         // so that 0 * x stays 0 (their scores are masked below)
         const int last_valid = n_b - (pg0 + np - 1) * PAGE;       // tokens in use in the block's last page
-        if (last_valid < PAGE) {
+        if (WIN) {
+            bool zeroed = false;
+            for (int j = 0; j < np; ++j) {
+                const uint32_t bits = window_bits(win.page(pg0 + j), win.lo, n_keys, p.sinks);
+                if (bits == 0xFFFFu) continue;
+                zeroed = true;
+                const uint32_t sV = stage + (uint32_t)(j * BLOCK) + half_bytes(D);
+                for (int i = threadIdx.x; i < (D / 8) * PAGE; i += blockDim.x)
+                    if (!((bits >> (i & (PAGE - 1))) & 1u))
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(sV + (uint32_t)(i * 16)), "r"(0u) : "memory");
+            }
+            if (zeroed) {                          // (the same for every thread)
+                fence_proxy_async();
+                __syncthreads();
+            }
+        } else if (last_valid < PAGE) {
             const uint32_t sV = stage + (uint32_t)((np - 1) * BLOCK) + half_bytes(D);
             for (int i = threadIdx.x; i < (D / 8) * PAGE; i += blockDim.x)
                 if ((i & (PAGE - 1)) >= last_valid)
@@ -151,12 +176,13 @@ __global__ void __launch_bounds__(128, 2) prefill_kernel(PrefillParams p, int G)
         float mx_lo = -INFINITY, mx_hi = -INFINITY;
 #pragma unroll
         for (int nt = 0; nt < 2 * KB; ++nt) {
-            const int t0 = (pg0 + (nt >> 1)) * PAGE + (nt & 1) * 8 + 2 * tig;    // key of elements [0] and [2]
+            const int page = WIN ? win.page(pg0 + (nt >> 1)) : pg0 + (nt >> 1);
+            const int t0 = page * PAGE + (nt & 1) * 8 + 2 * tig;                 // key of elements [0] and [2]
             const bool there = (nt >> 1) < np;
-            sc[nt][0] = (there && t0 <= pos_lo) ? sc[nt][0] * p.scale_log2 : -INFINITY;
-            sc[nt][1] = (there && t0 + 1 <= pos_lo) ? sc[nt][1] * p.scale_log2 : -INFINITY;
-            sc[nt][2] = (there && t0 <= pos_hi) ? sc[nt][2] * p.scale_log2 : -INFINITY;
-            sc[nt][3] = (there && t0 + 1 <= pos_hi) ? sc[nt][3] * p.scale_log2 : -INFINITY;
+            sc[nt][0] = (there && sees_lo(t0)) ? sc[nt][0] * p.scale_log2 : -INFINITY;
+            sc[nt][1] = (there && sees_lo(t0 + 1)) ? sc[nt][1] * p.scale_log2 : -INFINITY;
+            sc[nt][2] = (there && sees_hi(t0)) ? sc[nt][2] * p.scale_log2 : -INFINITY;
+            sc[nt][3] = (there && sees_hi(t0 + 1)) ? sc[nt][3] * p.scale_log2 : -INFINITY;
             mx_lo = fmaxf(mx_lo, fmaxf(sc[nt][0], sc[nt][1]));
             mx_hi = fmaxf(mx_hi, fmaxf(sc[nt][2], sc[nt][3]));
         }
@@ -167,14 +193,16 @@ __global__ void __launch_bounds__(128, 2) prefill_kernel(PrefillParams p, int G)
         // key 0 is visible to every row, so after the first block the running maxima are finite; a block
         // that is entirely in a row's future leaves that row unchanged (alpha = 1, all p = 0)
         const float mn_lo = fmaxf(m_lo, mx_lo), mn_hi = fmaxf(m_hi, mx_hi);
-        const float a_lo = fast_exp2(m_lo - mn_lo), a_hi = fast_exp2(m_hi - mn_hi);
+        // (with a window a row may not have seen any key yet: it then counts from 0, and -inf gives p = 0)
+        const float ref_lo = WIN && mn_lo == -INFINITY ? 0.f : mn_lo, ref_hi = WIN && mn_hi == -INFINITY ? 0.f : mn_hi;
+        const float a_lo = fast_exp2(m_lo - ref_lo), a_hi = fast_exp2(m_hi - ref_hi);
         m_lo = mn_lo;
         m_hi = mn_hi;
         float sum_lo = 0.f, sum_hi = 0.f;
 #pragma unroll
         for (int nt = 0; nt < 2 * KB; ++nt) {
-            sc[nt][0] = fast_exp2(sc[nt][0] - mn_lo); sc[nt][1] = fast_exp2(sc[nt][1] - mn_lo);
-            sc[nt][2] = fast_exp2(sc[nt][2] - mn_hi); sc[nt][3] = fast_exp2(sc[nt][3] - mn_hi);
+            sc[nt][0] = fast_exp2(sc[nt][0] - ref_lo); sc[nt][1] = fast_exp2(sc[nt][1] - ref_lo);
+            sc[nt][2] = fast_exp2(sc[nt][2] - ref_hi); sc[nt][3] = fast_exp2(sc[nt][3] - ref_hi);
             sum_lo += sc[nt][0] + sc[nt][1];
             sum_hi += sc[nt][2] + sc[nt][3];
         }
@@ -244,7 +272,7 @@ __global__ void __launch_bounds__(128, 2) prefill_kernel(PrefillParams p, int G)
 // take the page's key rows in the order 0,1,4,5,8,9,12,13 | 2,3,6,7,10,11,14,15, so that a thread's
 // four probabilities of a page are keys 4tig .. 4tig+3, the four keys of its V words.
 // ---------------------------------------------------------------------------
-template <int D>
+template <int D, bool WIN>
 __global__ void __launch_bounds__(128, 2) prefill_fp8_kernel(PrefillParams p, int G)
 {
     extern __shared__ __align__(128) uint8_t smem_raw[];
@@ -277,7 +305,9 @@ __global__ void __launch_bounds__(128, 2) prefill_fp8_kernel(PrefillParams p, in
     const int q_end = (q0 + TQ < q_len) ? q0 + TQ : q_len;
     const int pos0 = n_b - q_len;
     const int n_keys = pos0 + q_end;
-    const int n_pages = (n_keys + PAGE - 1) / PAGE;
+    WindowPages win = {};
+    if (WIN) win = window_pages(pos0 + q0, n_keys, p.window, p.sinks);
+    const int n_pages = WIN ? win.count : (n_keys + PAGE - 1) / PAGE;
     const int n_kb = (n_pages + KB - 1) / KB;
 
     auto issue = [&](int kb) {
@@ -286,7 +316,7 @@ __global__ void __launch_bounds__(128, 2) prefill_fp8_kernel(PrefillParams p, in
         const int np = (n_pages - pg0) < KB ? (n_pages - pg0) : KB;
         int ids[KB];
 #pragma unroll
-        for (int j = 0; j < KB; ++j) ids[j] = j < np ? __ldg(p.page_table + (int64_t)b * p.pt_stride + pg0 + j) : 0;
+        for (int j = 0; j < KB; ++j) ids[j] = j < np ? __ldg(p.page_table + (int64_t)b * p.pt_stride + (WIN ? win.page(pg0 + j) : pg0 + j)) : 0;
         const uint32_t bar = bars + 8 * s;
         mbar_expect_tx(bar, (uint32_t)(np * BLOCK));
 #pragma unroll
@@ -310,6 +340,10 @@ __global__ void __launch_bounds__(128, 2) prefill_fp8_kernel(PrefillParams p, in
     const int qi_lo = r_lo / G, g_lo = r_lo - qi_lo * G, qi_hi = r_hi / G, g_hi = r_hi - qi_hi * G;
     const bool ok_lo = qi_lo < TQ && q0 + qi_lo < q_end, ok_hi = qi_hi < TQ && q0 + qi_hi < q_end;
     const int pos_lo = ok_lo ? pos0 + q0 + qi_lo : 0x7FFFFFFF, pos_hi = ok_hi ? pos0 + q0 + qi_hi : 0x7FFFFFFF;
+    // first token inside the row's window
+    const int from_lo = WIN && pos_lo >= p.window ? pos_lo - p.window + 1 : 0, from_hi = WIN && pos_hi >= p.window ? pos_hi - p.window + 1 : 0;
+    auto sees_lo = [&](int key) { return key <= pos_lo && (!WIN || key >= from_lo || key < p.sinks); };
+    auto sees_hi = [&](int key) { return key <= pos_hi && (!WIN || key >= from_hi || key < p.sinks); };
     const int64_t row_lo = ((int64_t)(q_begin + q0 + qi_lo) * p.Hq + (int64_t)h * G + g_lo) * D;
     const int64_t row_hi = ((int64_t)(q_begin + q0 + qi_hi) * p.Hq + (int64_t)h * G + g_hi) * D;
 
@@ -394,16 +428,18 @@ __global__ void __launch_bounds__(128, 2) prefill_fp8_kernel(PrefillParams p, in
                              : "r"(blk + (uint32_t)(fp8_ks_off(D) + 16 * tig)));
                 asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(vsc[j].x), "=f"(vsc[j].y), "=f"(vsc[j].z), "=f"(vsc[j].w)
                              : "r"(blk + (uint32_t)(fp8_vs_off(D) + 16 * tig)));
-                const int t0 = (pg0 + j) * PAGE + 4 * tig;       // key of sc[2j][0]
+                const int page = WIN ? win.page(pg0 + j) : pg0 + j;
+                const int t0 = page * PAGE + 4 * tig;            // key of sc[2j][0]
                 const int nv = (j == np - 1) ? last_valid : PAGE; // slots past the sequence's end may hold anything
+                const uint32_t bits = WIN ? window_bits(page, win.lo, n_keys, p.sinks) : 0xFFFFu;   // ... and so may those no row sees
                 const float kk[4] = {ksc.x, ksc.y, ksc.z, ksc.w};
                 float *vv = &vsc[j].x;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const bool there = 4 * tig + i < nv;
+                    const bool there = WIN ? ((bits >> (4 * tig + i)) & 1u) != 0 : 4 * tig + i < nv;
                     float &e_lo = sc[2 * j + (i >> 1)][i & 1], &e_hi = sc[2 * j + (i >> 1)][2 + (i & 1)];
-                    e_lo = (there && t0 + i <= pos_lo) ? e_lo * (qs_lo * kk[i]) : -INFINITY;
-                    e_hi = (there && t0 + i <= pos_hi) ? e_hi * (qs_hi * kk[i]) : -INFINITY;
+                    e_lo = (there && sees_lo(t0 + i)) ? e_lo * (qs_lo * kk[i]) : -INFINITY;
+                    e_hi = (there && sees_hi(t0 + i)) ? e_hi * (qs_hi * kk[i]) : -INFINITY;
                     if (!there) vv[i] = 0.f;
                     svmax = fmaxf(svmax, vv[i]);
                 }
@@ -425,14 +461,15 @@ __global__ void __launch_bounds__(128, 2) prefill_fp8_kernel(PrefillParams p, in
         svmax = fmaxf(svmax, __shfl_xor_sync(FULL, svmax, 1));
         svmax = fmaxf(svmax, __shfl_xor_sync(FULL, svmax, 2));
         const float mn_lo = fmaxf(m_lo, mx_lo), mn_hi = fmaxf(m_hi, mx_hi);
-        float a_lo = fast_exp2(m_lo - mn_lo), a_hi = fast_exp2(m_hi - mn_hi);
+        const float ref_lo = WIN && mn_lo == -INFINITY ? 0.f : mn_lo, ref_hi = WIN && mn_hi == -INFINITY ? 0.f : mn_hi;
+        float a_lo = fast_exp2(m_lo - ref_lo), a_hi = fast_exp2(m_hi - ref_hi);
         m_lo = mn_lo;
         m_hi = mn_hi;
         float sum_lo = 0.f, sum_hi = 0.f;
 #pragma unroll
         for (int nt = 0; nt < 2 * KB; ++nt) {
-            sc[nt][0] = fast_exp2(sc[nt][0] - mn_lo); sc[nt][1] = fast_exp2(sc[nt][1] - mn_lo);
-            sc[nt][2] = fast_exp2(sc[nt][2] - mn_hi); sc[nt][3] = fast_exp2(sc[nt][3] - mn_hi);
+            sc[nt][0] = fast_exp2(sc[nt][0] - ref_lo); sc[nt][1] = fast_exp2(sc[nt][1] - ref_lo);
+            sc[nt][2] = fast_exp2(sc[nt][2] - ref_hi); sc[nt][3] = fast_exp2(sc[nt][3] - ref_hi);
             sum_lo += sc[nt][0] + sc[nt][1];
             sum_hi += sc[nt][2] + sc[nt][3];
         }
@@ -461,7 +498,10 @@ __global__ void __launch_bounds__(128, 2) prefill_fp8_kernel(PrefillParams p, in
                 const uint32_t pa2 = pack_f16x2(sc[2 * j + 1][0] * w2, sc[2 * j + 1][1] * w3);
                 const uint32_t pa3 = pack_f16x2(sc[2 * j + 1][2] * w2, sc[2 * j + 1][3] * w3);
                 uint32_t vmask = 0xFFFFFFFFu;              // bytes of a V word that belong to tokens in use
-                if (j == np - 1 && last_valid < PAGE) {
+                if (WIN) {
+                    const uint32_t b4 = (window_bits(win.page(pg0 + j), win.lo, n_keys, p.sinks) >> (4 * tig)) & 0xFu;
+                    vmask = ((b4 & 1u) | ((b4 & 2u) << 7) | ((b4 & 4u) << 14) | ((b4 & 8u) << 21)) * 0xFFu;
+                } else if (j == np - 1 && last_valid < PAGE) {
                     const int keep = last_valid - 4 * tig;
                     vmask = keep >= 4 ? 0xFFFFFFFFu : keep <= 0 ? 0u : (0xFFFFFFFFu >> (8 * (4 - keep)));
                 }
@@ -521,9 +561,9 @@ size_t prefill_fp8_smem_bytes(int D)
 
 int prefill_tile_tokens(int G) { return ROWS / G; }
 
-cudaError_t launch_prefill_fp8(const PrefillParams &p, int D, int G, int q_tiles, bool pdl, cudaStream_t s)
+namespace {
+cudaError_t launch_tiles(void (*kern)(PrefillParams, int), size_t smem, const PrefillParams &p, int G, int q_tiles, bool pdl, cudaStream_t s)
 {
-    const size_t smem = prefill_fp8_smem_bytes(D);
     if (smem == 0 || q_tiles <= 0) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)q_tiles, (unsigned)p.Hkv, (unsigned)p.B);
@@ -535,34 +575,24 @@ cudaError_t launch_prefill_fp8(const PrefillParams &p, int D, int G, int q_tiles
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = pdl ? 1 : 0;
-    auto kern = D == 128 ? prefill_fp8_kernel<128> : prefill_fp8_kernel<64>;
-    cudaError_t e = ensure_dynamic_smem(kern, smem);
+    const cudaError_t e = ensure_dynamic_smem(kern, smem);
     if (e != cudaSuccess) return e;
     return cudaLaunchKernelEx(&cfg, kern, p, G);
+}
+}  // namespace
+
+cudaError_t launch_prefill_fp8(const PrefillParams &p, int D, int G, int q_tiles, bool pdl, cudaStream_t s)
+{
+    auto kern = p.window > 0 ? (D == 128 ? prefill_fp8_kernel<128, true> : prefill_fp8_kernel<64, true>)
+                             : (D == 128 ? prefill_fp8_kernel<128, false> : prefill_fp8_kernel<64, false>);
+    return launch_tiles(kern, prefill_fp8_smem_bytes(D), p, G, q_tiles, pdl, s);
 }
 
 cudaError_t launch_prefill(const PrefillParams &p, int D, int G, int q_tiles, bool pdl, cudaStream_t s)
 {
-    const size_t smem = prefill_smem_bytes(D);
-    if (smem == 0 || q_tiles <= 0) return cudaErrorInvalidValue;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)q_tiles, (unsigned)p.Hkv, (unsigned)p.B);
-    cfg.blockDim = dim3(128);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = pdl ? 1 : 0;
-    if (D == 128) {
-        cudaError_t e = ensure_dynamic_smem(prefill_kernel<128>, smem);
-        if (e != cudaSuccess) return e;
-        return cudaLaunchKernelEx(&cfg, prefill_kernel<128>, p, G);
-    }
-    cudaError_t e = ensure_dynamic_smem(prefill_kernel<64>, smem);
-    if (e != cudaSuccess) return e;
-    return cudaLaunchKernelEx(&cfg, prefill_kernel<64>, p, G);
+    auto kern = p.window > 0 ? (D == 128 ? prefill_kernel<128, true> : prefill_kernel<64, true>)
+                             : (D == 128 ? prefill_kernel<128, false> : prefill_kernel<64, false>);
+    return launch_tiles(kern, prefill_smem_bytes(D), p, G, q_tiles, pdl, s);
 }
 
 }  // namespace skv

@@ -56,8 +56,9 @@ __device__ __forceinline__ void step(Cursor &c, const int32_t *prefix, int Hkv, 
 // per kv head; prefix[B] = all of them.  A length that needs more pages than a page-table row holds
 // (max_tokens = pt_stride * PAGE) is cut to what the row holds and flagged in the status word, so that no
 // page id is ever read past the end of a row.
-__device__ __forceinline__ void scan_lengths(const int32_t *seq_lens, int B, int unit_tokens, int64_t max_tokens,
-                                             int *status, int32_t *prefix, int32_t *lens, int lane)
+template <class Units>
+__device__ __forceinline__ void scan_lengths_by(const int32_t *seq_lens, int B, int64_t max_tokens, int *status, int32_t *prefix,
+                                                int32_t *lens, int lane, Units units_of)
 {
     int carry = 0;
     for (int i0 = 0; i0 < B; i0 += 32) {
@@ -70,7 +71,7 @@ __device__ __forceinline__ void scan_lengths(const int32_t *seq_lens, int B, int
                 n = (int)max_tokens;
                 if (status) atomicOr(status, STATUS_BOUNDS);
             }
-            v = (n + unit_tokens - 1) / unit_tokens;
+            v = units_of(n);
             lens[i] = n;
         }
 #pragma unroll
@@ -83,6 +84,49 @@ __device__ __forceinline__ void scan_lengths(const int32_t *seq_lens, int B, int
     }
     if (lane == 0) prefix[0] = 0;
 }
+
+__device__ __forceinline__ void scan_lengths(const int32_t *seq_lens, int B, int unit_tokens, int64_t max_tokens,
+                                             int *status, int32_t *prefix, int32_t *lens, int lane)
+{
+    scan_lengths_by(seq_lens, B, max_tokens, status, prefix, lens, lane, [=](int n) { return (n + unit_tokens - 1) / unit_tokens; });
+}
+
+// ---------------------------------------------------------------------------
+// Sliding window with sinks.  A row at position pos sees the tokens t <= pos with  t > pos - window  or
+// t < sinks.  For rows at positions [first, n) together that is [0, sinks) and [lo, n) with
+// lo = max(0, first - window + 1), so the pages to walk are the sinks' pages and those from lo / PAGE on: a list
+// of `count` pages in which the entries from `sink_pages` on stand `gap` pages further in the page table.
+// ---------------------------------------------------------------------------
+struct WindowPages {
+    int lo;             // first token inside some row's window
+    int sink_pages;     // pages before the gap (0: the list starts at the window)
+    int gap;            // pages that no row sees
+    int count;          // pages of the list
+    __device__ __forceinline__ int page(int j) const { return j < sink_pages ? j : j + gap; }
+};
+
+__host__ __device__ __forceinline__ WindowPages window_pages(int first, int n, int window, int sinks)
+{
+    WindowPages w;
+    w.lo = first >= window ? first - window + 1 : 0;        // (no sum that could pass 31 bits)
+    const int pages = (n >> 4) + ((n & (PAGE - 1)) != 0), s = sinks < n ? sinks : n;
+    w.sink_pages = (s >> 4) + ((s & (PAGE - 1)) != 0);
+    const int first_page = w.lo >> 4;
+    w.gap = first_page > w.sink_pages ? first_page - w.sink_pages : 0;
+    w.count = pages - w.gap;
+    return w;
+}
+
+// bit i: token 16 page + i is one of [lo, hi) or of [0, sinks) below hi
+__host__ __device__ __forceinline__ uint32_t window_bits(int page, int lo, int hi, int sinks)
+{
+    auto below = [&](int x) -> uint32_t {                   // tokens of the page below x
+        const int k = x - page * PAGE;
+        return k >= PAGE ? 0xFFFFu : k <= 0 ? 0u : (1u << k) - 1u;
+    };
+    return below(hi) & (~below(lo) | below(sinks));
+}
+static_assert(PAGE == 16, "the page arithmetic above");
 
 // Shared-memory carve-up (dynamic): prefix[B+1] | lens[B] | rings | barriers | CTA arrival word
 __host__ __device__ inline size_t table_bytes(int B) { return (((size_t)(2 * B + 1) * 4) + 127) & ~(size_t)127; }
