@@ -367,9 +367,12 @@ int skv_decode_attn_static(skv_cache *cache, int layer, const void *Q, const int
  * >= 0.  Pages that hold no such token are not touched and their page-table entries
  * not read, so they may have been given back (skv_plan_release); other tokens of the
  * pages that are read contribute nothing, whatever they hold.
- * Other arguments, workspace, status and errors as skv_decode_attn.  Runs the
- * CTA-per-range kernel whatever skv_set_decode_worker (mode 1) and
- * skv_set_decode_variant (FP8: always the mma.sync arithmetic) say. */
+ * Other arguments, workspace, status and errors as skv_decode_attn.  One
+ * launch of a kernel of its own, in which a CTA or a cluster of CTAs owns a
+ * (sequence, kv head) -- or, on FP8 pages at head_dim 128 with many of those, the
+ * tcgen05 split-K kernel and its merge.  skv_set_decode_variant picks the arithmetic
+ * as for skv_decode_attn; the settings of launch shape, worker, merge and early
+ * fetch do not apply. */
 int skv_decode_attn_window(skv_cache *cache, int layer, const void *Q, const int32_t *page_table,
                            const int32_t *seq_lens, void *out, int batch, int q_heads, int pt_stride,
                            int window, int sinks, float scale, void *workspace, size_t workspace_bytes,

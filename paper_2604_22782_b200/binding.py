@@ -4,6 +4,7 @@ memory and streams, nothing else)."""
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import re
 from typing import List, Optional, Sequence
@@ -37,6 +38,7 @@ def _load() -> ctypes.CDLL:
 
 
 lib = _load()
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 _vp, _i32p, _i64p, _szp = ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.POINTER(ctypes.c_size_t)
 _int, _i64, _f32, _sz = ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
@@ -182,9 +184,15 @@ def skv_plan_worker_of(n_blocks: int, n_workers: int, x: int) -> int:
     return rc
 
 
+@functools.lru_cache(None)
+def _has_cuda() -> bool:
+    return torch.cuda.is_available()
+
+
 def _stream_ptr(stream) -> int:
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else 0
+        # (torch.cuda.current_stream() builds a Stream object first: 4 us against 0.2 us)
+        return _raw_stream(torch.cuda.current_device()) if _has_cuda() else 0
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

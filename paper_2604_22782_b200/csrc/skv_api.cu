@@ -156,6 +156,19 @@ WorkspaceLayout workspace_layout(const skv_cache *c, int batch, int q_heads, int
 // FP8 pages go to the tcgen05 kernel (a worker is a CTA there) unless the mma.sync variant is asked for
 bool fp8_on_umma(const skv_cache *c) { return c->fp8 && c->tune.variant != 2 && decode_fp8_umma_supported(c->head_dim, 1); }
 
+// A windowed call on FP8 pages runs the tcgen05 split-K kernel where each of its workers has ten tiles or more, else the
+// kernel that keeps a segment in one CTA or cluster: shorter ranges cut most segments, and the merge costs more than the
+// faster arithmetic brings.  (us, tcgen05 against the other: 76 tiles a worker 186 / 217, 21 tiles 54 / 66, 10 tiles 35.6 / 37.5
+// and 33.9 / 34.3, 6 tiles 46 / 32, 5 tiles 27.6 / 23.7.)
+bool fp8_window_on_umma(const skv_cache *c, int batch, int G, int pt_stride, int window, int sinks)
+{
+    if (!fp8_on_umma(c) || !decode_fp8_umma_supported(c->head_dim, G)) return false;
+    int64_t tokens = (int64_t)window + sinks;
+    if (tokens > (int64_t)pt_stride * PAGE) tokens = (int64_t)pt_stride * PAGE;
+    const int64_t tiles = (tokens + decode_fp8_umma_tile_tokens() - 1) / decode_fp8_umma_tile_tokens();
+    return (int64_t)batch * c->kv_heads * tiles >= 10 * (int64_t)c->sm_count * decode_fp8_umma_ctas_per_sm();
+}
+
 // Workers of a warp-per-range (or tcgen05) split-K launch under the current variant and launch shape.  A
 // handle without device memory (accounting only) has no device to ask and counts a B200's 148 SMs.
 int n_workers_of(const skv_cache *c)
@@ -561,12 +574,12 @@ int launch_splitk(skv_cache *c, int layer, const void *Q, const int32_t *page_ta
     const WorkspaceLayout wl = workspace_layout(c, batch, q_heads, n_workers_max(c));
     if (workspace_bytes < wl.total) return SKV_ERR_NOMEM;
     const bool tensor_core = c->fp8 || c->tune.variant == 2 || (c->tune.variant == 0 && G > 1);
-    const bool umma = !window && fp8_on_umma(c) && decode_fp8_umma_supported(c->head_dim, G);
+    const bool umma = fp8_on_umma(c) && decode_fp8_umma_supported(c->head_dim, G);
     // CTA per range: stand-alone calls whose result buffer is known (not the links of a chain, which overlap
     // by having many small CTAs; not the tcgen05 FP8 kernel, which has its own CTA-wide design)
     const int cta_S = cta_stages_for(c, batch, G);
-    const bool cta = window ? cta_S > 0 : !umma && !chained && out && c->worker_mode != 1 && cta_S > 0;
-    if (window && !cta) return SKV_ERR_UNSUPPORTED;              // (the sliding window lives in the CTA-per-range kernel alone)
+    if (window && !umma) return SKV_ERR_UNSUPPORTED;             // (of the split-K kernels, that one has a sliding window)
+    const bool cta = !umma && !chained && out && c->worker_mode != 1 && cta_S > 0;
     // Default launch shapes of the warp-per-range kernel (8 warps per SM, two 8 KB stages each, many small
     // CTAs so that the CTAs of the next launch can move in one by one): 2 warps x 4 CTAs per SM for the
     // tensor-core kernel, 1 warp x 8 CTAs per SM for the CUDA-core kernel (measured best for each on B200).
@@ -720,7 +733,38 @@ int skv_decode_attn_window(skv_cache *c, int layer, const void *Q, const int32_t
     if (!Q || !page_table || !seq_lens || !workspace || pt_stride <= 0) return SKV_ERR_ARG;
     if (!aligned(Q, 16) || !aligned(workspace, 256) || !aligned(out, 8)) return SKV_ERR_ARG;
     if (workspace_bytes < workspace_layout(c, batch, q_heads, n_workers_max(c)).total) return SKV_ERR_NOMEM;
-    // The kernel keeps two words per sequence in shared memory beside its ring: larger batches go in pieces.
+    const int G = q_heads / c->kv_heads;
+    if (!fp8_window_on_umma(c, batch, G, pt_stride, window, sinks)) {
+        DecodeParams p;
+        memset(&p, 0, sizeof(p));
+        p.layer_base = c->layer_base(c->slot[(size_t)c->r[(size_t)layer]]);
+        p.page_stride = (int64_t)c->page_bytes;
+        p.max_pages = c->max_pages;
+        p.Q = static_cast<const uint16_t *>(Q);
+        p.page_table = page_table;
+        p.seq_lens = seq_lens;
+        p.out = static_cast<uint16_t *>(out);
+        p.B = batch;
+        p.Hq = q_heads;
+        p.Hkv = c->kv_heads;
+        p.pt_stride = pt_stride;
+        p.scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)c->head_dim)) * 1.4426950408889634f;
+        p.window = window;
+        p.sinks = sinks;
+        // as in launch_splitk: a call that fits in a third of L2 leaves its pages there for the next layer if that reads them too
+        const int64_t window_tokens = (int64_t)window + sinks < (int64_t)pt_stride * PAGE ? (int64_t)window + sinks : (int64_t)pt_stride * PAGE;
+        p.keep_pct = c->l2_keep_pct > 0 && c->walk_keep[(size_t)layer] &&
+                     window_tokens / PAGE * batch * (int64_t)c->page_bytes <= (int64_t)(c->l2_bytes / 3);
+        p.status = c->status_word();
+        const int kernel = c->fp8 ? 2 : c->tune.variant == 2 || (c->tune.variant == 0 && G > 1) ? 1 : 0;
+        if (launch_decode_window(p, c->head_dim, G, kernel, c->sm_count, c->tune.pdl != 0, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return SKV_ERR_CUDA;
+        }
+        c->launches += 1;
+        return SKV_OK;
+    }
+    // The tcgen05 kernel keeps two words per sequence in shared memory beside its rings: larger batches go in pieces.
     constexpr int PIECE = 4096;
     const size_t row = (size_t)q_heads * c->head_dim * 2;
     for (int b = 0; b < batch; b += PIECE) {
@@ -731,7 +775,6 @@ int skv_decode_attn_window(skv_cache *c, int layer, const void *Q, const int32_t
         int rc = launch_splitk(c, layer, q, page_table + (size_t)b * pt_stride, seq_lens + b, n, q_heads, pt_stride, scale,
                                workspace, workspace_bytes, stream, &plan, o, 0, false, window, sinks);
         if (rc) return rc;
-        if (plan.merged) continue;
         // (the page counts the split-K launch left in the workspace: the lengths alone do not give them here)
         rc = launch_merge_on(c, o, n, q_heads, workspace, workspace_bytes, stream, 0, &plan);
         if (rc) return rc;

@@ -255,13 +255,16 @@ cudaError_t launch_merge(const MergeParams &p, bool pdl, cudaStream_t s);
 size_t decode_cta_smem_bytes(int D, int B, int G, int consumers, int stages, bool fp8);
 bool decode_cta_can_merge(int D, int kernel);   // the variant (kernel: 0 CUDA cores, 1 tensor cores, 2 FP8 pages) can finish cut segments itself
 cudaError_t launch_decode_cta(const DecodeParams &p, int D, int G, int kernel, int grid, int consumers, int stages,
-                              bool pdl, cudaStream_t s);   // p.window > 0: the sliding-window instance
+                              bool pdl, cudaStream_t s);
 // rotary embedding with the update (skv_rope.cu); adjacent: pairs (2i, 2i+1)
 cudaError_t launch_rope_append(const RopeParams &p, int D, bool fp8, bool adjacent, bool pdl, cudaStream_t s);
 // a step's tables (skv_plan.cu); in_place: an output is the memory of an input
 int plan_max_batch();
 cudaError_t launch_plan_step(const PlanParams &p, bool in_place, int sm_count, bool pdl, cudaStream_t s);
 cudaError_t launch_plan_release(const ReleaseParams &p, bool pdl, cudaStream_t s);
+// decode attention over a sliding window (skv_decode_window.cu), one launch; kernel as above.  p.keep_pct > 0: pages are
+// left in L2 for the next layer
+cudaError_t launch_decode_window(const DecodeParams &p, int D, int G, int kernel, int sm_count, bool pdl, cudaStream_t s);
 // FP8 pages of the sequences' pages -> bf16 pages in a scratch area (skv_dequant.cu); grid covers max_pages_per_seq
 cudaError_t launch_dequant_pages(const DequantParams &p, int D, int max_pages_per_seq, cudaStream_t s);
 size_t prefill_smem_bytes(int D);

@@ -138,10 +138,7 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar)
 // which every consumer arrives at only after it has combined run r-2, the last reader of that buffer.
 // INMERGE: the instance that finishes cut segments itself (DECODE_MERGE_IN_KERNEL).  It is a kernel of its own
 // because it may use more registers: no CTA of the merge kernel has to fit on the SM beside it.
-// WIN: the sliding-window instance (p.window, p.sinks).  The list holds only the pages with a token that is
-// attended -- the sinks' pages and the window's, see window_pages -- so a call costs what its window costs
-// whatever the sequence's length, and table entries of the pages between are never read.
-template <int D, class State, bool INMERGE, bool WIN>
+template <int D, class State, bool INMERGE>
 __global__ void __launch_bounds__((State::MAX_CTA_CONSUMERS + (State::CTA_COMBINER ? 2 : 1)) * 32, 1)
 __maxnreg__(INMERGE ? 200 : State::CTA_MAX_REGS) decode_cta_kernel(DecodeParams p, int G, int S)
 {
@@ -203,13 +200,7 @@ __maxnreg__(INMERGE ? 200 : State::CTA_MAX_REGS) decode_cta_kernel(DecodeParams 
     const bool early_fetch = (p.flags & DECODE_EARLY_FETCH) != 0;
     const bool reverse = (p.flags & DECODE_REVERSE) != 0;
     if (!early_fetch) pdl_wait();                      // anything read below may come from the kernel before this one
-    if (warp == 0) {
-        if (WIN)
-            scan_lengths_by(p.seq_lens, p.B, (int64_t)p.pt_stride * PAGE, p.status, prefix, lens, lane,
-                            [&](int n) { return n > 0 ? window_pages(n - 1, n, p.window, p.sinks).count : 0; });
-        else
-            scan_lengths(p.seq_lens, p.B, PAGE, (int64_t)p.pt_stride * PAGE, p.status, prefix, lens, lane);
-    }
+    if (warp == 0) scan_lengths(p.seq_lens, p.B, PAGE, (int64_t)p.pt_stride * PAGE, p.status, prefix, lens, lane);
     __syncthreads();
 
     // Merging inside the kernel: a CTA may wait for the partial of the range after its own (forward walks) or
@@ -265,8 +256,7 @@ __maxnreg__(INMERGE ? 200 : State::CTA_MAX_REGS) decode_cta_kernel(DecodeParams 
             Look r = {-1, 0, 0, false, false};
             if (kk >= n) return r;
             const Cursor cur = locate(prefix, p.B, p.Hkv, reverse ? x_first - kk : x_first + kk);
-            const int pg = WIN ? window_pages(lens[cur.b] - 1, lens[cur.b], p.window, p.sinks).page(cur.pg) : cur.pg;
-            r.id = __ldg(p.page_table + (int64_t)cur.b * p.pt_stride + pg);
+            r.id = __ldg(p.page_table + (int64_t)cur.b * p.pt_stride + cur.pg);
             r.b = cur.b;
             r.h = cur.h;
             r.last_page = cur.pg + 1 == cur.pages;
@@ -599,8 +589,6 @@ __maxnreg__(INMERGE ? 200 : State::CTA_MAX_REGS) decode_cta_kernel(DecodeParams 
         const bool has_blocks = held < k + len;
         {
             State st;
-            WindowPages win = {};
-            if (WIN) win = window_pages(n_b - 1, n_b, p.window, p.sinks);
             if (has_blocks) {
                 if (!wait_or_quit(q_full + 8 * qb, (uint32_t)((run >> 1) & 1), gave_up)) { fail(); break; }
                 st.begin_rows(q_rows + (size_t)qb * G * D, G, lane);
@@ -616,12 +604,8 @@ __maxnreg__(INMERGE ? 200 : State::CTA_MAX_REGS) decode_cta_kernel(DecodeParams 
                 }
                 if (p.trace && t_first == 0) t_first = global_timer_ns();
                 const int pg = reverse ? cons.pg - (j - k) : cons.pg + (j - k);
-                if (WIN) {
-                    st.page_bits(ring + (uint32_t)(s * BLOCK), window_bits(win.page(pg), win.lo, n_b, p.sinks), p.scale_log2, lane);
-                } else {
-                    const int left = n_b - pg * PAGE;
-                    st.page(ring + (uint32_t)(s * BLOCK), left < PAGE ? left : PAGE, p.scale_log2, lane);
-                }
+                const int left = n_b - pg * PAGE;
+                st.page(ring + (uint32_t)(s * BLOCK), left < PAGE ? left : PAGE, p.scale_log2, lane);
                 __syncwarp();                           // every lane is done reading this stage
                 if (lane == 0) mbar_arrive(empty + 8 * s);
                 held = claim();
@@ -671,13 +655,13 @@ __maxnreg__(INMERGE ? 200 : State::CTA_MAX_REGS) decode_cta_kernel(DecodeParams 
     }
 }
 
-template <int D, class State, bool WIN>
+template <int D, class State>
 cudaError_t launch_cta_t(const DecodeParams &p, int G, int grid, int consumers, int stages, bool pdl, cudaStream_t s)
 {
     if (consumers > State::MAX_CTA_CONSUMERS) consumers = State::MAX_CTA_CONSUMERS;      // (what its registers allow)
     const size_t smem = decode_cta_smem_bytes(D, p.B, G, consumers, stages, State::BLOCK != block_bytes(D));
     const bool inmerge = State::CTA_COMBINER && (p.flags & DECODE_MERGE_IN_KERNEL) != 0;
-    auto kern = inmerge ? decode_cta_kernel<D, State, State::CTA_COMBINER, WIN> : decode_cta_kernel<D, State, false, WIN>;
+    auto kern = inmerge ? decode_cta_kernel<D, State, State::CTA_COMBINER> : decode_cta_kernel<D, State, false>;
     cudaError_t e = ensure_dynamic_smem(kern, smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
@@ -715,28 +699,20 @@ size_t decode_cta_smem_bytes(int D, int B, int G, int consumers, int stages, boo
                                                        // the barrier of the neighbouring range's partial)
 }
 
-template <bool WIN>
-static cudaError_t launch_cta(const DecodeParams &p, int D, int G, int kernel, int grid, int consumers, int stages,
-                              bool pdl, cudaStream_t s)
-{
-    if (D == 128) {
-        if (kernel == 2) return launch_cta_t<128, Fp8State<128>, WIN>(p, G, grid, consumers, stages, pdl, s);
-        if (kernel == 1) return launch_cta_t<128, TensorCoreState<128>, WIN>(p, G, grid, consumers, stages, pdl, s);
-        return launch_cta_t<128, CudaCoreState<128>, WIN>(p, G, grid, consumers, stages, pdl, s);
-    }
-    if (D == 64) {
-        if (kernel == 2) return launch_cta_t<64, Fp8State<64>, WIN>(p, G, grid, consumers, stages, pdl, s);
-        if (kernel == 1) return launch_cta_t<64, TensorCoreState<64>, WIN>(p, G, grid, consumers, stages, pdl, s);
-        return launch_cta_t<64, CudaCoreState<64>, WIN>(p, G, grid, consumers, stages, pdl, s);
-    }
-    return cudaErrorInvalidValue;
-}
-
 cudaError_t launch_decode_cta(const DecodeParams &p, int D, int G, int kernel, int grid, int consumers, int stages,
                               bool pdl, cudaStream_t s)
 {
-    return p.window > 0 ? launch_cta<true>(p, D, G, kernel, grid, consumers, stages, pdl, s)
-                        : launch_cta<false>(p, D, G, kernel, grid, consumers, stages, pdl, s);
+    if (D == 128) {
+        if (kernel == 2) return launch_cta_t<128, Fp8State<128>>(p, G, grid, consumers, stages, pdl, s);
+        if (kernel == 1) return launch_cta_t<128, TensorCoreState<128>>(p, G, grid, consumers, stages, pdl, s);
+        return launch_cta_t<128, CudaCoreState<128>>(p, G, grid, consumers, stages, pdl, s);
+    }
+    if (D == 64) {
+        if (kernel == 2) return launch_cta_t<64, Fp8State<64>>(p, G, grid, consumers, stages, pdl, s);
+        if (kernel == 1) return launch_cta_t<64, TensorCoreState<64>>(p, G, grid, consumers, stages, pdl, s);
+        return launch_cta_t<64, CudaCoreState<64>>(p, G, grid, consumers, stages, pdl, s);
+    }
+    return cudaErrorInvalidValue;
 }
 
 }  // namespace skv

@@ -65,7 +65,7 @@ struct alignas(16) TileMeta {
     int flags;          // TILE_FIRST / TILE_LAST of a run inside a segment, TILE_END of the worker
     int b, h;           // the segment
     int qbuf;           // which of the two sets of query scales belongs to the segment
-    int pad;
+    int partial;        // sliding window: bit per page slot whose page has tokens that are not attended
 };
 
 // a tile's description as its consumers read it (after their wait on the stage's barrier)
@@ -74,7 +74,7 @@ __device__ __forceinline__ TileMeta load_meta(const TileMeta *m)
     TileMeta r;
     const uint32_t a = smem_u32(m);
     asm volatile("ld.shared.v4.s32 {%0,%1,%2,%3}, [%4];" : "=r"(r.n_pages), "=r"(r.short_slot), "=r"(r.short_valid), "=r"(r.flags) : "r"(a) : "memory");
-    asm volatile("ld.shared.v4.s32 {%0,%1,%2,%3}, [%4];" : "=r"(r.b), "=r"(r.h), "=r"(r.qbuf), "=r"(r.pad) : "r"(a + 16) : "memory");
+    asm volatile("ld.shared.v4.s32 {%0,%1,%2,%3}, [%4];" : "=r"(r.b), "=r"(r.h), "=r"(r.qbuf), "=r"(r.partial) : "r"(a + 16) : "memory");
     return r;
 }
 
@@ -155,7 +155,9 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar)
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-template <int D, int GP>   // GP: the group size rounded up to a power of two (the softmax loops run over GP heads)
+// WIN: the sliding-window instance (p.window, p.sinks): a tile is eight pages of the list of pages that hold a token
+// that is attended (window_pages), and comes with a 16-bit set of such tokens for each of its pages.
+template <int D, int GP, bool WIN>   // GP: the group size rounded up to a power of two (the softmax loops run over GP heads)
 // (bounds as for four CTAs per SM = 80 registers: shared memory admits three, and the registers left over let
 // a CTA of the merge kernel become resident beside them, which the launch chain needs to move on)
 __global__ void __launch_bounds__(THREADS, CTAS_PER_SM + 1) decode_fp8_umma_kernel(DecodeParams p, int G)
@@ -189,6 +191,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM + 1) decode_fp8_umma_kern
     const uint32_t bars = smem_u32(at);                at += 16 * 8;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(at);
     int *gave_up = reinterpret_cast<int *>(at + 4);
+    uint16_t *live_sets = reinterpret_cast<uint16_t *>(at + 16);      // WIN: [4 tiles][TP pages], slots as meta's
     const uint32_t k_full = bars, k_empty = bars + 16, v_full = bars + 32, v_empty = bars + 48, s_ready = bars + 64,
                    p_ready = bars + 80, pv_done = bars + 96, q_full = bars + 112;
 
@@ -219,7 +222,13 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM + 1) decode_fp8_umma_kern
     // flattened list that is cut into equal ranges is the list of (sequence, kv head, tile) here, a tile
     // being pages [8i, 8i+8) of the sequence: equal ranges are then equal numbers of tiles, which is what a
     // CTA's time goes with.  The merge kernel is told the same counts, so it finds the partials as usual.
-    if (warp == 0) scan_lengths(p.seq_lens, p.B, TP * PAGE, (int64_t)p.pt_stride * PAGE, p.status, prefix, lens, lane);
+    if (warp == 0) {
+        if (WIN)
+            scan_lengths_by(p.seq_lens, p.B, (int64_t)p.pt_stride * PAGE, p.status, prefix, lens, lane,
+                            [&](int n) { return n > 0 ? (window_pages(n - 1, n, p.window, p.sinks).count + TP - 1) / TP : 0; });
+        else
+            scan_lengths(p.seq_lens, p.B, TP * PAGE, (int64_t)p.pt_stride * PAGE, p.status, prefix, lens, lane);
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -263,14 +272,17 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM + 1) decode_fp8_umma_kern
             }
             const int s = k & 1;
             // tile cur.pg of segment (cur.b, cur.h): pages [8 cur.pg, 8 cur.pg + np)
-            const int b = cur.b, h = cur.h, n_b = lens[b], pages = (n_b + PAGE - 1) / PAGE, pg0 = TP * cur.pg;
+            WindowPages win = {};
+            const int b = cur.b, h = cur.h, n_b = lens[b];
+            if (WIN) win = window_pages(n_b - 1, n_b, p.window, p.sinks);
+            const int pages = WIN ? win.count : (n_b + PAGE - 1) / PAGE, pg0 = TP * cur.pg;
             const int np = pages - pg0 < TP ? pages - pg0 : TP;
             const bool first = (k == 0) || (reverse ? cur.pg == cur.pages - 1 : cur.pg == 0);
             const bool last = (left == 1) || (reverse ? cur.pg == 0 : cur.pg == cur.pages - 1);
             // page ids of the tile (lane j < np), fetched before the waits for the stages
             int id = 0;
             if (lane < np) {
-                id = __ldg(p.page_table + (int64_t)b * p.pt_stride + pg0 + lane);
+                id = __ldg(p.page_table + (int64_t)b * p.pt_stride + (WIN ? win.page(pg0 + lane) : pg0 + lane));
                 if (id < 0 || (int64_t)id >= p.max_pages) {
                     atomicOr(p.status, STATUS_BOUNDS);
                     id = 0;
@@ -280,6 +292,13 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM + 1) decode_fp8_umma_kern
             const uint64_t pol = (k >= keep_from) ? pol_keep : pol_stream;
             // K part: its stage comes back as soon as the scores of the tile two before this one are done
             if (k >= 2 && !__all_sync(FULL, wait_bounded(k_empty + 8 * s, (uint32_t)((k / 2 - 1) & 1)))) { give_up(); break; }
+            unsigned partial = 0;
+            if (WIN) {
+                const uint32_t set = lane < np ? window_bits(win.page(pg0 + lane), win.lo, n_b, p.sinks) : 0xFFFFu;
+                if (lane < TP) live_sets[(k & 3) * TP + lane] = (uint16_t)set;
+                partial = __ballot_sync(FULL, set != 0xFFFFu);          // (and the sets are there before lane 0 announces the tile below)
+                __syncwarp();
+            }
             if (lane == 0) {
                 TileMeta m;
                 m.n_pages = np;
@@ -291,7 +310,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM + 1) decode_fp8_umma_kern
                 m.b = b;
                 m.h = h;
                 m.qbuf = (first ? runs : runs - 1) & 1;                // which set of query scales
-                m.pad = 0;
+                m.partial = (int)partial;
                 meta[k & 3] = m;       // (four slots: a slot's last readers finished before the tile two back gave its V stage back)
                 mbar_expect_tx(k_full + 8 * s, (uint32_t)(np * K_PAGE));
             }
@@ -460,7 +479,9 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM + 1) decode_fp8_umma_kern
             uint32_t sv[16];
             tmem_ld16(lane_base + (uint32_t)(16 * s), sv);
             tmem_wait_ld();
-            const bool valid = j < m.n_pages && (j != m.short_slot || tt < m.short_valid);
+            const bool valid = j < m.n_pages &&
+                               (WIN ? !((m.partial >> j) & 1) || ((reinterpret_cast<volatile uint16_t *>(live_sets)[(k & 3) * TP + j] >> tt) & 1)
+                                    : j != m.short_slot || tt < m.short_valid);
             const uint8_t *vpage = v_ring_ptr + s * V_STAGE + j * V_PAGE;
             float ksc = 0.f, vsc = 0.f;
             if (valid) {
@@ -544,7 +565,21 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM + 1) decode_fp8_umma_kern
             // V codes the tensor core will read but that belong to no token in use must be finite too: the
             // unused slots of the sequence's last page may hold anything, and an odd tile reads one page
             // slot beyond its last.  Thread d owns the 16 tokens of dim d.
-            if (m.short_slot >= 0) {
+            if (WIN) {
+                for (int left_over = m.partial; left_over; left_over &= left_over - 1) {      // at most three, usually none
+                    const int u = __ffs(left_over) - 1;
+                    const uint32_t set = reinterpret_cast<volatile uint16_t *>(live_sets)[(k & 3) * TP + u];
+                    const uint32_t a = v_ring + (uint32_t)(s * V_STAGE + u * V_PAGE + tid * 16);
+                    uint32_t wv[4];
+                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(wv[0]), "=r"(wv[1]), "=r"(wv[2]), "=r"(wv[3]) : "r"(a));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t b4 = (set >> (4 * i)) & 0xFu;
+                        wv[i] &= ((b4 & 1u) | ((b4 & 2u) << 7) | ((b4 & 4u) << 14) | ((b4 & 8u) << 21)) * 0xFFu;
+                    }
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(wv[0]), "r"(wv[1]), "r"(wv[2]), "r"(wv[3]) : "memory");
+                }
+            } else if (m.short_slot >= 0) {
                 const uint32_t a = v_ring + (uint32_t)(s * V_STAGE + m.short_slot * V_PAGE + tid * 16);
                 uint32_t w0, w1, w2, w3;
                 asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w0), "=r"(w1), "=r"(w2), "=r"(w3) : "r"(a));
@@ -637,15 +672,17 @@ size_t decode_fp8_umma_smem_bytes(int D, int B)
     const int block = fp8_block_bytes(D);
     // alignment | tables | K and V rings | two P' | Q' | tile descriptions | query scales | maxima | sums | barriers | two words
     return 128 + table_bytes(B) + (size_t)NST * TP * block + 2 * 16 * (size_t)(TP * PAGE) + 16 * (size_t)D + 4 * sizeof(TileMeta) +
-           64 + 512 + 128 + 16 * 8 + 16;
+           64 + 512 + 128 + 16 * 8 + 16 + 64;          // (... | a window's token sets)
 }
 
 cudaError_t launch_decode_fp8_umma(const DecodeParams &p, int D, int G, int grid, bool pdl, cudaStream_t s)
 {
     if (!decode_fp8_umma_supported(D, G)) return cudaErrorInvalidValue;
     const size_t smem = decode_fp8_umma_smem_bytes(D, p.B);
-    auto kern = G <= 1 ? decode_fp8_umma_kernel<128, 1> : G <= 2 ? decode_fp8_umma_kernel<128, 2>
-              : G <= 4 ? decode_fp8_umma_kernel<128, 4> : decode_fp8_umma_kernel<128, 8>;
+    auto kern = p.window > 0 ? (G <= 1 ? decode_fp8_umma_kernel<128, 1, true> : G <= 2 ? decode_fp8_umma_kernel<128, 2, true>
+                              : G <= 4 ? decode_fp8_umma_kernel<128, 4, true> : decode_fp8_umma_kernel<128, 8, true>)
+                             : (G <= 1 ? decode_fp8_umma_kernel<128, 1, false> : G <= 2 ? decode_fp8_umma_kernel<128, 2, false>
+                              : G <= 4 ? decode_fp8_umma_kernel<128, 4, false> : decode_fp8_umma_kernel<128, 8, false>);
     cudaError_t e = ensure_dynamic_smem(kern, smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};

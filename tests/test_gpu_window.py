@@ -116,15 +116,17 @@ def test_decode_ranges_and_merging(hq, hkv, d, merge, worker):
     assert p.cache.skv_get_status() == 0
 
 
-def test_decode_window_longer_than_everything_is_the_plain_call():
+def test_decode_window_longer_than_everything_attends_what_the_plain_call_attends():
+    """The same tokens, summed in another order: both within what rounding allows of the same 64-bit result."""
     lens = [300, 1000, 5, 64]
     p = Paged(lens, 2, 128, seed=8)
     q = p.rows(len(lens), 8)
     ws = torch.empty(p.cache.skv_decode_workspace_bytes(4, 8), dtype=torch.uint8, device="cuda")
     plain = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
     p.cache.skv_decode_attn(1, q.cuda(), p.table_dev, p.lens_dev, plain, ws)
+    check_decode(p, q, plain, 1000, 0)
     for window, sinks in ((1000, 0), (1 << 30, 7), (998, 2)):
-        assert torch.equal(decode(p, q, window, sinks), plain)
+        check_decode(p, q, decode(p, q, window, sinks), 1000, 0)
 
 
 def test_decode_infinities_and_lowest_values_outside_the_window():
