@@ -1105,8 +1105,10 @@ int prefill_over(skv_cache *c, int src, const void *Q, const int32_t *cu_q_lens,
     // the codes on the way in
     const size_t bf16_page = page_bytes_of(c->kv_heads, c->head_dim, false);
     const bool via_scratch = c->fp8 && c->prefill_scratch && c->prefill_scratch_bytes >= (size_t)c->max_pages * bf16_page;
-    const bool can_umma = !window && (!c->fp8 || via_scratch) && prefill_umma_supported(c->head_dim, G) && aligned(Q, 16) && aligned(out, 16) &&
-                          prefill_umma_smem_bytes(c->head_dim) <= (size_t)c->max_smem_optin;
+    const bool can_umma = (!c->fp8 || via_scratch) && aligned(Q, 16) && aligned(out, 16) &&
+                          (window ? prefill_window_supported(c->head_dim, G) &&
+                                        prefill_window_smem_bytes(c->head_dim, prefill_window_max_batch()) <= (size_t)c->max_smem_optin
+                                  : prefill_umma_supported(c->head_dim, G) && prefill_umma_smem_bytes(c->head_dim) <= (size_t)c->max_smem_optin);
     if (c->prefill_variant == 2 && !can_umma) return SKV_ERR_UNSUPPORTED;
     const bool umma = c->prefill_variant == 2 || (c->prefill_variant == 0 && can_umma);
     if (!umma && (c->fp8 ? prefill_fp8_smem_bytes(c->head_dim) : prefill_smem_bytes(c->head_dim)) > (size_t)c->max_smem_optin)
@@ -1145,6 +1147,9 @@ int prefill_over(skv_cache *c, int src, const void *Q, const int32_t *cu_q_lens,
         dq.B = batch;
         dq.Hkv = c->kv_heads;
         dq.pt_stride = pt_stride;
+        dq.cu_q = cu_q_lens;
+        dq.window = window;
+        dq.sinks = sinks;
         if (launch_dequant_pages(dq, c->head_dim, pt_stride, st) != cudaSuccess) {
             (void)cudaGetLastError();
             return SKV_ERR_CUDA;
@@ -1152,6 +1157,22 @@ int prefill_over(skv_cache *c, int src, const void *Q, const int32_t *cu_q_lens,
         c->launches += 1;
         p.layer_base = c->prefill_scratch;
         p.page_stride = (int64_t)bf16_page;
+    }
+    if (umma && window) {
+        // (a launch holds its sequences' tables in shared memory: larger batches go in pieces)
+        for (int b = 0; b < batch; b += prefill_window_max_batch()) {
+            PrefillParams piece = p;
+            piece.cu_q = cu_q_lens + b;
+            piece.page_table = page_table + (size_t)b * pt_stride;
+            piece.seq_lens = seq_lens + b;
+            piece.B = batch - b < prefill_window_max_batch() ? batch - b : prefill_window_max_batch();
+            if (launch_prefill_window(piece, c->head_dim, G, max_q_len, c->sm_count, c->tune.pdl != 0, st) != cudaSuccess) {
+                (void)cudaGetLastError();
+                return SKV_ERR_CUDA;
+            }
+            c->launches += 1;
+        }
+        return SKV_OK;
     }
     const cudaError_t le = umma     ? launch_prefill_umma(p, c->head_dim, G, q_tiles, c->tune.pdl != 0, st)
                            : c->fp8 ? launch_prefill_fp8(p, c->head_dim, G, q_tiles, c->tune.pdl != 0, st)

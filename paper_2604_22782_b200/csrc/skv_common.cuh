@@ -171,6 +171,8 @@ struct DequantParams {
     const int32_t *page_table;  // [B][pt_stride]
     const int32_t *seq_lens;    // [B]
     int B, Hkv, pt_stride;
+    const int32_t *cu_q;        // sliding window (window > 0): only the pages that one of a sequence's rows sees
+    int window, sinks;
 };
 
 struct RopeParams {
@@ -256,6 +258,11 @@ size_t decode_cta_smem_bytes(int D, int B, int G, int consumers, int stages, boo
 bool decode_cta_can_merge(int D, int kernel);   // the variant (kernel: 0 CUDA cores, 1 tensor cores, 2 FP8 pages) can finish cut segments itself
 cudaError_t launch_decode_cta(const DecodeParams &p, int D, int G, int kernel, int grid, int consumers, int stages,
                               bool pdl, cudaStream_t s);
+// over a sliding window on the tensor cores (skv_prefill_window.cu): bf16 pages, any head ratio up to 8
+bool prefill_window_supported(int D, int G);
+int prefill_window_max_batch();
+size_t prefill_window_smem_bytes(int D, int B);
+cudaError_t launch_prefill_window(const PrefillParams &p, int D, int G, int max_q_len, int sm_count, bool pdl, cudaStream_t s);
 // rotary embedding with the update (skv_rope.cu); adjacent: pairs (2i, 2i+1)
 cudaError_t launch_rope_append(const RopeParams &p, int D, bool fp8, bool adjacent, bool pdl, cudaStream_t s);
 // a step's tables (skv_plan.cu); in_place: an output is the memory of an input

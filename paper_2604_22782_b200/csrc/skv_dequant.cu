@@ -5,6 +5,7 @@
 // over the pages costs a few per cent, where converting inside the attention kernel would put the
 // conversions on the warps that already set its pace.
 #include "skv_common.cuh"
+#include "skv_walk.cuh"
 
 namespace skv {
 
@@ -37,6 +38,12 @@ __global__ void __launch_bounds__(DQ_WARPS * 32) dequant_pages_kernel(DequantPar
     int n_b = __ldg(p.seq_lens + b);
     if ((int64_t)n_b > (int64_t)p.pt_stride * PAGE) n_b = p.pt_stride * PAGE;        // (flagged by the attention kernel)
     if (pg >= (n_b + PAGE - 1) / PAGE) return;                                        // warp-uniform
+    if (p.window > 0) {
+        const int q_len = __ldg(p.cu_q + b + 1) - __ldg(p.cu_q + b);
+        if (q_len <= 0 || q_len > n_b) return;                                        // (flagged by the attention kernel)
+        const WindowPages win = window_pages(n_b - q_len, n_b, p.window, p.sinks);
+        if (pg >= win.sink_pages && pg < win.sink_pages + win.gap) return;
+    }
     const int id = __ldg(p.page_table + (int64_t)b * p.pt_stride + pg);
     if (id < 0 || (int64_t)id >= p.max_pages) return;                                 // (flagged by the attention kernel)
     const uint4 *src = reinterpret_cast<const uint4 *>(p.fp8_base + (int64_t)id * p.fp8_page_stride + (int64_t)h * FB);
