@@ -2,22 +2,26 @@
 // tensor cores: the row at position pos attends  t <= pos  and  (t > pos - window  or  t < sinks).
 //
 // An item is (sequence, kv head, two neighbouring tiles of 128 query rows): row r of a tile = token r / G, head r % G.
-// The tiles share every K and V read.  A persistent CTA per SM takes items in turn; twelve warps:
+// The tiles share every K and V read.  A persistent CTA per SM takes its share of the items, which are dealt out by their
+// place in the sequence, furthest first (those have the most keys, where the window does not make all alike), back and forth
+// over the CTAs: within 2 % of the mean where every CTA has some, by count (dealt in the order of the rows: 15 % over it).
+// Twelve warps:
 //   warps 0-3, 4-7  softmax of tile 0 / tile 1: thread = row (TMEM lane)
-//   warp 8          lane 0 issues the tensor-core instructions of both tiles
-//   warp 9          copies K and V of the key blocks (128 keys = 8 pages of the item's list of pages, window_pages)
-//   warp 10         copies the queries of the next item as soon as the last scores of this one are done
-//   warp 11         blocks with tokens that no row of the item sees: zeroes their V rows, whatever they hold
-// Shared memory: Q of both tiles, K ring and V ring of two blocks each.  K is brought in 256-byte pieces (16 keys x one
-// 8-dim chunk) that interleave the pages by chunk, so that a block is ONE N = 128 operand: with N = 64 the tensor core reads
-// 6 KB of operands per 32 cycles of work and waits for shared memory.  V pages are copied as they are: an MN-major operand.
+//   warps 8, 9      lane 0 issues the tensor-core instructions of tile 0 / tile 1
+//   warps 10, 11    copy K and V of the even / odd key blocks (128 keys = 8 pages of the item's list of pages, window_pages) and,
+//                   as soon as the last scores of an item are done, the queries of the next one's tile 0 / tile 1; V rows of
+//                   tokens that no row of the item sees are zeroed, whatever they hold
+// Shared memory: Q of both tiles, K ring and V ring of two blocks each.  K is copied 16 bytes at a time so that the pages
+// interleave by chunk and a block is ONE N = 128 operand: with N = 64 the tensor core reads 6 KB of operands per 32 cycles
+// of work and waits for shared memory.  (As 256-byte bulk copies, 128 to a block, the warp that issues them was the slowest
+// part.)  V pages are copied as they are: an MN-major operand.
 // Tensor memory (512 columns): scores of tile 0 and 1 [128 each], overwritten in place by the probabilities (bf16), and
 // the outputs of tile 0 and 1.
 //
 // While one tile's softmax runs, the tensor core works on the other's products: per tile and block  P V(kb), then
-// Q K^T(kb + 1).  The tiles need not be in step -- a block that one tile does not see is skipped by that tile alone, and
-// one may be an item ahead -- so the issuing thread polls: whichever instruction has its operands ready goes out.
-// Blocks return to the copy warp in order, when neither tile needs them any more.
+// Q K^T(kb + 1).  A warp per tile issues them: one thread for both took 600 cycles of bookkeeping per tile and block and
+// was slower than the tensor core (210 us of issue for 127 us of products).  The tiles need not be in step -- a block that one
+// tile does not see is skipped by that tile alone.  A ring stage goes back to its copy warp when both tiles have done with it.
 // Softmax as in skv_prefill_umma.cu: the reference maximum moves only when it has grown by more than 2^8, so O is rarely
 // rescaled.  A row that has seen nothing yet counts from reference 0.
 // Every wait is bounded and ends early when another warp has given up; copies in flight get their wait before the end.
@@ -40,6 +44,7 @@ constexpr int KEYS = KB * PAGE;
 constexpr int THREADS = 384;
 constexpr int COL_O = 2 * KEYS;       // scores of tile s at column 128 s, its output at 256 + 128 s
 constexpr float RESCALE_STEP = 8.f;
+constexpr int BY_FMA = 4;             // every fourth pair of exponentials is computed on the FMA units
 constexpr int MAX_BATCH = 1024;       // sequences of a launch: their tables are in shared memory
 
 __host__ __device__ constexpr uint32_t instr_desc(int M, int N, bool b_mn_major)
@@ -53,29 +58,16 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar)
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// a look that never suspends the thread
-__device__ __forceinline__ bool test(uint32_t bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-
 // bounded (two seconds); ends early when another warp of the CTA has given up
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up)
 {
-    if (mbar_try_wait(bar, parity)) return true;
-    const uint64_t t0 = global_timer_ns();
+    uint64_t t0 = 0;
     for (;;) {
-        for (int i = 0; i < 64; ++i)
+        for (int i = 0; i < 256; ++i)
             if (mbar_try_wait(bar, parity)) return true;
-        if (*gave_up || global_timer_ns() - t0 > 2000000000ull) return false;
+        const uint64_t now = global_timer_ns();            // (a read takes long: not before the wait has become one)
+        if (t0 == 0) t0 = now;
+        if (*gave_up || now - t0 > 2000000000ull) return false;
     }
 }
 
@@ -93,22 +85,31 @@ struct Item {
     __device__ __forceinline__ int last(int s, int TQ) const { return first(s, TQ) + n[s] - 1; }
 };
 
-struct Tables {             // in shared memory, per sequence
-    const int32_t *prefix;  // items per kv head of the sequences before
+// In shared memory.  Of the sequences, most items first: how many items (per kv head) the r-th has, and how many lie at
+// places below that number in all sequences together, below[r] = r count[r] + count[r] + ... + count[B-1].
+struct Tables {
+    const int32_t *order, *count, *below;
     const int32_t *q_begin, *q_len, *lens;
 };
 
-// item x of the call; per_item: tokens of an item
-__device__ __forceinline__ Item item_at(const PrefillParams &p, const Tables &t, int64_t x, int TQ, int per_item)
+// item of round `round` of this CTA; per_item: tokens of an item.  False: no more.
+__device__ __forceinline__ bool item_at(Item &it, const PrefillParams &p, const Tables &t, int total, int round, int TQ, int per_item)
 {
-    const Cursor c = locate(t.prefix, p.B, p.Hkv, x);
-    Item it;
-    it.b = c.b;
-    it.h = c.h;
-    it.q_begin = t.q_begin[c.b];
-    it.q_len = t.q_len[c.b];
-    it.q0 = (c.pages - 1 - c.pg) * per_item;                  // the sequence's last tokens, with the most keys, first
-    it.pos0 = t.lens[c.b] - it.q_len;
+    const int x = round * (int)gridDim.x + ((round & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
+    if (x >= total) return false;
+    const int back = total - 1 - x, y = back / p.Hkv;       // places ascending, over the sequences that have one
+    it.h = back - y * p.Hkv;
+    int lo = 0, hi = p.B;                                   // the smallest r with below[r] <= y  (below[0] is all, below[B] = 0)
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (t.below[mid] <= y) hi = mid; else lo = mid;
+    }
+    const int d = y - t.below[hi], place = d / hi;          // the first hi sequences have an item there
+    it.b = t.order[d - place * hi];
+    it.q_begin = t.q_begin[it.b];
+    it.q_len = t.q_len[it.b];
+    it.q0 = (t.count[hi] + place) * per_item;
+    it.pos0 = t.lens[it.b] - it.q_len;
     const int left = it.q_len - it.q0;
     it.n[0] = left < TQ ? left : TQ;
     const int second = (left < per_item ? left : per_item) - TQ;
@@ -116,83 +117,93 @@ __device__ __forceinline__ Item item_at(const PrefillParams &p, const Tables &t,
     it.n_keys = it.pos0 + it.q0 + it.n[0] + it.n[1];
     it.win = window_pages(it.pos0 + it.q0, it.n_keys, p.window, p.sinks);
     it.blocks = (it.win.count + KB - 1) / KB;
-    return it;
+    return true;
 }
 
-// whether some row of tile s sees a key of block kb
-__device__ __forceinline__ bool needs(const Item &it, int s, int kb, int TQ, int window, int sinks)
+// The blocks that some row of tile s sees: [0, sinks) and [from, to), sinks <= from; and those of them, [clear_from, clear_to),
+// of which every row of the tile sees every key.
+struct Plan { int sinks, from, to, clear_from, clear_to; };
+
+__device__ __forceinline__ Plan plan_of(const Item &it, int s, int TQ, int window, int sinks)
 {
-    if (it.n[s] == 0) return false;
-    const int j0 = kb * KB, j1 = (j0 + KB < it.win.count ? j0 + KB : it.win.count) - 1;
-    if (sinks > 0 && j0 < it.win.sink_pages) return true;
-    const int first = it.first(s, TQ), lo = first >= window ? first - window + 1 : 0;
-    return it.win.page(j1) * PAGE + PAGE > lo && it.win.page(j0) * PAGE <= it.last(s, TQ);
+    const int first = it.first(s, TQ), last = it.last(s, TQ);
+    const int lo = first >= window ? first - window + 1 : 0;                  // first key that the tile's first row sees, sinks apart
+    const int lo_last = last >= window ? last - window + 1 : 0;              // ... and its last row
+    const int gap = it.win.gap, sink_blocks = sinks > 0 ? (it.win.sink_pages + KB - 1) / KB : 0;
+    Plan q;
+    q.to = (last / PAGE - gap) / KB + 1;                                     // (the page of a row's own key is behind the gap)
+    q.sinks = sink_blocks < q.to ? sink_blocks : q.to;
+    const int x = lo / PAGE - gap;
+    q.from = x > 0 ? x / KB : 0;
+    if (q.from < q.sinks) q.from = q.sinks;
+    const int c = (lo_last + PAGE - 1) / PAGE - gap, behind_gap = gap > 0 ? (it.win.sink_pages + KB - 1) / KB : 0;
+    q.clear_from = c > 0 ? (c + KB - 1) / KB : 0;
+    if (q.clear_from < behind_gap) q.clear_from = behind_gap;
+    const int e = (first + 1) / PAGE - gap;
+    q.clear_to = e > 0 ? e / KB : 0;
+    return q;
 }
 
-// A tile's walk over its blocks, item by item.  Every role that walks it gets the same sequence.
-struct Walk {
-    int64_t x;              // item
-    int kb;                 // block of the item
-    int g;                  // blocks of the CTA before it, of either tile
-    int turn;               // items of this tile before this one
-    bool first, last;       // block of this tile in the item
-    bool over;
-    Item it;
-};
-
-__device__ __forceinline__ void find(Walk &w, const PrefillParams &p, const Tables &t, int s, int64_t total, int TQ, int per_item, int from)
+// a pair of fp32 in one 64-bit register: one instruction works on both
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi)
 {
-    // the next block >= from of the item that the tile needs, else the first one of the next item
-    for (;;) {
-        int kb = from;
-        if (w.it.n[s] > 0)
-            while (kb < w.it.blocks && !needs(w.it, s, kb, TQ, p.window, p.sinks)) ++kb;
-        else
-            kb = w.it.blocks;
-        if (kb < w.it.blocks) {
-            w.g += kb - w.kb;
-            w.kb = kb;
-            int after = kb + 1;
-            while (after < w.it.blocks && !needs(w.it, s, after, TQ, p.window, p.sinks)) ++after;
-            w.last = after >= w.it.blocks;
-            return;
-        }
-        w.g += w.it.blocks - w.kb;
-        w.kb = 0;
-        if (w.it.n[s] > 0) ++w.turn;
-        w.first = true;
-        w.x += gridDim.x;
-        if (w.x >= total) {
-            w.over = true;
-            return;
-        }
-        w.it = item_at(p, t, w.x, TQ, per_item);
-        from = 0;
-    }
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void halves(uint64_t v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float ex2(float x)          // (fast_exp2 without its place in the order of volatile instructions)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 
-__device__ __forceinline__ Walk begin_walk(const PrefillParams &p, const Tables &t, int s, int64_t total, int TQ, int per_item)
+// 2^x of a pair on the FMA units: x = n + f with n the nearest integer, a polynomial for 2^f on [-1/2, 1/2] (least largest
+// relative error, by Remez exchange: 2.7e-6 in fp32, a thousandth of the rounding to bf16 that follows), times 2^n.
+// x is clamped to -126: a hidden key's probability comes out as 2^-126 instead of 0, next to a sum of 2^-8 or more.
+__device__ __forceinline__ void exp2_by_fma(uint64_t x, float &lo, float &hi)
 {
-    Walk w;
-    w.x = blockIdx.x;
-    w.kb = w.g = w.turn = 0;
-    w.first = true;
-    w.last = false;
-    w.over = w.x >= total;
-    if (w.over) return w;
-    w.it = item_at(p, t, w.x, TQ, per_item);
-    find(w, p, t, s, total, TQ, per_item, 0);
-    return w;
+    const float magic = 12582912.f;                    // 1.5 * 2^23: x + magic has the nearest integer in its low bits
+    float x0, x1;
+    halves(x, x0, x1);
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(x0) : "f"(x0), "f"(-126.f));
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(x1) : "f"(x1), "f"(-126.f));
+    x = pair_of(x0, x1);
+    const uint64_t r = add2(x, pair_of(magic, magic));
+    const uint64_t n = add2(r, pair_of(-magic, -magic));
+    const uint64_t f = fma2(n, pair_of(-1.f, -1.f), x);
+    uint64_t y = pair_of(0.009570102207362652f, 0.009570102207362652f);
+    y = fma2(y, f, pair_of(0.05591785907745361f, 0.05591785907745361f));
+    y = fma2(y, f, pair_of(0.240247443318367f, 0.240247443318367f));
+    y = fma2(y, f, pair_of(0.6931217908859253f, 0.6931217908859253f));
+    y = fma2(y, f, pair_of(0.9999992847442627f, 0.9999992847442627f));
+    float r0, r1;
+    halves(r, r0, r1);
+    const uint64_t power = pair_of(__int_as_float((__float_as_int(r0) << 23) + 0x3F800000), __int_as_float((__float_as_int(r1) << 23) + 0x3F800000));
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(y), "l"(power));       // (a NaN stays one)
+    halves(y, lo, hi);
 }
 
-__device__ __forceinline__ void next_block(Walk &w, const PrefillParams &p, const Tables &t, int s, int64_t total, int TQ, int per_item)
-{
-    w.first = false;
-    find(w, p, t, s, total, TQ, per_item, w.kb + 1);
-}
+template <int REGS>
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS)); }
+template <int REGS>
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS)); }
 
 // Dynamic shared memory: Q [2][D/8 chunks][128 rows][16 B] | K ring [2][D/8][128 keys][16 B] | V ring [2][8 pages][V half]
-//                        | barriers | tensor-memory address, gave_up | tables [4][B + 1]
+//                        | barriers | tensor-memory address, gave_up, items | tables [6][B + 1]
 template <int D>
 __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid_constant__ PrefillParams p, int G, int tiles, int max_q_len)
 {
@@ -211,16 +222,17 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
     const uint32_t q_full = bars + 80, q_free = bars + 96, s_ready = bars + 112, p_ready = bars + 128, o_ready = bars + 144, o_free = bars + 160;
     uint8_t *words = smem_raw + pad + 2 * Q_BYTES + 4 * STAGE + 176;
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(words), *gave_up = tmem_slot + 1;
-    int32_t *prefix = reinterpret_cast<int32_t *>(words + 16), *q_begin = prefix + p.B + 1, *q_len = q_begin + p.B + 1, *lens = q_len + p.B + 1;
-    const Tables tables = {prefix, q_begin, q_len, lens};
+    int32_t *order = reinterpret_cast<int32_t *>(words + 16), *count = order + p.B + 1, *below = count + p.B + 1;
+    int32_t *q_begin = below + p.B + 1, *q_len = q_begin + p.B + 1, *lens = q_len + p.B + 1;
+    const Tables tables = {order, count, below, q_begin, q_len, lens};
 
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(k_full + 8 * i, 1);
             mbar_init(v_full + 8 * i, 1);
             mbar_init(v_landed + 8 * i, 1);
-            mbar_init(k_empty + 8 * i, 1);
-            mbar_init(v_empty + 8 * i, 1);
+            mbar_init(k_empty + 8 * i, 2);
+            mbar_init(v_empty + 8 * i, 2);
             mbar_init(q_full + 8 * i, 1);
             mbar_init(q_free + 8 * i, 1);
             mbar_init(s_ready + 8 * i, 1);
@@ -237,246 +249,255 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
     }
     pdl_wait();
     pdl_trigger();
-    // the sequences' tables: items per kv head of the sequences before (warp 0)
-    if (warp == 0) {
+    // the sequences' tables
+    for (int i = tid; i < p.B; i += THREADS) {
+        const int qb = __ldg(p.cu_q + i), ql = __ldg(p.cu_q + i + 1) - qb, n = __ldg(p.seq_lens + i);
+        const bool fits = ql >= 0 && ql <= n && ql <= max_q_len && (int64_t)n <= (int64_t)p.pt_stride * PAGE;
+        if (!fits && blockIdx.x == 0) atomicOr(p.status, STATUS_BOUNDS);
+        q_begin[i] = qb;
+        q_len[i] = ql;
+        lens[i] = n;
+        below[i] = fits ? (ql + per_item - 1) / per_item : 0;            // (for now: the sequence's items)
+    }
+    __syncthreads();
+    for (int i = tid; i < p.B; i += THREADS) {                           // its place among the others, most items first
+        const int mine = below[i];
+        int before = 0;
+        for (int j = 0; j < p.B; ++j) before += below[j] > mine || (below[j] == mine && j < i);
+        order[before] = i;
+        count[before] = mine;
+    }
+    if (tid == 0) count[p.B] = 0;
+    __syncthreads();
+    if (warp == 0) {                                                     // sums from the back
         int carry = 0;
-        for (int i0 = 0; i0 < p.B; i0 += 32) {
-            const int i = i0 + lane;
-            int items = 0;
-            if (i < p.B) {
-                const int qb = __ldg(p.cu_q + i), ql = __ldg(p.cu_q + i + 1) - qb, n = __ldg(p.seq_lens + i);
-                const bool fits = ql >= 0 && ql <= n && ql <= max_q_len && (int64_t)n <= (int64_t)p.pt_stride * PAGE;
-                if (!fits && blockIdx.x == 0) atomicOr(p.status, STATUS_BOUNDS);
-                items = fits ? (ql + per_item - 1) / per_item : 0;
-                q_begin[i] = qb;
-                q_len[i] = ql;
-                lens[i] = n;
-            }
-            int sum = items;
+        for (int i0 = 0; i0 <= p.B; i0 += 32) {
+            const int r = p.B - i0 - lane;
+            const int c = r >= 0 ? count[r] : 0;
+            int sum = c;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
                 const int u = __shfl_up_sync(FULL, sum, d);
                 if (lane >= d) sum += u;
             }
-            if (i < p.B) prefix[i + 1] = carry + sum;
+            if (r >= 0) below[r] = r * c + carry + sum;
             carry += __shfl_sync(FULL, sum, 31);
         }
-        if (lane == 0) prefix[0] = 0;
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-    const int64_t total = (int64_t)prefix[p.B] * p.Hkv;
+    const int total = below[0] * p.Hkv;
     auto give_up = [&]() {
         atomicOr(p.status, STATUS_TIMEOUT);
         *gave_up = 1;
     };
-    int copied = 0;                                // copy warp: blocks sent
 
     if (warp < 8) {
         // =================== softmax ===================
+        more_registers<208>();
         const int s = warp >> 2, row = tid & (ROWS - 1);
         const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16), scores = lane_base + (uint32_t)(s * KEYS),
                        output = lane_base + (uint32_t)(COL_O + s * KEYS);
         const int qi = row / G, g = row - qi * G;
-        float m_used = -INFINITY, l_sum = 0.f;
+        const uint64_t scale2 = pair_of(p.scale_log2, p.scale_log2);
         bool ok = true;
-        int count = 0;                             // blocks of this tile so far
-        for (Walk w = begin_walk(p, tables, s, total, TQ, per_item); !w.over && ok; ++count) {
-            const Item &it = w.it;
-            if (w.first) {
-                m_used = -INFINITY;
-                l_sum = 0.f;
-            }
+        uint32_t phase = 0;                        // of s_ready: blocks of this tile so far
+        int turn = 0;                              // items of this tile so far
+        Item it;
+        for (int round = 0; ok && item_at(it, p, tables, total, round, TQ, per_item); ++round) {
+            if (it.n[s] == 0) continue;
+            const Plan plan = plan_of(it, s, TQ, p.window, p.sinks);
             const bool row_ok = qi < it.n[s];
-            const int pos = row_ok ? it.first(s, TQ) + qi : 0x7FFFFFFF;
-            ok = __all_sync(FULL, wait(s_ready + 8 * s, (uint32_t)(count & 1), gave_up));
-            if (!ok) break;
-            tc_fence_after();
-            uint32_t raw[4][32];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) tmem_ld32(scores + 32 * i, raw[i]);
-            tmem_wait_ld();
-            // most blocks are visible to every row of the tile: neither the causal edge, nor the window's, nor a gap or an end
-            const int j0 = w.kb * KB, np = it.win.count - j0 < KB ? it.win.count - j0 : KB;
-            const int t0 = it.win.page(j0) * PAGE, t1 = it.win.page(j0 + np - 1) * PAGE + PAGE - 1;
-            const int last = it.last(s, TQ), lo_last = last >= p.window ? last - p.window + 1 : 0;
-            const bool whole = np == KB && t1 - t0 == KEYS - 1 && t1 <= it.first(s, TQ) && (t0 >= lo_last || t1 < p.sinks);
-            if (!whole) {
-                const int lo = pos >= p.window ? pos - p.window + 1 : 0;
-#pragma unroll
-                for (int j = 0; j < KB; ++j) {
-                    const uint32_t bits = j < np ? window_bits(it.win.page(j0 + j), lo, pos < 0x7FFFFFFF ? pos + 1 : pos, p.sinks) : 0u;
-#pragma unroll
-                    for (int i = 0; i < PAGE; ++i)
-                        if (!((bits >> i) & 1u)) raw[j / 2][(j & 1) * PAGE + i] = 0xFF800000u;      // -inf
-                }
-            }
-            float mx4[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                mx4[i] = __uint_as_float(raw[i][0]);
-#pragma unroll
-                for (int c = 1; c < 32; ++c) mx4[i] = fmaxf(mx4[i], __uint_as_float(raw[i][c]));
-            }
-            const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * p.scale_log2;      // the scale is positive
-            float alpha = 1.f;
-            const bool move = mx > m_used + RESCALE_STEP;      // also true for the first key that the row sees
-            if (move) {
-                alpha = fast_exp2(m_used - mx);                // 0 when m_used = -inf
-                m_used = mx;
-            }
-            if (!w.first && __any_sync(FULL, move)) {
-                // (the scores of this block were issued after P V of the one before: O holds all blocks so far)
-#pragma unroll
-                for (int q = 0; q < D / 16; ++q) {
-                    uint32_t ov[16];
-                    tmem_ld16(output + 16 * q, ov);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int c = 0; c < 16; ++c) ov[c] = __float_as_uint(__uint_as_float(ov[c]) * alpha);
-                    tmem_st16(output + 16 * q, ov);
-                }
-            }
-            const float neg_m = m_used == -INFINITY ? 0.f : -m_used;
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                uint32_t pk[32];
-#pragma unroll
-                for (int c = 0; c < 32; ++c) {
-                    const int i = 2 * half + (c >> 4), cc = (2 * c) & 31;
-                    const float p0 = fast_exp2(fmaf(__uint_as_float(raw[i][cc]), p.scale_log2, neg_m));
-                    const float p1 = fast_exp2(fmaf(__uint_as_float(raw[i][cc + 1]), p.scale_log2, neg_m));
-                    sum[c & 3] += p0 + p1;
-                    pk[c] = pack_bf16x2(p0, p1);
-                }
-                tmem_st32(scores + 32 * half, pk);             // P over the first half of the tile's scores
-            }
-            l_sum = l_sum * alpha + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_ready + 8 * s);
-            if (w.last) {
-                ok = __all_sync(FULL, wait(o_ready + 8 * s, (uint32_t)(w.turn & 1), gave_up));
+            const int pos = row_ok ? it.first(s, TQ) + qi : 0x7FFFFFFE, lo = pos >= p.window ? pos - p.window + 1 : 0;
+            float m_used = -INFINITY, l_sum = 0.f;
+            const int first = plan.sinks > 0 ? 0 : plan.from;
+            for (int kb = first; kb < plan.to; kb = (kb + 1 < plan.sinks || kb + 1 >= plan.from) ? kb + 1 : plan.from) {
+                ok = __all_sync(FULL, wait(s_ready + 8 * s, phase, gave_up));
                 if (!ok) break;
+                phase ^= 1u;
                 tc_fence_after();
-                const float inv = 1.f / l_sum;
-                uint16_t *dst = p.out + ((int64_t)(it.q_begin + it.q0 + s * TQ + qi) * p.Hq + (int64_t)it.h * G + g) * D;
+                uint32_t raw[4][32];
 #pragma unroll
-                for (int q = 0; q < D / 32; ++q) {
-                    uint32_t ov[32];
-                    tmem_ld32(output + 32 * q, ov);
-                    tmem_wait_ld();
-                    if (q == D / 32 - 1) {                     // the output's columns may be used again
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(o_free + 8 * s);
-                    }
-                    if (row_ok) {
+                for (int i = 0; i < 4; ++i) tmem_ld32(scores + 32 * i, raw[i]);
+                tmem_wait_ld();
+                if (kb < plan.clear_from || kb >= plan.clear_to) {
+                    // the causal edge, the window's, a gap or an end: key by key
+                    const int j0 = kb * KB;
 #pragma unroll
-                        for (int c = 0; c < 32; c += 8) {
-                            uint4 v;
-                            v.x = pack_bf16x2(__uint_as_float(ov[c]) * inv, __uint_as_float(ov[c + 1]) * inv);
-                            v.y = pack_bf16x2(__uint_as_float(ov[c + 2]) * inv, __uint_as_float(ov[c + 3]) * inv);
-                            v.z = pack_bf16x2(__uint_as_float(ov[c + 4]) * inv, __uint_as_float(ov[c + 5]) * inv);
-                            v.w = pack_bf16x2(__uint_as_float(ov[c + 6]) * inv, __uint_as_float(ov[c + 7]) * inv);
-                            *reinterpret_cast<uint4 *>(dst + 32 * q + c) = v;
-                        }
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t b0 = j0 + 2 * i < it.win.count ? window_bits(it.win.page(j0 + 2 * i), lo, pos + 1, p.sinks) : 0u;
+                        const uint32_t b1 = j0 + 2 * i + 1 < it.win.count ? window_bits(it.win.page(j0 + 2 * i + 1), lo, pos + 1, p.sinks) : 0u;
+                        const uint32_t bits = b0 | (b1 << 16);
+#pragma unroll
+                        for (int c = 0; c < 32; ++c)
+                            if (!((bits >> c) & 1u)) raw[i][c] = 0xFF800000u;      // -inf
                     }
                 }
+                float mx4[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    mx4[i] = fmaxf(__uint_as_float(raw[i][0]), __uint_as_float(raw[i][1]));
+#pragma unroll
+                    for (int c = 2; c < 32; c += 2) mx4[i] = fmaxf(mx4[i], fmaxf(__uint_as_float(raw[i][c]), __uint_as_float(raw[i][c + 1])));
+                }
+                const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * p.scale_log2;      // the scale is positive
+                float alpha = 1.f;
+                const bool move = mx > m_used + RESCALE_STEP;      // also true for the first key that the row sees
+                if (move) {
+                    alpha = ex2(m_used - mx);                      // 0 when m_used = -inf
+                    m_used = mx;
+                }
+                if (kb != first && __any_sync(FULL, move)) {
+                    // (the scores of this block were issued after P V of the one before: O holds all blocks so far)
+#pragma unroll
+                    for (int q = 0; q < D / 16; ++q) {
+                        uint32_t ov[16];
+                        tmem_ld16(output + 16 * q, ov);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) ov[c] = __float_as_uint(__uint_as_float(ov[c]) * alpha);
+                        tmem_st16(output + 16 * q, ov);
+                    }
+                }
+                const float neg_m = m_used == -INFINITY ? 0.f : -m_used;
+                const uint64_t neg2 = pair_of(neg_m, neg_m);
+                uint64_t sum2[2] = {0ull, 0ull};
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t pk[32];
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) {
+                        const int i = 2 * half + (c >> 4), cc = (2 * c) & 31;
+                        const uint64_t x = fma2(pair_of(__uint_as_float(raw[i][cc]), __uint_as_float(raw[i][cc + 1])), scale2, neg2);
+                        float p0, p1;
+                        if (c % BY_FMA == BY_FMA - 1) {
+                            exp2_by_fma(x, p0, p1);
+                        } else {
+                            halves(x, p0, p1);
+                            p0 = ex2(p0);
+                            p1 = ex2(p1);
+                        }
+                        sum2[c & 1] = add2(sum2[c & 1], pair_of(p0, p1));
+                        pk[c] = pack_bf16x2(p0, p1);
+                    }
+                    tmem_st32(scores + 32 * half, pk);             // P over the first half of the tile's scores
+                }
+                float s0, s1;
+                halves(add2(sum2[0], sum2[1]), s0, s1);
+                l_sum = l_sum * alpha + (s0 + s1);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_ready + 8 * s);
             }
-            next_block(w, p, tables, s, total, TQ, per_item);
+            if (!ok) break;
+            ok = __all_sync(FULL, wait(o_ready + 8 * s, (uint32_t)(turn & 1), gave_up));
+            if (!ok) break;
+            ++turn;
+            tc_fence_after();
+            const float inv = 1.f / l_sum;
+            uint16_t *dst = p.out + ((int64_t)(it.q_begin + it.q0 + s * TQ + qi) * p.Hq + (int64_t)it.h * G + g) * D;
+            uint32_t packed[D / 2];
+#pragma unroll
+            for (int q = 0; q < D / 32; ++q) {
+                uint32_t ov[32];
+                tmem_ld32(output + 32 * q, ov);
+                tmem_wait_ld();
+#pragma unroll
+                for (int c = 0; c < 16; ++c) packed[16 * q + c] = pack_bf16x2(__uint_as_float(ov[2 * c]) * inv, __uint_as_float(ov[2 * c + 1]) * inv);
+            }
+            tc_fence_before();                     // the output's columns may be used again
+            __syncwarp();
+            if (lane == 0) mbar_arrive(o_free + 8 * s);
+            if (row_ok) {
+#pragma unroll
+                for (int c = 0; c < D / 2; c += 4)
+                    *reinterpret_cast<uint4 *>(dst + 2 * c) = make_uint4(packed[c], packed[c + 1], packed[c + 2], packed[c + 3]);
+            }
         }
         if (!ok && lane == 0) give_up();
-    } else if (warp == 8) {
+    } else if (warp < 10) {
         // =================== tensor-core issue ===================
+        fewer_registers<88>();
         if (lane == 0) {
-            struct Block { int g, np, turn; bool first, last; };
-            Walk w[2];
-            Block cur[2];
-            bool held[2] = {false, false};         // scores are out, P V of them is not
-            int count[2] = {0, 0};
-            int freed_k = -1, freed_v = -1;        // blocks given back
-#pragma unroll
-            for (int s = 0; s < 2; ++s) w[s] = begin_walk(p, tables, s, total, TQ, per_item);
-            uint64_t t0 = global_timer_ns();
+            const int s = warp - 8;
+            const uint32_t my_s = s_ready + 8 * s, my_p = p_ready + 8 * s;
+            const uint32_t scores = tmem + (uint32_t)(s * KEYS), output = tmem + (uint32_t)(COL_O + s * KEYS);
+            // descriptors of the first instruction of each kind; the others are a constant further on in the address field
+            const uint64_t q_desc = smem_desc(q_smem + (uint32_t)(s * Q_BYTES), ROWS * 16, 128);
+            const uint64_t k_desc = smem_desc(k_ring, KEYS * 16, 128), v_desc = smem_desc(v_ring, 128, PAGE * 16);
             bool ok = true;
-            int idle = 0;
-            while (ok && !(w[0].over && w[1].over && !held[0] && !held[1])) {
-                bool issued = false;
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    if (held[s]) {
-                        const Block &c = cur[s];
-                        const int st = c.g & 1;
-                        // P of this block; V (the stage's phase before this one is over: the block before it has been given back);
-                        // for an item's first block, the output of the item before has been read
-                        if (test(p_ready + 8 * s, (uint32_t)(count[s] & 1)) && c.g <= freed_v + 2 &&
-                            test(v_full + 8 * st, (uint32_t)((c.g >> 1) & 1)) &&
-                            (!c.first || c.turn == 0 || test(o_free + 8 * s, (uint32_t)((c.turn - 1) & 1)))) {
-                            tc_fence_after();
-                            for (int j = 0; j < c.np; ++j)
-                                umma_ts(tmem + (uint32_t)(COL_O + s * KEYS), tmem + (uint32_t)(s * KEYS + 8 * j),
-                                        smem_desc(v_ring + (uint32_t)(st * STAGE + j * HALF), 128, PAGE * 16), IDESC_PV, (c.first && j == 0) ? 0u : 1u);
-                            if (c.last) tc_commit(o_ready + 8 * s);
-                            held[s] = false;
-                            ++count[s];
-                            issued = true;
-                        }
+            int g0 = 0, turn = 0, count = 0;       // blocks before the item; items and blocks of the tile before it
+            Item it;
+            for (int round = 0; ok && item_at(it, p, tables, total, round, TQ, per_item); ++round) {
+                const bool mine = it.n[s] > 0;
+                Plan plan = {};
+                if (mine) plan = plan_of(it, s, TQ, p.window, p.sinks);
+                for (int kb = 0; kb < it.blocks && ok; ++kb) {
+                    const int g = g0 + kb, st = g & 1;
+                    const uint32_t parity = (uint32_t)((g >> 1) & 1);
+                    if (!mine || (kb >= plan.sinks && kb < plan.from) || kb >= plan.to) {
+                        // not this tile's: once it is there (and the stage's block before it thus gone), it may go
+                        ok = wait(k_full + 8 * st, parity, gave_up);
+                        if (ok) mbar_arrive(k_empty + 8 * st);
+                        ok = ok && wait(v_full + 8 * st, parity, gave_up);
+                        if (ok) mbar_arrive(v_empty + 8 * st);
+                        continue;
                     }
-                    if (!held[s] && !w[s].over) {
-                        const int gk = w[s].g, st = gk & 1;
-                        if (gk <= freed_k + 2 && test(k_full + 8 * st, (uint32_t)((gk >> 1) & 1)) &&
-                            (!w[s].first || test(q_full + 8 * s, (uint32_t)(w[s].turn & 1)))) {
-                            tc_fence_after();
+                    const bool first = kb == (plan.sinks > 0 ? 0 : plan.from);
+                    const bool last = kb == plan.to - 1 || (kb == plan.sinks - 1 && plan.from >= plan.to);
+                    if (first) ok = wait(q_full + 8 * s, (uint32_t)(turn & 1), gave_up);
+                    ok = ok && wait(k_full + 8 * st, parity, gave_up);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t kd = k_desc + (uint64_t)((st * STAGE) >> 4);
 #pragma unroll
-                            for (int ks = 0; ks < D / 16; ++ks)
-                                umma_ss(tmem + (uint32_t)(s * KEYS), smem_desc(q_smem + (uint32_t)(s * Q_BYTES + ks * 2 * ROWS * 16), ROWS * 16, 128),
-                                        smem_desc(k_ring + (uint32_t)(st * STAGE + ks * 2 * KEYS * 16), KEYS * 16, 128), IDESC_QK, ks > 0);
-                            tc_commit(s_ready + 8 * s);
-                            if (w[s].last) tc_commit(q_free + 8 * s);
-                            const int np = w[s].it.win.count - w[s].kb * KB;
-                            cur[s] = {gk, np < KB ? np : KB, w[s].turn, w[s].first, w[s].last};
-                            held[s] = true;
-                            next_block(w[s], p, tables, s, total, TQ, per_item);
-                            issued = true;
-                        }
+                    for (int ks = 0; ks < D / 16; ++ks)
+                        umma_ss(scores, q_desc + (uint64_t)((ks * 2 * ROWS * 16) >> 4), kd + (uint64_t)((ks * 2 * KEYS * 16) >> 4), IDESC_QK, ks > 0);
+                    tc_commit(my_s);
+                    tc_commit(k_empty + 8 * st);
+                    if (last) tc_commit(q_free + 8 * s);
+                    ok = wait(v_full + 8 * st, parity, gave_up);
+                    // an item's first block: the output of the item before has been read
+                    if (ok && first && turn > 0) ok = wait(o_free + 8 * s, (uint32_t)((turn - 1) & 1), gave_up);
+                    ok = ok && wait(my_p, (uint32_t)(count & 1), gave_up);
+                    if (!ok) break;
+                    ++count;
+                    tc_fence_after();
+                    const uint64_t vd = v_desc + (uint64_t)((st * STAGE) >> 4);
+                    const int np = it.win.count - kb * KB;
+                    if (np >= KB) {
+#pragma unroll
+                        for (int j = 0; j < KB; ++j)
+                            umma_ts(output, scores + (uint32_t)(8 * j), vd + (uint64_t)((j * HALF) >> 4), IDESC_PV, (first && j == 0) ? 0u : 1u);
+                    } else {
+                        for (int j = 0; j < np; ++j)
+                            umma_ts(output, scores + (uint32_t)(8 * j), vd + (uint64_t)((j * HALF) >> 4), IDESC_PV, (first && j == 0) ? 0u : 1u);
                     }
+                    tc_commit(v_empty + 8 * st);
+                    if (last) tc_commit(o_ready + 8 * s);
                 }
-                if (issued) {
-                    // blocks that neither tile needs any more go back, in order (a commit arrives when all work issued so far is done)
-                    const int k0 = w[0].over ? 0x7FFFFFFF : w[0].g, k1 = w[1].over ? 0x7FFFFFFF : w[1].g;
-                    const int v0 = held[0] ? cur[0].g : k0, v1 = held[1] ? cur[1].g : k1;
-                    int to_k = (k0 < k1 ? k0 : k1) - 1, to_v = (v0 < v1 ? v0 : v1) - 1;
-                    const int most_k = freed_k + 2, most_v = freed_v + 2;        // (never more than the ring holds)
-                    to_k = to_k < most_k ? to_k : most_k;
-                    to_v = to_v < most_v ? to_v : most_v;
-                    while (freed_k < to_k) tc_commit(k_empty + 8 * (++freed_k & 1));
-                    while (freed_v < to_v) tc_commit(v_empty + 8 * (++freed_v & 1));
-                    idle = 0;
-                } else if (++idle == 1024) {
-                    idle = 0;
-                    if (*gave_up) ok = false;
-                    const uint64_t now = global_timer_ns();
-                    if (now - t0 > 2000000000ull) ok = false;
-                }
-                if (issued) t0 = global_timer_ns();
+                g0 += it.blocks;
+                if (mine) ++turn;
             }
             // the last commits arrive while the barriers are still there
-            if (ok && freed_k >= 0) ok = wait(k_empty + 8 * (freed_k & 1), (uint32_t)((freed_k >> 1) & 1), gave_up);
-            if (ok && freed_v >= 0) ok = wait(v_empty + 8 * (freed_v & 1), (uint32_t)((freed_v >> 1) & 1), gave_up);
+            for (int j = g0 > 2 ? g0 - 2 : 0; j < g0 && ok; ++j)
+                ok = wait(k_empty + 8 * (j & 1), (uint32_t)((j >> 1) & 1), gave_up) && wait(v_empty + 8 * (j & 1), (uint32_t)((j >> 1) & 1), gave_up);
             if (!ok) give_up();
         }
         __syncwarp();
-    } else if (warp == 9) {
-        // =================== copies of K and V ===================
+    } else {
+        // =================== copies ===================
+        fewer_registers<88>();
+        const int s = warp - 10;                   // parity of the blocks (= their ring stage), and the tile whose queries are copied
+        const uint32_t my_k = k_ring + (uint32_t)(s * STAGE), my_v = v_ring + (uint32_t)(s * STAGE);
         bool ok = true;
-        int g = 0;
-        for (int64_t x = blockIdx.x; x < total && ok; x += gridDim.x) {
-            const Item it = item_at(p, tables, x, TQ, per_item);
+        int g0 = 0, turn = 0, seen = 0;            // blocks before the item; items of the tile before it; blocks that were zeroed in
+        int sent = 0;                              // V blocks sent for
+        Item it;
+        for (int round = 0; ok && item_at(it, p, tables, total, round, TQ, per_item); ++round) {
             const int32_t *row = p.page_table + (int64_t)it.b * p.pt_stride;
             auto load_id = [&](int kb) -> int {                // lane j: page j of a block
                 const int j = kb * KB + lane;
@@ -486,61 +507,9 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                 atomicOr(p.status, STATUS_BOUNDS);
                 return 0;
             };
-            int id = load_id(0);
-            for (int kb = 0; kb < it.blocks && ok; ++kb, ++g) {
-                const int st = g & 1, np = it.win.count - kb * KB < KB ? it.win.count - kb * KB : KB;
-                const uint32_t again = (uint32_t)(((g >> 1) - 1) & 1);
-                bool partial = false;
-                if (lane < np) partial = window_bits(it.win.page(kb * KB + lane), it.win.lo, it.n_keys, p.sinks) != 0xFFFFu;
-                partial = __any_sync(FULL, partial);
-                if (g >= 2) ok = __all_sync(FULL, wait(k_empty + 8 * st, again, gave_up));
-                if (!ok) break;
-                if (lane == 0) mbar_expect_tx(k_full + 8 * st, (uint32_t)(np * HALF));
-                __syncwarp();
-                // a piece: 16 keys of one chunk, 256 bytes of the page; lane = (page, every 4th chunk)
-                const int pj = lane & 7;
-                const int page_id = __shfl_sync(FULL, id, pj);
-                if (pj < np) {
-                    const uint8_t *src = p.layer_base + (int64_t)page_id * p.page_stride + (int64_t)it.h * BLOCK;
-                    const uint32_t dst = k_ring + (uint32_t)(st * STAGE + pj * PAGE * 16);
-#pragma unroll
-                    for (int c = lane >> 3; c < CH; c += 4) bulk_copy_g2s(dst + (uint32_t)(c * KEYS * 16), src + c * PAGE * 16, PAGE * 16, k_full + 8 * st);
-                }
-                const int next_id = load_id(kb + 1);
-                if (g >= 2) ok = __all_sync(FULL, wait(v_empty + 8 * st, again, gave_up));
-                const uint32_t bar = (partial ? v_landed : v_full) + 8 * st;
-                if (ok) {
-                    if (lane == 0) mbar_expect_tx(bar, (uint32_t)(np * HALF));
-                    __syncwarp();
-                    if (lane < np)
-                        bulk_copy_g2s(v_ring + (uint32_t)(st * STAGE + lane * HALF),
-                                      p.layer_base + (int64_t)id * p.page_stride + (int64_t)it.h * BLOCK + HALF, HALF, bar);
-                }
-                copied = g + 1;
-                id = next_id;
-            }
-        }
-        if (!ok && lane == 0) give_up();
-        // leave only when every copy has landed (normally long the case)
-        for (int j = copied > 2 ? copied - 2 : 0; j < copied; ++j) {
-            mbar_wait_bounded(k_full + 8 * (j & 1), (uint32_t)((j >> 1) & 1));
-            if (ok) mbar_wait_bounded(v_full + 8 * (j & 1), (uint32_t)((j >> 1) & 1));
-        }
-        if (!ok) {
-            // (after a failure a block's V may have come through either barrier, or not have been sent for: give it time instead)
-            const uint64_t t = global_timer_ns();
-            while (global_timer_ns() - t < 1000000ull) __nanosleep(1000);
-        }
-    } else if (warp == 10) {
-        // =================== queries ===================
-        bool ok = true;
-        int turn[2] = {0, 0};
-        for (int64_t x = blockIdx.x; x < total && ok; x += gridDim.x) {
-            const Item it = item_at(p, tables, x, TQ, per_item);
-            for (int s = 0; s < 2 && ok; ++s) {
-                if (it.n[s] == 0) continue;
-                if (turn[s] > 0) ok = __all_sync(FULL, wait(q_free + 8 * s, (uint32_t)((turn[s] - 1) & 1), gave_up));
-                if (!ok) break;
+            auto queries = [&]() -> bool {
+                if (it.n[s] == 0) return true;
+                if (turn > 0 && !__all_sync(FULL, wait(q_free + 8 * s, (uint32_t)((turn - 1) & 1), gave_up))) return false;
                 for (int r0 = 0; r0 < ROWS; r0 += 32) {
                     const int r = r0 + lane, qi = r / G, g = r - qi * G;
                     if (qi >= it.n[s]) continue;               // (such a row runs on whatever is there; nothing of it is stored)
@@ -552,46 +521,86 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
                 asm volatile("cp.async.wait_group 0;" ::: "memory");
-                fence_proxy_async();                           // the tensor core reads Q through the async proxy
+                fence_proxy_async();                           // the tensor core reads it through the async proxy
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_full + 8 * s);
-                ++turn[s];
+                ++turn;
+                return true;
+            };
+            // The item's first block before its queries: the block's stage comes free first.
+            bool asked = false;
+            int kb = (s - g0) & 1;
+            int id = load_id(kb);
+            if (kb != 0) {
+                ok = queries();
+                asked = true;
             }
-        }
-        if (!ok && lane == 0) give_up();
-    } else {
-        // =================== V rows that no row of the item sees ===================
-        bool ok = true;
-        int g = 0, seen[2] = {0, 0};
-        for (int64_t x = blockIdx.x; x < total && ok; x += gridDim.x) {
-            const Item it = item_at(p, tables, x, TQ, per_item);
-            for (int kb = 0; kb < it.blocks && ok; ++kb, ++g) {
-                const int st = g & 1, np = it.win.count - kb * KB < KB ? it.win.count - kb * KB : KB;
-                const uint32_t bits = lane < np ? window_bits(it.win.page(kb * KB + lane), it.win.lo, it.n_keys, p.sinks) : 0xFFFFu;
-                unsigned todo = __ballot_sync(FULL, bits != 0xFFFFu);
-                if (!todo) continue;
-                ok = __all_sync(FULL, wait(v_landed + 8 * st, (uint32_t)(seen[st] & 1), gave_up));
+            for (; ok && kb < it.blocks; kb += 2) {
+                const int g = g0 + kb, np = it.win.count - kb * KB < KB ? it.win.count - kb * KB : KB;
+                const uint32_t again = (uint32_t)(((g >> 1) - 1) & 1);
+                if (g >= 2) ok = __all_sync(FULL, wait(k_empty + 8 * s, again, gave_up));
                 if (!ok) break;
-                ++seen[st];
-                for (; todo; todo &= todo - 1) {
-                    const int j = __ffs(todo) - 1;
-                    const uint32_t set = __shfl_sync(FULL, bits, j);
-                    const uint32_t sV = v_ring + (uint32_t)(st * STAGE + j * HALF);
-                    for (int i = lane; i < CH * PAGE; i += 32)
-                        if (!((set >> (i & (PAGE - 1))) & 1u))
-                            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(sV + (uint32_t)(i * 16)), "r"(0u) : "memory");
+                for (int j = 0; j < np; ++j) {
+                    const int page_id = __shfl_sync(FULL, id, j);
+                    const uint8_t *src = p.layer_base + (int64_t)page_id * p.page_stride + (int64_t)it.h * BLOCK + lane * 16;
+                    const uint32_t dst = my_k + (uint32_t)(j * PAGE * 16 + (lane >> 4) * KEYS * 16 + (lane & 15) * 16);
+#pragma unroll
+                    for (int i = 0; i < CH / 2; ++i)           // two chunks of 16 keys each time
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (uint32_t)(i * 2 * KEYS * 16)), "l"(src + i * 512) : "memory");
                 }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                const uint32_t bits = lane < np ? window_bits(it.win.page(kb * KB + lane), it.win.lo, it.n_keys, p.sinks) : 0xFFFFu;
+                unsigned todo = __ballot_sync(FULL, bits != 0xFFFFu);        // pages with tokens that no row sees
+                const uint32_t bar = (todo ? v_landed : v_full) + 8 * s;
+                if (g >= 2) ok = __all_sync(FULL, wait(v_empty + 8 * s, again, gave_up));
+                if (ok) {
+                    if (lane == 0) mbar_expect_tx(bar, (uint32_t)(np * HALF));
+                    __syncwarp();
+                    if (lane < np)
+                        bulk_copy_g2s(my_v + (uint32_t)(lane * HALF), p.layer_base + (int64_t)id * p.page_stride + (int64_t)it.h * BLOCK + HALF, HALF, bar);
+                    sent = (g >> 1) + 1;
+                }
+                id = load_id(kb + 2);
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+                if (!ok) break;
                 fence_proxy_async();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(v_full + 8 * st);
+                if (lane == 0) mbar_arrive(k_full + 8 * s);
+                if (todo) {                                    // (few blocks: the first and the last of an item, and the sinks')
+                    ok = __all_sync(FULL, wait(bar, (uint32_t)(seen++ & 1), gave_up));
+                    if (!ok) break;
+                    for (; todo; todo &= todo - 1) {
+                        const int j = __ffs(todo) - 1;
+                        const uint32_t set = __shfl_sync(FULL, bits, j);
+                        for (int i = lane; i < CH * PAGE; i += 32)
+                            if (!((set >> (i & (PAGE - 1))) & 1u))
+                                asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(my_v + (uint32_t)(j * HALF + i * 16)), "r"(0u) : "memory");
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(v_full + 8 * s);
+                }
+                if (!asked) {
+                    ok = queries();
+                    asked = true;
+                }
             }
+            g0 += it.blocks;
         }
         if (!ok && lane == 0) give_up();
+        if (ok) {
+            // leave only when every copy has landed (normally long the case)
+            if (sent > 0) mbar_wait_bounded(v_full + 8 * s, (uint32_t)((sent - 1) & 1));
+        } else {
+            // after a failure it is not known which barrier a copy still in flight will come through: give it time
+            const uint64_t t = global_timer_ns();
+            while (global_timer_ns() - t < 1000000ull) __nanosleep(1000);
+        }
     }
     // ---- common exit ----
     tc_fence_before();
     __syncthreads();
-    if (warp == 10) asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (warp >= 10) asm volatile("cp.async.wait_group 0;" ::: "memory");
     if (warp == 8) {
         __syncwarp();
         tmem_dealloc(tmem, 512);
@@ -606,7 +615,7 @@ int prefill_window_max_batch() { return MAX_BATCH; }
 size_t prefill_window_smem_bytes(int D, int B)
 {
     if (D != 64 && D != 128) return 0;
-    return 128 + 2 * (size_t)ROWS * D * 2 + 4 * (size_t)KEYS * D * 2 + 176 + 16 + 4 * (size_t)(B + 1) * sizeof(int32_t);
+    return 128 + 2 * (size_t)ROWS * D * 2 + 4 * (size_t)KEYS * D * 2 + 176 + 16 + 6 * (size_t)(B + 1) * sizeof(int32_t);
 }
 
 cudaError_t launch_prefill_window(const PrefillParams &p, int D, int G, int max_q_len, int sm_count, bool pdl, cudaStream_t s)
