@@ -8,20 +8,21 @@
 // Twelve warps:
 //   warps 0-3, 4-7  softmax of tile 0 / tile 1: thread = row (TMEM lane)
 //   warps 8, 9      lane 0 issues the tensor-core instructions of tile 0 / tile 1
-//   warps 10, 11    copy K and V of the even / odd key blocks (128 keys = 8 pages of the item's list of pages, window_pages) and,
+//   warps 10, 11    copy K and V of the even / odd key blocks (64 keys = 4 pages of the item's list of pages, window_pages) and,
 //                   as soon as the last scores of an item are done, the queries of the next one's tile 0 / tile 1; V rows of
 //                   tokens that no row of the item sees are zeroed, whatever they hold
-// Shared memory: Q of both tiles, K ring and V ring of two blocks each.  K is copied 16 bytes at a time so that the pages
-// interleave by chunk and a block is ONE N = 128 operand: with N = 64 the tensor core reads 6 KB of operands per 32 cycles
-// of work and waits for shared memory.  (As 256-byte bulk copies, 128 to a block, the warp that issues them was the slowest
+// Shared memory: Q of both tiles, K ring and V ring of four blocks each.  K is copied 16 bytes at a time so that the pages
+// interleave by chunk and a block is one operand.  (As 256-byte bulk copies, the warp that issues them was the slowest
 // part.)  V pages are copied as they are: an MN-major operand.
-// Tensor memory (512 columns): scores of tile 0 and 1 [128 each], overwritten in place by the probabilities (bf16), and
-// the outputs of tile 0 and 1.
+// Tensor memory (512 columns): per tile two score buffers [64 each], each overwritten in place by the probabilities (bf16)
+// of its block, and the outputs of tile 0 and 1.
 //
-// While one tile's softmax runs, the tensor core works on the other's products: per tile and block  P V(kb), then
-// Q K^T(kb + 1).  A warp per tile issues them: one thread for both took 600 cycles of bookkeeping per tile and block and
-// was slower than the tensor core (210 us of issue for 127 us of products).  The tiles need not be in step -- a block that one
-// tile does not see is skipped by that tile alone.  A ring stage goes back to its copy warp when both tiles have done with it.
+// A tile's scores of block kb + 1 are issued before its softmax of block kb has finished, so the softmax warps find the next
+// scores ready.  (With blocks of 128 keys there is room for one buffer per tile: each block then waits for its own chain
+// softmax -> P V -> Q K^T, 6500 cycles of which the tensor core works 2100: 306 us where this takes XXX.)  A warp per tile
+// issues the instructions: one thread for both took 600 cycles of bookkeeping per tile and block and was slower than the tensor
+// core.  The tiles need not be in step -- a block that one tile does not see is skipped by that tile alone.  A ring stage
+// goes back to its copy warp when both tiles have done with it.
 // Softmax as in skv_prefill_umma.cu: the reference maximum moves only when it has grown by more than 2^8, so O is rarely
 // rescaled.  A row that has seen nothing yet counts from reference 0.
 // Every wait is bounded and ends early when another warp has given up; copies in flight get their wait before the end.
@@ -39,12 +40,14 @@ using namespace tc5;
 
 constexpr unsigned FULL = 0xFFFFFFFFu;
 constexpr int ROWS = 128;             // query rows of a tile
-constexpr int KB = 8;                 // pages of a key block
+constexpr int KB = 4;                 // pages of a key block
 constexpr int KEYS = KB * PAGE;
 constexpr int THREADS = 384;
-constexpr int COL_O = 2 * KEYS;       // scores of tile s at column 128 s, its output at 256 + 128 s
+constexpr int STAGES = 4;             // key blocks of the K ring and of the V ring
+constexpr int COL_O = 4 * KEYS;       // scores of tile s, buffer i at column 128 s + 64 i, its output at 256 + 128 s
 constexpr float RESCALE_STEP = 8.f;
 constexpr int BY_FMA = 4;             // every fourth pair of exponentials is computed on the FMA units
+constexpr int BAR_BYTES = 5 * 8 * STAGES + 3 * 32 + 3 * 16;
 constexpr int MAX_BATCH = 1024;       // sequences of a launch: their tables are in shared memory
 
 __host__ __device__ constexpr uint32_t instr_desc(int M, int N, bool b_mn_major)
@@ -58,17 +61,14 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar)
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// bounded (two seconds); ends early when another warp of the CTA has given up
+// Bounded, by a number of tries (some seconds); ends early when another warp of the CTA has given up.  As small a loop as
+// it gets: with a clock read in it, a wait that was already over cost 240 cycles more, a dozen times per block.
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up)
 {
-    uint64_t t0 = 0;
-    for (;;) {
-        for (int i = 0; i < 256; ++i)
-            if (mbar_try_wait(bar, parity)) return true;
-        const uint64_t now = global_timer_ns();            // (a read takes long: not before the wait has become one)
-        if (t0 == 0) t0 = now;
-        if (*gave_up || now - t0 > 2000000000ull) return false;
-    }
+#pragma unroll 1
+    for (uint32_t n = 0; !mbar_try_wait(bar, parity);)
+        if (++n == (1u << 24) || ((n & 1023u) == 0 && *gave_up)) return false;
+    return true;
 }
 
 // What an item is made of.
@@ -197,12 +197,20 @@ __device__ __forceinline__ void exp2_by_fma(uint64_t x, float &lo, float &hi)
     halves(y, lo, hi);
 }
 
+// one lane of the warp, the same one every time
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t is;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+    return is != 0;
+}
+
 template <int REGS>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS)); }
 template <int REGS>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS)); }
 
-// Dynamic shared memory: Q [2][D/8 chunks][128 rows][16 B] | K ring [2][D/8][128 keys][16 B] | V ring [2][8 pages][V half]
+// Dynamic shared memory: Q [2][D/8 chunks][128 rows][16 B] | K ring [4][D/8][64 keys][16 B] | V ring [4][4 pages][V half]
 //                        | barriers | tensor-memory address, gave_up, items | tables [6][B + 1]
 template <int D>
 __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid_constant__ PrefillParams p, int G, int tiles, int max_q_len)
@@ -211,33 +219,36 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
     constexpr int BLOCK = block_bytes(D), HALF = half_bytes(D), CH = D / 8;
     constexpr int Q_BYTES = ROWS * D * 2, STAGE = KEYS * D * 2;
     constexpr uint32_t IDESC_QK = instr_desc(ROWS, KEYS, false), IDESC_PV = instr_desc(ROWS, D, true);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(FULL, tid >> 5, 0);      // (known to be the same for the warp)
     const int TQ = ROWS / G, per_item = TQ * tiles;
 
     const uint32_t base = smem_u32(smem_raw);
     const uint32_t pad = (128u - (base & 127u)) & 127u;
-    const uint32_t q_smem = base + pad, k_ring = q_smem + 2 * Q_BYTES, v_ring = k_ring + 2 * STAGE, bars = v_ring + 2 * STAGE;
-    // one barrier per ring stage: copied, given back; per tile: the rest
-    const uint32_t k_full = bars, v_full = bars + 16, v_landed = bars + 32, k_empty = bars + 48, v_empty = bars + 64;
-    const uint32_t q_full = bars + 80, q_free = bars + 96, s_ready = bars + 112, p_ready = bars + 128, o_ready = bars + 144, o_free = bars + 160;
-    uint8_t *words = smem_raw + pad + 2 * Q_BYTES + 4 * STAGE + 176;
+    const uint32_t q_smem = base + pad, k_ring = q_smem + 2 * Q_BYTES, v_ring = k_ring + STAGES * STAGE, bars = v_ring + STAGES * STAGE;
+    // a barrier per ring stage: copied, given back; per tile and score buffer: scores, probabilities, P V; per tile: the rest
+    const uint32_t k_full = bars, v_full = k_full + 8 * STAGES, v_landed = v_full + 8 * STAGES, k_empty = v_landed + 8 * STAGES, v_empty = k_empty + 8 * STAGES;
+    const uint32_t s_ready = v_empty + 8 * STAGES, p_ready = s_ready + 32, pv_done = p_ready + 32;
+    const uint32_t q_full = pv_done + 32, q_free = q_full + 16, o_free = q_free + 16;
+    uint8_t *words = smem_raw + pad + 2 * Q_BYTES + 2 * STAGES * STAGE + BAR_BYTES;
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(words), *gave_up = tmem_slot + 1;
     int32_t *order = reinterpret_cast<int32_t *>(words + 16), *count = order + p.B + 1, *below = count + p.B + 1;
     int32_t *q_begin = below + p.B + 1, *q_len = q_begin + p.B + 1, *lens = q_len + p.B + 1;
     const Tables tables = {order, count, below, q_begin, q_len, lens};
 
     if (tid == 0) {
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < STAGES; ++i) {
             mbar_init(k_full + 8 * i, 1);
             mbar_init(v_full + 8 * i, 1);
             mbar_init(v_landed + 8 * i, 1);
             mbar_init(k_empty + 8 * i, 2);
             mbar_init(v_empty + 8 * i, 2);
+            mbar_init(s_ready + 8 * i, 1);         // (two tiles x two buffers)
+            mbar_init(p_ready + 8 * i, 4);
+            mbar_init(pv_done + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
             mbar_init(q_full + 8 * i, 1);
             mbar_init(q_free + 8 * i, 1);
-            mbar_init(s_ready + 8 * i, 1);
-            mbar_init(p_ready + 8 * i, 4);
-            mbar_init(o_ready + 8 * i, 1);
             mbar_init(o_free + 8 * i, 4);
         }
         *gave_up = 0;
@@ -298,13 +309,12 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
         // =================== softmax ===================
         more_registers<208>();
         const int s = warp >> 2, row = tid & (ROWS - 1);
-        const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16), scores = lane_base + (uint32_t)(s * KEYS),
-                       output = lane_base + (uint32_t)(COL_O + s * KEYS);
+        const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16), scores0 = lane_base + (uint32_t)(2 * s * KEYS),
+                       output = lane_base + (uint32_t)(COL_O + 2 * s * KEYS);
         const int qi = row / G, g = row - qi * G;
         const uint64_t scale2 = pair_of(p.scale_log2, p.scale_log2);
         bool ok = true;
-        uint32_t phase = 0;                        // of s_ready: blocks of this tile so far
-        int turn = 0;                              // items of this tile so far
+        int count = 0;                             // blocks of this tile so far
         Item it;
         for (int round = 0; ok && item_at(it, p, tables, total, round, TQ, per_item); ++round) {
             if (it.n[s] == 0) continue;
@@ -314,19 +324,20 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
             float m_used = -INFINITY, l_sum = 0.f;
             const int first = plan.sinks > 0 ? 0 : plan.from;
             for (int kb = first; kb < plan.to; kb = (kb + 1 < plan.sinks || kb + 1 >= plan.from) ? kb + 1 : plan.from) {
-                ok = __all_sync(FULL, wait(s_ready + 8 * s, phase, gave_up));
+                const int buf = count & 1, bar = 8 * (2 * s + buf);
+                const uint32_t phase = (uint32_t)((count >> 1) & 1), scores = scores0 + (uint32_t)(buf * KEYS);
+                ok = __all_sync(FULL, wait(s_ready + bar, phase, gave_up));
                 if (!ok) break;
-                phase ^= 1u;
                 tc_fence_after();
-                uint32_t raw[4][32];
+                uint32_t raw[2][32];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) tmem_ld32(scores + 32 * i, raw[i]);
+                for (int i = 0; i < 2; ++i) tmem_ld32(scores + 32 * i, raw[i]);
                 tmem_wait_ld();
                 if (kb < plan.clear_from || kb >= plan.clear_to) {
                     // the causal edge, the window's, a gap or an end: key by key
                     const int j0 = kb * KB;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < 2; ++i) {
                         const uint32_t b0 = j0 + 2 * i < it.win.count ? window_bits(it.win.page(j0 + 2 * i), lo, pos + 1, p.sinks) : 0u;
                         const uint32_t b1 = j0 + 2 * i + 1 < it.win.count ? window_bits(it.win.page(j0 + 2 * i + 1), lo, pos + 1, p.sinks) : 0u;
                         const uint32_t bits = b0 | (b1 << 16);
@@ -338,9 +349,10 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                 float mx4[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    mx4[i] = fmaxf(__uint_as_float(raw[i][0]), __uint_as_float(raw[i][1]));
+                    const uint32_t *r = raw[i >> 1] + (i & 1) * 16;
+                    mx4[i] = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 #pragma unroll
-                    for (int c = 2; c < 32; c += 2) mx4[i] = fmaxf(mx4[i], fmaxf(__uint_as_float(raw[i][c]), __uint_as_float(raw[i][c + 1])));
+                    for (int c = 2; c < 16; c += 2) mx4[i] = fmaxf(mx4[i], fmaxf(__uint_as_float(r[c]), __uint_as_float(r[c + 1])));
                 }
                 const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * p.scale_log2;      // the scale is positive
                 float alpha = 1.f;
@@ -350,7 +362,10 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                     m_used = mx;
                 }
                 if (kb != first && __any_sync(FULL, move)) {
-                    // (the scores of this block were issued after P V of the one before: O holds all blocks so far)
+                    // O has to hold all blocks so far (P V two blocks back is over: these scores were issued after it)
+                    ok = __all_sync(FULL, wait(pv_done + 8 * (2 * s + (buf ^ 1)), (uint32_t)(((count - 1) >> 1) & 1), gave_up));
+                    if (!ok) break;
+                    tc_fence_after();
 #pragma unroll
                     for (int q = 0; q < D / 16; ++q) {
                         uint32_t ov[16];
@@ -364,38 +379,35 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                 const float neg_m = m_used == -INFINITY ? 0.f : -m_used;
                 const uint64_t neg2 = pair_of(neg_m, neg_m);
                 uint64_t sum2[2] = {0ull, 0ull};
+                uint32_t pk[32];
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    uint32_t pk[32];
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) {
-                        const int i = 2 * half + (c >> 4), cc = (2 * c) & 31;
-                        const uint64_t x = fma2(pair_of(__uint_as_float(raw[i][cc]), __uint_as_float(raw[i][cc + 1])), scale2, neg2);
-                        float p0, p1;
-                        if (c % BY_FMA == BY_FMA - 1) {
-                            exp2_by_fma(x, p0, p1);
-                        } else {
-                            halves(x, p0, p1);
-                            p0 = ex2(p0);
-                            p1 = ex2(p1);
-                        }
-                        sum2[c & 1] = add2(sum2[c & 1], pair_of(p0, p1));
-                        pk[c] = pack_bf16x2(p0, p1);
+                for (int c = 0; c < 32; ++c) {
+                    const uint64_t x = fma2(pair_of(__uint_as_float(raw[c >> 4][(2 * c) & 31]), __uint_as_float(raw[c >> 4][(2 * c + 1) & 31])), scale2, neg2);
+                    float p0, p1;
+                    if (c % BY_FMA == BY_FMA - 1) {
+                        exp2_by_fma(x, p0, p1);
+                    } else {
+                        halves(x, p0, p1);
+                        p0 = ex2(p0);
+                        p1 = ex2(p1);
                     }
-                    tmem_st32(scores + 32 * half, pk);             // P over the first half of the tile's scores
+                    sum2[c & 1] = add2(sum2[c & 1], pair_of(p0, p1));
+                    pk[c] = pack_bf16x2(p0, p1);
                 }
+                tmem_st32(scores, pk);                             // P over the first half of its scores
                 float s0, s1;
                 halves(add2(sum2[0], sum2[1]), s0, s1);
                 l_sum = l_sum * alpha + (s0 + s1);
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_ready + 8 * s);
+                if (lane == 0) mbar_arrive(p_ready + bar);
+                ++count;
             }
             if (!ok) break;
-            ok = __all_sync(FULL, wait(o_ready + 8 * s, (uint32_t)(turn & 1), gave_up));
+            // the item's last P V
+            ok = __all_sync(FULL, wait(pv_done + 8 * (2 * s + ((count - 1) & 1)), (uint32_t)(((count - 1) >> 1) & 1), gave_up));
             if (!ok) break;
-            ++turn;
             tc_fence_after();
             const float inv = 1.f / l_sum;
             uint16_t *dst = p.out + ((int64_t)(it.q_begin + it.q0 + s * TQ + qi) * p.Hq + (int64_t)it.h * G + g) * D;
@@ -420,82 +432,113 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
         if (!ok && lane == 0) give_up();
     } else if (warp < 10) {
         // =================== tensor-core issue ===================
+        // The whole warp walks along and one lane issues: descriptors and barriers are then the same for the warp as far as the
+        // compiler can see, and stay in uniform registers.  (In a branch of lane 0 alone every instruction moved them there anew:
+        // 60 to 100 cycles each, 2600 per tile and block.)
         fewer_registers<88>();
-        if (lane == 0) {
+        {
+            const bool leader = elect_one();
             const int s = warp - 8;
-            const uint32_t my_s = s_ready + 8 * s, my_p = p_ready + 8 * s;
-            const uint32_t scores = tmem + (uint32_t)(s * KEYS), output = tmem + (uint32_t)(COL_O + s * KEYS);
+            const uint32_t scores0 = tmem + (uint32_t)(2 * s * KEYS), output = tmem + (uint32_t)(COL_O + 2 * s * KEYS);
             // descriptors of the first instruction of each kind; the others are a constant further on in the address field
             const uint64_t q_desc = smem_desc(q_smem + (uint32_t)(s * Q_BYTES), ROWS * 16, 128);
             const uint64_t k_desc = smem_desc(k_ring, KEYS * 16, 128), v_desc = smem_desc(v_ring, 128, PAGE * 16);
             bool ok = true;
+            auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(FULL, wait(bar, parity, gave_up)) != 0; };
+            auto uniform = [](int v) { return __shfl_sync(FULL, v, 0); };
             int g0 = 0, turn = 0, count = 0;       // blocks before the item; items and blocks of the tile before it
             Item it;
             for (int round = 0; ok && item_at(it, p, tables, total, round, TQ, per_item); ++round) {
                 const bool mine = it.n[s] > 0;
                 Plan plan = {};
                 if (mine) plan = plan_of(it, s, TQ, p.window, p.sinks);
-                for (int kb = 0; kb < it.blocks && ok; ++kb) {
-                    const int g = g0 + kb, st = g & 1;
-                    const uint32_t parity = (uint32_t)((g >> 1) & 1);
-                    if (!mine || (kb >= plan.sinks && kb < plan.from) || kb >= plan.to) {
+                // Step kb: the scores of block kb, then P V of the tile's block before it.
+                int held = -1;                     // the block whose P V is still to come
+                bool begun = false;                // the item's output has a first block
+                for (int kb = 0; ok && (kb < it.blocks || held >= 0); ++kb) {
+                    const int g = uniform(g0 + kb), st = g & (STAGES - 1);
+                    const uint32_t parity = (uint32_t)((g / STAGES) & 1);
+                    const bool there = kb < it.blocks, wanted = there && mine && kb < plan.to && (kb < plan.sinks || kb >= plan.from);
+                    if (wanted) {
+                        const bool first = held < 0 && !begun;
+                        if (first) ok = wait_all(q_full + 8 * s, (uint32_t)(turn & 1));
+                        ok = ok && wait_all(k_full + 8 * st, parity);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const int buf = uniform(count & 1);
+                        const uint32_t bar = 8 * (2 * s + buf), scores = scores0 + (uint32_t)(buf * KEYS);
+                        const uint64_t kd = k_desc + (uint64_t)((st * STAGE) >> 4);
+                        const bool final = kb == plan.to - 1 || (kb == plan.sinks - 1 && plan.from >= plan.to);
+                        if (leader) {
+#pragma unroll
+                            for (int ks = 0; ks < D / 16; ++ks)
+                                umma_ss(scores, q_desc + (uint64_t)((ks * 2 * ROWS * 16) >> 4), kd + (uint64_t)((ks * 2 * KEYS * 16) >> 4), IDESC_QK, ks > 0);
+                            tc_commit(s_ready + bar);
+                            tc_commit(k_empty + 8 * st);
+                            if (final) tc_commit(q_free + 8 * s);
+                        }
+                        __syncwarp();
+                        ++count;
+                    }
+                    if (held >= 0) {
+                        const int gh = uniform(g0 + held), sth = gh & (STAGES - 1), nth = uniform(count - (wanted ? 2 : 1));
+                        const uint32_t bar = 8 * (2 * s + (nth & 1)), scores = scores0 + (uint32_t)((nth & 1) * KEYS);
+                        ok = wait_all(v_full + 8 * sth, (uint32_t)((gh / STAGES) & 1));
+                        // an item's first block: the output of the item before has been read
+                        if (ok && !begun && turn > 0) ok = wait_all(o_free + 8 * s, (uint32_t)((turn - 1) & 1));
+                        ok = ok && wait_all(p_ready + bar, (uint32_t)((nth >> 1) & 1));
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint64_t vd = v_desc + (uint64_t)((sth * STAGE) >> 4);
+                        const int np = uniform(it.win.count - held * KB);
+                        if (leader) {
+#pragma unroll
+                            for (int j = 0; j < KB; ++j)
+                                if (j < np)
+                                    umma_ts(output, scores + (uint32_t)(8 * j), vd + (uint64_t)((j * HALF) >> 4), IDESC_PV, (begun || j > 0) ? 1u : 0u);
+                            tc_commit(pv_done + bar);
+                            tc_commit(v_empty + 8 * sth);
+                        }
+                        __syncwarp();
+                        begun = true;
+                        held = -1;
+                    }
+                    if (wanted) {
+                        held = kb;
+                    } else if (there) {
                         // not this tile's: once it is there (and the stage's block before it thus gone), it may go
-                        ok = wait(k_full + 8 * st, parity, gave_up);
-                        if (ok) mbar_arrive(k_empty + 8 * st);
-                        ok = ok && wait(v_full + 8 * st, parity, gave_up);
-                        if (ok) mbar_arrive(v_empty + 8 * st);
-                        continue;
+                        ok = wait_all(k_full + 8 * st, parity);
+                        if (ok && leader) mbar_arrive(k_empty + 8 * st);
+                        ok = ok && wait_all(v_full + 8 * st, parity);
+                        if (ok && leader) mbar_arrive(v_empty + 8 * st);
+                        __syncwarp();
                     }
-                    const bool first = kb == (plan.sinks > 0 ? 0 : plan.from);
-                    const bool last = kb == plan.to - 1 || (kb == plan.sinks - 1 && plan.from >= plan.to);
-                    if (first) ok = wait(q_full + 8 * s, (uint32_t)(turn & 1), gave_up);
-                    ok = ok && wait(k_full + 8 * st, parity, gave_up);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint64_t kd = k_desc + (uint64_t)((st * STAGE) >> 4);
-#pragma unroll
-                    for (int ks = 0; ks < D / 16; ++ks)
-                        umma_ss(scores, q_desc + (uint64_t)((ks * 2 * ROWS * 16) >> 4), kd + (uint64_t)((ks * 2 * KEYS * 16) >> 4), IDESC_QK, ks > 0);
-                    tc_commit(my_s);
-                    tc_commit(k_empty + 8 * st);
-                    if (last) tc_commit(q_free + 8 * s);
-                    ok = wait(v_full + 8 * st, parity, gave_up);
-                    // an item's first block: the output of the item before has been read
-                    if (ok && first && turn > 0) ok = wait(o_free + 8 * s, (uint32_t)((turn - 1) & 1), gave_up);
-                    ok = ok && wait(my_p, (uint32_t)(count & 1), gave_up);
-                    if (!ok) break;
-                    ++count;
-                    tc_fence_after();
-                    const uint64_t vd = v_desc + (uint64_t)((st * STAGE) >> 4);
-                    const int np = it.win.count - kb * KB;
-                    if (np >= KB) {
-#pragma unroll
-                        for (int j = 0; j < KB; ++j)
-                            umma_ts(output, scores + (uint32_t)(8 * j), vd + (uint64_t)((j * HALF) >> 4), IDESC_PV, (first && j == 0) ? 0u : 1u);
-                    } else {
-                        for (int j = 0; j < np; ++j)
-                            umma_ts(output, scores + (uint32_t)(8 * j), vd + (uint64_t)((j * HALF) >> 4), IDESC_PV, (first && j == 0) ? 0u : 1u);
-                    }
-                    tc_commit(v_empty + 8 * st);
-                    if (last) tc_commit(o_ready + 8 * s);
                 }
                 g0 += it.blocks;
                 if (mine) ++turn;
             }
             // the last commits arrive while the barriers are still there
-            for (int j = g0 > 2 ? g0 - 2 : 0; j < g0 && ok; ++j)
-                ok = wait(k_empty + 8 * (j & 1), (uint32_t)((j >> 1) & 1), gave_up) && wait(v_empty + 8 * (j & 1), (uint32_t)((j >> 1) & 1), gave_up);
-            if (!ok) give_up();
+            for (int j = g0 > STAGES ? g0 - STAGES : 0; j < g0 && ok; ++j)
+                ok = wait_all(k_empty + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1)) &&
+                     wait_all(v_empty + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1));
+            if (!ok && leader) give_up();
         }
-        __syncwarp();
     } else {
         // =================== copies ===================
         fewer_registers<88>();
-        const int s = warp - 10;                   // parity of the blocks (= their ring stage), and the tile whose queries are copied
-        const uint32_t my_k = k_ring + (uint32_t)(s * STAGE), my_v = v_ring + (uint32_t)(s * STAGE);
+        const int s = warp - 10;                   // parity of the blocks, and the tile whose queries are copied
         bool ok = true;
-        int g0 = 0, turn = 0, seen = 0;            // blocks before the item; items of the tile before it; blocks that were zeroed in
-        int sent = 0;                              // V blocks sent for
+        int g0 = 0, turn = 0;                      // blocks before the item; items of the tile before it
+        int sent = -1;                             // the last V block sent for
+        int pending = -1;                          // the block whose K is on its way
+        uint32_t zeroed = 0;                       // bit per ring stage: parity of the blocks that came through v_landed
+        // the copies of K on their way have landed: the tensor core reads them through the async proxy
+        auto publish = [&]() {
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(k_full + 8 * (pending & (STAGES - 1)));
+            pending = -1;
+        };
         Item it;
         for (int round = 0; ok && item_at(it, p, tables, total, round, TQ, per_item); ++round) {
             const int32_t *row = p.page_table + (int64_t)it.b * p.pt_stride;
@@ -521,7 +564,8 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
                 asm volatile("cp.async.wait_group 0;" ::: "memory");
-                fence_proxy_async();                           // the tensor core reads it through the async proxy
+                if (pending >= 0) publish();
+                fence_proxy_async();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_full + 8 * s);
                 ++turn;
@@ -536,39 +580,48 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                 asked = true;
             }
             for (; ok && kb < it.blocks; kb += 2) {
-                const int g = g0 + kb, np = it.win.count - kb * KB < KB ? it.win.count - kb * KB : KB;
-                const uint32_t again = (uint32_t)(((g >> 1) - 1) & 1);
-                if (g >= 2) ok = __all_sync(FULL, wait(k_empty + 8 * s, again, gave_up));
+                const int g = g0 + kb, st = g & (STAGES - 1), np = it.win.count - kb * KB < KB ? it.win.count - kb * KB : KB;
+                const uint32_t again = (uint32_t)((g / STAGES - 1) & 1);
+                if (g >= STAGES) ok = __all_sync(FULL, wait(k_empty + 8 * st, again, gave_up));
                 if (!ok) break;
                 for (int j = 0; j < np; ++j) {
                     const int page_id = __shfl_sync(FULL, id, j);
                     const uint8_t *src = p.layer_base + (int64_t)page_id * p.page_stride + (int64_t)it.h * BLOCK + lane * 16;
-                    const uint32_t dst = my_k + (uint32_t)(j * PAGE * 16 + (lane >> 4) * KEYS * 16 + (lane & 15) * 16);
+                    const uint32_t dst = k_ring + (uint32_t)(st * STAGE + j * PAGE * 16 + (lane >> 4) * KEYS * 16 + (lane & 15) * 16);
 #pragma unroll
                     for (int i = 0; i < CH / 2; ++i)           // two chunks of 16 keys each time
                         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (uint32_t)(i * 2 * KEYS * 16)), "l"(src + i * 512) : "memory");
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
+                // the block before it in this warp's turn has landed by now, or is waited for while this one is under way
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
+                if (pending >= 0) publish();
+                pending = g;
                 const uint32_t bits = lane < np ? window_bits(it.win.page(kb * KB + lane), it.win.lo, it.n_keys, p.sinks) : 0xFFFFu;
                 unsigned todo = __ballot_sync(FULL, bits != 0xFFFFu);        // pages with tokens that no row sees
-                const uint32_t bar = (todo ? v_landed : v_full) + 8 * s;
-                if (g >= 2) ok = __all_sync(FULL, wait(v_empty + 8 * s, again, gave_up));
-                if (ok) {
-                    if (lane == 0) mbar_expect_tx(bar, (uint32_t)(np * HALF));
+                const uint32_t bar = (todo ? v_landed : v_full) + 8 * st, my_v = v_ring + (uint32_t)(st * STAGE);
+                if (g >= STAGES) {
+                    // (V comes back later than K: what is on its way of K goes out first)
+                    if (!__all_sync(FULL, mbar_try_wait(v_empty + 8 * st, again))) {
+                        asm volatile("cp.async.wait_group 0;" ::: "memory");
+                        publish();                     // (pending: this very block)
+                        ok = __all_sync(FULL, wait(v_empty + 8 * st, again, gave_up));
+                    }
                     __syncwarp();
-                    if (lane < np)
-                        bulk_copy_g2s(my_v + (uint32_t)(lane * HALF), p.layer_base + (int64_t)id * p.page_stride + (int64_t)it.h * BLOCK + HALF, HALF, bar);
-                    sent = (g >> 1) + 1;
                 }
-                id = load_id(kb + 2);
-                asm volatile("cp.async.wait_group 0;" ::: "memory");
                 if (!ok) break;
-                fence_proxy_async();
+                if (lane == 0) mbar_expect_tx(bar, (uint32_t)(np * HALF));
                 __syncwarp();
-                if (lane == 0) mbar_arrive(k_full + 8 * s);
+                if (lane < np)
+                    bulk_copy_g2s(my_v + (uint32_t)(lane * HALF), p.layer_base + (int64_t)id * p.page_stride + (int64_t)it.h * BLOCK + HALF, HALF, bar);
+                sent = g;
+                id = load_id(kb + 2);
                 if (todo) {                                    // (few blocks: the first and the last of an item, and the sinks')
-                    ok = __all_sync(FULL, wait(bar, (uint32_t)(seen++ & 1), gave_up));
+                    asm volatile("cp.async.wait_group 0;" ::: "memory");
+                    if (pending >= 0) publish();
+                    ok = __all_sync(FULL, wait(bar, (zeroed >> st) & 1u, gave_up));
                     if (!ok) break;
+                    zeroed ^= 1u << st;
                     for (; todo; todo &= todo - 1) {
                         const int j = __ffs(todo) - 1;
                         const uint32_t set = __shfl_sync(FULL, bits, j);
@@ -578,19 +631,23 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                     }
                     fence_proxy_async();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(v_full + 8 * s);
+                    if (lane == 0) mbar_arrive(v_full + 8 * st);
                 }
                 if (!asked) {
                     ok = queries();
                     asked = true;
                 }
             }
+            // an item's last K goes out with it
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            if (ok && pending >= 0) publish();
             g0 += it.blocks;
         }
         if (!ok && lane == 0) give_up();
         if (ok) {
             // leave only when every copy has landed (normally long the case)
-            if (sent > 0) mbar_wait_bounded(v_full + 8 * s, (uint32_t)((sent - 1) & 1));
+            for (int j = sent - 2; j <= sent; j += 2)
+                if (j >= 0) mbar_wait_bounded(v_full + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1));
         } else {
             // after a failure it is not known which barrier a copy still in flight will come through: give it time
             const uint64_t t = global_timer_ns();
@@ -615,7 +672,7 @@ int prefill_window_max_batch() { return MAX_BATCH; }
 size_t prefill_window_smem_bytes(int D, int B)
 {
     if (D != 64 && D != 128) return 0;
-    return 128 + 2 * (size_t)ROWS * D * 2 + 4 * (size_t)KEYS * D * 2 + 176 + 16 + 6 * (size_t)(B + 1) * sizeof(int32_t);
+    return 128 + 2 * (size_t)ROWS * D * 2 + 2 * STAGES * (size_t)KEYS * D * 2 + BAR_BYTES + 16 + 6 * (size_t)(B + 1) * sizeof(int32_t);
 }
 
 cudaError_t launch_prefill_window(const PrefillParams &p, int D, int G, int max_q_len, int sm_count, bool pdl, cudaStream_t s)
