@@ -25,7 +25,7 @@
 // goes back to its copy warp when both tiles have done with it.
 // Softmax as in skv_prefill_umma.cu: the reference maximum moves only when it has grown by more than 2^8, so O is rarely
 // rescaled.  A row that has seen nothing yet counts from reference 0.
-// Every wait is bounded and ends early when another warp has given up; copies in flight get their wait before the end.
+// Every wait is bounded; copies in flight get their wait before the end.
 #include "skv_common.cuh"
 #include "skv_tcgen05.cuh"
 #include "skv_walk.cuh"
@@ -61,14 +61,19 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar)
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// Bounded, by a number of tries (some seconds); ends early when another warp of the CTA has given up.  As small a loop as
-// it gets: with a clock read in it, a wait that was already over cost 240 cycles more, a dozen times per block.
-__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up)
+// By a whole warp.  Bounded, by a number of tries (some seconds).  A wait that runs out raises gave_up; everybody's waits
+// then end after a few tries, and the CTA runs through to its end on whatever it finds, which stays inside its buffers.
+// As small a loop as it gets and nothing to ask afterwards: with a clock read in it, and a vote and a branch on the outcome
+// after it, a wait that was already over cost 340 cycles, several of them per tile and block.
+__device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile uint32_t *gave_up)
 {
 #pragma unroll 1
-    for (uint32_t n = 0; !mbar_try_wait(bar, parity);)
-        if (++n == (1u << 24) || ((n & 1023u) == 0 && *gave_up)) return false;
-    return true;
+    for (uint32_t n = 1; !mbar_try_wait(bar, parity); ++n)
+        if ((n & 255u) == 0 && (n >> 24 || *gave_up)) {
+            *gave_up = 1;
+            break;
+        }
+    __syncwarp();
 }
 
 // What an item is made of.
@@ -300,10 +305,6 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     const int total = below[0] * p.Hkv;
-    auto give_up = [&]() {
-        atomicOr(p.status, STATUS_TIMEOUT);
-        *gave_up = 1;
-    };
 
     if (warp < 8) {
         // =================== softmax ===================
@@ -313,10 +314,9 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                        output = lane_base + (uint32_t)(COL_O + 2 * s * KEYS);
         const int qi = row / G, g = row - qi * G;
         const uint64_t scale2 = pair_of(p.scale_log2, p.scale_log2);
-        bool ok = true;
         int count = 0;                             // blocks of this tile so far
         Item it;
-        for (int round = 0; ok && item_at(it, p, tables, total, round, TQ, per_item); ++round) {
+        for (int round = 0; item_at(it, p, tables, total, round, TQ, per_item); ++round) {
             if (it.n[s] == 0) continue;
             const Plan plan = plan_of(it, s, TQ, p.window, p.sinks);
             const bool row_ok = qi < it.n[s];
@@ -326,8 +326,7 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
             for (int kb = first; kb < plan.to; kb = (kb + 1 < plan.sinks || kb + 1 >= plan.from) ? kb + 1 : plan.from) {
                 const int buf = count & 1, bar = 8 * (2 * s + buf);
                 const uint32_t phase = (uint32_t)((count >> 1) & 1), scores = scores0 + (uint32_t)(buf * KEYS);
-                ok = __all_sync(FULL, wait(s_ready + bar, phase, gave_up));
-                if (!ok) break;
+                wait(s_ready + bar, phase, gave_up);
                 tc_fence_after();
                 uint32_t raw[2][32];
 #pragma unroll
@@ -363,8 +362,7 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                 }
                 if (kb != first && __any_sync(FULL, move)) {
                     // O has to hold all blocks so far (P V two blocks back is over: these scores were issued after it)
-                    ok = __all_sync(FULL, wait(pv_done + 8 * (2 * s + (buf ^ 1)), (uint32_t)(((count - 1) >> 1) & 1), gave_up));
-                    if (!ok) break;
+                    wait(pv_done + 8 * (2 * s + (buf ^ 1)), (uint32_t)(((count - 1) >> 1) & 1), gave_up);
                     tc_fence_after();
 #pragma unroll
                     for (int q = 0; q < D / 16; ++q) {
@@ -404,10 +402,8 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                 if (lane == 0) mbar_arrive(p_ready + bar);
                 ++count;
             }
-            if (!ok) break;
             // the item's last P V
-            ok = __all_sync(FULL, wait(pv_done + 8 * (2 * s + ((count - 1) & 1)), (uint32_t)(((count - 1) >> 1) & 1), gave_up));
-            if (!ok) break;
+            wait(pv_done + 8 * (2 * s + ((count - 1) & 1)), (uint32_t)(((count - 1) >> 1) & 1), gave_up);
             tc_fence_after();
             const float inv = 1.f / l_sum;
             uint16_t *dst = p.out + ((int64_t)(it.q_begin + it.q0 + s * TQ + qi) * p.Hq + (int64_t)it.h * G + g) * D;
@@ -429,7 +425,6 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                     *reinterpret_cast<uint4 *>(dst + 2 * c) = make_uint4(packed[c], packed[c + 1], packed[c + 2], packed[c + 3]);
             }
         }
-        if (!ok && lane == 0) give_up();
     } else if (warp < 10) {
         // =================== tensor-core issue ===================
         // The whole warp walks along and one lane issues: descriptors and barriers are then the same for the warp as far as the
@@ -443,27 +438,24 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
             // descriptors of the first instruction of each kind; the others are a constant further on in the address field
             const uint64_t q_desc = smem_desc(q_smem + (uint32_t)(s * Q_BYTES), ROWS * 16, 128);
             const uint64_t k_desc = smem_desc(k_ring, KEYS * 16, 128), v_desc = smem_desc(v_ring, 128, PAGE * 16);
-            bool ok = true;
-            auto wait_all = [&](uint32_t bar, uint32_t parity) { return __all_sync(FULL, wait(bar, parity, gave_up)) != 0; };
             auto uniform = [](int v) { return __shfl_sync(FULL, v, 0); };
             int g0 = 0, turn = 0, count = 0;       // blocks before the item; items and blocks of the tile before it
             Item it;
-            for (int round = 0; ok && item_at(it, p, tables, total, round, TQ, per_item); ++round) {
+            for (int round = 0; item_at(it, p, tables, total, round, TQ, per_item); ++round) {
                 const bool mine = it.n[s] > 0;
                 Plan plan = {};
                 if (mine) plan = plan_of(it, s, TQ, p.window, p.sinks);
                 // Step kb: the scores of block kb, then P V of the tile's block before it.
                 int held = -1;                     // the block whose P V is still to come
                 bool begun = false;                // the item's output has a first block
-                for (int kb = 0; ok && (kb < it.blocks || held >= 0); ++kb) {
+                for (int kb = 0; kb < it.blocks || held >= 0; ++kb) {
                     const int g = uniform(g0 + kb), st = g & (STAGES - 1);
                     const uint32_t parity = (uint32_t)((g / STAGES) & 1);
                     const bool there = kb < it.blocks, wanted = there && mine && kb < plan.to && (kb < plan.sinks || kb >= plan.from);
                     if (wanted) {
                         const bool first = held < 0 && !begun;
-                        if (first) ok = wait_all(q_full + 8 * s, (uint32_t)(turn & 1));
-                        ok = ok && wait_all(k_full + 8 * st, parity);
-                        if (!ok) break;
+                        if (first) wait(q_full + 8 * s, (uint32_t)(turn & 1), gave_up);
+                        wait(k_full + 8 * st, parity, gave_up);
                         tc_fence_after();
                         const int buf = uniform(count & 1);
                         const uint32_t bar = 8 * (2 * s + buf), scores = scores0 + (uint32_t)(buf * KEYS);
@@ -483,11 +475,10 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                     if (held >= 0) {
                         const int gh = uniform(g0 + held), sth = gh & (STAGES - 1), nth = uniform(count - (wanted ? 2 : 1));
                         const uint32_t bar = 8 * (2 * s + (nth & 1)), scores = scores0 + (uint32_t)((nth & 1) * KEYS);
-                        ok = wait_all(v_full + 8 * sth, (uint32_t)((gh / STAGES) & 1));
+                        wait(v_full + 8 * sth, (uint32_t)((gh / STAGES) & 1), gave_up);
                         // an item's first block: the output of the item before has been read
-                        if (ok && !begun && turn > 0) ok = wait_all(o_free + 8 * s, (uint32_t)((turn - 1) & 1));
-                        ok = ok && wait_all(p_ready + bar, (uint32_t)((nth >> 1) & 1));
-                        if (!ok) break;
+                        if (!begun && turn > 0) wait(o_free + 8 * s, (uint32_t)((turn - 1) & 1), gave_up);
+                        wait(p_ready + bar, (uint32_t)((nth >> 1) & 1), gave_up);
                         tc_fence_after();
                         const uint64_t vd = v_desc + (uint64_t)((sth * STAGE) >> 4);
                         const int np = uniform(it.win.count - held * KB);
@@ -507,10 +498,10 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                         held = kb;
                     } else if (there) {
                         // not this tile's: once it is there (and the stage's block before it thus gone), it may go
-                        ok = wait_all(k_full + 8 * st, parity);
-                        if (ok && leader) mbar_arrive(k_empty + 8 * st);
-                        ok = ok && wait_all(v_full + 8 * st, parity);
-                        if (ok && leader) mbar_arrive(v_empty + 8 * st);
+                        wait(k_full + 8 * st, parity, gave_up);
+                        if (leader) mbar_arrive(k_empty + 8 * st);
+                        wait(v_full + 8 * st, parity, gave_up);
+                        if (leader) mbar_arrive(v_empty + 8 * st);
                         __syncwarp();
                     }
                 }
@@ -518,16 +509,15 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                 if (mine) ++turn;
             }
             // the last commits arrive while the barriers are still there
-            for (int j = g0 > STAGES ? g0 - STAGES : 0; j < g0 && ok; ++j)
-                ok = wait_all(k_empty + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1)) &&
-                     wait_all(v_empty + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1));
-            if (!ok && leader) give_up();
+            for (int j = g0 > STAGES ? g0 - STAGES : 0; j < g0; ++j) {
+                wait(k_empty + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1), gave_up);
+                wait(v_empty + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1), gave_up);
+            }
         }
     } else {
         // =================== copies ===================
         fewer_registers<88>();
         const int s = warp - 10;                   // parity of the blocks, and the tile whose queries are copied
-        bool ok = true;
         int g0 = 0, turn = 0;                      // blocks before the item; items of the tile before it
         int sent = -1;                             // the last V block sent for
         int pending = -1;                          // the block whose K is on its way
@@ -540,7 +530,7 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
             pending = -1;
         };
         Item it;
-        for (int round = 0; ok && item_at(it, p, tables, total, round, TQ, per_item); ++round) {
+        for (int round = 0; item_at(it, p, tables, total, round, TQ, per_item); ++round) {
             const int32_t *row = p.page_table + (int64_t)it.b * p.pt_stride;
             auto load_id = [&](int kb) -> int {                // lane j: page j of a block
                 const int j = kb * KB + lane;
@@ -550,9 +540,9 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                 atomicOr(p.status, STATUS_BOUNDS);
                 return 0;
             };
-            auto queries = [&]() -> bool {
-                if (it.n[s] == 0) return true;
-                if (turn > 0 && !__all_sync(FULL, wait(q_free + 8 * s, (uint32_t)((turn - 1) & 1), gave_up))) return false;
+            auto queries = [&]() {
+                if (it.n[s] == 0) return;
+                if (turn > 0) wait(q_free + 8 * s, (uint32_t)((turn - 1) & 1), gave_up);
                 for (int r0 = 0; r0 < ROWS; r0 += 32) {
                     const int r = r0 + lane, qi = r / G, g = r - qi * G;
                     if (qi >= it.n[s]) continue;               // (such a row runs on whatever is there; nothing of it is stored)
@@ -569,21 +559,19 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_full + 8 * s);
                 ++turn;
-                return true;
             };
             // The item's first block before its queries: the block's stage comes free first.
             bool asked = false;
             int kb = (s - g0) & 1;
             int id = load_id(kb);
             if (kb != 0) {
-                ok = queries();
+                queries();
                 asked = true;
             }
-            for (; ok && kb < it.blocks; kb += 2) {
+            for (; kb < it.blocks; kb += 2) {
                 const int g = g0 + kb, st = g & (STAGES - 1), np = it.win.count - kb * KB < KB ? it.win.count - kb * KB : KB;
                 const uint32_t again = (uint32_t)((g / STAGES - 1) & 1);
-                if (g >= STAGES) ok = __all_sync(FULL, wait(k_empty + 8 * st, again, gave_up));
-                if (!ok) break;
+                if (g >= STAGES) wait(k_empty + 8 * st, again, gave_up);
                 for (int j = 0; j < np; ++j) {
                     const int page_id = __shfl_sync(FULL, id, j);
                     const uint8_t *src = p.layer_base + (int64_t)page_id * p.page_stride + (int64_t)it.h * BLOCK + lane * 16;
@@ -605,11 +593,9 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                     if (!__all_sync(FULL, mbar_try_wait(v_empty + 8 * st, again))) {
                         asm volatile("cp.async.wait_group 0;" ::: "memory");
                         publish();                     // (pending: this very block)
-                        ok = __all_sync(FULL, wait(v_empty + 8 * st, again, gave_up));
+                        wait(v_empty + 8 * st, again, gave_up);
                     }
-                    __syncwarp();
                 }
-                if (!ok) break;
                 if (lane == 0) mbar_expect_tx(bar, (uint32_t)(np * HALF));
                 __syncwarp();
                 if (lane < np)
@@ -619,8 +605,7 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                 if (todo) {                                    // (few blocks: the first and the last of an item, and the sinks')
                     asm volatile("cp.async.wait_group 0;" ::: "memory");
                     if (pending >= 0) publish();
-                    ok = __all_sync(FULL, wait(bar, (zeroed >> st) & 1u, gave_up));
-                    if (!ok) break;
+                    wait(bar, (zeroed >> st) & 1u, gave_up);
                     zeroed ^= 1u << st;
                     for (; todo; todo &= todo - 1) {
                         const int j = __ffs(todo) - 1;
@@ -634,22 +619,20 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                     if (lane == 0) mbar_arrive(v_full + 8 * st);
                 }
                 if (!asked) {
-                    ok = queries();
+                    queries();
                     asked = true;
                 }
             }
             // an item's last K goes out with it
             asm volatile("cp.async.wait_group 0;" ::: "memory");
-            if (ok && pending >= 0) publish();
+            if (pending >= 0) publish();
             g0 += it.blocks;
         }
-        if (!ok && lane == 0) give_up();
-        if (ok) {
-            // leave only when every copy has landed (normally long the case)
-            for (int j = sent - 2; j <= sent; j += 2)
-                if (j >= 0) mbar_wait_bounded(v_full + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1));
-        } else {
-            // after a failure it is not known which barrier a copy still in flight will come through: give it time
+        // leave only when every copy has landed (normally long the case; after a failure it is not known which barrier one
+        // still in flight will come through, and it is given time)
+        for (int j = sent - 2; j <= sent; j += 2)
+            if (j >= 0) wait(v_full + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1), gave_up);
+        if (*gave_up) {
             const uint64_t t = global_timer_ns();
             while (global_timer_ns() - t < 1000000ull) __nanosleep(1000);
         }
@@ -657,6 +640,7 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
     // ---- common exit ----
     tc_fence_before();
     __syncthreads();
+    if (tid == 0 && *gave_up) atomicOr(p.status, STATUS_TIMEOUT);
     if (warp >= 10) asm volatile("cp.async.wait_group 0;" ::: "memory");
     if (warp == 8) {
         __syncwarp();
