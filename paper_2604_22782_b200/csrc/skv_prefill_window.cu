@@ -439,64 +439,66 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
             const uint64_t q_desc = smem_desc(q_smem + (uint32_t)(s * Q_BYTES), ROWS * 16, 128);
             const uint64_t k_desc = smem_desc(k_ring, KEYS * 16, 128), v_desc = smem_desc(v_ring, 128, PAGE * 16);
             auto uniform = [](int v) { return __shfl_sync(FULL, v, 0); };
-            int g0 = 0, turn = 0, count = 0;       // blocks before the item; items and blocks of the tile before it
+            int g = 0, turn = 0, count = 0;        // blocks before this one; items and blocks of the tile before it
             Item it;
             for (int round = 0; item_at(it, p, tables, total, round, TQ, per_item); ++round) {
-                const bool mine = it.n[s] > 0;
-                Plan plan = {};
+                const int blocks = uniform(it.blocks), pages = uniform(it.win.count);
+                const bool mine = uniform(it.n[s]) > 0;
+                Plan plan = {0, 0, 0, 0, 0};
                 if (mine) plan = plan_of(it, s, TQ, p.window, p.sinks);
+                const int sinks_to = uniform(plan.sinks), from = uniform(plan.from), to = uniform(plan.to);
+                const int final = from < to ? to - 1 : sinks_to - 1;
                 // Step kb: the scores of block kb, then P V of the tile's block before it.
-                int held = -1;                     // the block whose P V is still to come
-                bool begun = false;                // the item's output has a first block
-                for (int kb = 0; kb < it.blocks || held >= 0; ++kb) {
-                    const int g = uniform(g0 + kb), st = g & (STAGES - 1);
-                    const uint32_t parity = (uint32_t)((g / STAGES) & 1);
-                    const bool there = kb < it.blocks, wanted = there && mine && kb < plan.to && (kb < plan.sinks || kb >= plan.from);
+                bool held = false;                 // that block's P V is still to come
+                uint32_t held_stage = 0, held_parity = 0;
+                int held_pages = 0;
+                uint32_t into = 0;                 // 0: the item's output starts with the next P V
+                auto values = [&](int nth) {
+                    const uint32_t buf = (uint32_t)(nth & 1), bar = 8 * (2 * s + buf), scores = scores0 + buf * KEYS;
+                    wait(v_full + 8 * held_stage, held_parity, gave_up);
+                    // an item's first block: the output of the item before has been read
+                    if (into == 0 && turn > 0) wait(o_free + 8 * s, (uint32_t)((turn - 1) & 1), gave_up);
+                    wait(p_ready + bar, (uint32_t)((nth >> 1) & 1), gave_up);
+                    tc_fence_after();
+                    const uint64_t vd = v_desc + (uint64_t)(held_stage * (STAGE >> 4));
+                    if (leader) {
+#pragma unroll
+                        for (int j = 0; j < KB; ++j)
+                            if (j < held_pages)
+                                umma_ts(output, scores + (uint32_t)(8 * j), vd + (uint64_t)((j * HALF) >> 4), IDESC_PV, j > 0 ? 1u : into);
+                        tc_commit(pv_done + bar);
+                        tc_commit(v_empty + 8 * held_stage);
+                    }
+                    __syncwarp();
+                    into = 1;
+                };
+                for (int kb = 0; kb < blocks; ++kb, ++g) {
+                    const uint32_t st = (uint32_t)g & (STAGES - 1), parity = (uint32_t)(g / STAGES) & 1u;
+                    const bool wanted = kb < to && (kb < sinks_to || kb >= from);
                     if (wanted) {
-                        const bool first = held < 0 && !begun;
-                        if (first) wait(q_full + 8 * s, (uint32_t)(turn & 1), gave_up);
+                        if (!held && into == 0) wait(q_full + 8 * s, (uint32_t)(turn & 1), gave_up);
                         wait(k_full + 8 * st, parity, gave_up);
                         tc_fence_after();
-                        const int buf = uniform(count & 1);
-                        const uint32_t bar = 8 * (2 * s + buf), scores = scores0 + (uint32_t)(buf * KEYS);
-                        const uint64_t kd = k_desc + (uint64_t)((st * STAGE) >> 4);
-                        const bool final = kb == plan.to - 1 || (kb == plan.sinks - 1 && plan.from >= plan.to);
+                        const uint32_t buf = (uint32_t)(count & 1), scores = scores0 + buf * KEYS;
+                        const uint64_t kd = k_desc + (uint64_t)(st * (STAGE >> 4));
                         if (leader) {
 #pragma unroll
                             for (int ks = 0; ks < D / 16; ++ks)
                                 umma_ss(scores, q_desc + (uint64_t)((ks * 2 * ROWS * 16) >> 4), kd + (uint64_t)((ks * 2 * KEYS * 16) >> 4), IDESC_QK, ks > 0);
-                            tc_commit(s_ready + bar);
+                            tc_commit(s_ready + 8 * (2 * s + buf));
                             tc_commit(k_empty + 8 * st);
-                            if (final) tc_commit(q_free + 8 * s);
+                            if (kb == final) tc_commit(q_free + 8 * s);
                         }
                         __syncwarp();
+                        if (held) values(count - 1);
                         ++count;
-                    }
-                    if (held >= 0) {
-                        const int gh = uniform(g0 + held), sth = gh & (STAGES - 1), nth = uniform(count - (wanted ? 2 : 1));
-                        const uint32_t bar = 8 * (2 * s + (nth & 1)), scores = scores0 + (uint32_t)((nth & 1) * KEYS);
-                        wait(v_full + 8 * sth, (uint32_t)((gh / STAGES) & 1), gave_up);
-                        // an item's first block: the output of the item before has been read
-                        if (!begun && turn > 0) wait(o_free + 8 * s, (uint32_t)((turn - 1) & 1), gave_up);
-                        wait(p_ready + bar, (uint32_t)((nth >> 1) & 1), gave_up);
-                        tc_fence_after();
-                        const uint64_t vd = v_desc + (uint64_t)((sth * STAGE) >> 4);
-                        const int np = uniform(it.win.count - held * KB);
-                        if (leader) {
-#pragma unroll
-                            for (int j = 0; j < KB; ++j)
-                                if (j < np)
-                                    umma_ts(output, scores + (uint32_t)(8 * j), vd + (uint64_t)((j * HALF) >> 4), IDESC_PV, (begun || j > 0) ? 1u : 0u);
-                            tc_commit(pv_done + bar);
-                            tc_commit(v_empty + 8 * sth);
-                        }
-                        __syncwarp();
-                        begun = true;
-                        held = -1;
-                    }
-                    if (wanted) {
-                        held = kb;
-                    } else if (there) {
+                        held = true;
+                        held_stage = st;
+                        held_parity = parity;
+                        held_pages = pages - kb * KB;
+                    } else {
+                        if (held) values(count - 1);
+                        held = false;
                         // not this tile's: once it is there (and the stage's block before it thus gone), it may go
                         wait(k_full + 8 * st, parity, gave_up);
                         if (leader) mbar_arrive(k_empty + 8 * st);
@@ -505,11 +507,11 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                         __syncwarp();
                     }
                 }
-                g0 += it.blocks;
+                if (held) values(count - 1);
                 if (mine) ++turn;
             }
             // the last commits arrive while the barriers are still there
-            for (int j = g0 > STAGES ? g0 - STAGES : 0; j < g0; ++j) {
+            for (int j = g > STAGES ? g - STAGES : 0; j < g; ++j) {
                 wait(k_empty + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1), gave_up);
                 wait(v_empty + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1), gave_up);
             }
