@@ -8,12 +8,13 @@
 // Twelve warps:
 //   warps 0-3, 4-7  softmax of tile 0 / tile 1: thread = row (TMEM lane)
 //   warps 8, 9      lane 0 issues the tensor-core instructions of tile 0 / tile 1
-//   warps 10, 11    copy K and V of the even / odd key blocks (64 keys = 4 pages of the item's list of pages, window_pages) and,
-//                   as soon as the last scores of an item are done, the queries of the next one's tile 0 / tile 1; V rows of
-//                   tokens that no row of the item sees are zeroed, whatever they hold
-// Shared memory: Q of both tiles, K ring and V ring of four blocks each.  K is copied 16 bytes at a time so that the pages
-// interleave by chunk and a block is one operand.  (As 256-byte bulk copies, the warp that issues them was the slowest
-// part.)  V pages are copied as they are: an MN-major operand.
+//   warp 10         copies K and V of the key blocks (64 keys = 4 pages of the item's list of pages, window_pages)
+//   warp 11         copies the queries of the next item as soon as the last scores of this one are done, and zeroes the V
+//                   rows of tokens that no row of the item sees, whatever they hold
+// Shared memory: Q of both tiles (rows of 128 bytes in the 128-byte swizzle), K ring and V ring of four blocks each.  A page's
+// K half, [chunk of 8 dims][16 tokens][16 B], is fetched by one tensor copy that puts its two groups of 8 tokens one
+// behind the other, [group][chunk][8 tokens][16 B]: the groups of a block's pages then follow each other at one stride, and the
+// block is one operand.  V pages are copied as they are: an MN-major operand.
 // Tensor memory (512 columns): per tile two score buffers [64 each], each overwritten in place by the probabilities (bf16)
 // of its block, and the outputs of tile 0 and 1.
 //
@@ -30,6 +31,7 @@
 #include "skv_tcgen05.cuh"
 #include "skv_walk.cuh"
 
+#include <cuda.h>
 #include <math.h>
 
 namespace skv {
@@ -74,6 +76,20 @@ __device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile uin
             break;
         }
     __syncwarp();
+}
+
+// operand rows of 128 bytes in the 128-byte swizzle, groups of 8 rows 1024 bytes apart
+__device__ __forceinline__ uint64_t swizzled_desc(uint32_t saddr)
+{
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+
+// K half of page `page`, kv head `h`
+__device__ __forceinline__ void tensor_copy_k(uint32_t dst, const CUtensorMap *map, int h, int page, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %2, %2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(map), "r"(0), "r"(h), "r"(page), "r"(bar)
+                 : "memory");
 }
 
 // What an item is made of.
@@ -215,12 +231,13 @@ __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.
 template <int REGS>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS)); }
 
-// Dynamic shared memory: Q [2][D/8 chunks][128 rows][16 B] | K ring [4][D/8][64 keys][16 B] | V ring [4][4 pages][V half]
+// Dynamic shared memory: Q [2][D/64][128 rows][128 B] | K ring [4][8 groups][D/8 chunks][8 keys][16 B] | V ring [4][4 pages][V half]
 //                        | barriers | tensor-memory address, gave_up, items | tables [6][B + 1]
 template <int D>
-__global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid_constant__ PrefillParams p, int G, int tiles, int max_q_len)
+__global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid_constant__ PrefillParams p, const __grid_constant__ CUtensorMap k_map,
+                                                                       int G, int tiles, int max_q_len)
 {
-    extern __shared__ __align__(128) uint8_t smem_raw[];
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
     constexpr int BLOCK = block_bytes(D), HALF = half_bytes(D), CH = D / 8;
     constexpr int Q_BYTES = ROWS * D * 2, STAGE = KEYS * D * 2;
     constexpr uint32_t IDESC_QK = instr_desc(ROWS, KEYS, false), IDESC_PV = instr_desc(ROWS, D, true);
@@ -228,7 +245,7 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
     const int TQ = ROWS / G, per_item = TQ * tiles;
 
     const uint32_t base = smem_u32(smem_raw);
-    const uint32_t pad = (128u - (base & 127u)) & 127u;
+    const uint32_t pad = (1024u - (base & 1023u)) & 1023u;
     const uint32_t q_smem = base + pad, k_ring = q_smem + 2 * Q_BYTES, v_ring = k_ring + STAGES * STAGE, bars = v_ring + STAGES * STAGE;
     // a barrier per ring stage: copied, given back; per tile and score buffer: scores, probabilities, P V; per tile: the rest
     const uint32_t k_full = bars, v_full = k_full + 8 * STAGES, v_landed = v_full + 8 * STAGES, k_empty = v_landed + 8 * STAGES, v_empty = k_empty + 8 * STAGES;
@@ -436,8 +453,8 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
             const int s = warp - 8;
             const uint32_t scores0 = tmem + (uint32_t)(2 * s * KEYS), output = tmem + (uint32_t)(COL_O + 2 * s * KEYS);
             // descriptors of the first instruction of each kind; the others are a constant further on in the address field
-            const uint64_t q_desc = smem_desc(q_smem + (uint32_t)(s * Q_BYTES), ROWS * 16, 128);
-            const uint64_t k_desc = smem_desc(k_ring, KEYS * 16, 128), v_desc = smem_desc(v_ring, 128, PAGE * 16);
+            const uint64_t q_desc = swizzled_desc(q_smem + (uint32_t)(s * Q_BYTES));
+            const uint64_t k_desc = smem_desc(k_ring, 128, CH * 128), v_desc = smem_desc(v_ring, 128, PAGE * 16);
             auto uniform = [](int v) { return __shfl_sync(FULL, v, 0); };
             int g = 0, turn = 0, count = 0;        // blocks before this one; items and blocks of the tile before it
             Item it;
@@ -484,7 +501,7 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                         if (leader) {
 #pragma unroll
                             for (int ks = 0; ks < D / 16; ++ks)
-                                umma_ss(scores, q_desc + (uint64_t)((ks * 2 * ROWS * 16) >> 4), kd + (uint64_t)((ks * 2 * KEYS * 16) >> 4), IDESC_QK, ks > 0);
+                                umma_ss(scores, q_desc + (uint64_t)(((ks >> 2) * ROWS * 128 + (ks & 3) * 32) >> 4), kd + (uint64_t)((ks * 2 * 128) >> 4), IDESC_QK, ks > 0);
                             tc_commit(s_ready + 8 * (2 * s + buf));
                             tc_commit(k_empty + 8 * st);
                             if (kb == final) tc_commit(q_free + 8 * s);
@@ -516,21 +533,11 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                 wait(v_empty + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1), gave_up);
             }
         }
-    } else {
-        // =================== copies ===================
+    } else if (warp == 10) {
+        // =================== copies of K and V ===================
         fewer_registers<88>();
-        const int s = warp - 10;                   // parity of the blocks, and the tile whose queries are copied
-        int g0 = 0, turn = 0;                      // blocks before the item; items of the tile before it
-        int sent = -1;                             // the last V block sent for
-        int pending = -1;                          // the block whose K is on its way
-        uint32_t zeroed = 0;                       // bit per ring stage: parity of the blocks that came through v_landed
-        // the copies of K on their way have landed: the tensor core reads them through the async proxy
-        auto publish = [&]() {
-            fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(k_full + 8 * (pending & (STAGES - 1)));
-            pending = -1;
-        };
+        if (lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
+        int g = 0;
         Item it;
         for (int round = 0; item_at(it, p, tables, total, round, TQ, per_item); ++round) {
             const int32_t *row = p.page_table + (int64_t)it.b * p.pt_stride;
@@ -542,108 +549,90 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                 atomicOr(p.status, STATUS_BOUNDS);
                 return 0;
             };
-            auto queries = [&]() {
-                if (it.n[s] == 0) return;
-                if (turn > 0) wait(q_free + 8 * s, (uint32_t)((turn - 1) & 1), gave_up);
-                for (int r0 = 0; r0 < ROWS; r0 += 32) {
-                    const int r = r0 + lane, qi = r / G, g = r - qi * G;
-                    if (qi >= it.n[s]) continue;               // (such a row runs on whatever is there; nothing of it is stored)
-                    const uint16_t *src = p.Q + ((int64_t)(it.q_begin + it.q0 + s * TQ + qi) * p.Hq + (int64_t)it.h * G + g) * D;
-                    const uint32_t dst = q_smem + (uint32_t)(s * Q_BYTES + r * 16);
-#pragma unroll
-                    for (int c = 0; c < CH; ++c)
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (uint32_t)(c * ROWS * 16)), "l"(src + c * 8) : "memory");
-                }
-                asm volatile("cp.async.commit_group;" ::: "memory");
-                asm volatile("cp.async.wait_group 0;" ::: "memory");
-                if (pending >= 0) publish();
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(q_full + 8 * s);
-                ++turn;
-            };
-            // The item's first block before its queries: the block's stage comes free first.
-            bool asked = false;
-            int kb = (s - g0) & 1;
-            int id = load_id(kb);
-            if (kb != 0) {
-                queries();
-                asked = true;
-            }
-            for (; kb < it.blocks; kb += 2) {
-                const int g = g0 + kb, st = g & (STAGES - 1), np = it.win.count - kb * KB < KB ? it.win.count - kb * KB : KB;
+            int id = load_id(0), next_id = load_id(1);
+            for (int kb = 0; kb < it.blocks; ++kb, ++g) {
+                const int st = g & (STAGES - 1), np = it.win.count - kb * KB < KB ? it.win.count - kb * KB : KB;
                 const uint32_t again = (uint32_t)((g / STAGES - 1) & 1);
+                // a block with tokens that no row sees passes through the hands of warp 11 first
+                const bool partial = __any_sync(FULL, lane < np && window_bits(it.win.page(kb * KB + lane), it.win.lo, it.n_keys, p.sinks) != 0xFFFFu);
+                const uint32_t v_bar = (partial ? v_landed : v_full) + 8 * st;
                 if (g >= STAGES) wait(k_empty + 8 * st, again, gave_up);
-                for (int j = 0; j < np; ++j) {
-                    const int page_id = __shfl_sync(FULL, id, j);
-                    const uint8_t *src = p.layer_base + (int64_t)page_id * p.page_stride + (int64_t)it.h * BLOCK + lane * 16;
-                    const uint32_t dst = k_ring + (uint32_t)(st * STAGE + j * PAGE * 16 + (lane >> 4) * KEYS * 16 + (lane & 15) * 16);
-#pragma unroll
-                    for (int i = 0; i < CH / 2; ++i)           // two chunks of 16 keys each time
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (uint32_t)(i * 2 * KEYS * 16)), "l"(src + i * 512) : "memory");
-                }
-                asm volatile("cp.async.commit_group;" ::: "memory");
-                // the block before it in this warp's turn has landed by now, or is waited for while this one is under way
-                asm volatile("cp.async.wait_group 1;" ::: "memory");
-                if (pending >= 0) publish();
-                pending = g;
-                const uint32_t bits = lane < np ? window_bits(it.win.page(kb * KB + lane), it.win.lo, it.n_keys, p.sinks) : 0xFFFFu;
-                unsigned todo = __ballot_sync(FULL, bits != 0xFFFFu);        // pages with tokens that no row sees
-                const uint32_t bar = (todo ? v_landed : v_full) + 8 * st, my_v = v_ring + (uint32_t)(st * STAGE);
-                if (g >= STAGES) {
-                    // (V comes back later than K: what is on its way of K goes out first)
-                    if (!__all_sync(FULL, mbar_try_wait(v_empty + 8 * st, again))) {
-                        asm volatile("cp.async.wait_group 0;" ::: "memory");
-                        publish();                     // (pending: this very block)
-                        wait(v_empty + 8 * st, again, gave_up);
-                    }
-                }
-                if (lane == 0) mbar_expect_tx(bar, (uint32_t)(np * HALF));
+                if (lane == 0) mbar_expect_tx(k_full + 8 * st, (uint32_t)(np * HALF));
+                __syncwarp();
+                if (lane < np) tensor_copy_k(k_ring + (uint32_t)(st * STAGE + lane * HALF), &k_map, it.h, id, k_full + 8 * st);
+                if (g >= STAGES) wait(v_empty + 8 * st, again, gave_up);
+                if (lane == 0) mbar_expect_tx(v_bar, (uint32_t)(np * HALF));
                 __syncwarp();
                 if (lane < np)
-                    bulk_copy_g2s(my_v + (uint32_t)(lane * HALF), p.layer_base + (int64_t)id * p.page_stride + (int64_t)it.h * BLOCK + HALF, HALF, bar);
-                sent = g;
-                id = load_id(kb + 2);
-                if (todo) {                                    // (few blocks: the first and the last of an item, and the sinks')
-                    asm volatile("cp.async.wait_group 0;" ::: "memory");
-                    if (pending >= 0) publish();
-                    wait(bar, (zeroed >> st) & 1u, gave_up);
-                    zeroed ^= 1u << st;
-                    for (; todo; todo &= todo - 1) {
-                        const int j = __ffs(todo) - 1;
-                        const uint32_t set = __shfl_sync(FULL, bits, j);
-                        for (int i = lane; i < CH * PAGE; i += 32)
-                            if (!((set >> (i & (PAGE - 1))) & 1u))
-                                asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(my_v + (uint32_t)(j * HALF + i * 16)), "r"(0u) : "memory");
-                    }
-                    fence_proxy_async();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(v_full + 8 * st);
-                }
-                if (!asked) {
-                    queries();
-                    asked = true;
-                }
+                    bulk_copy_g2s(v_ring + (uint32_t)(st * STAGE + lane * HALF),
+                                  p.layer_base + (int64_t)id * p.page_stride + (int64_t)it.h * BLOCK + HALF, HALF, v_bar);
+                id = next_id;
+                next_id = load_id(kb + 2);
             }
-            // an item's last K goes out with it
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
-            if (pending >= 0) publish();
-            g0 += it.blocks;
         }
         // leave only when every copy has landed (normally long the case; after a failure it is not known which barrier one
         // still in flight will come through, and it is given time)
-        for (int j = sent - 2; j <= sent; j += 2)
-            if (j >= 0) wait(v_full + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1), gave_up);
+        for (int j = g > STAGES ? g - STAGES : 0; j < g; ++j) {
+            wait(k_full + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1), gave_up);
+            wait(v_full + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1), gave_up);
+        }
         if (*gave_up) {
             const uint64_t t = global_timer_ns();
             while (global_timer_ns() - t < 1000000ull) __nanosleep(1000);
+        }
+    } else {
+        // =================== queries; V rows that no row of the item sees ===================
+        fewer_registers<88>();
+        int g = 0, turn[2] = {0, 0};               // blocks before this one; items of the tiles before this one
+        uint32_t landed = 0;                       // bit per ring stage: parity of the blocks that came through v_landed
+        Item it;
+        for (int round = 0; item_at(it, p, tables, total, round, TQ, per_item); ++round) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                if (it.n[s] == 0) continue;
+                if (turn[s] > 0) wait(q_free + 8 * s, (uint32_t)((turn[s] - 1) & 1), gave_up);
+                // 8 lanes a row of 128 bytes: whole lines from memory, and no two lanes of a row's eight in one bank
+                const int c = lane & 7;
+                for (int r0 = 0; r0 < ROWS; r0 += 4) {
+                    const int r = r0 + (lane >> 3), qi = r / G, g8 = r - qi * G;
+                    if (qi >= it.n[s]) continue;               // (such a row runs on whatever is there; nothing of it is stored)
+                    const uint16_t *src = p.Q + ((int64_t)(it.q_begin + it.q0 + s * TQ + qi) * p.Hq + (int64_t)it.h * G + g8) * D + c * 8;
+                    const uint32_t dst = q_smem + (uint32_t)(s * Q_BYTES + r * 128 + ((c ^ (r & 7)) * 16));
+#pragma unroll
+                    for (int half = 0; half < D / 64; ++half)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (uint32_t)(half * ROWS * 128)), "l"(src + half * 64) : "memory");
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+                fence_proxy_async();                           // the tensor core reads them through the async proxy
+                __syncwarp();
+                if (lane == 0) mbar_arrive(q_full + 8 * s);
+                ++turn[s];
+            }
+            for (int kb = 0; kb < it.blocks; ++kb, ++g) {
+                const int st = g & (STAGES - 1), np = it.win.count - kb * KB < KB ? it.win.count - kb * KB : KB;
+                const uint32_t bits = lane < np ? window_bits(it.win.page(kb * KB + lane), it.win.lo, it.n_keys, p.sinks) : 0xFFFFu;
+                unsigned todo = __ballot_sync(FULL, bits != 0xFFFFu);
+                if (!todo) continue;                           // (few have any: the first and the last of an item, and the sinks')
+                wait(v_landed + 8 * st, (landed >> st) & 1u, gave_up);
+                landed ^= 1u << st;
+                for (; todo; todo &= todo - 1) {
+                    const int j = __ffs(todo) - 1;
+                    const uint32_t set = __shfl_sync(FULL, bits, j);
+                    for (int i = lane; i < CH * PAGE; i += 32)
+                        if (!((set >> (i & (PAGE - 1))) & 1u))
+                            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(v_ring + (uint32_t)(st * STAGE + j * HALF + i * 16)), "r"(0u) : "memory");
+                }
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(v_full + 8 * st);
+            }
         }
     }
     // ---- common exit ----
     tc_fence_before();
     __syncthreads();
     if (tid == 0 && *gave_up) atomicOr(p.status, STATUS_TIMEOUT);
-    if (warp >= 10) asm volatile("cp.async.wait_group 0;" ::: "memory");
     if (warp == 8) {
         __syncwarp();
         tmem_dealloc(tmem, 512);
@@ -652,13 +641,35 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
 
 }  // namespace
 
+namespace {
+// K halves of an owner layer's pages as a tensor: [page][head][2 groups of 8 tokens][D/8 chunks][8 tokens x 8 dims]; a box is one
+// page's half of one head.  (The encoder is the driver's; asked for through the runtime, nothing is linked.)
+bool encode_k_map(CUtensorMap *map, const PrefillParams &p, int D)
+{
+    using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static const Encode encode = [] {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) f = nullptr;
+        return reinterpret_cast<Encode>(f);
+    }();
+    if (!encode) return false;
+    const cuuint64_t dims[5] = {64, (cuuint64_t)(D / 8), 2, (cuuint64_t)p.Hkv, (cuuint64_t)p.max_pages};
+    const cuuint64_t strides[4] = {256, 128, (cuuint64_t)block_bytes(D), (cuuint64_t)p.page_stride};
+    const cuuint32_t box[5] = {64, (cuuint32_t)(D / 8), 2, 1, 1}, steps[5] = {1, 1, 1, 1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<uint8_t *>(p.layer_base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+}  // namespace
+
 bool prefill_window_supported(int D, int G) { return (D == 64 || D == 128) && G >= 1 && G <= 8; }
 int prefill_window_max_batch() { return MAX_BATCH; }
 
 size_t prefill_window_smem_bytes(int D, int B)
 {
     if (D != 64 && D != 128) return 0;
-    return 128 + 2 * (size_t)ROWS * D * 2 + 2 * STAGES * (size_t)KEYS * D * 2 + BAR_BYTES + 16 + 6 * (size_t)(B + 1) * sizeof(int32_t);
+    return 1024 + 2 * (size_t)ROWS * D * 2 + 2 * STAGES * (size_t)KEYS * D * 2 + BAR_BYTES + 16 + 6 * (size_t)(B + 1) * sizeof(int32_t);
 }
 
 cudaError_t launch_prefill_window(const PrefillParams &p, int D, int G, int max_q_len, int sm_count, bool pdl, cudaStream_t s)
@@ -669,6 +680,8 @@ cudaError_t launch_prefill_window(const PrefillParams &p, int D, int G, int max_
     const int tiles = most * (((int64_t)max_q_len + 2 * TQ - 1) / (2 * TQ)) >= sm_count ? 2 : 1;
     int64_t ctas = most * (((int64_t)max_q_len + tiles * TQ - 1) / (tiles * TQ));
     if (ctas > sm_count) ctas = sm_count;
+    CUtensorMap k_map;
+    if (!encode_k_map(&k_map, p, D)) return cudaErrorNotSupported;
     const size_t smem = prefill_window_smem_bytes(D, p.B);
     auto kern = D == 128 ? prefill_window_kernel<128> : prefill_window_kernel<64>;
     const cudaError_t e = ensure_dynamic_smem(kern, smem);
@@ -683,7 +696,7 @@ cudaError_t launch_prefill_window(const PrefillParams &p, int D, int G, int max_
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = pdl ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kern, p, G, tiles, max_q_len);
+    return cudaLaunchKernelEx(&cfg, kern, p, k_map, G, tiles, max_q_len);
 }
 
 }  // namespace skv
