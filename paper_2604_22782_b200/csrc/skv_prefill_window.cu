@@ -165,6 +165,50 @@ __device__ __forceinline__ Plan plan_of(const Item &it, int s, int TQ, int windo
     return q;
 }
 
+// The items of a CTA, round by round, as a warp goes through them.  Working one out takes some two thousand cycles, all of
+// latency: every lane does it for a round of its own, once in 32 rounds, and the rounds then only read their lane's.
+struct Items {
+    Item mine;
+    Plan plans[2];
+    bool any;
+
+    __device__ __forceinline__ bool at(Item &it, const PrefillParams &p, const Tables &t, int total, int round, int lane, int TQ, int per_item)
+    {
+        if ((round & 31) == 0) {
+            any = item_at(mine, p, t, total, round + lane, TQ, per_item);
+            if (any)
+                for (int s = 0; s < 2; ++s)
+                    if (mine.n[s] > 0) plans[s] = plan_of(mine, s, TQ, p.window, p.sinks);
+        }
+        const int from = round & 31;
+        if (!__shfl_sync(FULL, (int)any, from)) return false;
+        auto get = [&](int v) { return __shfl_sync(FULL, v, from); };
+        it.b = get(mine.b);
+        it.h = get(mine.h);
+        it.q_begin = get(mine.q_begin);
+        it.q_len = get(mine.q_len);
+        it.q0 = get(mine.q0);
+        it.pos0 = get(mine.pos0);
+        it.n[0] = get(mine.n[0]);
+        it.n[1] = get(mine.n[1]);
+        it.n_keys = get(mine.n_keys);
+        it.blocks = get(mine.blocks);
+        it.win.lo = get(mine.win.lo);
+        it.win.sink_pages = get(mine.win.sink_pages);
+        it.win.gap = get(mine.win.gap);
+        it.win.count = get(mine.win.count);
+        return true;
+    }
+    // of the round that at() was asked for last
+    __device__ __forceinline__ Plan plan(int s, int round) const
+    {
+        const Plan &q = plans[s];
+        const int from = round & 31;
+        return {__shfl_sync(FULL, q.sinks, from), __shfl_sync(FULL, q.from, from), __shfl_sync(FULL, q.to, from),
+                __shfl_sync(FULL, q.clear_from, from), __shfl_sync(FULL, q.clear_to, from)};
+    }
+};
+
 // a pair of fp32 in one 64-bit register: one instruction works on both
 __device__ __forceinline__ uint64_t pair_of(float lo, float hi)
 {
@@ -331,11 +375,13 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                        output = lane_base + (uint32_t)(COL_O + 2 * s * KEYS);
         const int qi = row / G, g = row - qi * G;
         const uint64_t scale2 = pair_of(p.scale_log2, p.scale_log2);
+        const bool wide_out = (reinterpret_cast<uintptr_t>(p.out) & 31) == 0;
         int count = 0;                             // blocks of this tile so far
         Item it;
-        for (int round = 0; item_at(it, p, tables, total, round, TQ, per_item); ++round) {
+        Items items = {};
+        for (int round = 0; items.at(it, p, tables, total, round, lane, TQ, per_item); ++round) {
             if (it.n[s] == 0) continue;
-            const Plan plan = plan_of(it, s, TQ, p.window, p.sinks);
+            const Plan plan = s == 0 ? items.plan(0, round) : items.plan(1, round);
             const bool row_ok = qi < it.n[s];
             const int pos = row_ok ? it.first(s, TQ) + qi : 0x7FFFFFFE, lo = pos >= p.window ? pos - p.window + 1 : 0;
             float m_used = -INFINITY, l_sum = 0.f;
@@ -437,9 +483,16 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
             __syncwarp();
             if (lane == 0) mbar_arrive(o_free + 8 * s);
             if (row_ok) {
+                if (wide_out) {                    // whole sectors: half as many, and none written twice
 #pragma unroll
-                for (int c = 0; c < D / 2; c += 4)
-                    *reinterpret_cast<uint4 *>(dst + 2 * c) = make_uint4(packed[c], packed[c + 1], packed[c + 2], packed[c + 3]);
+                    for (int c = 0; c < D / 2; c += 8)
+                        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + 2 * c), "r"(packed[c]), "r"(packed[c + 1]),
+                                     "r"(packed[c + 2]), "r"(packed[c + 3]), "r"(packed[c + 4]), "r"(packed[c + 5]), "r"(packed[c + 6]), "r"(packed[c + 7]) : "memory");
+                } else {
+#pragma unroll
+                    for (int c = 0; c < D / 2; c += 4)
+                        *reinterpret_cast<uint4 *>(dst + 2 * c) = make_uint4(packed[c], packed[c + 1], packed[c + 2], packed[c + 3]);
+                }
             }
         }
     } else if (warp < 10) {
@@ -455,15 +508,14 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
             // descriptors of the first instruction of each kind; the others are a constant further on in the address field
             const uint64_t q_desc = swizzled_desc(q_smem + (uint32_t)(s * Q_BYTES));
             const uint64_t k_desc = smem_desc(k_ring, 128, CH * 128), v_desc = smem_desc(v_ring, 128, PAGE * 16);
-            auto uniform = [](int v) { return __shfl_sync(FULL, v, 0); };
             int g = 0, turn = 0, count = 0;        // blocks before this one; items and blocks of the tile before it
             Item it;
-            for (int round = 0; item_at(it, p, tables, total, round, TQ, per_item); ++round) {
-                const int blocks = uniform(it.blocks), pages = uniform(it.win.count);
-                const bool mine = uniform(it.n[s]) > 0;
-                Plan plan = {0, 0, 0, 0, 0};
-                if (mine) plan = plan_of(it, s, TQ, p.window, p.sinks);
-                const int sinks_to = uniform(plan.sinks), from = uniform(plan.from), to = uniform(plan.to);
+            Items items = {};
+            for (int round = 0; items.at(it, p, tables, total, round, lane, TQ, per_item); ++round) {
+                const int blocks = it.blocks, pages = it.win.count;
+                const bool mine = it.n[s] > 0;
+                const Plan plan = s == 0 ? items.plan(0, round) : items.plan(1, round);
+                const int sinks_to = mine ? plan.sinks : 0, from = mine ? plan.from : 0, to = mine ? plan.to : 0;
                 const int final = from < to ? to - 1 : sinks_to - 1;
                 // Step kb: the scores of block kb, then P V of the tile's block before it.
                 bool held = false;                 // that block's P V is still to come
@@ -539,7 +591,8 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
         if (lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
         int g = 0;
         Item it;
-        for (int round = 0; item_at(it, p, tables, total, round, TQ, per_item); ++round) {
+        Items items = {};
+        for (int round = 0; items.at(it, p, tables, total, round, lane, TQ, per_item); ++round) {
             const int32_t *row = p.page_table + (int64_t)it.b * p.pt_stride;
             auto load_id = [&](int kb) -> int {                // lane j: page j of a block
                 const int j = kb * KB + lane;
@@ -586,21 +639,37 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
         int g = 0, turn[2] = {0, 0};               // blocks before this one; items of the tiles before this one
         uint32_t landed = 0;                       // bit per ring stage: parity of the blocks that came through v_landed
         Item it;
-        for (int round = 0; item_at(it, p, tables, total, round, TQ, per_item); ++round) {
+        Items items = {};
+        for (int round = 0; items.at(it, p, tables, total, round, lane, TQ, per_item); ++round) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 if (it.n[s] == 0) continue;
                 if (turn[s] > 0) wait(q_free + 8 * s, (uint32_t)((turn[s] - 1) & 1), gave_up);
-                // 8 lanes a row of 128 bytes: whole lines from memory, and no two lanes of a row's eight in one bank
-                const int c = lane & 7;
-                for (int r0 = 0; r0 < ROWS; r0 += 4) {
-                    const int r = r0 + (lane >> 3), qi = r / G, g8 = r - qi * G;
-                    if (qi >= it.n[s]) continue;               // (such a row runs on whatever is there; nothing of it is stored)
-                    const uint16_t *src = p.Q + ((int64_t)(it.q_begin + it.q0 + s * TQ + qi) * p.Hq + (int64_t)it.h * G + g8) * D + c * 8;
-                    const uint32_t dst = q_smem + (uint32_t)(s * Q_BYTES + r * 128 + ((c ^ (r & 7)) * 16));
+                // 8 lanes a row of 128 bytes: whole lines from memory, and no two lanes of a row's eight in one bank.  Rows r, r + 4, ...
+                // of a lane: the token and head are counted along (a division per row made this the slowest part of an item).
+                const int c = lane & 7, r4 = lane >> 3;
+                int qi = r4 / G, g8 = r4 - qi * G;
+                const int step_q = 4 / G, step_g = 4 - step_q * G;
+                const uint16_t *src = p.Q + ((int64_t)(it.q_begin + it.q0 + s * TQ + qi) * p.Hq + (int64_t)it.h * G + g8) * D + c * 8;
+                const int64_t step = (int64_t)(step_q * p.Hq + step_g) * D, wrap = (int64_t)(p.Hq - G) * D;
+                const uint32_t dst = q_smem + (uint32_t)(s * Q_BYTES + r4 * 128);
+                const uint32_t at[2] = {(uint32_t)((c ^ r4) * 16), (uint32_t)(512 + ((c ^ (r4 + 4)) * 16))};
+                for (int r0 = 0; r0 < ROWS * 128; r0 += 1024) {
 #pragma unroll
-                    for (int half = 0; half < D / 64; ++half)
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (uint32_t)(half * ROWS * 128)), "l"(src + half * 64) : "memory");
+                    for (int odd = 0; odd < 2; ++odd) {
+                        if (qi < it.n[s])                      // (another row runs on whatever is there; nothing of it is stored)
+#pragma unroll
+                            for (int half = 0; half < D / 64; ++half)
+                                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + at[odd] + (uint32_t)(r0 + half * ROWS * 128)), "l"(src + half * 64) : "memory");
+                        qi += step_q;
+                        g8 += step_g;
+                        src += step;
+                        if (g8 >= G) {
+                            g8 -= G;
+                            ++qi;
+                            src += wrap;
+                        }
+                    }
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
                 asm volatile("cp.async.wait_group 0;" ::: "memory");
