@@ -5,12 +5,12 @@
 // The tiles share every K and V read.  A persistent CTA per SM takes its share of the items, which are dealt out by their
 // place in the sequence, furthest first (those have the most keys, where the window does not make all alike), back and forth
 // over the CTAs: within 2 % of the mean where every CTA has some, by count (dealt in the order of the rows: 15 % over it).
-// Twelve warps:
+// Sixteen warps:
 //   warps 0-3, 4-7  softmax of tile 0 / tile 1: thread = row (TMEM lane)
-//   warps 8, 9      lane 0 issues the tensor-core instructions of tile 0 / tile 1
-//   warp 10         copies K and V of the key blocks (64 keys = 4 pages of the item's list of pages, window_pages)
-//   warp 11         copies the queries of the next item as soon as the last scores of this one are done, and zeroes the V
-//                   rows of tokens that no row of the item sees, whatever they hold
+//   warps 8, 9      issue the scores Q K^T of tile 0 / tile 1,  warps 10, 11 the outputs P V
+//   warp 12         copies K and V of the key blocks (64 keys = 4 pages of the item's list of pages, window_pages)
+//   warps 13, 14    copy the queries of the next item's tile 0 / tile 1 as soon as the last scores of this one are done
+//   warp 15         zeroes the V rows of tokens that no row of the item sees, whatever they hold
 // Shared memory: Q of both tiles (rows of 128 bytes in the 128-byte swizzle), K ring and V ring of four blocks each.  A page's
 // K half, [chunk of 8 dims][16 tokens][16 B], is fetched by one tensor copy that puts its two groups of 8 tokens one
 // behind the other, [group][chunk][8 tokens][16 B]: the groups of a block's pages then follow each other at one stride, and the
@@ -44,11 +44,11 @@ constexpr unsigned FULL = 0xFFFFFFFFu;
 constexpr int ROWS = 128;             // query rows of a tile
 constexpr int KB = 4;                 // pages of a key block
 constexpr int KEYS = KB * PAGE;
-constexpr int THREADS = 384;
+constexpr int THREADS = 512;
 constexpr int STAGES = 4;             // key blocks of the K ring and of the V ring
 constexpr int COL_O = 4 * KEYS;       // scores of tile s, buffer i at column 128 s + 64 i, its output at 256 + 128 s
 constexpr float RESCALE_STEP = 8.f;
-constexpr int BY_FMA = 4;             // every fourth pair of exponentials is computed on the FMA units
+constexpr int BY_FMA = 8;             // every eighth pair of exponentials is computed on the FMA units
 constexpr int BAR_BYTES = 5 * 8 * STAGES + 3 * 32 + 3 * 16;
 constexpr int MAX_BATCH = 1024;       // sequences of a launch: their tables are in shared memory
 
@@ -495,99 +495,80 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                 }
             }
         }
-    } else if (warp < 10) {
+    } else if (warp < 12) {
         // =================== tensor-core issue ===================
         // The whole warp walks along and one lane issues: descriptors and barriers are then the same for the warp as far as the
         // compiler can see, and stay in uniform registers.  (In a branch of lane 0 alone every instruction moved them there anew:
         // 60 to 100 cycles each, 2600 per tile and block.)
-        fewer_registers<88>();
-        {
-            const bool leader = elect_one();
-            const int s = warp - 8;
-            const uint32_t scores0 = tmem + (uint32_t)(2 * s * KEYS), output = tmem + (uint32_t)(COL_O + 2 * s * KEYS);
-            // descriptors of the first instruction of each kind; the others are a constant further on in the address field
-            const uint64_t q_desc = swizzled_desc(q_smem + (uint32_t)(s * Q_BYTES));
-            const uint64_t k_desc = smem_desc(k_ring, 128, CH * 128), v_desc = smem_desc(v_ring, 128, PAGE * 16);
-            int g = 0, turn = 0, count = 0;        // blocks before this one; items and blocks of the tile before it
-            Item it;
-            Items items = {};
-            for (int round = 0; items.at(it, p, tables, total, round, lane, TQ, per_item); ++round) {
-                const int blocks = it.blocks, pages = it.win.count;
-                const bool mine = it.n[s] > 0;
-                const Plan plan = s == 0 ? items.plan(0, round) : items.plan(1, round);
-                const int sinks_to = mine ? plan.sinks : 0, from = mine ? plan.from : 0, to = mine ? plan.to : 0;
-                const int final = from < to ? to - 1 : sinks_to - 1;
-                // Step kb: the scores of block kb, then P V of the tile's block before it.
-                bool held = false;                 // that block's P V is still to come
-                uint32_t held_stage = 0, held_parity = 0;
-                int held_pages = 0;
-                uint32_t into = 0;                 // 0: the item's output starts with the next P V
-                auto values = [&](int nth) {
-                    const uint32_t buf = (uint32_t)(nth & 1), bar = 8 * (2 * s + buf), scores = scores0 + buf * KEYS;
-                    wait(v_full + 8 * held_stage, held_parity, gave_up);
-                    // an item's first block: the output of the item before has been read
-                    if (into == 0 && turn > 0) wait(o_free + 8 * s, (uint32_t)((turn - 1) & 1), gave_up);
-                    wait(p_ready + bar, (uint32_t)((nth >> 1) & 1), gave_up);
+        fewer_registers<48>();
+        const bool leader = elect_one(), values = warp >= 10;
+        const int s = warp & 1;
+        const uint32_t scores0 = tmem + (uint32_t)(2 * s * KEYS), output = tmem + (uint32_t)(COL_O + 2 * s * KEYS);
+        // descriptors of the first instruction of each kind; the others are a constant further on in the address field
+        const uint64_t q_desc = swizzled_desc(q_smem + (uint32_t)(s * Q_BYTES));
+        const uint64_t ring_desc = values ? smem_desc(v_ring, 128, PAGE * 16) : smem_desc(k_ring, 128, CH * 128);
+        const uint32_t full = values ? v_full : k_full, empty = values ? v_empty : k_empty;
+        int g = 0, turn = 0, count = 0;            // blocks before this one; items and blocks of the tile before it
+        Item it;
+        Items items = {};
+        for (int round = 0; items.at(it, p, tables, total, round, lane, TQ, per_item); ++round) {
+            const int blocks = it.blocks, pages = it.win.count;
+            const bool mine = it.n[s] > 0;
+            const Plan plan = s == 0 ? items.plan(0, round) : items.plan(1, round);
+            const int sinks_to = mine ? plan.sinks : 0, from = mine ? plan.from : 0, to = mine ? plan.to : 0;
+            const int final = from < to ? to - 1 : sinks_to - 1;
+            bool begun = false;
+            for (int kb = 0; kb < blocks; ++kb, ++g) {
+                const uint32_t st = (uint32_t)g & (STAGES - 1), parity = (uint32_t)(g / STAGES) & 1u;
+                const uint32_t buf = (uint32_t)count & 1u, turn_of_buf = (uint32_t)(count >> 1), bar = 8 * (2 * s + buf), scores = scores0 + buf * KEYS;
+                const uint64_t desc = ring_desc + (uint64_t)(st * (STAGE >> 4));
+                if (kb >= to || (kb >= sinks_to && kb < from)) {
+                    // not this tile's: once it is there (and the stage's block before it thus gone), it may go
+                    wait(full + 8 * st, parity, gave_up);
+                    if (leader) mbar_arrive(empty + 8 * st);
+                    continue;
+                }
+                if (!values) {
+                    if (!begun) wait(q_full + 8 * s, (uint32_t)(turn & 1), gave_up);
+                    // the buffer: P V two blocks back is over
+                    if (count >= 2) wait(pv_done + bar, (turn_of_buf - 1) & 1u, gave_up);
+                    wait(full + 8 * st, parity, gave_up);
                     tc_fence_after();
-                    const uint64_t vd = v_desc + (uint64_t)(held_stage * (STAGE >> 4));
                     if (leader) {
 #pragma unroll
-                        for (int j = 0; j < KB; ++j)
-                            if (j < held_pages)
-                                umma_ts(output, scores + (uint32_t)(8 * j), vd + (uint64_t)((j * HALF) >> 4), IDESC_PV, j > 0 ? 1u : into);
-                        tc_commit(pv_done + bar);
-                        tc_commit(v_empty + 8 * held_stage);
+                        for (int ks = 0; ks < D / 16; ++ks)
+                            umma_ss(scores, q_desc + (uint64_t)(((ks >> 2) * ROWS * 128 + (ks & 3) * 32) >> 4), desc + (uint64_t)((ks * 2 * 128) >> 4), IDESC_QK, ks > 0);
+                        tc_commit(s_ready + bar);
+                        tc_commit(empty + 8 * st);
+                        if (kb == final) tc_commit(q_free + 8 * s);
                     }
-                    __syncwarp();
-                    into = 1;
-                };
-                for (int kb = 0; kb < blocks; ++kb, ++g) {
-                    const uint32_t st = (uint32_t)g & (STAGES - 1), parity = (uint32_t)(g / STAGES) & 1u;
-                    const bool wanted = kb < to && (kb < sinks_to || kb >= from);
-                    if (wanted) {
-                        if (!held && into == 0) wait(q_full + 8 * s, (uint32_t)(turn & 1), gave_up);
-                        wait(k_full + 8 * st, parity, gave_up);
-                        tc_fence_after();
-                        const uint32_t buf = (uint32_t)(count & 1), scores = scores0 + buf * KEYS;
-                        const uint64_t kd = k_desc + (uint64_t)(st * (STAGE >> 4));
-                        if (leader) {
+                } else {
+                    wait(full + 8 * st, parity, gave_up);
+                    // an item's first block: the output of the item before has been read
+                    if (!begun && turn > 0) wait(o_free + 8 * s, (uint32_t)((turn - 1) & 1), gave_up);
+                    wait(p_ready + bar, turn_of_buf & 1u, gave_up);
+                    tc_fence_after();
+                    if (leader) {
+                        const int np = pages - kb * KB;
 #pragma unroll
-                            for (int ks = 0; ks < D / 16; ++ks)
-                                umma_ss(scores, q_desc + (uint64_t)(((ks >> 2) * ROWS * 128 + (ks & 3) * 32) >> 4), kd + (uint64_t)((ks * 2 * 128) >> 4), IDESC_QK, ks > 0);
-                            tc_commit(s_ready + 8 * (2 * s + buf));
-                            tc_commit(k_empty + 8 * st);
-                            if (kb == final) tc_commit(q_free + 8 * s);
-                        }
-                        __syncwarp();
-                        if (held) values(count - 1);
-                        ++count;
-                        held = true;
-                        held_stage = st;
-                        held_parity = parity;
-                        held_pages = pages - kb * KB;
-                    } else {
-                        if (held) values(count - 1);
-                        held = false;
-                        // not this tile's: once it is there (and the stage's block before it thus gone), it may go
-                        wait(k_full + 8 * st, parity, gave_up);
-                        if (leader) mbar_arrive(k_empty + 8 * st);
-                        wait(v_full + 8 * st, parity, gave_up);
-                        if (leader) mbar_arrive(v_empty + 8 * st);
-                        __syncwarp();
+                        for (int j = 0; j < KB; ++j)
+                            if (j < np)
+                                umma_ts(output, scores + (uint32_t)(8 * j), desc + (uint64_t)((j * HALF) >> 4), IDESC_PV, j > 0 || begun ? 1u : 0u);
+                        tc_commit(pv_done + bar);
+                        tc_commit(empty + 8 * st);
                     }
                 }
-                if (held) values(count - 1);
-                if (mine) ++turn;
+                __syncwarp();
+                begun = true;
+                ++count;
             }
-            // the last commits arrive while the barriers are still there
-            for (int j = g > STAGES ? g - STAGES : 0; j < g; ++j) {
-                wait(k_empty + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1), gave_up);
-                wait(v_empty + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1), gave_up);
-            }
+            if (mine) ++turn;
         }
-    } else if (warp == 10) {
+        // the last commits arrive while the barriers are still there
+        for (int j = g > STAGES ? g - STAGES : 0; j < g; ++j) wait(empty + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1), gave_up);
+    } else if (warp == 12) {
         // =================== copies of K and V ===================
-        fewer_registers<88>();
+        fewer_registers<48>();
         if (lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
         int g = 0;
         Item it;
@@ -606,7 +587,7 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
             for (int kb = 0; kb < it.blocks; ++kb, ++g) {
                 const int st = g & (STAGES - 1), np = it.win.count - kb * KB < KB ? it.win.count - kb * KB : KB;
                 const uint32_t again = (uint32_t)((g / STAGES - 1) & 1);
-                // a block with tokens that no row sees passes through the hands of warp 11 first
+                // a block with tokens that no row sees passes through the hands of warp 15 first
                 const bool partial = __any_sync(FULL, lane < np && window_bits(it.win.page(kb * KB + lane), it.win.lo, it.n_keys, p.sinks) != 0xFFFFu);
                 const uint32_t v_bar = (partial ? v_landed : v_full) + 8 * st;
                 if (g >= STAGES) wait(k_empty + 8 * st, again, gave_up);
@@ -633,51 +614,57 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
             const uint64_t t = global_timer_ns();
             while (global_timer_ns() - t < 1000000ull) __nanosleep(1000);
         }
+    } else if (warp < 15) {
+        // =================== queries ===================
+        fewer_registers<48>();
+        const int s = warp - 13;
+        int turn = 0;                              // items of the tile before this one
+        Item it;
+        Items items = {};
+        for (int round = 0; items.at(it, p, tables, total, round, lane, TQ, per_item); ++round) {
+            if (it.n[s] == 0) continue;
+            if (turn > 0) wait(q_free + 8 * s, (uint32_t)((turn - 1) & 1), gave_up);
+            // 8 lanes a row of 128 bytes: whole lines from memory, and no two lanes of a row's eight in one bank.  Rows r, r + 4, ...
+            // of a lane: the token and head are counted along (a division per row made this the slowest part of an item).
+            const int c = lane & 7, r4 = lane >> 3;
+            int qi = r4 / G, g8 = r4 - qi * G;
+            const int step_q = 4 / G, step_g = 4 - step_q * G;
+            const uint16_t *src = p.Q + ((int64_t)(it.q_begin + it.q0 + s * TQ + qi) * p.Hq + (int64_t)it.h * G + g8) * D + c * 8;
+            const int64_t step = (int64_t)(step_q * p.Hq + step_g) * D, wrap = (int64_t)(p.Hq - G) * D;
+            const uint32_t dst = q_smem + (uint32_t)(s * Q_BYTES + r4 * 128);
+            const uint32_t at[2] = {(uint32_t)((c ^ r4) * 16), (uint32_t)(512 + ((c ^ (r4 + 4)) * 16))};
+            for (int r0 = 0; r0 < ROWS * 128; r0 += 1024) {
+#pragma unroll
+                for (int odd = 0; odd < 2; ++odd) {
+                    if (qi < it.n[s])                      // (another row runs on whatever is there; nothing of it is stored)
+#pragma unroll
+                        for (int half = 0; half < D / 64; ++half)
+                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + at[odd] + (uint32_t)(r0 + half * ROWS * 128)), "l"(src + half * 64) : "memory");
+                    qi += step_q;
+                    g8 += step_g;
+                    src += step;
+                    if (g8 >= G) {
+                        g8 -= G;
+                        ++qi;
+                        src += wrap;
+                    }
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            fence_proxy_async();                           // the tensor core reads them through the async proxy
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q_full + 8 * s);
+            ++turn;
+        }
     } else {
-        // =================== queries; V rows that no row of the item sees ===================
-        fewer_registers<88>();
-        int g = 0, turn[2] = {0, 0};               // blocks before this one; items of the tiles before this one
+        // =================== V rows that no row of the item sees ===================
+        fewer_registers<48>();
+        int g = 0;                                 // blocks before this one
         uint32_t landed = 0;                       // bit per ring stage: parity of the blocks that came through v_landed
         Item it;
         Items items = {};
         for (int round = 0; items.at(it, p, tables, total, round, lane, TQ, per_item); ++round) {
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                if (it.n[s] == 0) continue;
-                if (turn[s] > 0) wait(q_free + 8 * s, (uint32_t)((turn[s] - 1) & 1), gave_up);
-                // 8 lanes a row of 128 bytes: whole lines from memory, and no two lanes of a row's eight in one bank.  Rows r, r + 4, ...
-                // of a lane: the token and head are counted along (a division per row made this the slowest part of an item).
-                const int c = lane & 7, r4 = lane >> 3;
-                int qi = r4 / G, g8 = r4 - qi * G;
-                const int step_q = 4 / G, step_g = 4 - step_q * G;
-                const uint16_t *src = p.Q + ((int64_t)(it.q_begin + it.q0 + s * TQ + qi) * p.Hq + (int64_t)it.h * G + g8) * D + c * 8;
-                const int64_t step = (int64_t)(step_q * p.Hq + step_g) * D, wrap = (int64_t)(p.Hq - G) * D;
-                const uint32_t dst = q_smem + (uint32_t)(s * Q_BYTES + r4 * 128);
-                const uint32_t at[2] = {(uint32_t)((c ^ r4) * 16), (uint32_t)(512 + ((c ^ (r4 + 4)) * 16))};
-                for (int r0 = 0; r0 < ROWS * 128; r0 += 1024) {
-#pragma unroll
-                    for (int odd = 0; odd < 2; ++odd) {
-                        if (qi < it.n[s])                      // (another row runs on whatever is there; nothing of it is stored)
-#pragma unroll
-                            for (int half = 0; half < D / 64; ++half)
-                                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + at[odd] + (uint32_t)(r0 + half * ROWS * 128)), "l"(src + half * 64) : "memory");
-                        qi += step_q;
-                        g8 += step_g;
-                        src += step;
-                        if (g8 >= G) {
-                            g8 -= G;
-                            ++qi;
-                            src += wrap;
-                        }
-                    }
-                }
-                asm volatile("cp.async.commit_group;" ::: "memory");
-                asm volatile("cp.async.wait_group 0;" ::: "memory");
-                fence_proxy_async();                           // the tensor core reads them through the async proxy
-                __syncwarp();
-                if (lane == 0) mbar_arrive(q_full + 8 * s);
-                ++turn[s];
-            }
             for (int kb = 0; kb < it.blocks; ++kb, ++g) {
                 const int st = g & (STAGES - 1), np = it.win.count - kb * KB < KB ? it.win.count - kb * KB : KB;
                 const uint32_t bits = lane < np ? window_bits(it.win.page(kb * KB + lane), it.win.lo, it.n_keys, p.sinks) : 0xFFFFu;
