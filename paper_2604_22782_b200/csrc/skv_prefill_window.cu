@@ -408,57 +408,58 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                             if (!((bits >> c) & 1u)) raw[i][c] = 0xFF800000u;      // -inf
                     }
                 }
-                float mx4[4];
+                // The probabilities are taken against the reference as it stands while the block's maximum is being found; should that
+                // turn out to have run away from it (an item's first block, rarely another), they are taken again.  The maximum first
+                // and the exponentials then cost 280 cycles more a block.
+                for (;;) {
+                    const float neg_m = m_used == -INFINITY ? 0.f : -m_used;
+                    const uint64_t neg2 = pair_of(neg_m, neg_m);
+                    uint64_t sum2[2] = {0ull, 0ull};
+                    float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    uint32_t pk[32];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t *r = raw[i >> 1] + (i & 1) * 16;
-                    mx4[i] = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+                    for (int c = 0; c < 32; ++c) {
+                        const float s0 = __uint_as_float(raw[c >> 4][(2 * c) & 31]), s1 = __uint_as_float(raw[c >> 4][(2 * c + 1) & 31]);
+                        const uint64_t x = fma2(pair_of(s0, s1), scale2, neg2);
+                        float p0, p1;
+                        if (c % BY_FMA == BY_FMA - 1) {
+                            exp2_by_fma(x, p0, p1);
+                        } else {
+                            halves(x, p0, p1);
+                            p0 = ex2(p0);
+                            p1 = ex2(p1);
+                        }
+                        mx4[c & 3] = fmaxf(mx4[c & 3], fmaxf(s0, s1));
+                        sum2[c & 1] = add2(sum2[c & 1], pair_of(p0, p1));
+                        pk[c] = pack_bf16x2(p0, p1);
+                    }
+                    const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * p.scale_log2;      // the scale is positive
+                    const bool move = mx > m_used + RESCALE_STEP;      // also true for the first key that the row sees
+                    if (!__any_sync(FULL, move)) {
+                        float s0, s1;
+                        halves(add2(sum2[0], sum2[1]), s0, s1);
+                        l_sum += s0 + s1;
+                        tmem_st32(scores, pk);                         // P over the first half of its scores
+                        break;
+                    }
+                    const float alpha = move ? ex2(m_used - mx) : 1.f;         // 0 when m_used = -inf
+                    if (move) m_used = mx;
+                    l_sum *= alpha;
+                    if (kb != first) {
+                        // O has to hold all blocks so far (P V two blocks back is over: these scores were issued after it)
+                        wait(pv_done + 8 * (2 * s + (buf ^ 1)), (uint32_t)(((count - 1) >> 1) & 1), gave_up);
+                        tc_fence_after();
 #pragma unroll
-                    for (int c = 2; c < 16; c += 2) mx4[i] = fmaxf(mx4[i], fmaxf(__uint_as_float(r[c]), __uint_as_float(r[c + 1])));
-                }
-                const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * p.scale_log2;      // the scale is positive
-                float alpha = 1.f;
-                const bool move = mx > m_used + RESCALE_STEP;      // also true for the first key that the row sees
-                if (move) {
-                    alpha = ex2(m_used - mx);                      // 0 when m_used = -inf
-                    m_used = mx;
-                }
-                if (kb != first && __any_sync(FULL, move)) {
-                    // O has to hold all blocks so far (P V two blocks back is over: these scores were issued after it)
-                    wait(pv_done + 8 * (2 * s + (buf ^ 1)), (uint32_t)(((count - 1) >> 1) & 1), gave_up);
-                    tc_fence_after();
+                        for (int q = 0; q < D / 16; ++q) {
+                            uint32_t ov[16];
+                            tmem_ld16(output + 16 * q, ov);
+                            tmem_wait_ld();
 #pragma unroll
-                    for (int q = 0; q < D / 16; ++q) {
-                        uint32_t ov[16];
-                        tmem_ld16(output + 16 * q, ov);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int c = 0; c < 16; ++c) ov[c] = __float_as_uint(__uint_as_float(ov[c]) * alpha);
-                        tmem_st16(output + 16 * q, ov);
+                            for (int c = 0; c < 16; ++c) ov[c] = __float_as_uint(__uint_as_float(ov[c]) * alpha);
+                            tmem_st16(output + 16 * q, ov);
+                        }
                     }
                 }
-                const float neg_m = m_used == -INFINITY ? 0.f : -m_used;
-                const uint64_t neg2 = pair_of(neg_m, neg_m);
-                uint64_t sum2[2] = {0ull, 0ull};
-                uint32_t pk[32];
-#pragma unroll
-                for (int c = 0; c < 32; ++c) {
-                    const uint64_t x = fma2(pair_of(__uint_as_float(raw[c >> 4][(2 * c) & 31]), __uint_as_float(raw[c >> 4][(2 * c + 1) & 31])), scale2, neg2);
-                    float p0, p1;
-                    if (c % BY_FMA == BY_FMA - 1) {
-                        exp2_by_fma(x, p0, p1);
-                    } else {
-                        halves(x, p0, p1);
-                        p0 = ex2(p0);
-                        p1 = ex2(p1);
-                    }
-                    sum2[c & 1] = add2(sum2[c & 1], pair_of(p0, p1));
-                    pk[c] = pack_bf16x2(p0, p1);
-                }
-                tmem_st32(scores, pk);                             // P over the first half of its scores
-                float s0, s1;
-                halves(add2(sum2[0], sum2[1]), s0, s1);
-                l_sum = l_sum * alpha + (s0 + s1);
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
