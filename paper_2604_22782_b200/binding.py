@@ -233,28 +233,30 @@ def _nbytes(t: torch.Tensor) -> int:
     return t.numel() * t.element_size()
 
 
-def _rows(name: str, t: Optional[torch.Tensor], shape) -> Optional[torch.Tensor]:
-    """Checks bf16 rows [n][heads][dim] on the device whose heads are dense and whose rows may be further apart
-    (a slice of a fused projection)."""
-    if t is None:
-        return None
-    if t.dtype != torch.bfloat16:
+def _checked(name: str, t: torch.Tensor, dtype, shape, device: int) -> int:
+    """The pointer of a dense tensor on the current device; `_arg` says what is wrong with another one.  (These calls
+    are a few microseconds long: what is asked of a tensor is asked once.)"""
+    if t.dtype is dtype and t.get_device() == device and t.is_contiguous() and t.shape == shape:
+        return t.data_ptr()
+    _arg(name, t, dtype, shape)
+    raise ValueError(f"{name}: is on {t.device}, the current device is cuda:{device}")
+
+
+def _rows(name: str, t: torch.Tensor, n: int, heads: int, dim: int, device: int):
+    """Pointer and row stride (elements) of bf16 rows [n][heads][dim] whose heads are dense and whose rows may be further
+    apart (a slice of a fused projection)."""
+    if t.dtype is not torch.bfloat16:
         raise TypeError(f"{name}: expected {torch.bfloat16}, got {t.dtype}")
-    if not t.is_cuda:
-        raise ValueError(f"{name}: expected a CUDA tensor")
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    n, heads, dim = shape
-    if n and heads and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim) or (n > 1 and t.stride(0) < heads * dim)):
+    if t.get_device() != device:
+        raise ValueError(f"{name}: expected a tensor on cuda:{device}, got {t.device}")
+    if t.shape != (n, heads, dim):
+        raise ValueError(f"{name}: expected shape {(n, heads, dim)}, got {tuple(t.shape)}")
+    row, head, one = t.stride()
+    if n <= 1:                      # (a single row's stride says nothing)
+        row = heads * dim
+    if n and heads and (one != 1 or (heads > 1 and head != dim) or row < heads * dim):
         raise ValueError(f"{name}: the rows' heads must be dense")
-    return t
-
-
-def _row_stride(t: Optional[torch.Tensor]) -> int:
-    """Elements from row to row; a single row's stride says nothing and may not even be a row long."""
-    if t is None:
-        return 0
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    return t.data_ptr(), row
 
 
 class SkvRope:
@@ -372,29 +374,30 @@ class SkvCache:
                         slot_map: Optional[torch.Tensor], stream=None) -> None:
         """Q, Q_out [n][q_heads][head_dim], K, V [n][kv_heads][head_dim] with any row stride; positions [n] or
         [n_axes][n] int32; slot_map [n] int64.  On a layer that is not an owner K, V, slot_map are not used."""
-        self._on_current_device(Q, Q_out, K, V, positions, slot_map)
-        n = positions.shape[-1]
-        q_heads = 0 if Q is None else Q.shape[1]
-        _rows("Q", Q, (n, q_heads, self.head_dim))
-        _rows("Q_out", Q_out, (n, q_heads, self.head_dim))
+        device = self._current_device()
+        n = positions.shape[-1] if positions.dim() else -1
+        axes = 1 if positions.dim() == 1 else positions.shape[0] if positions.dim() == 2 else -1
+        if positions.dtype is not torch.int32:
+            raise TypeError("positions: expected an int32 tensor")
+        if positions.get_device() != device:
+            raise ValueError(f"positions: expected a tensor on cuda:{device}, got {positions.device}")
+        if axes != rope.n_axes or (n > 1 and positions.stride(-1) != 1):
+            raise ValueError(f"positions: expected [{rope.n_axes}][n] with dense rows, got {tuple(positions.shape)}")
         if (Q is None) != (Q_out is None):
             raise ValueError("Q and Q_out go together")
-        if positions.dtype != torch.int32 or not positions.is_cuda:
-            raise TypeError("positions: expected an int32 CUDA tensor")
-        axes = 1 if positions.dim() == 1 else positions.shape[0]
-        if positions.dim() not in (1, 2) or axes != rope.n_axes or (n > 1 and positions.stride(-1) != 1):
-            raise ValueError(f"positions: expected [{rope.n_axes}][n] with dense rows, got {tuple(positions.shape)}")
-        pos_stride = positions.stride(0) if axes > 1 else n
-        if 0 <= layer < self.n_layers and self.r[layer] == layer:
-            _rows("K", K, (n, self.kv_heads, self.head_dim))
-            _rows("V", V, (n, self.kv_heads, self.head_dim))
-            _arg("slot_map", slot_map, torch.int64, (n,))
-        else:
-            K = V = slot_map = None
-        rc = lib.skv_rope_append(self._h, layer, rope._h, _ptr(Q), _row_stride(Q), _ptr(Q_out), _row_stride(Q_out), _ptr(K),
-                                 _row_stride(K), _ptr(V), _row_stride(V), _ptr(positions), pos_stride, _ptr(slot_map), n,
-                                 q_heads, _stream_ptr(stream))
-        _check(rc, "skv_rope_append")
+        q_heads = 0 if Q is None else Q.shape[1]
+        q, qs = (None, 0) if Q is None else _rows("Q", Q, n, q_heads, self.head_dim, device)
+        o, os_ = (None, 0) if Q is None else _rows("Q_out", Q_out, n, q_heads, self.head_dim, device)
+        k = v = slots = None
+        ks = vs = 0
+        if 0 <= layer < self.n_layers and self.r[layer] == layer and K is not None and V is not None and slot_map is not None:
+            k, ks = _rows("K", K, n, self.kv_heads, self.head_dim, device)
+            v, vs = _rows("V", V, n, self.kv_heads, self.head_dim, device)
+            slots = _checked("slot_map", slot_map, torch.int64, (n,), device)
+        rc = lib.skv_rope_append(self._h, layer, rope._h, q, qs, o, os_, k, ks, v, vs, positions.data_ptr(),
+                                 positions.stride(0) if axes > 1 else n, slots, n, q_heads, _stream_ptr(stream))
+        if rc:
+            _check(rc, "skv_rope_append")
 
     # -- a step's tables
     def skv_plan_step(self, page_table: torch.Tensor, seq_lens: torch.Tensor, new_lens: torch.Tensor,
@@ -403,52 +406,54 @@ class SkvCache:
                       stream=None) -> None:
         """page_table [batch][width], seq_lens, new_lens, seq_lens_out [batch], free_pages [capacity], n_free, n_free_out [1],
         cu_q_lens [batch+1], positions [max_tokens]: int32; slot_map [max_tokens]: int64."""
-        self._on_current_device(page_table, seq_lens, new_lens, free_pages, n_free, slot_map, cu_q_lens, seq_lens_out, n_free_out, positions)
-        _arg("seq_lens", seq_lens, torch.int32)
+        device, i32 = self._current_device(), torch.int32
         if seq_lens.dim() != 1:
             raise ValueError("seq_lens: expected [batch]")
-        batch, i32 = seq_lens.shape[0], torch.int32
-        _arg("page_table", page_table, i32)
+        batch = seq_lens.shape[0]
         if page_table.dim() != 2 or page_table.shape[0] != batch:
             raise ValueError(f"page_table: expected [{batch}][width], got {tuple(page_table.shape)}")
-        _arg("new_lens", new_lens, i32, (batch,))
-        _arg("seq_lens_out", seq_lens_out, i32, (batch,))
-        _arg("cu_q_lens", cu_q_lens, i32, (batch + 1,))
-        _arg("free_pages", free_pages, i32)
-        _arg("n_free", n_free, i32, (1,))
-        _arg("n_free_out", n_free_out, i32, (1,))
-        _arg("slot_map", slot_map, torch.int64)
-        _arg("positions", positions, i32, min_numel=slot_map.numel())
-        rc = lib.skv_plan_step(self._h, _ptr(page_table), page_table.shape[1], _ptr(seq_lens), _ptr(new_lens), batch,
-                               _ptr(free_pages), free_pages.numel(), _ptr(n_free), slot_map.numel(), _ptr(slot_map),
-                               _ptr(positions), _ptr(cu_q_lens), _ptr(seq_lens_out), _ptr(n_free_out), _stream_ptr(stream))
-        _check(rc, "skv_plan_step")
+        row, width, capacity, tokens = (batch,), page_table.shape[1], free_pages.numel(), slot_map.numel()
+        pos = None
+        if positions is not None:
+            if positions.numel() < tokens:
+                raise ValueError(f"positions: needs at least {tokens} elements, has {positions.numel()}")
+            pos = _checked("positions", positions, i32, positions.shape, device)
+        rc = lib.skv_plan_step(self._h, _checked("page_table", page_table, i32, (batch, width), device), width,
+                               _checked("seq_lens", seq_lens, i32, row, device), _checked("new_lens", new_lens, i32, row, device), batch,
+                               _checked("free_pages", free_pages, i32, (capacity,), device), capacity,
+                               _checked("n_free", n_free, i32, (1,), device), tokens,
+                               _checked("slot_map", slot_map, torch.int64, (tokens,), device), pos,
+                               _checked("cu_q_lens", cu_q_lens, i32, (batch + 1,), device),
+                               _checked("seq_lens_out", seq_lens_out, i32, row, device),
+                               _checked("n_free_out", n_free_out, i32, (1,), device), _stream_ptr(stream))
+        if rc:
+            _check(rc, "skv_plan_step")
 
     def skv_plan_release(self, page_table: torch.Tensor, first_page: torch.Tensor, end_page: torch.Tensor,
                          free_pages: torch.Tensor, n_free: torch.Tensor, n_free_out: torch.Tensor, stream=None) -> None:
-        self._on_current_device(page_table, first_page, end_page, free_pages, n_free, n_free_out)
-        _arg("page_table", page_table, torch.int32)
+        device, i32 = self._current_device(), torch.int32
         if page_table.dim() != 2:
             raise ValueError(f"page_table: expected [batch][width], got {tuple(page_table.shape)}")
-        batch = page_table.shape[0]
-        _arg("first_page", first_page, torch.int32, (batch,))
-        _arg("end_page", end_page, torch.int32, (batch,))
-        _arg("free_pages", free_pages, torch.int32)
-        _arg("n_free", n_free, torch.int32, (1,))
-        _arg("n_free_out", n_free_out, torch.int32, (1,))
-        rc = lib.skv_plan_release(self._h, _ptr(page_table), page_table.shape[1], _ptr(first_page), _ptr(end_page), batch,
-                                  _ptr(free_pages), free_pages.numel(), _ptr(n_free), _ptr(n_free_out), _stream_ptr(stream))
-        _check(rc, "skv_plan_release")
+        batch, width = page_table.shape
+        capacity = free_pages.numel()
+        rc = lib.skv_plan_release(self._h, _checked("page_table", page_table, i32, (batch, width), device), width,
+                                  _checked("first_page", first_page, i32, (batch,), device),
+                                  _checked("end_page", end_page, i32, (batch,), device), batch,
+                                  _checked("free_pages", free_pages, i32, (capacity,), device), capacity,
+                                  _checked("n_free", n_free, i32, (1,), device), _checked("n_free_out", n_free_out, i32, (1,), device),
+                                  _stream_ptr(stream))
+        if rc:
+            _check(rc, "skv_plan_release")
 
-    def _on_current_device(self, *tensors: Optional[torch.Tensor]) -> None:
-        """Launches go to the current device: it has to be the pool's, and the tensors' (host tensors are told apart
-        by the checks that follow)."""
+    def _current_device(self) -> int:
+        """The current device, to which launches go: it has to be the pool's.  (-2, where no tensor is, for a handle
+        without memory, which launches nothing.)"""
         if self.pool is None:
-            return
+            return -2
         device = torch.cuda.current_device()
-        for t in (self.pool,) + tensors:
-            if t is not None and t.is_cuda and t.get_device() != device:
-                raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{device}")
+        if self.pool.get_device() != device:
+            raise ValueError(f"the cache's pool is on {self.pool.device}, the current device is cuda:{device}")
+        return device
 
     # -- Load + Attn
     def _decode_args(self, Q, page_table, seq_lens, out):
@@ -484,13 +489,20 @@ class SkvCache:
     def skv_decode_attn_window(self, layer: int, Q: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor,
                                out: torch.Tensor, workspace: torch.Tensor, window: int, sinks: int = 0,
                                scale: float = 0.0, stream=None) -> None:
-        self._on_current_device(Q, page_table, seq_lens, out, workspace)
-        batch, q_heads = self._decode_args(Q, page_table, seq_lens, out)
-        _arg("workspace", workspace, torch.uint8)
-        rc = lib.skv_decode_attn_window(self._h, layer, _ptr(Q), _ptr(page_table), _ptr(seq_lens), _ptr(out), batch,
-                                        q_heads, page_table.shape[1], _i32("window", window), _i32("sinks", sinks), scale,
-                                        _ptr(workspace), _nbytes(workspace), _stream_ptr(stream))
-        _check(rc, "skv_decode_attn_window")
+        device, bf16, i32 = self._current_device(), torch.bfloat16, torch.int32
+        if Q.dim() != 3 or Q.shape[2] != self.head_dim:
+            raise ValueError(f"Q: expected [batch][q_heads][{self.head_dim}], got {tuple(Q.shape)}")
+        batch, q_heads, _ = shape = Q.shape
+        if page_table.dim() != 2 or page_table.shape[0] != batch:
+            raise ValueError(f"page_table: expected [{batch}][width], got {tuple(page_table.shape)}")
+        width, nbytes = page_table.shape[1], workspace.numel()
+        rc = lib.skv_decode_attn_window(self._h, layer, _checked("Q", Q, bf16, shape, device),
+                                        _checked("page_table", page_table, i32, (batch, width), device),
+                                        _checked("seq_lens", seq_lens, i32, (batch,), device), _checked("out", out, bf16, shape, device),
+                                        batch, q_heads, width, _i32("window", window), _i32("sinks", sinks), scale,
+                                        _checked("workspace", workspace, torch.uint8, (nbytes,), device), nbytes, _stream_ptr(stream))
+        if rc:
+            _check(rc, "skv_decode_attn_window")
 
     def skv_decode_attn_static(self, layer: int, Q: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor,
                                out: torch.Tensor, scale: float = 0.0, stream=None) -> None:
@@ -527,12 +539,23 @@ class SkvCache:
     def skv_prefill_attn_window(self, layer: int, Q: torch.Tensor, cu_q_lens: torch.Tensor, page_table: torch.Tensor,
                                 seq_lens: torch.Tensor, out: torch.Tensor, max_q_len: int, window: int, sinks: int = 0,
                                 scale: float = 0.0, stream=None) -> None:
-        self._on_current_device(Q, cu_q_lens, page_table, seq_lens, out)
-        batch, q_heads = self._prefill_args(Q, cu_q_lens, page_table, seq_lens, out)
-        rc = lib.skv_prefill_attn_window(self._h, layer, _ptr(Q), _ptr(cu_q_lens), _ptr(page_table), _ptr(seq_lens),
-                                         _ptr(out), batch, max_q_len, q_heads, page_table.shape[1], _i32("window", window),
-                                         _i32("sinks", sinks), scale, _stream_ptr(stream))
-        _check(rc, "skv_prefill_attn_window")
+        device, bf16, i32 = self._current_device(), torch.bfloat16, torch.int32
+        if Q.dim() != 3 or Q.shape[2] != self.head_dim:
+            raise ValueError(f"Q: expected [n_q][q_heads][{self.head_dim}], got {tuple(Q.shape)}")
+        if seq_lens.dim() != 1:
+            raise ValueError("seq_lens: expected [batch]")
+        batch = seq_lens.shape[0]
+        if page_table.dim() != 2 or page_table.shape[0] != batch:
+            raise ValueError(f"page_table: expected [{batch}][width], got {tuple(page_table.shape)}")
+        shape, width = Q.shape, page_table.shape[1]
+        rc = lib.skv_prefill_attn_window(self._h, layer, _checked("Q", Q, bf16, shape, device),
+                                         _checked("cu_q_lens", cu_q_lens, i32, (batch + 1,), device),
+                                         _checked("page_table", page_table, i32, (batch, width), device),
+                                         _checked("seq_lens", seq_lens, i32, (batch,), device), _checked("out", out, bf16, shape, device),
+                                         batch, _i32("max_q_len", max_q_len), shape[1], width, _i32("window", window), _i32("sinks", sinks),
+                                         scale, _stream_ptr(stream))
+        if rc:
+            _check(rc, "skv_prefill_attn_window")
 
     def skv_prefill_attn_src(self, src_layer: int, Q: torch.Tensor, cu_q_lens: torch.Tensor, page_table: torch.Tensor,
                              seq_lens: torch.Tensor, out: torch.Tensor, max_q_len: int, scale: float = 0.0,

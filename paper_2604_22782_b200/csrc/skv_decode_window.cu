@@ -14,6 +14,7 @@
 #include "skv_common.cuh"
 #include "skv_decode_states.cuh"
 #include "skv_walk.cuh"
+#include <atomic>
 #include <type_traits>
 
 namespace skv {
@@ -259,8 +260,15 @@ cudaError_t launch_t(const DecodeParams &p, int G, int sm_count, bool pdl, cudaS
     cudaError_t e = ensure_dynamic_smem(kern, smem);
     if (e != cudaSuccess) return e;
     if (f.ranks > 8) {
-        e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-        if (e != cudaSuccess) return e;
+        static std::atomic<uint64_t> allowed[2];           // (bit per device: asking every time costs more than the launch)
+        int dev = 0;
+        if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
+        const uint64_t bit = 1ull << (dev & 63);
+        if (dev > 63 || !(allowed[f.warps == 8] & bit)) {
+            e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+            if (e != cudaSuccess) return e;
+            allowed[f.warps == 8] |= bit;
+        }
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(segments * f.ranks));

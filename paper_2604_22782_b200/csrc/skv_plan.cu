@@ -232,10 +232,10 @@ int plan_max_batch() { return PLAN_MAX_BATCH; }
 
 cudaError_t launch_plan_step(const PlanParams &p, bool in_place, int sm_count, bool pdl, cudaStream_t s)
 {
-    // A CTA per 4096 tokens (the scans are repeated by each), at most one per SM, or one cluster of the portable
+    // A token per thread (the scans are repeated by each CTA), at most a CTA per SM, or one cluster of the portable
     // size where outputs may lie on inputs.
     const int most = in_place ? 8 : sm_count;
-    int64_t ctas = (p.max_tokens + 4095) / 4096;
+    int64_t ctas = (p.max_tokens + 1023) / 1024;
     ctas = ctas < 1 ? 1 : ctas > most ? most : ctas;
     const int threads = p.B <= 256 && p.max_tokens <= 1024 ? 256 : 1024;
     const size_t smem = (size_t)(3 * p.B + 2) * sizeof(int32_t);
