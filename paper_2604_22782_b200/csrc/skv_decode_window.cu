@@ -185,33 +185,6 @@ __global__ void __launch_bounds__(NW * 32) decode_window_kernel(DecodeParams p, 
     cluster_wait();
 }
 
-template <int D, class State, int NW>
-cudaError_t launch_tt(const DecodeParams &p, int G, int ranks, int stages, bool pdl, cudaStream_t s)
-{
-    const size_t smem = 128 + (size_t)NW * stages * State::BLOCK + (size_t)(NW + 1) * part_floats(G, D) * 4 + (size_t)NW * stages * 8;
-    auto kern = decode_window_kernel<D, State, NW>;
-    cudaError_t e = ensure_dynamic_smem(kern, smem);
-    if (e != cudaSuccess) return e;
-    if (ranks > 8) {
-        e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-        if (e != cudaSuccess) return e;
-    }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(p.B * p.Hkv * ranks));
-    cfg.blockDim = dim3(NW * 32);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)ranks;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = pdl ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kern, p, G, stages);
-}
-
 // How a call is laid out: warps per CTA, pages in flight per warp, CTAs per segment.
 struct Shape { int warps, stages, ranks; };
 
@@ -276,13 +249,20 @@ cudaError_t launch_t(const DecodeParams &p, int G, int sm_count, bool pdl, cudaS
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)f.ranks;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    int n = 0;
+    if (f.ranks > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = (unsigned)f.ranks;
+        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (pdl) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
     cfg.attrs = attr;
-    cfg.numAttrs = pdl ? 2 : 1;
+    cfg.numAttrs = n;
     return cudaLaunchKernelEx(&cfg, kern, p, G, f.stages);
 }
 
