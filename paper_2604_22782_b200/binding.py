@@ -385,7 +385,7 @@ class SkvCache:
             raise ValueError(f"positions: expected [{rope.n_axes}][n] with dense rows, got {tuple(positions.shape)}")
         if (Q is None) != (Q_out is None):
             raise ValueError("Q and Q_out go together")
-        q_heads = 0 if Q is None else Q.shape[1]
+        q_heads = 0 if Q is None else Q.shape[1] if Q.dim() == 3 else -1
         q, qs = (None, 0) if Q is None else _rows("Q", Q, n, q_heads, self.head_dim, device)
         o, os_ = (None, 0) if Q is None else _rows("Q_out", Q_out, n, q_heads, self.head_dim, device)
         k = v = slots = None
