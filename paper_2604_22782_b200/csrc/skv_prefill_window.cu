@@ -329,7 +329,7 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
     // the sequences' tables
     for (int i = tid; i < p.B; i += THREADS) {
         const int qb = __ldg(p.cu_q + i), ql = __ldg(p.cu_q + i + 1) - qb, n = __ldg(p.seq_lens + i);
-        const bool fits = ql >= 0 && ql <= n && ql <= max_q_len && (int64_t)n <= (int64_t)p.pt_stride * PAGE;
+        const bool fits = qb >= 0 && ql >= 0 && ql <= n && ql <= max_q_len && (int64_t)n <= (int64_t)p.pt_stride * PAGE;
         if (!fits && blockIdx.x == 0) atomicOr(p.status, STATUS_BOUNDS);
         q_begin[i] = qb;
         q_len[i] = ql;

@@ -121,8 +121,8 @@ __host__ __device__ __forceinline__ WindowPages window_pages(int first, int n, i
 __host__ __device__ __forceinline__ uint32_t window_bits(int page, int lo, int hi, int sinks)
 {
     auto below = [&](int x) -> uint32_t {                   // tokens of the page below x
-        const int k = x - page * PAGE;
-        return k >= PAGE ? 0xFFFFu : k <= 0 ? 0u : (1u << k) - 1u;
+        const int k = x - page * PAGE, n = k < 0 ? 0 : k < PAGE ? k : PAGE;         // (no branches)
+        return (1u << n) - 1u;
     };
     return below(hi) & (~below(lo) | below(sinks));
 }
