@@ -651,7 +651,7 @@ int launch_splitk(skv_cache *c, int layer, const void *Q, const int32_t *page_ta
         plan->n_workers = W;
         plan->unit_tokens = umma ? decode_fp8_umma_tile_tokens() : PAGE;
         plan->finished_single = cta ? 1 : 0;
-        plan->merged = in_kernel_merge ? 1 : 0;
+        plan->merged = in_kernel_merge || window ? 1 : 0;
     }
     return SKV_OK;
 }
@@ -771,12 +771,8 @@ int skv_decode_attn_window(skv_cache *c, int layer, const void *Q, const int32_t
         const int n = batch - b < PIECE ? batch - b : PIECE;
         const uint8_t *q = static_cast<const uint8_t *>(Q) + (size_t)b * row;
         uint8_t *o = static_cast<uint8_t *>(out) + (size_t)b * row;
-        SplitkPlan plan;
-        int rc = launch_splitk(c, layer, q, page_table + (size_t)b * pt_stride, seq_lens + b, n, q_heads, pt_stride, scale,
-                               workspace, workspace_bytes, stream, &plan, o, 0, false, window, sinks);
-        if (rc) return rc;
-        // (the page counts the split-K launch left in the workspace: the lengths alone do not give them here)
-        rc = launch_merge_on(c, o, n, q_heads, workspace, workspace_bytes, stream, 0, &plan);
+        const int rc = launch_splitk(c, layer, q, page_table + (size_t)b * pt_stride, seq_lens + b, n, q_heads, pt_stride, scale,
+                                     workspace, workspace_bytes, stream, nullptr, o, 0, false, window, sinks);
         if (rc) return rc;
     }
     return SKV_OK;

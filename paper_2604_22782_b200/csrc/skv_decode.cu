@@ -23,19 +23,6 @@ namespace skv {
 
 namespace {
 
-__device__ __forceinline__ void segment_partials(int64_t T, int64_t W, int64_t seg, int64_t s0, int pages, int &slot0,
-                                                 int &n)
-{
-    if (T < W) {
-        slot0 = (int)(s0 + seg);
-        n = pages;
-    } else {
-        const int w_first = worker_of(s0, T, W);
-        slot0 = (int)(w_first + seg);
-        n = worker_of(s0 + pages - 1, T, W) - w_first + 1;
-    }
-}
-
 // Log-sum-exp merge of the n partials at slots slot0 .. slot0+n-1 for the G query heads of a
 // segment, by one warp:
 //   out[g, :] = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i,  M = max_i m_i.

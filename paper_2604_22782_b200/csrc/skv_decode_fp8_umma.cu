@@ -155,12 +155,31 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar)
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+// A segment's partials are counted at one word, by the launch's epoch (whatever the word held before): true for the n-th
+// arrival, which also clears it -- a launch replayed from a CUDA graph has the same epoch every time.
+__device__ __forceinline__ bool arrive_last(unsigned long long *word, unsigned long long epoch, int n)
+{
+    const unsigned long long key = epoch << 12;                  // (a segment has fewer than 2^12 partials: one per CTA)
+    __threadfence();                                             // the partial is there before its count ...
+    unsigned long long seen = *reinterpret_cast<volatile unsigned long long *>(word);
+    for (;;) {
+        const unsigned long long count = (seen & ~0xFFFull) == key ? (seen & 0xFFFull) + 1 : 1;
+        const unsigned long long was = atomicCAS(word, seen, count == (unsigned long long)n ? 0ull : key | count);
+        if (was == seen) {
+            __threadfence();                                     // ... and the others' are, for whoever came last
+            return count == (unsigned long long)n;
+        }
+        seen = was;
+    }
+}
+
 // WIN: the sliding-window instance (p.window, p.sinks): a tile is eight pages of the list of pages that hold a token
 // that is attended (window_pages), and comes with a 16-bit set of such tokens for each of its pages.
 template <int D, int GP, bool WIN>   // GP: the group size rounded up to a power of two (the softmax loops run over GP heads)
 // (bounds as for four CTAs per SM = 80 registers: shared memory admits three, and the registers left over let
-// a CTA of the merge kernel become resident beside them, which the launch chain needs to move on)
-__global__ void __launch_bounds__(THREADS, CTAS_PER_SM + 1) decode_fp8_umma_kernel(DecodeParams p, int G)
+// a CTA of the merge kernel become resident beside them, which the launch chain needs to move on; the
+// sliding-window instance has no merge launch behind it)
+__global__ void __launch_bounds__(THREADS, WIN ? CTAS_PER_SM : CTAS_PER_SM + 1) decode_fp8_umma_kernel(DecodeParams p, int G)
 {
     static_assert(D == 128, "the tile shapes below are those of head_dim 128");
     extern __shared__ __align__(128) uint8_t smem_raw[];
@@ -191,6 +210,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM + 1) decode_fp8_umma_kern
     const uint32_t bars = smem_u32(at);                at += 16 * 8;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(at);
     int *gave_up = reinterpret_cast<int *>(at + 4);
+    int *last_one = reinterpret_cast<int *>(at + 8);
     uint16_t *live_sets = reinterpret_cast<uint16_t *>(at + 16);      // WIN: [4 tiles][TP pages], slots as meta's
     const uint32_t k_full = bars, k_empty = bars + 16, v_full = bars + 32, v_empty = bars + 48, s_ready = bars + 64,
                    p_ready = bars + 80, pv_done = bars + 96, q_full = bars + 112;
@@ -233,8 +253,13 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM + 1) decode_fp8_umma_kern
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-    if (blockIdx.x == 0)       // the merge kernel reads the counts from global memory
+    if (WIN) {                 // a sequence without tokens: rows of zeros
+        for (int b = blockIdx.x; b < p.B; b += gridDim.x)
+            if (prefix[b + 1] == prefix[b])
+                for (int i = tid; i < p.Hq * D / 2; i += THREADS) reinterpret_cast<uint32_t *>(p.out + (int64_t)b * p.Hq * D)[i] = 0u;
+    } else if (blockIdx.x == 0) {       // the merge kernel reads the counts from global memory
         for (int i = tid; i <= p.B; i += THREADS) p.prefix[i] = prefix[i];
+    }
 
     const int64_t W = gridDim.x, w = blockIdx.x;
     const int64_t T = (int64_t)prefix[p.B] * p.Hkv;
@@ -457,6 +482,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM + 1) decode_fp8_umma_kern
 #pragma unroll
         for (int h = 0; h < GP; ++h) { m_ref[h] = -INFINITY; l_sum[h] = 0.f; qs[h] = 0.f; }
         bool ok = true;
+        int pieces = 0;                                  // WIN, thread 0: segments shared with other ranges so far
         for (int k = 0; ok; ++k) {
             const int s = k & 1;
             // (after a timeout the thread goes on with whatever it finds, up to the barrier below, where all leave)
@@ -616,8 +642,24 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM + 1) decode_fp8_umma_kern
                 }
                 softmax_sync();
                 const int64_t seg = (int64_t)m.b * p.Hkv + m.h;
-                const int64_t slot = partial_slot(T, W, w, x0, seg);
                 const float back = 1.f / P_SCALE;
+                auto write_row = [&](int h, float o) {         // dim tid of head h, two dims a store
+                    const float next = __shfl_down_sync(FULL, o, 1);
+                    if (h < G && !(tid & 1))
+                        reinterpret_cast<uint32_t *>(p.out + ((int64_t)m.b * p.Hq + (int64_t)m.h * G + h) * D)[tid >> 1] = pack_bf16x2(o, next);
+                };
+                const int64_t tiles = WIN ? prefix[m.b + 1] - prefix[m.b] : 0, s0 = WIN ? (int64_t)prefix[m.b] * p.Hkv + m.h * tiles : 0;
+                if (WIN && s0 >= x0 && s0 + tiles <= x0 + n) {
+                    // the segment lies inside this range: finished here
+                    const volatile float *r = red_l;
+#pragma unroll
+                    for (int h = 0; h < GP; ++h)
+                        write_row(h, (__uint_as_float(ov[h]) + __uint_as_float(ov[8 + h]) * (1.f / REM_SCALE)) * (back / ((r[h] + r[8 + h]) + (r[16 + h] + r[24 + h]))));
+                    tc_fence_before();
+                    if (m.flags & TILE_END) break;
+                    continue;
+                }
+                const int64_t slot = partial_slot(T, W, w, x0, seg);
 #pragma unroll
                 for (int h = 0; h < GP; ++h)
                     if (h < G)
@@ -629,11 +671,63 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM + 1) decode_fp8_umma_kern
                     for (int h = 1; h < GP; ++h) mine = tid == h ? m_ref[h] : mine;
                     *reinterpret_cast<float2 *>(p.part_ml + (slot * G + tid) * 2) = make_float2(mine, (r[0] + r[8]) + (r[16] + r[24]));
                 }
+                if (WIN) {
+                    int slot0, n_part;
+                    segment_partials(T, W, seg, s0, (int)tiles, slot0, n_part);
+                    softmax_sync();
+                    if (tid == 0) {
+                        *last_one = arrive_last(p.tags + slot0, p.epoch, n_part);
+                        ++pieces;
+                    }
+                    softmax_sync();
+                    if (*reinterpret_cast<volatile int *>(last_one)) {
+                        __threadfence();
+                        float M[GP], L[GP], acc[GP];
+#pragma unroll
+                        for (int h = 0; h < GP; ++h) { M[h] = -INFINITY; L[h] = 0.f; acc[h] = 0.f; }
+#pragma unroll 2
+                        for (int i = 0; i < n_part; ++i) {
+                            float2 ml[GP];
+                            float o[GP];
+#pragma unroll
+                            for (int h = 0; h < GP; ++h) {
+                                const int64_t at = (int64_t)(slot0 + i) * G + (h < G ? h : 0);
+                                ml[h] = __ldcg(reinterpret_cast<const float2 *>(p.part_ml) + at);
+                                o[h] = __ldcg(p.part_o + at * D + tid);
+                            }
+#pragma unroll
+                            for (int h = 0; h < GP; ++h) {
+                                const float M_new = fmaxf(M[h], ml[h].x), keep = fast_exp2(M[h] - M_new), wt = fast_exp2(ml[h].x - M_new);
+                                L[h] = fmaf(wt, ml[h].y, L[h] * keep);
+                                acc[h] = fmaf(wt, o[h], acc[h] * keep);
+                                M[h] = M_new;
+                            }
+                        }
+#pragma unroll
+                        for (int h = 0; h < GP; ++h) write_row(h, acc[h] * (1.f / L[h]));
+                    }
+                }
                 tc_fence_before();
             }
             if (m.flags & TILE_END) break;
         }
-        if (!ok && tid == 0) { atomicOr(p.status, STATUS_TIMEOUT); *gave_up = 1; }
+        if (!ok && tid == 0) {
+            atomicOr(p.status, STATUS_TIMEOUT);
+            *gave_up = 1;
+            if (WIN) {
+                // The segments that this range shares are waited for by the others' counts, now and (a captured call) at the next
+                // replay: those it has not arrived at yet get their arrival, in the order of the walk.
+                const int64_t ends[2] = {x_first, reverse ? x0 : x0 + n - 1};
+                for (int i = 0, k = 0; i < 2; ++i) {
+                    const Cursor c = locate(prefix, p.B, p.Hkv, ends[i]);
+                    const int64_t tiles = prefix[c.b + 1] - prefix[c.b], s0 = (int64_t)prefix[c.b] * p.Hkv + c.h * tiles;
+                    if ((s0 >= x0 && s0 + tiles <= x0 + n) || (i == 1 && ends[0] >= s0 && ends[0] < s0 + tiles)) continue;
+                    int slot0, n_part;
+                    segment_partials(T, W, (int64_t)c.b * p.Hkv + c.h, s0, (int)tiles, slot0, n_part);
+                    if (k++ >= pieces) arrive_last(p.tags + slot0, p.epoch, n_part);
+                }
+            }
+        }
     }
 
     // ---- common exit ----

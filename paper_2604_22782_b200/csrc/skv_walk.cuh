@@ -142,4 +142,18 @@ __device__ __forceinline__ int partial_slot(int64_t T, int64_t W, int64_t w, int
     return (int)((T < W ? x_any : w) + seg);
 }
 
+// the partials of segment seg, whose units are [s0, s0 + pages): n of them from slot slot0 on
+__device__ __forceinline__ void segment_partials(int64_t T, int64_t W, int64_t seg, int64_t s0, int pages, int &slot0,
+                                                 int &n)
+{
+    if (T < W) {
+        slot0 = (int)(s0 + seg);
+        n = pages;
+    } else {
+        const int w_first = worker_of(s0, T, W);
+        slot0 = (int)(w_first + seg);
+        n = worker_of(s0 + pages - 1, T, W) - w_first + 1;
+    }
+}
+
 }  // namespace skv
