@@ -156,17 +156,29 @@ WorkspaceLayout workspace_layout(const skv_cache *c, int batch, int q_heads, int
 // FP8 pages go to the tcgen05 kernel (a worker is a CTA there) unless the mma.sync variant is asked for
 bool fp8_on_umma(const skv_cache *c) { return c->fp8 && c->tune.variant != 2 && decode_fp8_umma_supported(c->head_dim, 1); }
 
-// A windowed call on FP8 pages runs the tcgen05 split-K kernel where each of its workers has ten tiles or more, else the
-// kernel that keeps a segment in one CTA or cluster: shorter ranges cut most segments, and the merge costs more than the
-// faster arithmetic brings.  (us, tcgen05 against the other: 76 tiles a worker 186 / 217, 21 tiles 54 / 66, 10 tiles 35.6 / 37.5
-// and 33.9 / 34.3, 6 tiles 46 / 32, 5 tiles 27.6 / 23.7.)
+// sequences of one such launch: a larger batch goes in pieces
+constexpr int FP8_WINDOW_PIECE = 4096;
+
+// Ranges of the tcgen05 FP8 kernel's sliding-window form: as many CTAs to an SM as fit beside each other with the batch's table
+int fp8_window_workers(const skv_cache *c, int batch)
+{
+    const size_t smem = decode_fp8_umma_smem_bytes(c->head_dim, batch < FP8_WINDOW_PIECE ? batch : FP8_WINDOW_PIECE, true);
+    int ctas = decode_fp8_umma_ctas_per_sm();
+    while (ctas > 1 && smem > ((size_t)c->max_smem_optin + 1024) / ctas - 1024) --ctas;
+    return c->sm_count * ctas;
+}
+
+// A windowed call on FP8 pages runs the tcgen05 split-K kernel where each of its workers has six tiles or more, else the
+// kernel that keeps a segment in one CTA or cluster: that one starts and ends faster, by some 10 us, and the tcgen05
+// arithmetic is faster by half.  (us, tcgen05 against the other, by tiles a worker: 76 169 / 233, 21 47 / 65, 14 39 / 52, 10 31.4 / 37.0,
+// 7.4 26.0 / 33.7 and with 8 heads a kv head 29.5 / 34.8, 5.8 22.8 / 23.4, 5.2 23.6 / 20.2, 4.8 24.8 / 21.5, 2.4 25.6 / 13.9.)
 bool fp8_window_on_umma(const skv_cache *c, int batch, int G, int pt_stride, int window, int sinks)
 {
     if (!fp8_on_umma(c) || !decode_fp8_umma_supported(c->head_dim, G)) return false;
     int64_t tokens = (int64_t)window + sinks;
     if (tokens > (int64_t)pt_stride * PAGE) tokens = (int64_t)pt_stride * PAGE;
     const int64_t tiles = (tokens + decode_fp8_umma_tile_tokens() - 1) / decode_fp8_umma_tile_tokens();
-    return (int64_t)batch * c->kv_heads * tiles >= 10 * (int64_t)c->sm_count * decode_fp8_umma_ctas_per_sm();
+    return (int64_t)batch * c->kv_heads * tiles >= 6 * (int64_t)fp8_window_workers(c, batch);
 }
 
 // Workers of a warp-per-range (or tcgen05) split-K launch under the current variant and launch shape.  A
@@ -588,8 +600,8 @@ int launch_splitk(skv_cache *c, int layer, const void *Q, const int32_t *page_ta
         warps = 1;
         ctas = 8;
     }
-    const int W = cta ? n_cta_workers_of(c) : n_workers_of(c);
-    const size_t smem = umma  ? decode_fp8_umma_smem_bytes(c->head_dim, batch)
+    const int W = cta ? n_cta_workers_of(c) : umma && window ? fp8_window_workers(c, batch) : n_workers_of(c);
+    const size_t smem = umma  ? decode_fp8_umma_smem_bytes(c->head_dim, batch, window > 0)
                         : cta ? decode_cta_smem_bytes(c->head_dim, batch, G, c->cta_consumers, cta_S, c->fp8)
                               : decode_smem_bytes(c->head_dim, batch, warps, c->tune.stages, c->fp8);
     if (smem == 0 || smem > (size_t)c->max_smem_optin) return SKV_ERR_UNSUPPORTED;
@@ -764,8 +776,7 @@ int skv_decode_attn_window(skv_cache *c, int layer, const void *Q, const int32_t
         c->launches += 1;
         return SKV_OK;
     }
-    // The tcgen05 kernel keeps two words per sequence in shared memory beside its rings: larger batches go in pieces.
-    constexpr int PIECE = 4096;
+    constexpr int PIECE = FP8_WINDOW_PIECE;
     const size_t row = (size_t)q_heads * c->head_dim * 2;
     for (int b = 0; b < batch; b += PIECE) {
         const int n = batch - b < PIECE ? batch - b : PIECE;

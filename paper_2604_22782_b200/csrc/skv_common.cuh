@@ -243,7 +243,7 @@ cudaError_t launch_gather(const GatherParams &p, cudaStream_t s);
 bool decode_fp8_umma_supported(int D, int G);
 int decode_fp8_umma_ctas_per_sm();
 int decode_fp8_umma_tile_tokens();           // tokens per unit of its flattened list
-size_t decode_fp8_umma_smem_bytes(int D, int B);
+size_t decode_fp8_umma_smem_bytes(int D, int B, bool window);
 cudaError_t launch_decode_fp8_umma(const DecodeParams &p, int D, int G, int grid, bool pdl, cudaStream_t s);
 cudaError_t launch_append_fp8(const AppendFp8Params &p, int n_layers, bool pdl, cudaStream_t s);
 cudaError_t launch_gather_fp8(const GatherFp8Params &p, cudaStream_t s);

@@ -19,6 +19,10 @@
 // the output, and only moves when the maximum of e has grown by more than 2^3.5: P' <= 362 fits E4M3
 // whatever the spread of the V scales, O^T is rescaled (through registers) rarely, and the partial
 // (reference, sum of 2^(score - reference), O^T / 32) is in the merge kernel's usual form.
+// Over a sliding window (skv_decode_attn_window) segments are short and most lie inside one range: those are finished here,
+// and of a segment that several CTAs share the last one to arrive joins the partials, in their order, so that results repeat.
+// No merge launch follows: with one the same call (128 sequences, window 4096, 1.07 GB) took 193 us, 27 of them from the end
+// of this kernel to the start of the next call's, and takes 169 (6.3 TB/s, 0.965 of the measured copy peak).
 //
 // Six warps:
 //   warps 0-3  softmax: thread t owns token t of the tile (TMEM lane t); at the end of a run thread
@@ -166,8 +170,9 @@ __device__ __forceinline__ bool arrive_last(unsigned long long *word, unsigned l
         const unsigned long long count = (seen & ~0xFFFull) == key ? (seen & 0xFFFull) + 1 : 1;
         const unsigned long long was = atomicCAS(word, seen, count == (unsigned long long)n ? 0ull : key | count);
         if (was == seen) {
+            if (count != (unsigned long long)n) return false;
             __threadfence();                                     // ... and the others' are, for whoever came last
-            return count == (unsigned long long)n;
+            return true;
         }
         seen = was;
     }
@@ -195,8 +200,8 @@ __global__ void __launch_bounds__(THREADS, WIN ? CTAS_PER_SM : CTAS_PER_SM + 1) 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 127) & ~(uintptr_t)127);
     int32_t *prefix = reinterpret_cast<int32_t *>(base);
-    int32_t *lens = prefix + p.B + 1;
-    uint8_t *at = base + table_bytes(p.B);
+    int32_t *lens = prefix + p.B + 1;                  // (WIN: not kept -- a third CTA fits on the SM up to twice the batch)
+    uint8_t *at = base + (WIN ? ((size_t)(p.B + 1) * 4 + 127) & ~(size_t)127 : table_bytes(p.B));
     const uint32_t k_ring = smem_u32(at);              at += NST * K_STAGE;
     const uint32_t v_ring = smem_u32(at);
     const uint8_t *v_ring_ptr = at;                    at += NST * V_STAGE;
@@ -242,12 +247,35 @@ __global__ void __launch_bounds__(THREADS, WIN ? CTAS_PER_SM : CTAS_PER_SM + 1) 
     // flattened list that is cut into equal ranges is the list of (sequence, kv head, tile) here, a tile
     // being pages [8i, 8i+8) of the sequence: equal ranges are then equal numbers of tiles, which is what a
     // CTA's time goes with.  The merge kernel is told the same counts, so it finds the partials as usual.
-    if (warp == 0) {
-        if (WIN)
-            scan_lengths_by(p.seq_lens, p.B, (int64_t)p.pt_stride * PAGE, p.status, prefix, lens, lane,
-                            [&](int n) { return n > 0 ? (window_pages(n - 1, n, p.window, p.sinks).count + TP - 1) / TP : 0; });
-        else
-            scan_lengths(p.seq_lens, p.B, TP * PAGE, (int64_t)p.pt_stride * PAGE, p.status, prefix, lens, lane);
+    auto length_of = [&](int b) -> int {               // what the page-table row holds of it
+        const int64_t n = __ldg(p.seq_lens + b), most = (int64_t)p.pt_stride * PAGE;
+        return n < 0 ? 0 : n > most ? (int)most : (int)n;
+    };
+    if (WIN) {
+        // (a window's calls are short: all lengths at once, then sums over a stretch per lane -- 32 sequences at a time, each
+        // round waiting for its lengths, takes 8 us longer with 512 sequences)
+        for (int i = tid; i < p.B; i += THREADS) {
+            const int n = length_of(i);
+            if (n < __ldg(p.seq_lens + i)) atomicOr(p.status, STATUS_BOUNDS);
+            prefix[i + 1] = n > 0 ? (window_pages(n - 1, n, p.window, p.sinks).count + TP - 1) / TP : 0;
+        }
+        __syncthreads();
+        if (warp == 0) {
+            const int per = (p.B + 31) / 32, from = lane * per < p.B ? lane * per : p.B, to = from + per < p.B ? from + per : p.B;
+            int sum = 0;
+            for (int i = from; i < to; ++i) sum += prefix[i + 1];
+            int upto = sum;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int u = __shfl_up_sync(FULL, upto, d);
+                if (lane >= d) upto += u;
+            }
+            sum = upto - sum;
+            for (int i = from; i < to; ++i) prefix[i + 1] = sum += prefix[i + 1];
+            if (lane == 0) prefix[0] = 0;
+        }
+    } else if (warp == 0) {
+        scan_lengths(p.seq_lens, p.B, TP * PAGE, (int64_t)p.pt_stride * PAGE, p.status, prefix, lens, lane);
     }
     tc_fence_before();
     __syncthreads();
@@ -284,7 +312,7 @@ __global__ void __launch_bounds__(THREADS, WIN ? CTAS_PER_SM : CTAS_PER_SM + 1) 
         bool triggered = false;
         Cursor cur = {0, 0, 0, 1};
         if (n > 0) cur = locate(prefix, p.B, p.Hkv, x_first);
-        int left = n, k = 0, runs = 0;
+        int left = n, k = 0, runs = 0, b_of_n = -1, n_of = 0;
         auto give_up = [&]() { if (lane == 0) { atomicOr(p.status, STATUS_TIMEOUT); *gave_up = 1; } };
         while (left > 0) {
             if (!triggered && k >= trigger_at) {
@@ -298,13 +326,24 @@ __global__ void __launch_bounds__(THREADS, WIN ? CTAS_PER_SM : CTAS_PER_SM + 1) 
             const int s = k & 1;
             // tile cur.pg of segment (cur.b, cur.h): pages [8 cur.pg, 8 cur.pg + np)
             WindowPages win = {};
-            const int b = cur.b, h = cur.h, n_b = lens[b];
+            const int b = cur.b, h = cur.h;
+            if (WIN && b != b_of_n) n_of = length_of(b_of_n = b);
+            const int n_b = WIN ? n_of : lens[b];
             if (WIN) win = window_pages(n_b - 1, n_b, p.window, p.sinks);
             const int pages = WIN ? win.count : (n_b + PAGE - 1) / PAGE, pg0 = TP * cur.pg;
             const int np = pages - pg0 < TP ? pages - pg0 : TP;
             const bool first = (k == 0) || (reverse ? cur.pg == cur.pages - 1 : cur.pg == 0);
             const bool last = (left == 1) || (reverse ? cur.pg == 0 : cur.pg == cur.pages - 1);
-            // page ids of the tile (lane j < np), fetched before the waits for the stages
+            // page ids of the tile (lane j < np), fetched before the waits for the stages; so are a window's queries
+            const int g = lane >> 2, qd = lane & 3;
+            uint4 wq[4];
+            auto load_q = [&]() {
+                if (g >= G) return;
+                const uint4 *qsrc = reinterpret_cast<const uint4 *>(p.Q + ((int64_t)b * p.Hq + (int64_t)h * G + g) * D + 32 * qd);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) wq[c] = __ldg(qsrc + c);
+            };
+            if (WIN && first) load_q();
             int id = 0;
             if (lane < np) {
                 id = __ldg(p.page_table + (int64_t)b * p.pt_stride + (WIN ? win.page(pg0 + lane) : pg0 + lane));
@@ -352,18 +391,16 @@ __global__ void __launch_bounds__(THREADS, WIN ? CTAS_PER_SM : CTAS_PER_SM + 1) 
                 // the two sets of scales alternate (the set's last reader finished before the V stage came back).
                 if (k >= 1 && !__all_sync(FULL, wait_bounded(k_empty + 8 * ((k - 1) & 1), (uint32_t)(((k - 1) / 2) & 1)))) { give_up(); break; }
                 const int qset = runs & 1;
-                const int g = lane >> 2, qd = lane & 3;
+                if (!WIN) load_q();
                 float q[32];
                 float amax = 0.f;
                 if (g < G) {
-                    const uint4 *qsrc = reinterpret_cast<const uint4 *>(p.Q + ((int64_t)b * p.Hq + (int64_t)h * G + g) * D + 32 * qd);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const uint4 wq = __ldg(qsrc + c);
-                        q[8 * c + 0] = bf16_lo(wq.x); q[8 * c + 1] = bf16_hi(wq.x);
-                        q[8 * c + 2] = bf16_lo(wq.y); q[8 * c + 3] = bf16_hi(wq.y);
-                        q[8 * c + 4] = bf16_lo(wq.z); q[8 * c + 5] = bf16_hi(wq.z);
-                        q[8 * c + 6] = bf16_lo(wq.w); q[8 * c + 7] = bf16_hi(wq.w);
+                        q[8 * c + 0] = bf16_lo(wq[c].x); q[8 * c + 1] = bf16_hi(wq[c].x);
+                        q[8 * c + 2] = bf16_lo(wq[c].y); q[8 * c + 3] = bf16_hi(wq[c].y);
+                        q[8 * c + 4] = bf16_lo(wq[c].z); q[8 * c + 5] = bf16_hi(wq[c].z);
+                        q[8 * c + 6] = bf16_lo(wq[c].w); q[8 * c + 7] = bf16_hi(wq[c].w);
                     }
 #pragma unroll
                     for (int i = 0; i < 32; ++i) amax = fmaxf(amax, fabsf(q[i]));
@@ -681,7 +718,6 @@ __global__ void __launch_bounds__(THREADS, WIN ? CTAS_PER_SM : CTAS_PER_SM + 1) 
                     }
                     softmax_sync();
                     if (*reinterpret_cast<volatile int *>(last_one)) {
-                        __threadfence();
                         float M[GP], L[GP], acc[GP];
 #pragma unroll
                         for (int h = 0; h < GP; ++h) { M[h] = -INFINITY; L[h] = 0.f; acc[h] = 0.f; }
@@ -761,18 +797,19 @@ bool decode_fp8_umma_supported(int D, int G) { return D == 128 && G >= 1 && G <=
 int decode_fp8_umma_ctas_per_sm() { return CTAS_PER_SM; }
 int decode_fp8_umma_tile_tokens() { return TP * PAGE; }
 
-size_t decode_fp8_umma_smem_bytes(int D, int B)
+size_t decode_fp8_umma_smem_bytes(int D, int B, bool window)
 {
     const int block = fp8_block_bytes(D);
     // alignment | tables | K and V rings | two P' | Q' | tile descriptions | query scales | maxima | sums | barriers | two words
-    return 128 + table_bytes(B) + (size_t)NST * TP * block + 2 * 16 * (size_t)(TP * PAGE) + 16 * (size_t)D + 4 * sizeof(TileMeta) +
+    const size_t tables = window ? ((size_t)(B + 1) * 4 + 127) & ~(size_t)127 : table_bytes(B);
+    return 128 + tables + (size_t)NST * TP * block + 2 * 16 * (size_t)(TP * PAGE) + 16 * (size_t)D + 4 * sizeof(TileMeta) +
            64 + 512 + 128 + 16 * 8 + 16 + 64;          // (... | a window's token sets)
 }
 
 cudaError_t launch_decode_fp8_umma(const DecodeParams &p, int D, int G, int grid, bool pdl, cudaStream_t s)
 {
     if (!decode_fp8_umma_supported(D, G)) return cudaErrorInvalidValue;
-    const size_t smem = decode_fp8_umma_smem_bytes(D, p.B);
+    const size_t smem = decode_fp8_umma_smem_bytes(D, p.B, p.window > 0);
     auto kern = p.window > 0 ? (G <= 1 ? decode_fp8_umma_kernel<128, 1, true> : G <= 2 ? decode_fp8_umma_kernel<128, 2, true>
                               : G <= 4 ? decode_fp8_umma_kernel<128, 4, true> : decode_fp8_umma_kernel<128, 8, true>)
                              : (G <= 1 ? decode_fp8_umma_kernel<128, 1, false> : G <= 2 ? decode_fp8_umma_kernel<128, 2, false>

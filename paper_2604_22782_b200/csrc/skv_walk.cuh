@@ -56,9 +56,8 @@ __device__ __forceinline__ void step(Cursor &c, const int32_t *prefix, int Hkv, 
 // per kv head; prefix[B] = all of them.  A length that needs more pages than a page-table row holds
 // (max_tokens = pt_stride * PAGE) is cut to what the row holds and flagged in the status word, so that no
 // page id is ever read past the end of a row.
-template <class Units>
-__device__ __forceinline__ void scan_lengths_by(const int32_t *seq_lens, int B, int64_t max_tokens, int *status, int32_t *prefix,
-                                                int32_t *lens, int lane, Units units_of)
+__device__ __forceinline__ void scan_lengths(const int32_t *seq_lens, int B, int unit_tokens, int64_t max_tokens,
+                                             int *status, int32_t *prefix, int32_t *lens, int lane)
 {
     int carry = 0;
     for (int i0 = 0; i0 < B; i0 += 32) {
@@ -71,7 +70,7 @@ __device__ __forceinline__ void scan_lengths_by(const int32_t *seq_lens, int B, 
                 n = (int)max_tokens;
                 if (status) atomicOr(status, STATUS_BOUNDS);
             }
-            v = units_of(n);
+            v = (n + unit_tokens - 1) / unit_tokens;
             lens[i] = n;
         }
 #pragma unroll
@@ -83,12 +82,6 @@ __device__ __forceinline__ void scan_lengths_by(const int32_t *seq_lens, int B, 
         carry += __shfl_sync(0xFFFFFFFFu, v, 31);
     }
     if (lane == 0) prefix[0] = 0;
-}
-
-__device__ __forceinline__ void scan_lengths(const int32_t *seq_lens, int B, int unit_tokens, int64_t max_tokens,
-                                             int *status, int32_t *prefix, int32_t *lens, int lane)
-{
-    scan_lengths_by(seq_lens, B, max_tokens, status, prefix, lens, lane, [=](int n) { return (n + unit_tokens - 1) / unit_tokens; });
 }
 
 // ---------------------------------------------------------------------------

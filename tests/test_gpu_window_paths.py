@@ -168,3 +168,57 @@ def test_decode_of_fp8_sequences_in_pieces():
         want = ref.attention(q[b:b + 1], p.k[b], p.v[b], torch.tensor([lens[b] - 1]), 30, 2)
         check(out[b:b + 1], want + (32, True, float(p.v[b].double().abs().max()) if lens[b] else 0.0), f"sequence {b}")
     assert p.cache.skv_get_status() == 0
+
+
+@pytest.mark.parametrize("lens", [[32700, 9000], [0, 0], [16, 1], [32768, 1], [130, 32768], [5000, 0]])
+@pytest.mark.parametrize("layer", [0, 1])
+def test_decode_of_fp8_segments_shared_by_many_workers(lens, layer):
+    """Few sequences whose table has room for enough tiles: a segment is joined from up to a worker per tile, whatever the
+    workspace held before; layer 1 walks the other way."""
+    p = Paged(lens, 8, 128, fp8=True, seed=41)
+    width = torch.full((2, 2048), -1, dtype=torch.int32)
+    width[:, :p.table.shape[1]] = p.table
+    p.table = width
+    p.table_dev = width.cuda()
+    q = p.rows(2, 32)
+    ws = torch.empty(p.cache.skv_decode_workspace_bytes(2, 32), dtype=torch.uint8, device="cuda")
+    outs = []
+    for fill in (0, 0xFF, 0x5A):
+        ws.fill_(fill)
+        for _ in range(3):
+            out = torch.full(q.shape, float("nan"), dtype=torch.bfloat16, device="cuda")
+            p.cache.skv_decode_attn_window(layer, q.cuda(), p.table_dev, p.lens_dev, out, ws, 32000, 700)
+            outs.append(out)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, outs[0]) for o in outs)
+    check_decode(p, q, outs[0], 32000, 700)
+    assert p.cache.skv_get_status() == 0
+
+
+def test_decode_of_fp8_sequences_captured_and_replayed():
+    lens = [300 + 37 * b % 800 for b in range(200)]
+    p = Paged(lens, 8, 128, fp8=True, seed=42)
+    qs = [p.rows(len(lens), 16) for _ in range(2)]
+    ws = torch.full((p.cache.skv_decode_workspace_bytes(len(lens), 16),), 0x77, dtype=torch.uint8, device="cuda")
+    qd = qs[0].cuda()
+    out = torch.empty_like(qd)
+    s = torch.cuda.Stream()
+    graphs = []
+    with torch.cuda.stream(s):
+        for calls in (1, 2):
+            p.cache.skv_decode_attn_window(1, qd, p.table_dev, p.lens_dev, out, ws, 600, 4)
+            s.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=s):
+                for _ in range(calls):
+                    p.cache.skv_decode_attn_window(1, qd, p.table_dev, p.lens_dev, out, ws, 600, 4)
+            graphs.append(g)
+    for i in (0, 1, 0):
+        qd.copy_(qs[i])
+        for g in graphs:
+            out.fill_(float("nan"))
+            torch.cuda.synchronize()
+            for _ in range(3):
+                g.replay()
+            torch.cuda.synchronize()
+            check_decode(p, qs[i], out, 600, 4)
