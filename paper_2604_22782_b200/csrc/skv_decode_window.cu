@@ -43,7 +43,7 @@ __device__ __forceinline__ float2 ld_cluster_f2(uint32_t a)
 }
 
 // Dynamic shared memory: rings [NW][ST] blocks | states [NW] | the CTA's state | barriers [NW][ST]
-template <int D, class State, int NW>
+template <int D, class State, int NW, bool EARLY>
 __global__ void __launch_bounds__(NW * 32) decode_window_kernel(DecodeParams p, int G, int ST)
 {
     extern __shared__ __align__(128) uint8_t smem_raw[];
@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(NW * 32) decode_window_kernel(DecodeParams p, 
     }
     __syncwarp();
     pdl_wait();
-    pdl_trigger();
+    if (EARLY) pdl_trigger();
     const int seg = (int)(blockIdx.x / ranks), b = seg / p.Hkv, h = seg - b * p.Hkv;
     int n = __ldg(p.seq_lens + b);
     n = n > 0 ? n : 0;
@@ -229,18 +229,23 @@ cudaError_t launch_t(const DecodeParams &p, int G, int sm_count, bool pdl, cudaS
     const Shape f = shape_of(State::BLOCK, segments, pages, sm_count);
     if (segments * f.ranks > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
     const size_t smem = 128 + (size_t)f.warps * f.stages * State::BLOCK + (size_t)(f.warps + 1) * part_floats(G, D) * 4 + (size_t)f.warps * f.stages * 8;
-    auto kern = f.warps == 8 ? decode_window_kernel<D, State, 8> : decode_window_kernel<D, State, 4>;
+    // The next launch may be let in at once where there is an SM for every CTA; else it would fill what this one leaves
+    // free, two CTAs here and none there, and run as unevenly (64 x 129 pages: 42 us, and 51 let in at once; 1024 x 257 pages
+    // 79 and 84; 8 x 65 pages 6.0 and 5.6).
+    const bool early = segments * f.ranks <= sm_count;
+    auto kern = f.warps == 8 ? (early ? decode_window_kernel<D, State, 8, true> : decode_window_kernel<D, State, 8, false>)
+                             : (early ? decode_window_kernel<D, State, 4, true> : decode_window_kernel<D, State, 4, false>);
     cudaError_t e = ensure_dynamic_smem(kern, smem);
     if (e != cudaSuccess) return e;
     if (f.ranks > 8) {
-        static std::atomic<uint64_t> allowed[2];           // (bit per device: asking every time costs more than the launch)
+        static std::atomic<uint64_t> allowed[4];           // (bit per device: asking every time costs more than the launch)
         int dev = 0;
         if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
         const uint64_t bit = 1ull << (dev & 63);
-        if (dev > 63 || !(allowed[f.warps == 8] & bit)) {
+        if (dev > 63 || !(allowed[2 * (f.warps == 8) + early] & bit)) {
             e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
             if (e != cudaSuccess) return e;
-            allowed[f.warps == 8] |= bit;
+            allowed[2 * (f.warps == 8) + early] |= bit;
         }
     }
     cudaLaunchConfig_t cfg = {};
