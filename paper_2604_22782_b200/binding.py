@@ -1,5 +1,6 @@
-"""ctypes binding of ``libskv.so``: same names as the C entry points, argument
-marshalling only.  Tensors are torch CUDA tensors (torch is used for device
+"""Binding of ``libskv.so``: same names as the C entry points, argument marshalling only, through ctypes; the entry
+points of a serving step, which are a few microseconds long, through ``_calls.so`` (csrc/skv_calls.cpp) where their
+arguments are plain.  Tensors are torch CUDA tensors (torch is used for device
 memory and streams, nothing else)."""
 from __future__ import annotations
 
@@ -38,6 +39,22 @@ def _load() -> ctypes.CDLL:
 
 
 lib = _load()
+
+
+def _load_calls():
+    if not os.path.exists(_build.CALLS):
+        try:
+            _build.build_calls()
+        except Exception as e:
+            raise ImportError(f"_calls.so is missing and could not be built: {e}") from e
+    from . import _calls
+    _calls.connect(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        lib.skv_is_owner, lib.skv_rope_append, lib.skv_plan_step, lib.skv_plan_release, lib.skv_decode_attn_window,
+        lib.skv_prefill_attn_window)))
+    return _calls
+
+
+_calls = _load_calls()
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 _vp, _i32p, _i64p, _szp = ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.POINTER(ctypes.c_size_t)
@@ -272,11 +289,12 @@ class SkvRope:
         self._h = _vp()
         _check(lib.skv_rope_create(ctypes.byref(self._h), self.rotary_dim, _f64_array(inv_freq),
                                    None if axis is None else _i32_array(axis), n_axes, int(bool(adjacent_pairs))), "skv_rope_create")
+        self._handle = self._h.value
 
     def close(self):
         if getattr(self, "_h", None):
             lib.skv_rope_destroy(self._h)
-            self._h = None
+            self._h = self._handle = None
 
     __del__ = close
 
@@ -301,6 +319,7 @@ class SkvCache:
             rc = create(ctypes.byref(self._h), self.n_layers, _i32_array(self.r), kv_heads, head_dim,
                         page_size, max_pages, None, 0, None)
             _check(rc, "skv_cache_create")
+            self._handle = self._h.value
             return
         need = (skv_cache_pool_bytes_fp8 if fp8 else skv_cache_pool_bytes)(self.r, kv_heads, head_dim, page_size, max_pages)
         if device_pool is None:
@@ -312,12 +331,13 @@ class SkvCache:
         rc = create(ctypes.byref(self._h), self.n_layers, _i32_array(self.r), kv_heads, head_dim,
                     page_size, max_pages, device_pool.data_ptr(), device_pool.numel(), _stream_ptr(stream))
         _check(rc, "skv_cache_create")
+        self._handle = self._h.value
 
     # -- lifetime
     def close(self):
         if getattr(self, "_h", None):
             lib.skv_cache_destroy(self._h)
-            self._h = None
+            self._h = self._handle = None
 
     __del__ = close
 
@@ -374,6 +394,10 @@ class SkvCache:
                         slot_map: Optional[torch.Tensor], stream=None) -> None:
         """Q, Q_out [n][q_heads][head_dim], K, V [n][kv_heads][head_dim] with any row stride; positions [n] or
         [n_axes][n] int32; slot_map [n] int64.  On a layer that is not an owner K, V, slot_map are not used."""
+        rc = _calls.rope_append(self._handle, self.pool, self.head_dim, self.kv_heads, rope.n_axes, layer, rope._handle, Q, Q_out, K, V,
+                                positions, slot_map, stream)
+        if rc is not None:
+            return _check(rc, "skv_rope_append") if rc else None
         device = self._current_device()
         n = positions.shape[-1] if positions.dim() else -1
         axes = 1 if positions.dim() == 1 else positions.shape[0] if positions.dim() == 2 else -1
@@ -406,6 +430,10 @@ class SkvCache:
                       stream=None) -> None:
         """page_table [batch][width], seq_lens, new_lens, seq_lens_out [batch], free_pages [capacity], n_free, n_free_out [1],
         cu_q_lens [batch+1], positions [max_tokens]: int32; slot_map [max_tokens]: int64."""
+        rc = _calls.plan_step(self._handle, self.pool, page_table, seq_lens, new_lens, free_pages, n_free, slot_map, cu_q_lens, seq_lens_out,
+                              n_free_out, positions, stream)
+        if rc is not None:
+            return _check(rc, "skv_plan_step") if rc else None
         device, i32 = self._current_device(), torch.int32
         if seq_lens.dim() != 1:
             raise ValueError("seq_lens: expected [batch]")
@@ -431,6 +459,9 @@ class SkvCache:
 
     def skv_plan_release(self, page_table: torch.Tensor, first_page: torch.Tensor, end_page: torch.Tensor,
                          free_pages: torch.Tensor, n_free: torch.Tensor, n_free_out: torch.Tensor, stream=None) -> None:
+        rc = _calls.plan_release(self._handle, self.pool, page_table, first_page, end_page, free_pages, n_free, n_free_out, stream)
+        if rc is not None:
+            return _check(rc, "skv_plan_release") if rc else None
         device, i32 = self._current_device(), torch.int32
         if page_table.dim() != 2:
             raise ValueError(f"page_table: expected [batch][width], got {tuple(page_table.shape)}")
@@ -489,6 +520,10 @@ class SkvCache:
     def skv_decode_attn_window(self, layer: int, Q: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor,
                                out: torch.Tensor, workspace: torch.Tensor, window: int, sinks: int = 0,
                                scale: float = 0.0, stream=None) -> None:
+        rc = _calls.decode_attn_window(self._handle, self.pool, self.head_dim, layer, Q, page_table, seq_lens, out, workspace, window, sinks,
+                                       scale, stream)
+        if rc is not None:
+            return _check(rc, "skv_decode_attn_window") if rc else None
         device, bf16, i32 = self._current_device(), torch.bfloat16, torch.int32
         if Q.dim() != 3 or Q.shape[2] != self.head_dim:
             raise ValueError(f"Q: expected [batch][q_heads][{self.head_dim}], got {tuple(Q.shape)}")
@@ -539,6 +574,10 @@ class SkvCache:
     def skv_prefill_attn_window(self, layer: int, Q: torch.Tensor, cu_q_lens: torch.Tensor, page_table: torch.Tensor,
                                 seq_lens: torch.Tensor, out: torch.Tensor, max_q_len: int, window: int, sinks: int = 0,
                                 scale: float = 0.0, stream=None) -> None:
+        rc = _calls.prefill_attn_window(self._handle, self.pool, self.head_dim, layer, Q, cu_q_lens, page_table, seq_lens, out, max_q_len,
+                                        window, sinks, scale, stream)
+        if rc is not None:
+            return _check(rc, "skv_prefill_attn_window") if rc else None
         device, bf16, i32 = self._current_device(), torch.bfloat16, torch.int32
         if Q.dim() != 3 or Q.shape[2] != self.head_dim:
             raise ValueError(f"Q: expected [n_q][q_heads][{self.head_dim}], got {tuple(Q.shape)}")

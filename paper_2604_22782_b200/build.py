@@ -9,11 +9,13 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 OBJ_DIR = os.path.join(_HERE, "_build")
 LIB = os.path.join(_HERE, "libskv.so")
+CALLS = os.path.join(_HERE, "_calls.so")                          # csrc/skv_calls.cpp: the binding's argument marshalling
 LIB_TEST_HOOKS = os.path.join(_HERE, "libskv_testhooks.so")      # the library plus include/skv_test_hooks.h's entry points
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
@@ -73,7 +75,26 @@ def build_test_hooks(force: bool = False) -> str:
     return build(force=force, lib=LIB_TEST_HOOKS, defines=["SKV_TEST_HOOKS"])
 
 
+def build_calls(force: bool = False) -> str:
+    """The CPython extension that marshals the serving step's arguments (g++, against the installed torch's headers)."""
+    src = os.path.join(CSRC, "skv_calls.cpp")
+    if not force and os.path.exists(CALLS) and os.path.getmtime(CALLS) >= max(os.path.getmtime(f) for f in [src] + _headers()):
+        return CALLS
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    tmp = CALLS + f".tmp{os.getpid()}"
+    subprocess.check_call(
+        [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+         "-isystem", os.path.join(root, "include"), "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
+         "-isystem", os.path.join(cuda, "include"), "-isystem", sysconfig.get_paths()["include"], src, "-o", tmp,
+         "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10_cuda", "-lc10"])
+    os.replace(tmp, CALLS)
+    return CALLS
+
+
 if __name__ == "__main__":
     print(build(force="--force" in sys.argv, verbose="-v" in sys.argv))
+    print(build_calls(force="--force" in sys.argv))
     if "--test-hooks" in sys.argv:
         print(build_test_hooks(force="--force" in sys.argv))
