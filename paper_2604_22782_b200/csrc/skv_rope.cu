@@ -18,7 +18,7 @@
 // tokens) and kv head each: four lanes swap words so that each ends up with 16 tokens of four dims and stores 16 bytes
 // at a time (byte by byte it took longer than all the rest).
 // Bound by memory: every row is read once and written once.  32768 tokens of 32 query and 8 kv heads onto FP8 pages 120 us,
-// 6.2 TB/s (0.94 of the measured copy peak); 8191 tokens with three axes 37.6 us, 5.4 TB/s (0.82: two waves of blocks and a bit);
+// 6.2 TB/s (0.94 of the measured copy peak); 8191 tokens with three axes 36.1 us, 5.6 TB/s (0.85);
 // 64 tokens 3.6 us, a launch.
 #include "skv_common.cuh"
 
@@ -147,7 +147,8 @@ __device__ __forceinline__ void store_v_fp8(const RopeParams &p, int64_t group, 
 
 // ADJACENT: pairs (2i, 2i+1) instead of (i, i + rotary_dim / 2)
 template <int D, bool FP8, bool ADJACENT>
-__global__ void __launch_bounds__(ROPE_THREADS) rope_append_kernel(const __grid_constant__ RopeParams p)
+// (six blocks to an SM: 8191 tokens 36.1 us, five 37.6; FP8 pages want the registers)
+__global__ void __launch_bounds__(ROPE_THREADS, FP8 ? 5 : 6) rope_append_kernel(const __grid_constant__ RopeParams p)
 {
     constexpr int CP = D / 16;                     // lanes of a head
     constexpr int TOK = 32 / CP;                   // tokens of a warp
