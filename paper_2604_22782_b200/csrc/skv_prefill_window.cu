@@ -27,6 +27,8 @@
 // Softmax as in skv_prefill_umma.cu: the reference maximum moves only when it has grown by more than 2^8, so O is rarely
 // rescaled.  A row that has seen nothing yet counts from reference 0.
 // Every wait is bounded; copies in flight get their wait before the end.
+// Few rows behind long windows (a chunk of a prompt, a drafted run of tokens) leave most SMs idle and each item a long chain of
+// blocks: there a cluster of CTAs shares an item's blocks and joins the outputs over distributed shared memory.
 // Measured: 2 prompts of 4096 tokens, 32 query / 8 kv heads, head_dim 128, window 2048: 190 us, 1.09 PFLOP/s of visible pairs (0.67 of
 // the measured bf16 peak; 222 us in a long loop, at the clock the power limit leaves); 8 chunks of 257 to 512 rows behind 3000 to
 // 6000 tokens, window 1024: 64 to 77 us.  The tensor pipe is busy 70 % of the cycles, the exponentials 50 %, issue slots
@@ -55,6 +57,7 @@ constexpr int COL_O = 4 * KEYS;       // scores of tile s, buffer i at column 12
 constexpr float RESCALE_STEP = 8.f;
 constexpr int BY_FMA = 8;             // every eighth pair of exponentials is computed on the FMA units
 constexpr int BAR_BYTES = 5 * 8 * STAGES + 3 * 32 + 3 * 16;
+constexpr int MAX_RANKS = 8;          // CTAs that may share an item
 constexpr int MAX_BATCH = 1024;       // sequences of a launch: their tables are in shared memory
 
 __host__ __device__ constexpr uint32_t instr_desc(int M, int N, bool b_mn_major)
@@ -103,8 +106,9 @@ struct Item {
     int q0, q_len;          // first token of the item among the sequence's new ones; all of those
     int pos0;               // position of the sequence's first new token
     int n[2];               // tokens of the two tiles
+    int rows;               // tokens of tile 0, also where none of its blocks is this CTA's
     int n_keys;             // keys below this one are visible to some row
-    int blocks;
+    int kb0, blocks;        // blocks [kb0, blocks) of its list are this CTA's
     WindowPages win;
     // tokens of tile s: positions first(s) .. last(s)
     __device__ __forceinline__ int first(int s, int TQ) const { return pos0 + q0 + s * TQ; }
@@ -116,12 +120,15 @@ struct Item {
 struct Tables {
     const int32_t *order, *count, *below;
     const int32_t *q_begin, *q_len, *lens;
+    int rank, ranks;        // SPLIT: of this CTA in its cluster
 };
 
 // item of round `round` of this CTA; per_item: tokens of an item.  False: no more.
+template <bool SPLIT>
 __device__ __forceinline__ bool item_at(Item &it, const PrefillParams &p, const Tables &t, int total, int round, int TQ, int per_item)
 {
-    const int x = round * (int)gridDim.x + ((round & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
+    if (SPLIT && round > 0) return false;                   // (there is a cluster for every item)
+    const int x = SPLIT ? (int)blockIdx.x / t.ranks : round * (int)gridDim.x + ((round & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
     if (x >= total) return false;
     const int back = total - 1 - x, y = back / p.Hkv;       // places ascending, over the sequences that have one
     it.h = back - y * p.Hkv;
@@ -142,7 +149,14 @@ __device__ __forceinline__ bool item_at(Item &it, const PrefillParams &p, const 
     it.n[1] = second > 0 ? second : 0;
     it.n_keys = it.pos0 + it.q0 + it.n[0] + it.n[1];
     it.win = window_pages(it.pos0 + it.q0, it.n_keys, p.window, p.sinks);
+    it.kb0 = 0;
     it.blocks = (it.win.count + KB - 1) / KB;
+    it.rows = it.n[0];
+    if (SPLIT) {
+        const int all = it.blocks;
+        it.kb0 = all * t.rank / t.ranks;
+        it.blocks = all * (t.rank + 1) / t.ranks;
+    }
     return true;
 }
 
@@ -167,11 +181,16 @@ __device__ __forceinline__ Plan plan_of(const Item &it, int s, int TQ, int windo
     if (q.clear_from < behind_gap) q.clear_from = behind_gap;
     const int e = (first + 1) / PAGE - gap;
     q.clear_to = e > 0 ? e / KB : 0;
+    // this CTA's part of them
+    if (q.sinks > it.blocks) q.sinks = it.blocks;
+    if (q.from < it.kb0) q.from = it.kb0;
+    if (q.to > it.blocks) q.to = it.blocks;
     return q;
 }
 
 // The items of a CTA, round by round, as a warp goes through them.  Working one out takes some two thousand cycles, all of
 // latency: every lane does it for a round of its own, once in 32 rounds, and the rounds then only read their lane's.
+template <bool SPLIT>
 struct Items {
     Item mine;
     Plan plans[2];
@@ -180,7 +199,7 @@ struct Items {
     __device__ __forceinline__ bool at(Item &it, const PrefillParams &p, const Tables &t, int total, int round, int lane, int TQ, int per_item)
     {
         if ((round & 31) == 0) {
-            any = item_at(mine, p, t, total, round + lane, TQ, per_item);
+            any = item_at<SPLIT>(mine, p, t, total, round + lane, TQ, per_item);
             if (any)
                 for (int s = 0; s < 2; ++s)
                     if (mine.n[s] > 0) plans[s] = plan_of(mine, s, TQ, p.window, p.sinks);
@@ -198,6 +217,8 @@ struct Items {
         it.n[1] = get(mine.n[1]);
         it.n_keys = get(mine.n_keys);
         it.blocks = get(mine.blocks);
+        it.kb0 = SPLIT ? get(mine.kb0) : 0;
+        if (SPLIT && it.kb0 == it.blocks) it.n[0] = 0;          // nothing to do for this CTA
         it.win.lo = get(mine.win.lo);
         it.win.sink_pages = get(mine.win.sink_pages);
         it.win.gap = get(mine.win.gap);
@@ -275,6 +296,29 @@ __device__ __forceinline__ bool elect_one()
     return is != 0;
 }
 
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// shared-memory address `a` of this CTA as the CTA of the given rank has it
+__device__ __forceinline__ uint32_t at_rank(uint32_t a, uint32_t rank)
+{
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float2 ld_cluster_f2(uint32_t a)
+{
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t a)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+    return v;
+}
+
 template <int REGS>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS)); }
 template <int REGS>
@@ -282,7 +326,9 @@ __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec
 
 // Dynamic shared memory: Q [2][D/64][128 rows][128 B] | K ring [4][8 groups][D/8 chunks][8 keys][16 B] | V ring [4][4 pages][V half]
 //                        | barriers | tensor-memory address, gave_up, items | tables [6][B + 1]
-template <int D>
+// SPLIT: a cluster of CTAs to an item of one tile, each with its part of the key blocks, where that leaves no SM out: the outputs
+// are joined over distributed shared memory.
+template <int D, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid_constant__ PrefillParams p, const __grid_constant__ CUtensorMap k_map,
                                                                        int G, int tiles, int max_q_len)
 {
@@ -304,7 +350,17 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(words), *gave_up = tmem_slot + 1;
     int32_t *order = reinterpret_cast<int32_t *>(words + 16), *count = order + p.B + 1, *below = count + p.B + 1;
     int32_t *q_begin = below + p.B + 1, *q_len = q_begin + p.B + 1, *lens = q_len + p.B + 1;
-    const Tables tables = {order, count, below, q_begin, q_len, lens};
+    uint32_t rank = 0, ranks = 1;
+    if (SPLIT) {
+        asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+        asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ranks));
+    }
+    const Tables tables = {order, count, below, q_begin, q_len, lens, (int)rank, (int)ranks};
+    // SPLIT, in place of the K ring once the item is done: a row's output [128][D + 4] (four words of padding: no two lanes in one
+    // bank), and its reference and sum [128]
+    constexpr int STATE_ROW = D + 4;
+    const uint32_t state = k_ring, state_ml = state + (uint32_t)(ROWS * STATE_ROW * 4);
+    static_assert(ROWS * (STATE_ROW + 2) * 4 <= 2 * STAGES * STAGE, "the joined state fits the rings");
 
     if (tid == 0) {
         for (int i = 0; i < STAGES; ++i) {
@@ -383,14 +439,14 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
         const bool wide_out = (reinterpret_cast<uintptr_t>(p.out) & 31) == 0;
         int count = 0;                             // blocks of this tile so far
         Item it;
-        Items items = {};
+        Items<SPLIT> items = {};
         for (int round = 0; items.at(it, p, tables, total, round, lane, TQ, per_item); ++round) {
             if (it.n[s] == 0) continue;
             const Plan plan = s == 0 ? items.plan(0, round) : items.plan(1, round);
             const bool row_ok = qi < it.n[s];
             const int pos = row_ok ? it.first(s, TQ) + qi : 0x7FFFFFFE, lo = pos >= p.window ? pos - p.window + 1 : 0;
             float m_used = -INFINITY, l_sum = 0.f;
-            const int first = plan.sinks > 0 ? 0 : plan.from;
+            const int first = plan.sinks > it.kb0 ? it.kb0 : plan.from;
             for (int kb = first; kb < plan.to; kb = (kb + 1 < plan.sinks || kb + 1 >= plan.from) ? kb + 1 : plan.from) {
                 const int buf = count & 1, bar = 8 * (2 * s + buf);
                 const uint32_t phase = (uint32_t)((count >> 1) & 1), scores = scores0 + (uint32_t)(buf * KEYS);
@@ -474,6 +530,19 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
             // the item's last P V
             wait(pv_done + 8 * (2 * s + ((count - 1) & 1)), (uint32_t)(((count - 1) >> 1) & 1), gave_up);
             tc_fence_after();
+            if (SPLIT) {
+#pragma unroll
+                for (int q = 0; q < D / 32; ++q) {
+                    uint32_t ov[32];
+                    tmem_ld32(output + 32 * q, ov);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int c = 0; c < 32; c += 4)
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(state + (uint32_t)((row * STATE_ROW + 32 * q + c) * 4)), "r"(ov[c]), "r"(ov[c + 1]), "r"(ov[c + 2]), "r"(ov[c + 3]) : "memory");
+                }
+                asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(state_ml + (uint32_t)(row * 8)), "f"(m_used), "f"(l_sum) : "memory");
+                continue;
+            }
             const float inv = 1.f / l_sum;
             uint16_t *dst = p.out + ((int64_t)(it.q_begin + it.q0 + s * TQ + qi) * p.Hq + (int64_t)it.h * G + g) * D;
             uint32_t packed[D / 2];
@@ -501,6 +570,45 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                 }
             }
         }
+        if (SPLIT) {
+            const bool any = item_at<SPLIT>(it, p, tables, total, 0, TQ, per_item);
+            if (any && it.kb0 == it.blocks && tid < ROWS)          // no block of the item is this CTA's
+                asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(state_ml + (uint32_t)(tid * 8)), "f"(-INFINITY), "f"(0.f) : "memory");
+            __syncwarp();
+            cluster_arrive();                      // every CTA's part is in place
+            cluster_wait();
+            // rows row_from .. row_to - 1 of the tile are joined by this CTA, four dims a thread at a time
+            const int row_from = ROWS * (int)rank / (int)ranks, row_to = ROWS * (int)(rank + 1) / (int)ranks;
+            for (int i = tid; any && i < (row_to - row_from) * (D / 4); i += 256) {
+                const int r = row_from + i / (D / 4), d = i % (D / 4) * 4, token = r / G, g = r - token * G;
+                if (token >= it.rows) break;       // (rows ascend)
+                float2 ml[MAX_RANKS];
+                float4 v[MAX_RANKS];
+#pragma unroll
+                for (int c = 0; c < MAX_RANKS; ++c) {
+                    ml[c] = make_float2(-INFINITY, 0.f);
+                    v[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (c < (int)ranks) {
+                        ml[c] = ld_cluster_f2(at_rank(state_ml + (uint32_t)(r * 8), (uint32_t)c));
+                        if (ml[c].x != -INFINITY) v[c] = ld_cluster_f4(at_rank(state + (uint32_t)((r * STATE_ROW + d) * 4), (uint32_t)c));
+                    }
+                }
+                float M = -INFINITY, L = 0.f;
+                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int c = 0; c < MAX_RANKS; ++c) M = fmaxf(M, ml[c].x);
+#pragma unroll
+                for (int c = 0; c < MAX_RANKS; ++c) {
+                    if (ml[c].x == -INFINITY) continue;            // (the row sees nothing there)
+                    const float w = ex2(ml[c].x - M);
+                    L = fmaf(w, ml[c].y, L);
+                    o = make_float4(fmaf(w, v[c].x, o.x), fmaf(w, v[c].y, o.y), fmaf(w, v[c].z, o.z), fmaf(w, v[c].w, o.w));
+                }
+                const float inv = 1.f / L;
+                *reinterpret_cast<uint2 *>(p.out + ((int64_t)(it.q_begin + it.q0 + token) * p.Hq + (int64_t)it.h * G + g) * D + d) =
+                    make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+            }
+        }
     } else if (warp < 12) {
         // =================== tensor-core issue ===================
         // The whole warp walks along and one lane issues: descriptors and barriers are then the same for the warp as far as the
@@ -516,7 +624,7 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
         const uint32_t full = values ? v_full : k_full, empty = values ? v_empty : k_empty;
         int g = 0, turn = 0, count = 0;            // blocks before this one; items and blocks of the tile before it
         Item it;
-        Items items = {};
+        Items<SPLIT> items = {};
         for (int round = 0; items.at(it, p, tables, total, round, lane, TQ, per_item); ++round) {
             const int blocks = it.blocks, pages = it.win.count;
             const bool mine = it.n[s] > 0;
@@ -524,7 +632,7 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
             const int sinks_to = mine ? plan.sinks : 0, from = mine ? plan.from : 0, to = mine ? plan.to : 0;
             const int final = from < to ? to - 1 : sinks_to - 1;
             bool begun = false;
-            for (int kb = 0; kb < blocks; ++kb, ++g) {
+            for (int kb = it.kb0; kb < blocks; ++kb, ++g) {
                 const uint32_t st = (uint32_t)g & (STAGES - 1), parity = (uint32_t)(g / STAGES) & 1u;
                 const uint32_t buf = (uint32_t)count & 1u, turn_of_buf = (uint32_t)(count >> 1), bar = 8 * (2 * s + buf), scores = scores0 + buf * KEYS;
                 const uint64_t desc = ring_desc + (uint64_t)(st * (STAGE >> 4));
@@ -578,7 +686,7 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
         if (lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
         int g = 0;
         Item it;
-        Items items = {};
+        Items<SPLIT> items = {};
         for (int round = 0; items.at(it, p, tables, total, round, lane, TQ, per_item); ++round) {
             const int32_t *row = p.page_table + (int64_t)it.b * p.pt_stride;
             auto load_id = [&](int kb) -> int {                // lane j: page j of a block
@@ -589,8 +697,8 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                 atomicOr(p.status, STATUS_BOUNDS);
                 return 0;
             };
-            int id = load_id(0), next_id = load_id(1);
-            for (int kb = 0; kb < it.blocks; ++kb, ++g) {
+            int id = load_id(it.kb0), next_id = load_id(it.kb0 + 1);
+            for (int kb = it.kb0; kb < it.blocks; ++kb, ++g) {
                 const int st = g & (STAGES - 1), np = it.win.count - kb * KB < KB ? it.win.count - kb * KB : KB;
                 const uint32_t again = (uint32_t)((g / STAGES - 1) & 1);
                 // a block with tokens that no row sees passes through the hands of warp 15 first
@@ -626,7 +734,7 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
         const int s = warp - 13;
         int turn = 0;                              // items of the tile before this one
         Item it;
-        Items items = {};
+        Items<SPLIT> items = {};
         for (int round = 0; items.at(it, p, tables, total, round, lane, TQ, per_item); ++round) {
             if (it.n[s] == 0) continue;
             if (turn > 0) wait(q_free + 8 * s, (uint32_t)((turn - 1) & 1), gave_up);
@@ -669,9 +777,9 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
         int g = 0;                                 // blocks before this one
         uint32_t landed = 0;                       // bit per ring stage: parity of the blocks that came through v_landed
         Item it;
-        Items items = {};
+        Items<SPLIT> items = {};
         for (int round = 0; items.at(it, p, tables, total, round, lane, TQ, per_item); ++round) {
-            for (int kb = 0; kb < it.blocks; ++kb, ++g) {
+            for (int kb = it.kb0; kb < it.blocks; ++kb, ++g) {
                 const int st = g & (STAGES - 1), np = it.win.count - kb * KB < KB ? it.win.count - kb * KB : KB;
                 const uint32_t bits = lane < np ? window_bits(it.win.page(kb * KB + lane), it.win.lo, it.n_keys, p.sinks) : 0xFFFFu;
                 unsigned todo = __ballot_sync(FULL, bits != 0xFFFFu);
@@ -692,6 +800,15 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
         }
     }
     // ---- common exit ----
+    if (SPLIT) {
+        __syncwarp();
+        if (warp >= 8) {                           // (the softmax warps were there before they joined the parts)
+            cluster_arrive();
+            cluster_wait();
+        }
+        cluster_arrive();                          // nobody leaves while its part is being read
+        cluster_wait();
+    }
     tc_fence_before();
     __syncthreads();
     if (tid == 0 && *gave_up) atomicOr(p.status, STATUS_TIMEOUT);
@@ -742,22 +859,42 @@ cudaError_t launch_prefill_window(const PrefillParams &p, int D, int G, int max_
     const int tiles = most * (((int64_t)max_q_len + 2 * TQ - 1) / (2 * TQ)) >= sm_count ? 2 : 1;
     int64_t ctas = most * (((int64_t)max_q_len + tiles * TQ - 1) / (tiles * TQ));
     if (ctas > sm_count) ctas = sm_count;
+    // A cluster to an item, as large as leaves every CTA an SM (of a GPC's 16 to 18, of which clusters use 16) and three key blocks,
+    // from 14 blocks on: joining costs some 5 us.  (16 rows of one sequence, 32 / 8 heads, by blocks: 9 11.6 us, and 14.7 in a
+    // cluster of two; 14 15.5, and 13.4 in one of four; 17 17.9 / 13.9; 33 30.2 / 14.6 in one of eight; 66 54 / 17.  Four
+    // sequences: 14 15.9 / 16.3, 17 18.3 / 16.4, 66 55 / 25.)
+    int64_t tokens = (int64_t)p.window + p.sinks + TQ, blocks;
+    if (tokens > (int64_t)p.pt_stride * PAGE) tokens = (int64_t)p.pt_stride * PAGE;
+    blocks = (tokens + KEYS - 1) / KEYS;
+    int ranks = 1;
+    while (tiles == 1 && blocks >= 14 && 2 * ranks <= MAX_RANKS && 8 * ctas * 2 * ranks <= 7 * (int64_t)sm_count && blocks >= 3 * 2 * ranks) ranks *= 2;
     CUtensorMap k_map;
     if (!encode_k_map(&k_map, p, D)) return cudaErrorNotSupported;
     const size_t smem = prefill_window_smem_bytes(D, p.B);
-    auto kern = D == 128 ? prefill_window_kernel<128> : prefill_window_kernel<64>;
+    auto kern = ranks > 1 ? (D == 128 ? prefill_window_kernel<128, true> : prefill_window_kernel<64, true>)
+                          : (D == 128 ? prefill_window_kernel<128, false> : prefill_window_kernel<64, false>);
     const cudaError_t e = ensure_dynamic_smem(kern, smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.gridDim = dim3((unsigned)(ctas * ranks));
     cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchAttribute attr[2];
+    int n = 0;
+    if (ranks > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = (unsigned)ranks;
+        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (pdl) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
     cfg.attrs = attr;
-    cfg.numAttrs = pdl ? 1 : 0;
+    cfg.numAttrs = n;
     return cudaLaunchKernelEx(&cfg, kern, p, k_map, G, tiles, max_q_len);
 }
 

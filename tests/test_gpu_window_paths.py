@@ -222,3 +222,45 @@ def test_decode_of_fp8_sequences_captured_and_replayed():
                 g.replay()
             torch.cuda.synchronize()
             check_decode(p, qs[i], out, 600, 4)
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (6, 2, 64), (5, 1, 128), (4, 4, 64)])
+@pytest.mark.parametrize("window,sinks", [(900, 0), (900, 40), (2000, 700), (1, 3000), (5000, 0), (2147483647, 2147483647)])
+def test_chunk_of_few_rows_shared_by_a_cluster(hq, hkv, d, window, sinks):
+    """Long windows and few rows: an item's key blocks are several CTAs', some of them with none or with keys that some rows do
+    not see; what nobody sees is NaN."""
+    lens, rows = [3000, 40, 1111, 5, 0, 2047], [17, 40, 1, 5, 0, 33]
+    p = Paged(lens, hkv, d, seed=43)
+    q = p.rows(sum(rows), hq)
+    p.forget([n - m for n, m in zip(lens, rows)], window, sinks)
+    out = chunk(p, q, rows, window, sinks)
+    check_chunk(p, q, rows, out, window, sinks)
+    assert torch.equal(out, chunk(p, q, rows, window, sinks))
+    assert p.cache.skv_get_status() == 0
+
+
+@pytest.mark.parametrize("sequences", [1, 2, 3, 4, 8])
+def test_chunk_of_few_rows_captured_and_beside_another_stream(sequences):
+    lens = [2500 + 100 * b for b in range(sequences)]
+    rows = [20 + b for b in range(sequences)]
+    p = Paged(lens, 4, 128, seed=44)
+    q = p.rows(sum(rows), 16)
+    cu = torch.tensor([0] + torch.tensor(rows).cumsum(0).tolist(), dtype=torch.int32, device="cuda")
+    qd, outs = q.cuda(), [torch.empty(q.shape, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(streams[0]):
+        p.cache.skv_prefill_attn_window(1, qd, cu, p.table_dev, p.lens_dev, outs[0], max(rows), 2048, 4)
+        streams[0].synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=streams[0]):
+            p.cache.skv_prefill_attn_window(1, qd, cu, p.table_dev, p.lens_dev, outs[0], max(rows), 2048, 4)
+    outs[0].fill_(float("nan"))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        with torch.cuda.stream(streams[0]):
+            g.replay()
+        p.cache.skv_prefill_attn_window(1, qd, cu, p.table_dev, p.lens_dev, outs[1], max(rows), 2048, 4, stream=streams[1])
+    torch.cuda.synchronize()
+    check_chunk(p, q, rows, outs[0], 2048, 4)
+    assert torch.equal(outs[0], outs[1]) and p.cache.skv_get_status() == 0
