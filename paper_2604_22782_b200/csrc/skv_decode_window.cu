@@ -191,17 +191,20 @@ struct Shape { int warps, stages, ranks; };
 
 // `block` bytes per page and kv head, `segments` of at most `pages` pages.  Measured (us; rows of the sweep: segments x
 // pages at 8 KB blocks; W warps, S stages, R ranks):
-//       8 x   65   W8 S1 R16  5.6   W8 S2 R8  5.9   W4 S2 R16  5.7
-//       8 x  513   W8 S1 R16 11.2   W8 S2 R8 12.9   W4 S2 R16 12.2
-//      16 x  513   W4 S2 R16 14.8   W8 S1 R8 17.5   W8 S2 R8  25.2
-//      64 x   65   W8 S2 R2   9.7   W8 S1 R4  9.9   W4 S2 R4  10.4
-//     128 x   65   W8 S2 R1  12.9   W8 S1 R2 13.7   W4 S2 R2  15.0
-//     160 x  129   W4 S2 R2  26.3   W8 S1 R1 31.0   W8 S2 R1  39.2
-//     320 x  257   W4 S2 R1  97.9   W8 S1 R1 127.6  W8 S2 R1 115.5
-//    1024 x   65   W4 S2 R1  73.1   W8 S1 R1 75.7   W8 S2 R1  80.9
+//       8 x   65   W8 S1 R16  5.7   W8 S2 R8  6.0   W4 S2 R16  5.8
+//       8 x  513   W8 S1 R16 11.1   W4 S2 R16 12.2
+//      16 x   65   W4 S2 R16  6.3   W8 S2 R8 11.1
+//      16 x  513   W4 S2 R16 14.9   W8 S2 R8 25.2
+//      64 x   65   W8 S2 R2   9.7   W4 S2 R4 10.0   W8 S1 R4 10.1
+//     128 x   65   W8 S2 R1  13.1   W8 S1 R2 14.1   W4 S2 R2 14.5
+//     256 x  129   W4 S2 R1  37.2   W8 S1 R1 37.1   W8 S2 R1 41.5
+//     320 x  257   W4 S2 R1  93.0   W4 S2 R2 100
+//    1024 x   65   W4 S2 R1  72.8   W8 S1 R1 75.7   W8 S2 R1 80.5
 // So: a CTA of 8 warps and two stages (one per SM) where a power of two of them per segment comes close to one for every
-// SM, and 4 warps with two stages (three per SM) else, as many ranks as still leave all CTAs resident at once.  Blocks of
-// half the size (FP8, head_dim 64) take 8 warps in the same space.  A rank has at least four pages.
+// SM, and 4 warps with two stages (three per SM) else, as many ranks as still leave all CTAs resident at once.  A cluster's CTAs
+// share a GPC, whose SMs are not a multiple of 8: of 8 CTAs with an SM each 15 clusters run at once, and the 16th doubles the time.
+// Blocks of half the size (FP8, head_dim 64) take 8 warps in the same space, and 16 ranks of them only with an SM for each
+// (16 segments x 257 pages: 11.5 us, in clusters of 8 7.8).  A rank has at least four pages.
 Shape shape_of(int block, int64_t segments, int64_t pages, int sm)
 {
     Shape best = {block >= 8192 ? 4 : 8, 2, 1};
@@ -210,10 +213,11 @@ Shape shape_of(int block, int64_t segments, int64_t pages, int sm)
         while (2 * r <= most && segments * 2 * r <= ctas && pages >= 4 * 2 * r) r *= 2;
         return r;
     };
-    best.ranks = ranks_up_to(2 * (int64_t)sm + sm / 4, MAX_RANKS);
+    best.ranks = ranks_up_to(2 * (int64_t)sm + sm / 4, block >= 8192 || 16 * segments <= sm ? MAX_RANKS : 8);
     if (block >= 8192) {
         const int r = ranks_up_to(sm, MAX_RANKS);
-        const bool fills = 4 * segments * r >= 3 * (int64_t)sm && segments * r <= sm;
+        const int64_t room = r == 8 ? 3 * (int64_t)sm / 4 : r == 4 ? 7 * (int64_t)sm / 8 : sm;
+        const bool fills = 4 * segments * r >= 3 * (int64_t)sm && segments * r <= room;
         if (fills) best = {8, r > 8 ? 1 : 2, r};             // (a cluster of 16 needs two CTAs to an SM: a GPC may not have 16 SMs)
     }
     const int64_t per_warp = (pages + (int64_t)best.ranks * best.warps - 1) / ((int64_t)best.ranks * best.warps);

@@ -859,15 +859,15 @@ cudaError_t launch_prefill_window(const PrefillParams &p, int D, int G, int max_
     const int tiles = most * (((int64_t)max_q_len + 2 * TQ - 1) / (2 * TQ)) >= sm_count ? 2 : 1;
     int64_t ctas = most * (((int64_t)max_q_len + tiles * TQ - 1) / (tiles * TQ));
     if (ctas > sm_count) ctas = sm_count;
-    // A cluster to an item, as large as leaves every CTA an SM (of a GPC's 16 to 18, of which clusters use 16) and three key blocks,
-    // from 14 blocks on: joining costs some 5 us.  (16 rows of one sequence, 32 / 8 heads, by blocks: 9 11.6 us, and 14.7 in a
+    // A cluster to an item, as large as leaves every CTA an SM and three key blocks, from 14 blocks on: joining costs some 5 us.  (A
+    // cluster's SMs are of one GPC: of 8 CTAs 15 fit beside each other here, and 16 items of 66 blocks take 33 us in them, 24 in clusters of 4.)  (16 rows of one sequence, 32 / 8 heads, by blocks: 9 11.6 us, and 14.7 in a
     // cluster of two; 14 15.5, and 13.4 in one of four; 17 17.9 / 13.9; 33 30.2 / 14.6 in one of eight; 66 54 / 17.  Four
     // sequences: 14 15.9 / 16.3, 17 18.3 / 16.4, 66 55 / 25.)
     int64_t tokens = (int64_t)p.window + p.sinks + TQ, blocks;
     if (tokens > (int64_t)p.pt_stride * PAGE) tokens = (int64_t)p.pt_stride * PAGE;
     blocks = (tokens + KEYS - 1) / KEYS;
     int ranks = 1;
-    while (tiles == 1 && blocks >= 14 && 2 * ranks <= MAX_RANKS && 8 * ctas * 2 * ranks <= 7 * (int64_t)sm_count && blocks >= 3 * 2 * ranks) ranks *= 2;
+    while (tiles == 1 && blocks >= 14 && 2 * ranks <= MAX_RANKS && ctas * 2 * ranks <= (2 * ranks == 8 ? 6 : 7) * (int64_t)sm_count / 8 && blocks >= 3 * 2 * ranks) ranks *= 2;
     CUtensorMap k_map;
     if (!encode_k_map(&k_map, p, D)) return cudaErrorNotSupported;
     const size_t smem = prefill_window_smem_bytes(D, p.B);
