@@ -437,7 +437,10 @@ int skv_prefill_attn_src(skv_cache *cache, int src_layer, const void *Q, const i
  * the FP8 scratch area apply.  The tcgen05 kernel takes any q_heads / kv_heads up to 8 at
  * head_dim 64 and 128, in one launch for every 1024 sequences (Q, out 16-byte aligned;
  * FP8 pages through the scratch area), the mma.sync kernel the rest.  A negative
- * cu_q_lens entry raises SKV_ERR_BOUNDS there as a length that does not fit does. */
+ * cu_q_lens entry raises SKV_ERR_BOUNDS there as a length that does not fit does.
+ * Calls of few rows (batch * max_q_len * kv_heads up to some hundreds, or max_q_len 1)
+ * run the kernel of skv_decode_attn_window, a row at a time, unless a pre-fill variant
+ * is set; skv_set_decode_variant then picks the arithmetic. */
 int skv_prefill_attn_window(skv_cache *cache, int layer, const void *Q, const int32_t *cu_q_lens,
                             const int32_t *page_table, const int32_t *seq_lens, void *out, int batch,
                             int max_q_len, int q_heads, int pt_stride, int window, int sinks,

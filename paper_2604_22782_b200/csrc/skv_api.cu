@@ -1117,6 +1117,45 @@ int prefill_over(skv_cache *c, int src, const void *Q, const int32_t *cu_q_lens,
                           (window ? prefill_window_supported(c->head_dim, G) &&
                                         prefill_window_smem_bytes(c->head_dim, prefill_window_max_batch()) <= (size_t)c->max_smem_optin
                                   : prefill_umma_supported(c->head_dim, G) && prefill_umma_smem_bytes(c->head_dim) <= (size_t)c->max_smem_optin);
+    // Few rows over a window: each goes through the decode kernel as a sequence of its own, cut off behind the row's token.  That reads
+    // K and V once per row instead of once per tile, but spreads the rows and their keys over the whole GPU.  (us, tile kernel / decode
+    // kernel, 8 kv heads of 4: bf16, window 1024, 1 row 10.8 / 6.2, 8 13.6 / 9.8, 16 13.8 / 12.0, 32 14.3 / 18.9; window 4096, 4 rows
+    // 16.6 / 13.6, 8 17.0 / 21.3; window 128, 32 rows 8.6 / 6.0, 64 8.7 / 10.5; 64 sequences of a row each, window 1024 63 / 54.
+    // FP8 pages without a scratch area: window 128, 32 rows 11.1 / 6.9, 64 11.2 / 12.3; window 1024, 64 rows 53.6 / 35.8, 128 53 / 64; window
+    // 4096, 16 rows 198 / 34, 64 199 / 116, 128 204 / 231.)
+    const int64_t row_heads = (int64_t)batch * max_q_len * c->kv_heads,
+                  row_tokens = (int64_t)window + sinks < (int64_t)pt_stride * PAGE ? (int64_t)window + sinks : (int64_t)pt_stride * PAGE;
+    const bool few_rows = max_q_len == 1 || (c->fp8 && !via_scratch ? row_heads <= 256 || (row_heads <= 512 && row_tokens >= 512)
+                                                                    : row_heads <= 256 && row_heads * row_tokens * c->head_dim <= 19200000);
+    if (window && few_rows && c->prefill_variant == 0 && aligned(Q, 16) && aligned(out, 8)) {
+        DecodeParams d;
+        memset(&d, 0, sizeof(d));
+        d.layer_base = c->layer_base(c->slot[(size_t)src]);
+        d.page_stride = (int64_t)c->page_bytes;
+        d.max_pages = c->max_pages;
+        d.Q = static_cast<const uint16_t *>(Q);
+        d.page_table = page_table;
+        d.seq_lens = seq_lens;
+        d.out = static_cast<uint16_t *>(out);
+        d.B = batch * max_q_len;
+        d.Hq = q_heads;
+        d.Hkv = c->kv_heads;
+        d.pt_stride = pt_stride;
+        d.scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)c->head_dim)) * 1.4426950408889634f;
+        d.window = window;
+        d.sinks = sinks;
+        d.cu_q = cu_q_lens;
+        d.max_q_len = max_q_len;
+        d.keep_pct = 1;                                          // (the rows of a sequence read the same pages)
+        d.status = c->status_word();
+        const int kernel = c->fp8 ? 2 : c->tune.variant == 2 || (c->tune.variant == 0 && G > 1) ? 1 : 0;
+        if (launch_decode_window(d, c->head_dim, G, kernel, c->sm_count, c->tune.pdl != 0, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return SKV_ERR_CUDA;
+        }
+        c->launches += 1;
+        return SKV_OK;
+    }
     if (c->prefill_variant == 2 && !can_umma) return SKV_ERR_UNSUPPORTED;
     const bool umma = c->prefill_variant == 2 || (c->prefill_variant == 0 && can_umma);
     if (!umma && (c->fp8 ? prefill_fp8_smem_bytes(c->head_dim) : prefill_smem_bytes(c->head_dim)) > (size_t)c->max_smem_optin)

@@ -127,6 +127,8 @@ struct DecodeParams {
     int64_t l2_fit_blocks;      // a call with at most this many blocks in all is small enough to stay in L2 for
                                 // the next layer that reads the same owner: all of it is loaded with normal priority
     int window, sinks;          // sliding-window instances only: tokens t >= n - window or t < sinks are attended
+    const int32_t *cu_q;        // the same, for a call of few rows: [B / max_q_len + 1] as in PrefillParams; "sequence" b is then row
+    int max_q_len;              // b % max_q_len of sequence b / max_q_len (null: a row per sequence)
     int *status;
     unsigned long long *trace;  // optional [n_workers][4]: sm id, entry ns, first-page ns, exit ns
     unsigned long long *tags;   // [n_slots]: `epoch` once the partial at that slot is complete (DECODE_MERGE_IN_KERNEL)

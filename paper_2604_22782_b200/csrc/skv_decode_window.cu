@@ -44,7 +44,7 @@ __device__ __forceinline__ float2 ld_cluster_f2(uint32_t a)
 }
 
 // Dynamic shared memory: rings [NW][ST] blocks | states [NW] | the CTA's state | barriers [NW][ST]
-template <int D, class State, int NW, bool EARLY>
+template <int D, class State, int NW, bool EARLY, bool CHUNK>
 __global__ void __launch_bounds__(NW * 32) decode_window_kernel(DecodeParams p, int G, int ST)
 {
     extern __shared__ __align__(128) uint8_t smem_raw[];
@@ -67,14 +67,28 @@ __global__ void __launch_bounds__(NW * 32) decode_window_kernel(DecodeParams p, 
     __syncwarp();
     pdl_wait();
     if (EARLY) pdl_trigger();
-    const int seg = (int)(blockIdx.x / ranks), b = seg / p.Hkv, h = seg - b * p.Hkv;
-    int n = __ldg(p.seq_lens + b);
-    n = n > 0 ? n : 0;
-    if ((int64_t)n > (int64_t)p.pt_stride * PAGE) {
-        n = p.pt_stride * PAGE;
-        if (rank == 0 && h == 0 && threadIdx.x == 0) atomicOr(p.status, STATUS_BOUNDS);
+    const int seg = (int)(blockIdx.x / ranks), slot = seg / p.Hkv, h = seg - slot * p.Hkv;
+    int b = slot, row = slot, n;               // sequence, row of Q and out, tokens up to the row's own
+    if (CHUNK) {                               // (every exit is the whole cluster's)
+        b = slot / p.max_q_len;
+        const int i = slot - b * p.max_q_len, first = __ldg(p.cu_q + b), q_len = __ldg(p.cu_q + b + 1) - first;
+        n = __ldg(p.seq_lens + b);
+        if (first < 0 || q_len < 0 || q_len > n || q_len > p.max_q_len || (int64_t)n > (int64_t)p.pt_stride * PAGE) {
+            if (i == 0 && h == 0 && rank == 0 && threadIdx.x == 0) atomicOr(p.status, STATUS_BOUNDS);
+            return;
+        }
+        if (i >= q_len) return;
+        n -= q_len - 1 - i;
+        row = first + i;
+    } else {
+        n = __ldg(p.seq_lens + b);
+        n = n > 0 ? n : 0;
+        if ((int64_t)n > (int64_t)p.pt_stride * PAGE) {
+            n = p.pt_stride * PAGE;
+            if (rank == 0 && h == 0 && threadIdx.x == 0) atomicOr(p.status, STATUS_BOUNDS);
+        }
     }
-    uint32_t *rows = reinterpret_cast<uint32_t *>(p.out + ((int64_t)b * p.Hq + (int64_t)h * G) * D);     // pairs of bf16
+    uint32_t *rows = reinterpret_cast<uint32_t *>(p.out + ((int64_t)row * p.Hq + (int64_t)h * G) * D);     // pairs of bf16
     if (n == 0) {                              // (the same for the whole cluster: no barrier is left half-way)
         if (rank == 0)
             for (int i = threadIdx.x; i < G * D / 2; i += NW * 32) rows[i] = 0u;
@@ -99,7 +113,7 @@ __global__ void __launch_bounds__(NW * 32) decode_window_kernel(DecodeParams p, 
     if (lane < ST && lane < count) send(lane, next_id);
     next_id = __shfl_sync(FULL, next_id, ST);
     State st;
-    st.begin(p, b, h, G, lane);
+    st.begin(p, row, h, G, lane);
     int sent = count < ST ? count : ST, done = 0;
     bool ok = true;
     for (; done < count; ++done) {
@@ -225,7 +239,7 @@ Shape shape_of(int block, int64_t segments, int64_t pages, int sm)
     return best;
 }
 
-template <int D, class State>
+template <int D, class State, bool CHUNK>
 cudaError_t launch_t(const DecodeParams &p, int G, int sm_count, bool pdl, cudaStream_t s)
 {
     const int64_t segments = (int64_t)p.B * p.Hkv;
@@ -238,8 +252,9 @@ cudaError_t launch_t(const DecodeParams &p, int G, int sm_count, bool pdl, cudaS
     // free, two CTAs here and none there, and run as unevenly (64 x 129 pages: 42 us, and 51 let in at once; 1024 x 257 pages
     // 79 and 84; 8 x 65 pages 6.0 and 5.6).
     const bool early = segments * f.ranks <= sm_count;
-    auto kern = f.warps == 8 ? (early ? decode_window_kernel<D, State, 8, true> : decode_window_kernel<D, State, 8, false>)
-                             : (early ? decode_window_kernel<D, State, 4, true> : decode_window_kernel<D, State, 4, false>);
+    auto kern = CHUNK        ? (f.warps == 8 ? decode_window_kernel<D, State, 8, false, CHUNK> : decode_window_kernel<D, State, 4, false, CHUNK>)
+                : f.warps == 8 ? (early ? decode_window_kernel<D, State, 8, true, CHUNK> : decode_window_kernel<D, State, 8, false, CHUNK>)
+                               : (early ? decode_window_kernel<D, State, 4, true, CHUNK> : decode_window_kernel<D, State, 4, false, CHUNK>);
     cudaError_t e = ensure_dynamic_smem(kern, smem);
     if (e != cudaSuccess) return e;
     if (f.ranks > 8) {
@@ -281,14 +296,14 @@ cudaError_t launch_t(const DecodeParams &p, int G, int sm_count, bool pdl, cudaS
 cudaError_t launch_decode_window(const DecodeParams &p, int D, int G, int kernel, int sm_count, bool pdl, cudaStream_t s)
 {
     if (D == 128) {
-        if (kernel == 2) return launch_t<128, Fp8State<128>>(p, G, sm_count, pdl, s);
-        if (kernel == 1) return launch_t<128, TensorCoreState<128>>(p, G, sm_count, pdl, s);
-        return launch_t<128, CudaCoreState<128>>(p, G, sm_count, pdl, s);
+        if (kernel == 2) return p.cu_q ? launch_t<128, Fp8State<128>, true>(p, G, sm_count, pdl, s) : launch_t<128, Fp8State<128>, false>(p, G, sm_count, pdl, s);
+        if (kernel == 1) return p.cu_q ? launch_t<128, TensorCoreState<128>, true>(p, G, sm_count, pdl, s) : launch_t<128, TensorCoreState<128>, false>(p, G, sm_count, pdl, s);
+        return p.cu_q ? launch_t<128, CudaCoreState<128>, true>(p, G, sm_count, pdl, s) : launch_t<128, CudaCoreState<128>, false>(p, G, sm_count, pdl, s);
     }
     if (D == 64) {
-        if (kernel == 2) return launch_t<64, Fp8State<64>>(p, G, sm_count, pdl, s);
-        if (kernel == 1) return launch_t<64, TensorCoreState<64>>(p, G, sm_count, pdl, s);
-        return launch_t<64, CudaCoreState<64>>(p, G, sm_count, pdl, s);
+        if (kernel == 2) return p.cu_q ? launch_t<64, Fp8State<64>, true>(p, G, sm_count, pdl, s) : launch_t<64, Fp8State<64>, false>(p, G, sm_count, pdl, s);
+        if (kernel == 1) return p.cu_q ? launch_t<64, TensorCoreState<64>, true>(p, G, sm_count, pdl, s) : launch_t<64, TensorCoreState<64>, false>(p, G, sm_count, pdl, s);
+        return p.cu_q ? launch_t<64, CudaCoreState<64>, true>(p, G, sm_count, pdl, s) : launch_t<64, CudaCoreState<64>, false>(p, G, sm_count, pdl, s);
     }
     return cudaErrorInvalidValue;
 }

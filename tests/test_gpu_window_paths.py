@@ -264,3 +264,33 @@ def test_chunk_of_few_rows_captured_and_beside_another_stream(sequences):
     torch.cuda.synchronize()
     check_chunk(p, q, rows, outs[0], 2048, 4)
     assert torch.equal(outs[0], outs[1]) and p.cache.skv_get_status() == 0
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (4, 4, 128), (6, 2, 64), (4, 4, 64)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (40, 20), (700, 0), (129, 200), (5000, 0), (2147483647, 2147483647)])
+@pytest.mark.parametrize("rows", [[1, 1, 0, 1, 1], [5, 17, 0, 1, 3], [12, 3, 2, 9, 5]])
+def test_chunk_of_rows_that_go_one_by_one(hq, hkv, d, window, sinks, rows, fp8):
+    """Through the decode kernel and, asked for, through the tile kernel: both against the definition, rows behind the last one left."""
+    lens = [900, 17, 2, 2049, 65]
+    p = Paged(lens, hkv, d, fp8, seed=45)
+    q = p.rows(sum(rows), hq)
+    p.forget([n - m for n, m in zip(lens, rows)], window, sinks)
+    for variant in (0, 1):
+        p.cache.skv_set_prefill_variant(variant)
+        check_chunk(p, q, rows, chunk(p, q, rows, window, sinks), window, sinks)
+        assert p.cache.skv_get_status() == 0
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_few_rows_that_do_not_fit_are_flagged(fp8):
+    from paper_2604_22782_b200.binding import SKV_ERR_BOUNDS
+    p = Paged([6, 40], 2, 128, fp8, seed=46)
+    q = p.rows(12, 4).cuda()
+    for offsets, most, left in (([0, 7, 12], 7, slice(0, 7)), ([0, 6, 12], 5, slice(0, 12)), ([-2, 3, 12], 9, slice(0, 3))):
+        out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+        cu = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+        p.cache.skv_prefill_attn_window(1, q, cu, p.table_dev, p.lens_dev, out, most, 30, 4)
+        assert p.cache.skv_get_status() == SKV_ERR_BOUNDS
+        assert bool((out[left] == 7.0).all())
+        assert left.stop == 12 or bool((out[left.stop:] != 7.0).any())
