@@ -264,14 +264,15 @@ __device__ __forceinline__ float ex2(float x)          // (fast_exp2 without its
 
 // 2^x of a pair on the FMA units: x = n + f with n the nearest integer, a polynomial for 2^f on [-1/2, 1/2] (least largest
 // relative error, by Remez exchange: 2.7e-6 in fp32, a thousandth of the rounding to bf16 that follows), times 2^n.
-// x is clamped to -126: a hidden key's probability comes out as 2^-126 instead of 0, next to a sum of 2^-8 or more.
+// x is clamped to -127, whose power of two has the bits of 0: a hidden key (x = -inf) gets exactly 0, as from ex2, and its V,
+// however large, does not show.
 __device__ __forceinline__ void exp2_by_fma(uint64_t x, float &lo, float &hi)
 {
     const float magic = 12582912.f;                    // 1.5 * 2^23: x + magic has the nearest integer in its low bits
     float x0, x1;
     halves(x, x0, x1);
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(x0) : "f"(x0), "f"(-126.f));
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(x1) : "f"(x1), "f"(-126.f));
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(x0) : "f"(x0), "f"(-127.f));
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(x1) : "f"(x1), "f"(-127.f));
     x = pair_of(x0, x1);
     const uint64_t r = add2(x, pair_of(magic, magic));
     const uint64_t n = add2(r, pair_of(-magic, -magic));
