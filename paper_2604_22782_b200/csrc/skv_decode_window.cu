@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(NW * 32) decode_window_kernel(DecodeParams p, 
         __syncwarp();
     }
     if (count > 0) st.finish(mine, mine + G * D, 0, G, lane);
-    else if (lane < G) mine[G * D + 2 * lane] = -INFINITY;
+    else if (lane < G) *reinterpret_cast<float2 *>(mine + G * D + 2 * lane) = make_float2(-INFINITY, 0.f);
     __syncthreads();
     // sum of n_states states, weighted: the pair e2 of the segment's rows and its head's (max, sum)
     auto combine = [&](auto most, int n_states, int e2, auto ml_of, auto pair_of, float &M, float &L, float2 &a) {
@@ -159,7 +159,9 @@ __global__ void __launch_bounds__(NW * 32) decode_window_kernel(DecodeParams p, 
         a = make_float2(0.f, 0.f);
 #pragma unroll
         for (int c = 0; c < N; ++c) {
-            if (ml[c].x == -INFINITY) continue;                      // (no page there, or not there)
+            // No page there, or not there: the sum says so, which is 1 or more where there is one, or NaN.  (Not the maximum:
+            // that is -inf too where every score is NaN, and the result has to be NaN then.)
+            if (ml[c].y == 0.f) continue;
             const float w = fast_exp2(ml[c].x - M);
             L = fmaf(w, ml[c].y, L);
             a.x = fmaf(w, v[c].x, a.x);
@@ -167,7 +169,7 @@ __global__ void __launch_bounds__(NW * 32) decode_window_kernel(DecodeParams p, 
         }
     };
     auto write_row = [&](int e2, float L, float2 a) {
-        const float inv = L > 0.f ? 1.f / L : 0.f;
+        const float inv = L == 0.f ? 0.f : 1.f / L;          // (a NaN stays one)
         rows[e2] = pack_bf16x2(a.x * inv, a.y * inv);
     };
     for (int e2 = threadIdx.x; e2 < G * D / 2; e2 += NW * 32) {
