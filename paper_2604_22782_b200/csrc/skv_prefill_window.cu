@@ -591,7 +591,7 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                     v[c] = make_float4(0.f, 0.f, 0.f, 0.f);
                     if (c < (int)ranks) {
                         ml[c] = ld_cluster_f2(at_rank(state_ml + (uint32_t)(r * 8), (uint32_t)c));
-                        if (ml[c].x != -INFINITY) v[c] = ld_cluster_f4(at_rank(state + (uint32_t)((r * STATE_ROW + d) * 4), (uint32_t)c));
+                        if (ml[c].y != 0.f) v[c] = ld_cluster_f4(at_rank(state + (uint32_t)((r * STATE_ROW + d) * 4), (uint32_t)c));
                     }
                 }
                 float M = -INFINITY, L = 0.f;
@@ -600,7 +600,9 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_window_kernel(const __grid
                 for (int c = 0; c < MAX_RANKS; ++c) M = fmaxf(M, ml[c].x);
 #pragma unroll
                 for (int c = 0; c < MAX_RANKS; ++c) {
-                    if (ml[c].x == -INFINITY) continue;            // (the row sees nothing there)
+                    // The row sees nothing there: its weights, and so their sum, are exactly 0.  (Its maximum is -inf, but that is
+                    // so too where all the scores are NaN; their sum is NaN, and the result has to be.)
+                    if (ml[c].y == 0.f) continue;
                     const float w = ex2(ml[c].x - M);
                     L = fmaf(w, ml[c].y, L);
                     o = make_float4(fmaf(w, v[c].x, o.x), fmaf(w, v[c].y, o.y), fmaf(w, v[c].z, o.z), fmaf(w, v[c].w, o.w));

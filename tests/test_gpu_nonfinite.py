@@ -90,3 +90,21 @@ def test_window_chunk_of_what_is_not_finite(rows, variant, hq, hkv, d, fp8):
     for window, sinks in ((1024, 0), (30, 4)):
         compare_chunk(p, q, rows, chunk(p, q, rows, window, sinks), window, sinks)
     assert p.cache.skv_get_status() == 0
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (6, 2, 64), (5, 1, 128)])
+@pytest.mark.parametrize("first,count", [(1184, 384), (1500, 900), (2800, 216), (64, 1)])
+@pytest.mark.parametrize("sequences", [1, 3])
+def test_chunk_shared_by_a_cluster_of_what_is_not_finite(sequences, first, count, hq, hkv, d):
+    """All the keys of one CTA's part are NaN and no others (one sequence, window 2900: blocks 17 to 22 of the 46 from token 96
+    on), of several, those behind the first row's place, a single one; and a NaN query."""
+    lens, rows = [3020, 2500, 3000][:sequences], [17, 20, 5][:sequences]
+    p = Paged(lens, hkv, d, seed=54)
+    p.cache.skv_set_prefill_variant(2)
+    spoil_keys(p, 0, torch.arange(first, first + count))
+    q = p.rows(sum(rows), hq)
+    q[2, 1] = NAN
+    q[4, 0, 9] = INF
+    for window, sinks in ((2900, 0), (1600, 100), (1200, 0), (210, 3)):
+        compare_chunk(p, q, rows, chunk(p, q, rows, window, sinks), window, sinks)
+    assert p.cache.skv_get_status() == 0
