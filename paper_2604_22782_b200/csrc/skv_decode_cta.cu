@@ -421,14 +421,16 @@ __maxnreg__(INMERGE ? 200 : State::CTA_MAX_REGS) decode_cta_kernel(DecodeParams 
             float L = 0.f, a0 = 0.f, a1 = 0.f;
 #pragma unroll
             for (int c = 0; c < MAX_CONSUMERS + 1; ++c) {
-                if (m_c[c] == -INFINITY) continue;      // this consumer had no block in the run (or is not there)
+                // This consumer had no block in the run (or is not there): its sum is 0.  (A maximum of -inf would not do: it is
+                // that too where every score is NaN, which has to reach the result.)
+                if (l_c[c] == 0.f) continue;
                 const float wt = fast_exp2(m_c[c] - M);
                 L = fmaf(wt, l_c[c], L);
                 a0 = fmaf(wt, v_c[c].x, a0);
                 a1 = fmaf(wt, v_c[c].y, a1);
             }
             if (rows) {
-                const float inv = L > 0.f ? 1.f / L : 0.f;
+                const float inv = L == 0.f ? 0.f : 1.f / L;          // (a NaN stays one)
                 uint32_t *dst = reinterpret_cast<uint32_t *>(p.out + ((int64_t)b * p.Hq + (int64_t)h * G) * D);
                 dst[e2] = pack_bf16x2(a0 * inv, a1 * inv);
             } else {
@@ -622,7 +624,7 @@ __maxnreg__(INMERGE ? 200 : State::CTA_MAX_REGS) decode_cta_kernel(DecodeParams 
             // with a combining warp: the scratch buffer of this run's parity is free once run - 2 has been combined
             if (COMBINER && run >= 2 && !wait_or_quit(scratch_free + 8 * qb, (uint32_t)(((run >> 1) - 1) & 1), gave_up)) { fail(); break; }
             if (has_blocks) st.finish(mine, mine + G * D, 0, G, lane);
-            else if (lane < G) mine[G * D + 2 * lane] = -INFINITY;             // no block of this run: nothing to contribute
+            else if (lane < G) *reinterpret_cast<float2 *>(mine + G * D + 2 * lane) = make_float2(-INFINITY, 0.f);   // no block of this run: nothing to contribute
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(run_done + 8 * qb);

@@ -108,3 +108,25 @@ def test_chunk_shared_by_a_cluster_of_what_is_not_finite(sequences, first, count
     for window, sinks in ((2900, 0), (1600, 100), (1200, 0), (210, 3)):
         compare_chunk(p, q, rows, chunk(p, q, rows, window, sinks), window, sinks)
     assert p.cache.skv_get_status() == 0
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("hq,hkv,d", SHAPES)
+@pytest.mark.parametrize("worker,merge", [(1, 0), (2, 1), (2, 2)])
+@pytest.mark.parametrize("lens", LENGTHS)
+def test_plain_decode_of_what_is_not_finite(lens, worker, merge, hq, hkv, d, fp8):
+    """The call without a window: a warp per range, a CTA per range, with the merge launch and without."""
+    p = Paged(lens, hkv, d, fp8, seed=55)
+    p.cache.skv_set_decode_worker(worker)
+    p.cache.skv_set_decode_merge(merge)
+    spoil_keys(p, 0, torch.arange(272, 288))
+    q = p.rows(len(lens), hq)
+    if len(lens) > 1:
+        q[1, 1] = NAN
+        q[2, 0, 5] = NAN
+    ws = torch.empty(p.cache.skv_decode_workspace_bytes(len(lens), hq), dtype=torch.uint8, device="cuda")
+    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+    p.cache.skv_decode_attn(1, q.cuda(), p.table_dev, p.lens_dev, out, ws)
+    torch.cuda.synchronize()
+    compare_decode(p, q, out, 1 << 30, 0)
+    assert p.cache.skv_get_status() == 0
