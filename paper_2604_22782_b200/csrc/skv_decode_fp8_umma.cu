@@ -434,7 +434,9 @@ __global__ void __launch_bounds__(THREADS, WIN ? CTAS_PER_SM : CTAS_PER_SM + 1) 
                     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(lead[0]), "r"(lead[1]), "r"(lead[2]), "r"(lead[3]) : "memory");
                     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a + 1024u), "r"(rem[0]), "r"(rem[1]), "r"(rem[2]), "r"(rem[3]) : "memory");
                 }
-                if (qd == 0) qscale[qset * 8 + g] = back_q * p.scale_log2;
+                // (0 * amax: NaN for a row with an infinite element, which E4M3 does not hold -- it would count as 448.  That
+                // element's product with any key's is infinite or NaN, and so the row's softmax is NaN.)
+                if (qd == 0) qscale[qset * 8 + g] = fmaf(0.f, amax, back_q * p.scale_log2);
                 fence_proxy_async();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_full);

@@ -130,3 +130,26 @@ def test_plain_decode_of_what_is_not_finite(lens, worker, merge, hq, hkv, d, fp8
     torch.cuda.synchronize()
     compare_decode(p, q, out, 1 << 30, 0)
     assert p.cache.skv_get_status() == 0
+
+
+@pytest.mark.parametrize("value", [INF, -INF, NAN])
+@pytest.mark.parametrize("hq,hkv", [(8, 8), (32, 8), (64, 8)])
+@pytest.mark.parametrize("window", [0, 300])
+def test_decode_of_many_fp8_sequences_with_a_query_that_is_not_finite(window, hq, hkv, value):
+    """The tcgen05 kernel, without and with a window.  (An infinite element times a key's element is infinite or NaN for every
+    token, so the definition's weights are NaN.)"""
+    lens = [1 + (b * 37) % 600 for b in range(200)] + [1200]
+    p = Paged(lens, hkv, 128, fp8=True, seed=56)
+    q = p.rows(len(lens), hq)
+    q[0, 0, 5] = value
+    q[17, hq - 1, 127] = value
+    q[200, 1] = value
+    ws = torch.empty(p.cache.skv_decode_workspace_bytes(len(lens), hq), dtype=torch.uint8, device="cuda")
+    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+    if window:
+        p.cache.skv_decode_attn_window(1, q.cuda(), p.table_dev, p.lens_dev, out, ws, window, 4)
+    else:
+        p.cache.skv_decode_attn(1, q.cuda(), p.table_dev, p.lens_dev, out, ws)
+    torch.cuda.synchronize()
+    compare_decode(p, q, out, window or 1 << 30, 4)
+    assert p.cache.skv_get_status() == 0
