@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(128, 2) prefill_kernel(PrefillParams p, int G)
 // The same tile scheme on FP8 pages (E4M3 codes + one fp32 scale per token and kv head): the codes go
 // to mma.sync as f16 (exact), the scales stay outside the contractions as in the decode kernel:
 //   score = qmax_row kscale_key (Q/qmax . Kc),     P' = p vscale_key / c,     O = c sum P' Vc,
-// c a power of two >= every vscale seen so far.  Fragments are 32-bit shared-memory loads of four
+// c a power of two >= every vscale that the row has seen so far.  Fragments are 32-bit shared-memory loads of four
 // consecutive dims (scores) or keys (values) of one row of the page: the order of the contraction
 // index inside an instruction is free as long as both operands agree, and the score instructions
 // take the page's key rows in the order 0,1,4,5,8,9,12,13 | 2,3,6,7,10,11,14,15, so that a thread's
@@ -344,6 +344,7 @@ __global__ void __launch_bounds__(128, 2) prefill_fp8_kernel(PrefillParams p, in
     const int from_lo = WIN && pos_lo >= p.window ? pos_lo - p.window + 1 : 0, from_hi = WIN && pos_hi >= p.window ? pos_hi - p.window + 1 : 0;
     auto sees_lo = [&](int key) { return key <= pos_lo && (!WIN || key >= from_lo || key < p.sinks); };
     auto sees_hi = [&](int key) { return key <= pos_hi && (!WIN || key >= from_hi || key < p.sinks); };
+    const int last = pos0 + q_end - 1, from_last = WIN && last >= p.window ? last - p.window + 1 : 0;      // ... inside the tile's last row's
     const int64_t row_lo = ((int64_t)(q_begin + q0 + qi_lo) * p.Hq + (int64_t)h * G + g_lo) * D;
     const int64_t row_hi = ((int64_t)(q_begin + q0 + qi_hi) * p.Hq + (int64_t)h * G + g_hi) * D;
 
@@ -382,7 +383,7 @@ __global__ void __launch_bounds__(128, 2) prefill_fp8_kernel(PrefillParams p, in
     float o[D / 8][4];
 #pragma unroll
     for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    float m_lo = -INFINITY, m_hi = -INFINITY, l_lo = 0.f, l_hi = 0.f, cs = 0.f;
+    float m_lo = -INFINITY, m_hi = -INFINITY, l_lo = 0.f, l_hi = 0.f, cs_lo = 0.f, cs_hi = 0.f;
 
     // key rows of the two score tiles of a page, and this thread's bytes in them
     const int krow = 4 * (gid >> 1) + (gid & 1);
@@ -458,8 +459,30 @@ __global__ void __launch_bounds__(128, 2) prefill_fp8_kernel(PrefillParams p, in
         mx_lo = fmaxf(mx_lo, __shfl_xor_sync(FULL, mx_lo, 2));
         mx_hi = fmaxf(mx_hi, __shfl_xor_sync(FULL, mx_hi, 1));
         mx_hi = fmaxf(mx_hi, __shfl_xor_sync(FULL, mx_hi, 2));
-        svmax = fmaxf(svmax, __shfl_xor_sync(FULL, svmax, 1));
-        svmax = fmaxf(svmax, __shfl_xor_sync(FULL, svmax, 2));
+        // WIN: the largest V scale that each row sees -- the same where all rows of the tile see all of the block
+        float sv_lo = svmax, sv_hi = svmax;
+        bool edge = false;
+        if (WIN) {
+            const int key_from = win.page(pg0) * PAGE, key_to = (win.page(pg0 + np - 1) + 1) * PAGE;
+            edge = key_to > pos0 + q0 + 1 || key_from < from_last;
+        }
+        if (edge) {
+            sv_lo = sv_hi = 0.f;
+#pragma unroll
+            for (int j = 0; j < KB; ++j) {
+                const float *vv = &vsc[j].x;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (sc[2 * j + (i >> 1)][i & 1] != -INFINITY) sv_lo = fmaxf(sv_lo, vv[i]);
+                    if (sc[2 * j + (i >> 1)][2 + (i & 1)] != -INFINITY) sv_hi = fmaxf(sv_hi, vv[i]);
+                }
+            }
+            sv_hi = fmaxf(sv_hi, __shfl_xor_sync(FULL, sv_hi, 1));
+            sv_hi = fmaxf(sv_hi, __shfl_xor_sync(FULL, sv_hi, 2));
+        }
+        sv_lo = fmaxf(sv_lo, __shfl_xor_sync(FULL, sv_lo, 1));
+        sv_lo = fmaxf(sv_lo, __shfl_xor_sync(FULL, sv_lo, 2));
+        if (!edge) sv_hi = sv_lo;
         const float mn_lo = fmaxf(m_lo, mx_lo), mn_hi = fmaxf(m_hi, mx_hi);
         const float ref_lo = WIN && mn_lo == -INFINITY ? 0.f : mn_lo, ref_hi = WIN && mn_hi == -INFINITY ? 0.f : mn_hi;
         float a_lo = fast_exp2(m_lo - ref_lo), a_hi = fast_exp2(m_hi - ref_hi);
@@ -475,28 +498,42 @@ __global__ void __launch_bounds__(128, 2) prefill_fp8_kernel(PrefillParams p, in
         }
         l_lo = l_lo * a_lo + sum_lo;
         l_hi = l_hi * a_hi + sum_hi;
-        // reference scale of the V side: the smallest power of two >= every vscale so far
-        const float up = __uint_as_float((__float_as_uint(svmax) + 0x007FFFFFu) & 0x7F800000u);
-        const float cs_new = fmaxf(cs, up);
-        const float inv_cs = cs_new > 0.f ? __uint_as_float(0x7F000000u - __float_as_uint(cs_new)) : 0.f;
-        const float ca = cs * inv_cs;                      // 1 unless the reference grew
-        cs = cs_new;
-        a_lo *= ca;
-        a_hi *= ca;
+        // reference scale of the V side: the smallest power of two >= every vscale so far.  WIN: of the row's, not of the tile's --
+        // a value that only other rows see, if large enough, would push this row's P' out of f16's range.  (3 % slower: 128 rows
+        // over 4096 tokens 206 us against 200.  Without a window one reference serves the tile: a row's result is exact to f16 while no
+        // token behind it has a V scale more than some 2^10 times its own.)
+        auto refer = [](float svmax, float &cs, float &ratio) -> float {
+            const float up = __uint_as_float((__float_as_uint(svmax) + 0x007FFFFFu) & 0x7F800000u);
+            const float cs_new = fmaxf(cs, up);
+            const float inv = cs_new > 0.f ? __uint_as_float(0x7F000000u - __float_as_uint(cs_new)) : 0.f;
+            ratio = cs * inv;                              // 1 unless the reference grew
+            cs = cs_new;
+            return inv;
+        };
+        float ca_lo, ca_hi;
+        const float inv_lo = refer(sv_lo, cs_lo, ca_lo);
+        float inv_hi = inv_lo;
+        ca_hi = ca_lo;
+        if (WIN) inv_hi = refer(sv_hi, cs_hi, ca_hi);
+        a_lo *= ca_lo;
+        a_hi *= ca_hi;
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) {
             o[i][0] *= a_lo; o[i][1] *= a_lo;
             o[i][2] *= a_hi; o[i][3] *= a_hi;
         }
+        // P' of a weight and its token's scale.  (WIN: the product of the two first -- a weight of 0 stays 0 then, however large
+        // the scale of a token that the row does not see is beside the row's reference.)
+        auto weigh = [](float w, float vs, float inv) { return WIN ? w * vs * inv : w * (vs * inv); };
         // O += P' Vc
 #pragma unroll
         for (int j = 0; j < KB; ++j) {
             if (j < np) {
-                const float w0 = vsc[j].x * inv_cs, w1 = vsc[j].y * inv_cs, w2 = vsc[j].z * inv_cs, w3 = vsc[j].w * inv_cs;
-                const uint32_t pa0 = pack_f16x2(sc[2 * j][0] * w0, sc[2 * j][1] * w1);
-                const uint32_t pa1 = pack_f16x2(sc[2 * j][2] * w0, sc[2 * j][3] * w1);
-                const uint32_t pa2 = pack_f16x2(sc[2 * j + 1][0] * w2, sc[2 * j + 1][1] * w3);
-                const uint32_t pa3 = pack_f16x2(sc[2 * j + 1][2] * w2, sc[2 * j + 1][3] * w3);
+                const float v0 = vsc[j].x, v1 = vsc[j].y, v2 = vsc[j].z, v3 = vsc[j].w;
+                const uint32_t pa0 = pack_f16x2(weigh(sc[2 * j][0], v0, inv_lo), weigh(sc[2 * j][1], v1, inv_lo));
+                const uint32_t pa1 = pack_f16x2(weigh(sc[2 * j][2], v0, inv_hi), weigh(sc[2 * j][3], v1, inv_hi));
+                const uint32_t pa2 = pack_f16x2(weigh(sc[2 * j + 1][0], v2, inv_lo), weigh(sc[2 * j + 1][1], v3, inv_lo));
+                const uint32_t pa3 = pack_f16x2(weigh(sc[2 * j + 1][2], v2, inv_hi), weigh(sc[2 * j + 1][3], v3, inv_hi));
                 uint32_t vmask = 0xFFFFFFFFu;              // bytes of a V word that belong to tokens in use
                 if (WIN) {
                     const uint32_t b4 = (window_bits(win.page(pg0 + j), win.lo, n_keys, p.sinks) >> (4 * tig)) & 0xFu;
@@ -530,14 +567,14 @@ __global__ void __launch_bounds__(128, 2) prefill_fp8_kernel(PrefillParams p, in
     l_hi += __shfl_xor_sync(FULL, l_hi, 1);
     l_hi += __shfl_xor_sync(FULL, l_hi, 2);
     if (ok_lo) {
-        const float inv = cs / l_lo;
+        const float inv = cs_lo / l_lo;
         uint16_t *dst = p.out + row_lo + 2 * tig;
 #pragma unroll
         for (int i = 0; i < D / 8; ++i)
             *reinterpret_cast<uint32_t *>(dst + 8 * i) = pack_bf16x2(o[i][0] * inv, o[i][1] * inv);
     }
     if (ok_hi) {
-        const float inv = cs / l_hi;
+        const float inv = (WIN ? cs_hi : cs_lo) / l_hi;
         uint16_t *dst = p.out + row_hi + 2 * tig;
 #pragma unroll
         for (int i = 0; i < D / 8; ++i)

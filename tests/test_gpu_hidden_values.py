@@ -53,3 +53,18 @@ def hold(p, hq, window, sinks, value, more=lambda size, reach: 0.0):
         at += n
     assert compared >= 100
     assert p.cache.skv_get_status() == 0
+
+
+@pytest.mark.parametrize("value", [torch.finfo(torch.bfloat16).min, torch.finfo(torch.bfloat16).max])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (4, 4, 128), (6, 2, 64)])
+@pytest.mark.parametrize("scratch", [False, True])
+@pytest.mark.parametrize("window,sinks", [(20, 0), (100, 4), (5000, 0)])
+def test_rows_on_fp8_pages_that_do_not_see_an_extreme_value(window, sinks, scratch, hq, hkv, d, value):
+    """By the kernel that reads the codes, and through a scratch area (K, V rounded to bf16 there: 2^-8 of themselves, which moves
+    a score by 2^-8 of the row's reach, and a weight and the weights' sum by as much)."""
+    p = Paged(LENS, hkv, d, fp8=True, seed=62)
+    if not scratch:
+        return hold(p, hq, window, sinks, value)
+    p.cache.skv_set_prefill_scratch(torch.empty(p.cache.skv_prefill_scratch_bytes(), dtype=torch.uint8, device="cuda"))
+    hold(p, hq, window, sinks, value, lambda size, reach: size * (2 ** -8 + 2 * 2 ** -8 * reach) + size * 2 ** -8)
+    p.cache.skv_set_prefill_scratch(None)
