@@ -41,6 +41,10 @@ int skv_test_wait_expires(void *device_status_word, int limit_ms, void *stream);
  * Errors: SKV_ERR_ARG, SKV_ERR_CUDA. */
 int skv_test_query_kernel(const void *q_in, const void *prev_out, void *q_out, long long n_elems, void *stream);
 
+/* Shared memory of a CTA of the tcgen05 FP8 decode kernel for a batch, without
+ * (window 0) or with a sliding window.  Host only. */
+size_t skv_test_fp8_decode_smem_bytes(int head_dim, int batch, int window);
+
 #ifdef __cplusplus
 }
 #endif

@@ -802,10 +802,10 @@ int decode_fp8_umma_tile_tokens() { return TP * PAGE; }
 size_t decode_fp8_umma_smem_bytes(int D, int B, bool window)
 {
     const int block = fp8_block_bytes(D);
-    // alignment | tables | K and V rings | two P' | Q' | tile descriptions | query scales | maxima | sums | barriers | two words
+    // alignment | tables | K and V rings | two P' | Q' | tile descriptions | query scales | maxima | sums | barriers | three words
     const size_t tables = window ? ((size_t)(B + 1) * 4 + 127) & ~(size_t)127 : table_bytes(B);
     return 128 + tables + (size_t)NST * TP * block + 2 * 16 * (size_t)(TP * PAGE) + 16 * (size_t)D + 4 * sizeof(TileMeta) +
-           64 + 512 + 128 + 16 * 8 + 16 + 64;          // (... | a window's token sets)
+           64 + 512 + 128 + 16 * 8 + 16 + (window ? 4 * TP * sizeof(uint16_t) : 0);          // (... | a window's token sets)
 }
 
 cudaError_t launch_decode_fp8_umma(const DecodeParams &p, int D, int G, int grid, bool pdl, cudaStream_t s)

@@ -75,4 +75,9 @@ extern "C" int skv_test_wait_expires(void *device_status_word, int limit_ms, voi
     if (cudaGetLastError() != cudaSuccess) return SKV_ERR_CUDA;
     return SKV_OK;
 }
+
+extern "C" size_t skv_test_fp8_decode_smem_bytes(int head_dim, int batch, int window)
+{
+    return skv::decode_fp8_umma_smem_bytes(head_dim, batch, window != 0);
+}
 #endif  // SKV_TEST_HOOKS
