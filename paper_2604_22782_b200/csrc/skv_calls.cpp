@@ -4,8 +4,8 @@
 // microseconds on the GPU, and asking the same of the tensors from Python, then passing 15 to 20 arguments through ctypes, takes 7
 // to 9 on the host.
 // A function returns the entry point's status, or None where anything is not as the plain case has it (another type, shape
-// or device, a stream of the caller's, an integer out of range, a handle that is closed): binding.py then goes through
-// its own checks, which say what is wrong or make the call.
+// or device, a stream of the caller's, an integer out of range, a handle that is closed), or where asking throws (a tensor
+// without memory, no device): binding.py then goes through its own checks, which say what is wrong or make the call.
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <c10/cuda/CUDAFunctions.h>
@@ -91,14 +91,27 @@ struct Args {
     }
 };
 
-template <class Call>
-PyObject *status_of(Call call)
+// The entry point's status; its arguments are all evaluated before the interpreter is let go, since looking at a tensor may throw.
+template <class Entry, class... A>
+PyObject *status_of(Entry entry, A... args)
 {
     int rc;
     Py_BEGIN_ALLOW_THREADS
-    rc = call();
+    rc = entry(args...);
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(rc);
+}
+
+// A method as Python calls it: no C++ exception may pass through its frames.
+template <PyObject *(*F)(PyObject *, PyObject *const *, Py_ssize_t)>
+PyObject *declining(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    try {
+        return F(self, a, n);
+    } catch (...) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
 }
 
 template <class T>
@@ -116,10 +129,8 @@ PyObject *decode_attn_window(PyObject *, PyObject *const *a, Py_ssize_t n)
     const float scale = x.real();
     if (!x.end() || q->size(2) != head_dim || out->sizes() != q->sizes() || table->size(0) != q->size(0) || lens->size(0) != q->size(0)) Py_RETURN_NONE;
     const int batch = (int)q->size(0), heads = (int)q->size(1), width = (int)table->size(1);
-    return status_of([&] {
-        return decode_window_entry(x.cache, layer, ptr<void>(q), ptr<int32_t>(table), ptr<int32_t>(lens), ptr<void>(out), batch, heads, width, window,
-                                   sinks, scale, ptr<void>(work), (size_t)work->numel(), x.stream);
-    });
+    return status_of(decode_window_entry, x.cache, layer, ptr<void>(q), ptr<int32_t>(table), ptr<int32_t>(lens), ptr<void>(out), batch, heads, width, window,
+                     sinks, scale, ptr<void>(work), (size_t)work->numel(), x.stream);
 }
 
 // (cache, pool, head_dim, layer, Q, cu_q_lens, page_table, seq_lens, out, max_q_len, window, sinks, scale, stream)
@@ -135,10 +146,8 @@ PyObject *prefill_attn_window(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (!x.end() || q->size(2) != head_dim || out->sizes() != q->sizes() || table->size(0) != lens->size(0) || cu->size(0) != lens->size(0) + 1)
         Py_RETURN_NONE;
     const int batch = (int)lens->size(0), heads = (int)q->size(1), width = (int)table->size(1);
-    return status_of([&] {
-        return prefill_window_entry(x.cache, layer, ptr<void>(q), ptr<int32_t>(cu), ptr<int32_t>(table), ptr<int32_t>(lens), ptr<void>(out), batch, most,
-                                    heads, width, window, sinks, scale, x.stream);
-    });
+    return status_of(prefill_window_entry, x.cache, layer, ptr<void>(q), ptr<int32_t>(cu), ptr<int32_t>(table), ptr<int32_t>(lens), ptr<void>(out), batch, most,
+                     heads, width, window, sinks, scale, x.stream);
 }
 
 // rows [n][heads][dim] whose heads are dense and whose rows may be further apart; their distance in elements, or -1
@@ -174,11 +183,9 @@ PyObject *rope_append(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     const int64_t qs = row_stride(q, n, heads, head_dim), os = row_stride(q_out, n, heads, head_dim);
     const int64_t ks = owner ? row_stride(k, n, kv_heads, head_dim) : 0, vs = owner ? row_stride(v, n, kv_heads, head_dim) : 0;
     if (qs < 0 || os < 0 || ks < 0 || vs < 0 || (owner && slots->size(0) != n)) Py_RETURN_NONE;
-    return status_of([&] {
-        return rope_append_entry(x.cache, layer, rope, ptr<void>(q), qs, ptr<void>(q_out), os, owner ? ptr<void>(k) : nullptr, ks,
-                                 owner ? ptr<void>(v) : nullptr, vs, ptr<int32_t>(pos), axes > 1 ? pos->stride(0) : n,
-                                 owner ? ptr<int64_t>(slots) : nullptr, n, (int)heads, x.stream);
-    });
+    return status_of(rope_append_entry, x.cache, layer, rope, ptr<void>(q), qs, ptr<void>(q_out), os, owner ? ptr<void>(k) : nullptr, ks,
+                     owner ? ptr<void>(v) : nullptr, vs, ptr<int32_t>(pos), axes > 1 ? pos->stride(0) : n,
+                     owner ? ptr<int64_t>(slots) : nullptr, n, (int)heads, x.stream);
 }
 
 // (cache, pool, page_table, seq_lens, new_lens, free_pages, n_free, slot_map, cu_q_lens, seq_lens_out, n_free_out, positions, stream)
@@ -196,11 +203,9 @@ PyObject *plan_step(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (table->size(0) != batch || news->size(0) != batch || lens_out->size(0) != batch || cu->size(0) != batch + 1 || n_free->size(0) != 1 ||
         free_out->size(0) != 1 || (pos && pos->size(0) < slots->size(0)))
         Py_RETURN_NONE;
-    return status_of([&] {
-        return plan_step_entry(x.cache, ptr<int32_t>(table), (int)table->size(1), ptr<int32_t>(lens), ptr<int32_t>(news), (int)batch, ptr<int32_t>(pages),
-                               (int)pages->size(0), ptr<int32_t>(n_free), slots->size(0), ptr<int64_t>(slots), pos ? ptr<int32_t>(pos) : nullptr,
-                               ptr<int32_t>(cu), ptr<int32_t>(lens_out), ptr<int32_t>(free_out), x.stream);
-    });
+    return status_of(plan_step_entry, x.cache, ptr<int32_t>(table), (int)table->size(1), ptr<int32_t>(lens), ptr<int32_t>(news), (int)batch, ptr<int32_t>(pages),
+                     (int)pages->size(0), ptr<int32_t>(n_free), slots->size(0), ptr<int64_t>(slots), pos ? ptr<int32_t>(pos) : nullptr,
+                     ptr<int32_t>(cu), ptr<int32_t>(lens_out), ptr<int32_t>(free_out), x.stream);
 }
 
 // (cache, pool, page_table, first_page, end_page, free_pages, n_free, n_free_out, stream)
@@ -213,10 +218,8 @@ PyObject *plan_release(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (!x.end()) Py_RETURN_NONE;
     const int64_t batch = table->size(0);
     if (first->size(0) != batch || end->size(0) != batch || n_free->size(0) != 1 || free_out->size(0) != 1) Py_RETURN_NONE;
-    return status_of([&] {
-        return plan_release_entry(x.cache, ptr<int32_t>(table), (int)table->size(1), ptr<int32_t>(first), ptr<int32_t>(end), (int)batch,
-                                  ptr<int32_t>(pages), (int)pages->size(0), ptr<int32_t>(n_free), ptr<int32_t>(free_out), x.stream);
-    });
+    return status_of(plan_release_entry, x.cache, ptr<int32_t>(table), (int)table->size(1), ptr<int32_t>(first), ptr<int32_t>(end), (int)batch,
+                     ptr<int32_t>(pages), (int)pages->size(0), ptr<int32_t>(n_free), ptr<int32_t>(free_out), x.stream);
 }
 
 // connect(address, ...): the entry points of the loaded library, in the order of the declarations above
@@ -241,8 +244,9 @@ PyObject *connect(PyObject *, PyObject *const *a, Py_ssize_t n)
     Py_RETURN_NONE;
 }
 
-#define METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(f)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {METHOD(connect), METHOD(decode_attn_window), METHOD(prefill_attn_window), METHOD(rope_append), METHOD(plan_step),
+#define METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(declining<f>)), METH_FASTCALL, nullptr}
+PyMethodDef methods[] = {{"connect", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(connect)), METH_FASTCALL, nullptr},
+                         METHOD(decode_attn_window), METHOD(prefill_attn_window), METHOD(rope_append), METHOD(plan_step),
                          METHOD(plan_release), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
