@@ -8,6 +8,8 @@ import ctypes
 import functools
 import os
 import re
+import subprocess
+import warnings
 from typing import List, Optional, Sequence
 
 import torch
@@ -41,13 +43,25 @@ def _load() -> ctypes.CDLL:
 lib = _load()
 
 
+class _Declines:
+    """Stands in for the marshalling extension where there is none: every call is declined."""
+
+    def __getattr__(self, name):
+        return lambda *args: None
+
+
 def _load_calls():
-    if not os.path.exists(_build.CALLS):
-        try:
+    """The marshalling extension, which only saves time: without it every call goes through the ctypes form beside it."""
+    try:
+        if not os.path.exists(_build.CALLS):
             _build.build_calls()
-        except Exception as e:
-            raise ImportError(f"_calls.so is missing and could not be built: {e}") from e
-    from . import _calls
+        from . import _calls
+        if _calls.torch_version != torch.__version__:
+            raise ImportError(f"built for torch {_calls.torch_version}, this is {torch.__version__}")
+    except (ImportError, OSError, subprocess.SubprocessError) as e:
+        warnings.warn(f"_calls.so is not used: {e}.  The serving step's calls go through ctypes, which takes 4 to 6 us more for each; "
+                      f"python -m {__package__}.build --force builds it", RuntimeWarning, stacklevel=2)
+        return _Declines()
     _calls.connect(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
         lib.skv_is_owner, lib.skv_rope_append, lib.skv_plan_step, lib.skv_plan_release, lib.skv_decode_attn_window,
         lib.skv_prefill_attn_window)))

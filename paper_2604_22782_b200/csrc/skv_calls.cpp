@@ -252,4 +252,12 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nul
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__calls() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__calls()
+{
+    PyObject *m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "torch_version", SKV_TORCH_VERSION) != 0) {     // (whose headers say how a tensor lies in memory)
+        Py_DECREF(m);
+        return nullptr;
+    }
+    return m;
+}
