@@ -219,8 +219,8 @@ void skv_rope_destroy(skv_rope *rope);
  *   K, V       device bf16, rows of [kv_heads][head_dim], row strides in elements
  *              (a fused projection's rows can be given as they are); not changed
  *   positions  device int32 [n_axes][pos_stride], pos_stride >= n_tokens: the
- *              token's position on every axis.  Any value; the angle is exact to
- *              2^-31 of a turn at every one of them
+ *              token's position on every axis.  Any value; the angle is off by less
+ *              than 2^-25 of a turn (2e-7 rad) at every one of them
  *   slot_map   as in skv_append (negative: the token's K,V are not stored; its
  *              query is turned all the same).  No slot twice: what such a slot
  *              holds afterwards is unspecified

@@ -45,6 +45,10 @@ int skv_test_query_kernel(const void *q_in, const void *prev_out, void *q_out, l
  * (window 0) or with a sliding window.  Host only. */
 size_t skv_test_fp8_decode_smem_bytes(int head_dim, int batch, int window);
 
+/* A rotary frequency as skv_rope_create keeps it: the fraction of a turn per
+ * position, 2^64 = one turn.  Host only. */
+uint64_t skv_test_rope_phase(double inv_freq);
+
 #ifdef __cplusplus
 }
 #endif

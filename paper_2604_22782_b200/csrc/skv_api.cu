@@ -43,6 +43,34 @@ cudaError_t ensure_dynamic_smem_fn(const void *kernel, size_t smem)
 }
 }  // namespace skv
 
+namespace skv {
+// Exact but for its last rounding (Payne and Hanek's reduction): inv_freq = m 2^e with an integer m of 53 bits, times
+// 1 / 2 pi to 192 bits; of the product 2^e m / 2 pi the 64 bits below the point are kept, and whole turns fall off the
+// top.  (An extended-precision quotient is off by 2^-64 of the TURNS, which at 10^6 radians a position is 2^-16 of a
+// turn at the furthest position.)
+uint64_t rope_phase(double inv_freq)
+{
+    static const uint64_t inverse[3] = {0x36d8a5664f10e410ull, 0x7f09d5f47d4d3770ull, 0x28be60db9391054aull};      // lowest word first
+    int e = 0;
+    const uint64_t m = (uint64_t)ldexp(frexp(fabs(inv_freq), &e), 53);
+    uint64_t p[4];
+    unsigned __int128 carry = 0;
+    for (int i = 0; i < 3; ++i) {
+        carry += (unsigned __int128)m * inverse[i];
+        p[i] = (uint64_t)carry;
+        carry >>= 64;
+    }
+    p[3] = (uint64_t)carry;
+    // the product is p 2^(e - 53 - 192), and 2^64 of it p >> shift
+    const int shift = 181 - e, word = shift >> 6, off = shift & 63;            // (161 or more: e is 20 at most)
+    if (shift >= 256) return 0;                                                // (p has 245 bits: less than half)
+    uint64_t phase = p[word] >> off;
+    if (off && word < 3) phase |= p[word + 1] << (64 - off);
+    phase += p[(shift - 1) >> 6] >> ((shift - 1) & 63) & 1;
+    return inv_freq < 0 ? 0 - phase : phase;
+}
+}  // namespace skv
+
 struct skv_cache {
     int n_layers = 0, kv_heads = 0, head_dim = 0, page_size = 0, n_owners = 0;
     int64_t max_pages = 0;
@@ -917,11 +945,7 @@ int skv_rope_create(skv_rope **out, int rotary_dim, const double *inv_freq, cons
     r->n_axes = n_axes;
     r->adjacent = adjacent_pairs != 0;
     for (int i = 0; i < rotary_dim / 2; ++i) {
-        // turns per position; only the fraction matters.  An extended-precision quotient is off by under 2^-62 of a
-        // turn, by under 2^-31 at the furthest position.
-        const long double turns = (long double)inv_freq[i] / 6.283185307179586476925286766559L;
-        const long double part = turns - floorl(turns);
-        r->freq[i] = part >= 1.0L ? 0 : (uint64_t)(part * 18446744073709551616.0L);
+        r->freq[i] = rope_phase(inv_freq[i]);
         r->axis[i] = (uint8_t)(axis ? axis[i] : 0);
     }
     *out = r;

@@ -266,6 +266,7 @@ int prefill_window_max_batch();
 size_t prefill_window_smem_bytes(int D, int B);
 cudaError_t launch_prefill_window(const PrefillParams &p, int D, int G, int max_q_len, int sm_count, bool pdl, cudaStream_t s);
 // rotary embedding with the update (skv_rope.cu); adjacent: pairs (2i, 2i+1)
+uint64_t rope_phase(double inv_freq);        // host: 2^64 inv_freq / 2 pi mod 2^64, to the nearest integer; |inv_freq| < 2^20
 cudaError_t launch_rope_append(const RopeParams &p, int D, bool fp8, bool adjacent, bool pdl, cudaStream_t s);
 // a step's tables (skv_plan.cu); in_place: an output is the memory of an input
 int plan_max_batch();

@@ -3,9 +3,9 @@
 // Frequency i of a token turns the pair (x1, x2) of a row by  angle = position * inv_freq[i]:
 //     x1' = x1 cos - x2 sin,   x2' = x2 cos + x1 sin.
 // The angle is kept as a fraction of a turn in 64-bit fixed point: with F = 2^64 inv_freq / 2 pi (mod 2^64, from
-// the host) the product position * F mod 2^64 IS the angle modulo a full turn, for every 32-bit position, with an
-// error below 2^-32 of a turn.  (A product in fp32 is off by 0.03 rad at position 10^6.)  Only then does it become
-// a float, and cos / sin of it are taken with sincospi.  The rows are turned in fp32 and rounded once: to bf16, or
+// the host, off by half at most) the product position * F mod 2^64 IS the angle modulo a full turn, for every 32-bit
+// position, with an error of 2^-34 of a turn at most.  (A product in fp32 is off by 0.03 rad at position 10^6.)  Only then does it
+// become a float, between -1 and 1 half turns (2^-26 of a turn at most), and cos / sin of it are taken with sincospi.  The rows are turned in fp32 and rounded once: to bf16, or
 // on FP8 pages to the code of the row's own scale.
 //
 // Work split.  A lane owns a pair of 16-byte pieces of a row (a chunk of 8 elements and its partners), so a head

@@ -80,4 +80,9 @@ extern "C" size_t skv_test_fp8_decode_smem_bytes(int head_dim, int batch, int wi
 {
     return skv::decode_fp8_umma_smem_bytes(head_dim, batch, window != 0);
 }
+
+extern "C" uint64_t skv_test_rope_phase(double inv_freq)
+{
+    return skv::rope_phase(inv_freq);
+}
 #endif  // SKV_TEST_HOOKS
