@@ -49,6 +49,11 @@ size_t skv_test_fp8_decode_smem_bytes(int head_dim, int batch, int window);
  * position, 2^64 = one turn.  Host only. */
 uint64_t skv_test_rope_phase(double inv_freq);
 
+/* skv_plan_release: the place behind *n_free of the entry with `have` held ones
+ * before it in its warp's 32, of a warp that starts `before` pages on, or -1
+ * where the stack has room for `room` pages only.  Host only. */
+int64_t skv_test_release_place(int64_t before, int have, int room);
+
 #ifdef __cplusplus
 }
 #endif

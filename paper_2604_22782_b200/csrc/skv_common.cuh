@@ -230,6 +230,16 @@ struct ReleaseParams {
     int *status;
 };
 
+// Where a warp of skv_plan_release puts pages on the stack, counted from *n_free: it starts behind the `sum` pages of the
+// rows before its own, but no further than the stack's room, and so it goes on from 32 entries to the next; an entry's place is
+// as many further on as the warp's 32 hold before it, and there if below the room.  Unsigned: room + 32 need not fit 31 bits.
+__host__ __device__ __forceinline__ uint32_t release_start(int64_t sum, uint32_t room) { return sum < room ? (uint32_t)sum : room; }
+__host__ __device__ __forceinline__ uint32_t release_next(uint32_t start, int held, uint32_t room)
+{
+    const uint32_t k = start + (uint32_t)held;
+    return k < room ? k : room;
+}
+
 struct DecodeTuning {
     int variant;                // 0 auto, 1 CUDA-core (G=1), 2 tensor-core
     int warps;                  // per CTA

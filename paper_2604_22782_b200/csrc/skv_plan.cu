@@ -185,8 +185,8 @@ __global__ void __launch_bounds__(1024) plan_release_kernel(const __grid_constan
         int from, to, n = 0;
         range(rows[r], from, to);
         const int32_t *row = p.page_table + (int64_t)rows[r] * p.pt_stride;
-        for (int at = from; at < to; at += 32) {
-            const int32_t id = at + lane < to ? row[at + lane] : -1;
+        for (unsigned at = from; at < (unsigned)to; at += 32) {                // (unsigned: the last step may pass 31 bits)
+            const int32_t id = at + lane < (unsigned)to ? row[at + lane] : -1;
             bad |= id >= 0 && !holds(id);
             n += __popc(__ballot_sync(ALL, holds(id)));
         }
@@ -198,27 +198,27 @@ __global__ void __launch_bounds__(1024) plan_release_kernel(const __grid_constan
     int64_t sum = 0, zero = 0, total;
     for (int r = r0; r < r1; ++r) sum += count[r];
     block_scan2(sum, zero, total, tot, part);
+    const uint32_t room = (uint32_t)(p.free_capacity - n_free);
     for (int r = r0; r < r1; ++r) {
         const int n = count[r];
-        count[r] = sum > 0x7FFFFFFF ? 0x7FFFFFFF : (int)sum;
+        count[r] = (int)release_start(sum, room);
         sum += n;
     }
     __syncthreads();
-    const int room = p.free_capacity - n_free;
     for (int r = warp; r < n_rows; r += warps) {
-        int from, to, at_stack = count[r];
+        int from, to;
         range(rows[r], from, to);
+        uint32_t start = (uint32_t)count[r];
         int32_t *row = p.page_table + (int64_t)rows[r] * p.pt_stride;
-        for (int at = from; at < to; at += 32) {
-            const int32_t id = at + lane < to ? row[at + lane] : -1;
+        for (unsigned at = from; at < (unsigned)to; at += 32) {
+            const int32_t id = at + lane < (unsigned)to ? row[at + lane] : -1;
             const unsigned have = __ballot_sync(ALL, holds(id));
-            const int k = at_stack + __popc(have & ((1u << lane) - 1u));
+            const uint32_t k = release_next(start, __popc(have & ((1u << lane) - 1u)), room);
             if (holds(id) && k < room) {
-                p.free_pages[n_free + k] = id;
+                p.free_pages[n_free + (int)k] = id;
                 row[at + lane] = -1;
             }
-            at_stack += __popc(have);
-            if (at_stack >= room) at_stack = room;           // (full: nothing more is taken, and the sum cannot run over)
+            start = release_next(start, __popc(have), room);
         }
     }
     if (tid == 0) {

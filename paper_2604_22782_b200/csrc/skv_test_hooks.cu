@@ -85,4 +85,10 @@ extern "C" uint64_t skv_test_rope_phase(double inv_freq)
 {
     return skv::rope_phase(inv_freq);
 }
+
+extern "C" int64_t skv_test_release_place(int64_t before, int have, int room)
+{
+    const uint32_t k = skv::release_next(skv::release_start(before, (uint32_t)room), have, (uint32_t)room);
+    return k < (uint32_t)room ? (int64_t)k : -1;
+}
 #endif  // SKV_TEST_HOOKS
