@@ -260,7 +260,9 @@ int skv_rope_append(skv_cache *cache, int layer, const skv_rope *rope, const voi
  *                 (skv_prefill_attn's cu_q_lens)
  *   seq_lens_out  device int32 [batch]: lengths after the step; may be seq_lens
  *   n_free_out    device int32 [1]: pages left on the stack; may be n_free
- * Other buffers must not overlap.  One launch.  batch at most 16384
+ * Other buffers must not overlap.  It writes seq_lens and page_table, so an attention
+ * call with early fetch (skv_set_decode_early_fetch) must not follow it directly, nor
+ * behind nothing but skv_append.  One launch.  batch at most 16384
  * (SKV_ERR_UNSUPPORTED), max_tokens below 2^31.  Errors: SKV_ERR_ARG, SKV_ERR_CUDA. */
 int skv_plan_step(skv_cache *cache, int32_t *page_table, int pt_stride, const int32_t *seq_lens,
                   const int32_t *new_lens, int batch, const int32_t *free_pages, int free_capacity,
@@ -368,7 +370,8 @@ int skv_decode_attn_static(skv_cache *cache, int layer, const void *Q, const int
  * each once (n <= window + sinks: all of them, as skv_decode_attn).  window >= 1, sinks
  * >= 0.  Pages that hold no such token are not touched and their page-table entries
  * not read, so they may have been given back (skv_plan_release); other tokens of the
- * pages that are read contribute nothing, whatever they hold.
+ * pages that are read contribute nothing, whatever they hold.  NaN in a query or in an
+ * attended key makes the result NaN.
  * Other arguments, workspace, status and errors as skv_decode_attn.  One
  * launch: of a kernel of its own, in which a CTA or a cluster of CTAs owns a
  * (sequence, kv head) -- or, on FP8 pages at head_dim 128 with enough work, of the
@@ -432,7 +435,9 @@ int skv_prefill_attn_src(skv_cache *cache, int src_layer, const void *Q, const i
  * window >= 1 (a row always sees itself), sinks >= 0.  Pages that no row of a sequence
  * sees are not touched and their page-table entries not read.  A token that no row
  * of a sequence's call sees contributes nothing, whatever it holds; one that some rows
- * see should be finite, as its V may be multiplied by the zero weight of another row.
+ * see should be finite, as its V may be multiplied by the zero weight of another row (which
+ * is exactly zero: the largest finite V does not show there).  NaN in a query or in a key
+ * that a row sees makes the row's result NaN.
  * Other arguments, status and errors as skv_prefill_attn; skv_set_prefill_variant and
  * the FP8 scratch area apply.  The tcgen05 kernel takes any q_heads / kv_heads up to 8 at
  * head_dim 64 and 128, in one launch for every 1024 sequences (Q, out 16-byte aligned;

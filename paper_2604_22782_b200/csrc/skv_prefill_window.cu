@@ -19,8 +19,11 @@
 // of its block, and the outputs of tile 0 and 1.
 //
 // A tile's scores of block kb + 1 are issued before its softmax of block kb has finished, so the softmax warps find the next
-// scores ready.  (With blocks of 128 keys there is room for one buffer per tile: each block then waits for its own chain
-// softmax -> P V -> Q K^T, 6500 cycles of which the tensor core works 2100: 306 us where this takes 190.)  A warp per tile
+// scores ready.  (A first form had blocks of 128 keys and one buffer per tile: each block then waited for its own chain
+// softmax -> P V -> Q K^T, 6500 cycles of which the tensor core worked 2100, 306 us in all.  Blocks of 64 keys came together with
+// shorter waits, tensor copies of K and uniform issue, which would have served 128 keys as well, so the 190 us of today do not
+// tell the two apart; 128 keys have not been timed with the rest as it is now.  What 64 keys cost: an N = 64 instruction reads 6 KB
+// of operands for 32 cycles of work, which take 48 cycles at 128 bytes a cycle.)  A warp per tile
 // issues the instructions: one thread for both took 600 cycles of bookkeeping per tile and block and was slower than the tensor
 // core.  The tiles need not be in step -- a block that one tile does not see is skipped by that tile alone.  A ring stage
 // goes back to its copy warp when both tiles have done with it.
@@ -30,9 +33,11 @@
 // Few rows behind long windows (a chunk of a prompt, a drafted run of tokens) leave most SMs idle and each item a long chain of
 // blocks: there a cluster of CTAs shares an item's blocks and joins the outputs over distributed shared memory.
 // Measured: 2 prompts of 4096 tokens, 32 query / 8 kv heads, head_dim 128, window 2048: 190 us, 1.09 PFLOP/s of visible pairs (0.67 of
-// the measured bf16 peak; 222 us in a long loop, at the clock the power limit leaves); 8 chunks of 257 to 512 rows behind 3000 to
-// 6000 tokens, window 1024: 64 to 77 us.  The tensor pipe is busy 70 % of the cycles, the exponentials 50 %, issue slots
-// 48 %: what is left is the chain scores -> maximum -> probabilities -> store of two tiles that overlap in part.  Tried and slower:
+// the measured bf16 peak) alone, 222 us (0.93 PFLOP/s) in a long loop, at the clock the power limit leaves; 8 chunks of 257 to 512 rows behind 3000 to
+// 6000 tokens, window 1024: 64 to 77 us.  The tensor pipe has work in flight in 70 % of the cycles and computes in 55 %, the exponentials
+// take 50 %, issue slots 48 %: what is left is operand reads (above), the chain scores -> maximum -> probabilities -> store of two tiles
+// that overlap in part, and, in items of few blocks, an item's beginning (queries, first scores, a softmax taken twice), which nothing
+// overlaps: the queries' one buffer comes back with the last scores of the item before.  Tried and slower:
 // two threads to a row (199 us), the first maximum of an item before its exponentials (199), masks page by page (189).
 #include "skv_common.cuh"
 #include "skv_tcgen05.cuh"
