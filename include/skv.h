@@ -412,7 +412,9 @@ int skv_decode_merge(skv_cache *cache, void *out, int batch, int q_heads, void *
  *   max_q_len  host bound on q_len_b (sizes the grid; no host synchronisation)
  * One launch, no workspace: a CTA owns 64 or 128 query rows (that many /
  * (q_heads/kv_heads) tokens x the query heads of one kv head) and streams the
- * pages they see (skv_set_prefill_variant).
+ * pages they see (skv_set_prefill_variant).  On FP8 pages without a scratch area a
+ * CTA's rows share one reference for the V scales: a row is as exact as f16 while no
+ * V row of the tokens just behind it is some 2^10 times larger than its own.
  * Errors as skv_decode_attn; a sequence with q_len_b > seq_lens[b],
  * q_len_b > max_q_len or seq_lens[b] > pt_stride * page_size raises
  * SKV_ERR_BOUNDS in the device status and its rows are left untouched. */
