@@ -468,6 +468,111 @@ int skv_prefill_attn_window(skv_cache *cache, int layer, const void *Q, const in
 int skv_prefill_scratch_bytes(const skv_cache *cache, size_t *out_bytes);
 int skv_set_prefill_scratch(skv_cache *cache, void *device_scratch, size_t bytes);
 
+/* ---- attention over selected pages ------------------------------------------- */
+
+/* Long caches need not be read in full: an index holds bounds of every page's keys,
+ * a cheap score on it selects, for each query and kv head, the pages that can matter,
+ * and attention reads those.  In a layer of a step: skv_append or skv_rope_append,
+ * skv_index_pages, skv_select_pages, then skv_decode_attn_pages or
+ * skv_prefill_attn_pages.  Layers that read the same owner may share an owner's lists
+ * or select for themselves.
+ *
+ * Bytes of the index of all owner layers: per page and kv head 2 * head_dim + 4 (1/32
+ * of the bf16 K,V at head_dim 128), padded to 256 bytes twice per layer. */
+int skv_page_index_bytes(const skv_cache *cache, size_t *out_bytes);
+
+/* Gives the cache an index in device_memory (device, 256-byte aligned, bytes >=
+ * skv_page_index_bytes, the caller's, kept until another is given or NULL takes it
+ * back), zero-filled on `stream` by this call.  Errors: SKV_ERR_ARG, SKV_ERR_NOMEM,
+ * SKV_ERR_CUDA. */
+int skv_set_page_index(skv_cache *cache, void *device_memory, size_t bytes, void *stream);
+
+/* Indexes the pages of `layer` that a step's new tokens, whose K,V have been stored, have
+ * filled: of sequence b with n = seq_lens[b] tokens, the last
+ * a = cu_q_lens[b+1] - cu_q_lens[b] of them new, pages (n - a) / 16 <= p < n / 16.
+ * On a layer that is not an owner this is a no-op that launches nothing.  For page p and
+ * kv head h, from the 16 tokens' keys (FP8 pages: code value x scale, in fp32):
+ *   highest[d], lowest[d]  over the tokens,   amax = max |highest|, |lowest|,
+ *   scale = amax / 127,  codes = the nearest whole numbers to x * (127 / amax)
+ * (each step one fp32 operation; amax below 2^-100: scale 0, codes 0; a key that is not
+ * finite: scale +inf, codes 0, and the page is selected before all others).
+ * Last, partly filled pages are not indexed: skv_select_pages always lists them.
+ *   page_table  device int32 [batch][pt_stride]
+ *   seq_lens    device int32 [batch], including the new tokens
+ *   cu_q_lens   device int32 [batch+1] as in skv_prefill_attn (skv_plan_step's), or NULL:
+ *               one new token per sequence (max_q_len is not read)
+ *   max_q_len   host bound on the new tokens of a sequence
+ * A sequence whose a, n or page ids do not fit raises SKV_ERR_BOUNDS in the device
+ * status and is left out (of a bad page id, that page).  One launch.  Errors:
+ * SKV_ERR_ARG (also: no index), SKV_ERR_LAYER, SKV_ERR_UNSUPPORTED (more than 2^34
+ * pages of kv heads), SKV_ERR_CUDA. */
+int skv_index_pages(skv_cache *cache, int layer, const int32_t *page_table, const int32_t *seq_lens,
+                    const int32_t *cu_q_lens, int batch, int max_q_len, int pt_stride, void *stream);
+
+/* Entries that skv_select_pages writes at most: top + first_pages + last_pages +
+ * (run + 14) / 16.  Pure host. */
+int skv_page_list_width(int top, int first_pages, int last_pages, int run, int *out_width);
+
+/* Lists of pages to attend, one for each run of `run` rows of a sequence and each kv
+ * head.  Run r of sequence b has rows r * run to min((r + 1) * run, q_len_b) - 1, at
+ * positions p0 to p1; its list is number  b * ceil(max_q_len / run) + r.  It holds, in
+ * ascending order,
+ *   the pages below first_pages,
+ *   the pages above p0 / 16 - last_pages up to p1 / 16 (last_pages >= 1: every row sees
+ *   itself), and
+ *   of those between, the `top` with the highest score, of equal ones the lower.
+ * With  a = the largest |Q| element of the run's rows and the kv head's query heads,
+ * c = the nearest whole numbers to Q * (127 / a)  (a below 2^-100: 0; elements that
+ * are not finite count as 0),
+ *   dot(p) = max over rows, query heads of sum_d max(c_d, 0) highest_p,d + min(c_d, 0) lowest_p,d
+ *   score(p) = dot(p) * scale_p   (one fp32 product of a whole number below 2^24; scale
+ *   +inf: +inf),
+ * which is, up to the rounding to steps, the largest score that any key inside the page's bounds
+ * could give any of the rows.  The lists do not depend on how the work is cut: they
+ * repeat bit for bit.
+ *   Q          device bf16 [n_q][q_heads][head_dim], 16-byte aligned
+ *   cu_q_lens  as in skv_prefill_attn; NULL: one row per sequence, at seq_lens[b] - 1
+ *              (max_q_len and run must be 1; a length of 0 gives an empty list)
+ *   lists      device int32 [batch * ceil(max_q_len / run)][kv_heads][list_stride]: page
+ *              numbers within the sequence (not page ids), -1 behind the last
+ *   counts     device int32 [batch * ceil(max_q_len / run)][kv_heads]; 0 for a run that a
+ *              sequence has no rows for
+ *   list_stride  at least the smaller of skv_page_list_width and pt_stride
+ * min(run, max_q_len) * q_heads / kv_heads may be 128 at most, pt_stride 45056
+ * (SKV_ERR_UNSUPPORTED).  A sequence that does not fit raises SKV_ERR_BOUNDS and gets
+ * empty lists, or without cu_q_lens is cut to pt_stride pages; so does a page id out of
+ * range (the page is scored as page 0).  One launch.  Errors as skv_decode_attn, and
+ * SKV_ERR_ARG without an index. */
+int skv_select_pages(skv_cache *cache, int layer, const void *Q, const int32_t *cu_q_lens,
+                     const int32_t *page_table, const int32_t *seq_lens, int32_t *lists, int32_t *counts,
+                     int batch, int max_q_len, int q_heads, int pt_stride, int run, int top,
+                     int first_pages, int last_pages, int list_stride, void *stream);
+
+/* skv_decode_attn over the listed pages: row b, kv head h attends the tokens t < seq_lens[b]
+ * of the pages lists[b][h][0 .. counts[b][h]); other pages and their page-table entries
+ * are not read.  Lists may be the caller's own: any order, each page once (a page listed
+ * twice is attended twice).  An entry outside the sequence's pages raises
+ * SKV_ERR_BOUNDS and is left out; a count above list_stride is cut to it and raises
+ * SKV_ERR_BOUNDS; one of 0 or less gives an all-zero output row.
+ *   lists   device int32 [batch][kv_heads][list_stride],  counts device int32 [batch][kv_heads]
+ * Other arguments, status and errors as skv_decode_attn; no workspace.  One launch.
+ * NaN in a query or in an attended key makes the result NaN.  Results repeat bit for
+ * bit; skv_set_decode_variant picks the arithmetic on bf16 pages (on FP8 pages it is
+ * the mma.sync kernel's). */
+int skv_decode_attn_pages(skv_cache *cache, int layer, const void *Q, const int32_t *page_table,
+                          const int32_t *seq_lens, const int32_t *lists, const int32_t *counts, void *out,
+                          int batch, int q_heads, int pt_stride, int list_stride, float scale, void *stream);
+
+/* skv_prefill_attn over the listed pages: the row at position pos attends the tokens
+ * t <= pos of its run's pages (lists and counts as skv_select_pages writes them with the same
+ * run and max_q_len, or the caller's own under the rules above).  A row whose pages hold no
+ * such token gives zeros.  min(run, max_q_len) * q_heads / kv_heads may be 128 at most.
+ * Other arguments, status and errors as skv_prefill_attn; Q 16-byte, out 8-byte aligned. */
+int skv_prefill_attn_pages(skv_cache *cache, int layer, const void *Q, const int32_t *cu_q_lens,
+                           const int32_t *page_table, const int32_t *seq_lens, const int32_t *lists,
+                           const int32_t *counts, void *out, int batch, int max_q_len, int q_heads,
+                           int pt_stride, int run, int list_stride, float scale, void *stream);
+
 /* One whole decode step of Algorithm 2 with inputs already on the device:
  * for l = 0..L-1: append (owners only) then decode attention, on `stream`.
  * Because every input of the step exists when it starts, and the update of

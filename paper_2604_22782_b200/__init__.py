@@ -10,11 +10,11 @@ does, may be missing: a warning says so.)
 from .binding import (  # noqa: F401
     SkvError, SkvCache, SkvRope, lib, lib_path, exported_symbols,
     skv_routing_from_owners, skv_routing_groups, skv_routing_rcla, skv_routing_rdcla, skv_cache_pool_bytes,
-    skv_strerror,
+    skv_page_list_width, skv_strerror,
 )
 
 __all__ = [
     "SkvError", "SkvCache", "SkvRope", "lib", "lib_path", "exported_symbols",
     "skv_routing_from_owners", "skv_routing_groups", "skv_routing_rcla", "skv_routing_rdcla",
-    "skv_cache_pool_bytes", "skv_strerror",
+    "skv_cache_pool_bytes", "skv_page_list_width", "skv_strerror",
 ]

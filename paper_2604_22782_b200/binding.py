@@ -58,6 +58,8 @@ def _load_calls():
         from . import _calls
         if _calls.torch_version != torch.__version__:
             raise ImportError(f"built for torch {_calls.torch_version}, this is {torch.__version__}")
+        if not hasattr(_calls, "connect_pages"):
+            raise ImportError("built from an earlier version of its source")
     except (ImportError, OSError, subprocess.SubprocessError) as e:
         warnings.warn(f"_calls.so is not used: {e}.  The serving step's calls go through ctypes, which takes 4 to 6 us more for each; "
                       f"python -m {__package__}.build --force builds it", RuntimeWarning, stacklevel=2)
@@ -65,6 +67,8 @@ def _load_calls():
     _calls.connect(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
         lib.skv_is_owner, lib.skv_rope_append, lib.skv_plan_step, lib.skv_plan_release, lib.skv_decode_attn_window,
         lib.skv_prefill_attn_window)))
+    _calls.connect_pages(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        lib.skv_index_pages, lib.skv_select_pages, lib.skv_decode_attn_pages, lib.skv_prefill_attn_pages)))
     return _calls
 
 
@@ -105,6 +109,13 @@ lib.skv_plan_step.argtypes = [_vp, _i32p, _int, _i32p, _i32p, _int, _i32p, _int,
 lib.skv_plan_release.argtypes = [_vp, _i32p, _int, _i32p, _i32p, _int, _i32p, _int, _i32p, _i32p, _vp]
 lib.skv_decode_attn_window.argtypes = [_vp, _int, _vp, _i32p, _i32p, _vp, _int, _int, _int, _int, _int, _f32, _vp, _sz, _vp]
 lib.skv_prefill_attn_window.argtypes = [_vp, _int, _vp, _i32p, _i32p, _i32p, _vp, _int, _int, _int, _int, _int, _int, _f32, _vp]
+lib.skv_page_index_bytes.argtypes = [_vp, _szp]
+lib.skv_set_page_index.argtypes = [_vp, _vp, _sz, _vp]
+lib.skv_index_pages.argtypes = [_vp, _int, _i32p, _i32p, _i32p, _int, _int, _int, _vp]
+lib.skv_page_list_width.argtypes = [_int, _int, _int, _int, ctypes.POINTER(_int)]
+lib.skv_select_pages.argtypes = [_vp, _int, _vp, _i32p, _i32p, _i32p, _i32p, _i32p] + [_int] * 9 + [_vp]
+lib.skv_decode_attn_pages.argtypes = [_vp, _int, _vp, _i32p, _i32p, _i32p, _i32p, _vp] + [_int] * 4 + [_f32, _vp]
+lib.skv_prefill_attn_pages.argtypes = [_vp, _int, _vp, _i32p, _i32p, _i32p, _i32p, _i32p, _vp] + [_int] * 6 + [_f32, _vp]
 lib.skv_decode_splitk.argtypes = [_vp, _int, _vp, _i32p, _i32p, _int, _int, _int, _f32, _vp, _sz, _vp]
 lib.skv_decode_merge.argtypes = [_vp, _vp, _int, _int, _vp, _sz, _vp]
 lib.skv_decode_step.argtypes = [_vp, _vp, _vp, _vp, _i64p, _i32p, _i32p, _vp, _int, _int, _int, _f32, _vp, _sz, _vp]
@@ -198,6 +209,14 @@ def skv_cache_pool_bytes_fp8(r: Sequence[int], kv_heads: int, head_dim: int, pag
     out = _sz(0)
     _check(lib.skv_cache_pool_bytes_fp8(len(r), _i32_array(r), kv_heads, head_dim, page_size, max_pages,
                                         ctypes.byref(out)), "skv_cache_pool_bytes_fp8")
+    return out.value
+
+
+def skv_page_list_width(top: int, first_pages: int, last_pages: int, run: int = 1) -> int:
+    """Entries of a list that ``skv_select_pages`` writes at most."""
+    out = _int(0)
+    _check(lib.skv_page_list_width(_i32("top", top), _i32("first_pages", first_pages), _i32("last_pages", last_pages), _i32("run", run),
+                                   ctypes.byref(out)), "skv_page_list_width")
     return out.value
 
 
@@ -680,6 +699,112 @@ class SkvCache:
                                       _ptr(h_seq_lens), _ptr(h_out), batch, q_heads, h_page_table.shape[1], scale,
                                       _ptr(staging), _nbytes(staging), _stream_ptr(stream))
         _check(rc, "skv_decode_step_host")
+
+    # -- attention over selected pages
+    def skv_page_index_bytes(self) -> int:
+        out = _sz(0)
+        _check(lib.skv_page_index_bytes(self._h, ctypes.byref(out)), "skv_page_index_bytes")
+        return out.value
+
+    def skv_set_page_index(self, memory: Optional[torch.Tensor], stream=None) -> None:
+        """Give (or, with None, take back) the memory of the page index, uint8; it is zero-filled, and has to stay alive
+        while it is set."""
+        _arg("memory", memory, torch.uint8)
+        if memory is not None and memory.get_device() != self._current_device():
+            raise ValueError(f"memory: is on {memory.device}, the cache is elsewhere")
+        _check(lib.skv_set_page_index(self._h, _ptr(memory), 0 if memory is None else _nbytes(memory), _stream_ptr(stream)),
+               "skv_set_page_index")
+        self._page_index = memory
+
+    def skv_index_pages(self, layer: int, page_table: torch.Tensor, seq_lens: torch.Tensor, cu_q_lens: Optional[torch.Tensor] = None,
+                        max_q_len: int = 1, stream=None) -> None:
+        """page_table [batch][width], seq_lens [batch], cu_q_lens [batch+1] (None: one new token per sequence): int32."""
+        rc = _calls.index_pages(self._handle, self.pool, layer, page_table, seq_lens, cu_q_lens, max_q_len, stream)
+        if rc is not None:
+            return _check(rc, "skv_index_pages") if rc else None
+        device = self._current_device()
+        batch, table, width, lens, cu = self._page_args(page_table, seq_lens, cu_q_lens, device)
+        rc = lib.skv_index_pages(self._h, _i32("layer", layer), table, lens, cu, batch, _i32("max_q_len", max_q_len), width, _stream_ptr(stream))
+        if rc:
+            _check(rc, "skv_index_pages")
+
+    def skv_select_pages(self, layer: int, Q: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor, lists: torch.Tensor,
+                         counts: torch.Tensor, top: int, first_pages: int = 1, last_pages: int = 1,
+                         cu_q_lens: Optional[torch.Tensor] = None, max_q_len: int = 1, run: int = 1, stream=None) -> None:
+        """Q [n_q][q_heads][head_dim]; lists [batch * ceil(max_q_len / run)][kv_heads][width] and counts [...][kv_heads] int32
+        are written; without cu_q_lens one row per sequence."""
+        rc = _calls.select_pages(self._handle, self.pool, self.head_dim, self.kv_heads, layer, Q, cu_q_lens, page_table, seq_lens, lists, counts,
+                                 max_q_len, run, top, first_pages, last_pages, stream)
+        if rc is not None:
+            return _check(rc, "skv_select_pages") if rc else None
+        device = self._current_device()
+        batch, table, width, lens, cu = self._page_args(page_table, seq_lens, cu_q_lens, device)
+        heads, q = self._query_rows(Q, batch if cu is None else None, device)
+        ls, ct, entries = self._list_args(lists, counts, batch, _i32("max_q_len", max_q_len), _i32("run", run), device)
+        rc = lib.skv_select_pages(self._h, _i32("layer", layer), q, cu, table, lens, ls, ct, batch, max_q_len, heads, width, run, _i32("top", top),
+                                  _i32("first_pages", first_pages), _i32("last_pages", last_pages), entries, _stream_ptr(stream))
+        if rc:
+            _check(rc, "skv_select_pages")
+
+    def skv_decode_attn_pages(self, layer: int, Q: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor, lists: torch.Tensor,
+                              counts: torch.Tensor, out: torch.Tensor, scale: float = 0.0, stream=None) -> None:
+        """lists [batch][kv_heads][width], counts [batch][kv_heads]: int32, as skv_select_pages writes them."""
+        rc = _calls.decode_attn_pages(self._handle, self.pool, self.head_dim, self.kv_heads, layer, Q, page_table, seq_lens, lists, counts, out,
+                                      scale, stream)
+        if rc is not None:
+            return _check(rc, "skv_decode_attn_pages") if rc else None
+        device = self._current_device()
+        batch, table, width, lens, _ = self._page_args(page_table, seq_lens, None, device)
+        heads, q = self._query_rows(Q, batch, device)
+        ls, ct, entries = self._list_args(lists, counts, batch, 1, 1, device)
+        rc = lib.skv_decode_attn_pages(self._h, _i32("layer", layer), q, table, lens, ls, ct, _checked("out", out, torch.bfloat16, Q.shape, device),
+                                       batch, heads, width, entries, scale, _stream_ptr(stream))
+        if rc:
+            _check(rc, "skv_decode_attn_pages")
+
+    def skv_prefill_attn_pages(self, layer: int, Q: torch.Tensor, cu_q_lens: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor,
+                               lists: torch.Tensor, counts: torch.Tensor, out: torch.Tensor, max_q_len: int, run: int = 1, scale: float = 0.0,
+                               stream=None) -> None:
+        rc = _calls.prefill_attn_pages(self._handle, self.pool, self.head_dim, self.kv_heads, layer, Q, cu_q_lens, page_table, seq_lens, lists,
+                                       counts, out, max_q_len, run, scale, stream)
+        if rc is not None:
+            return _check(rc, "skv_prefill_attn_pages") if rc else None
+        device = self._current_device()
+        batch, table, width, lens, cu = self._page_args(page_table, seq_lens, cu_q_lens, device)
+        heads, q = self._query_rows(Q, None, device)
+        ls, ct, entries = self._list_args(lists, counts, batch, _i32("max_q_len", max_q_len), _i32("run", run), device)
+        rc = lib.skv_prefill_attn_pages(self._h, _i32("layer", layer), q, cu, table, lens, ls, ct,
+                                        _checked("out", out, torch.bfloat16, Q.shape, device), batch, max_q_len, heads, width, run, entries, scale,
+                                        _stream_ptr(stream))
+        if rc:
+            _check(rc, "skv_prefill_attn_pages")
+
+    def _page_args(self, page_table, seq_lens, cu_q_lens, device):
+        """Batch, table pointer and width, pointers of the lengths and of the row offsets (None where there are none)."""
+        i32 = torch.int32
+        if seq_lens.dim() != 1:
+            raise ValueError("seq_lens: expected [batch]")
+        batch = seq_lens.shape[0]
+        if page_table.dim() != 2 or page_table.shape[0] != batch:
+            raise ValueError(f"page_table: expected [{batch}][width], got {tuple(page_table.shape)}")
+        width = page_table.shape[1]
+        return (batch, _checked("page_table", page_table, i32, (batch, width), device), width, _checked("seq_lens", seq_lens, i32, (batch,), device),
+                None if cu_q_lens is None else _checked("cu_q_lens", cu_q_lens, i32, (batch + 1,), device))
+
+    def _query_rows(self, Q, rows, device):
+        if Q.dim() != 3 or Q.shape[2] != self.head_dim or (rows is not None and Q.shape[0] != rows):
+            raise ValueError(f"Q: expected [{'n_q' if rows is None else rows}][q_heads][{self.head_dim}], got {tuple(Q.shape)}")
+        return Q.shape[1], _checked("Q", Q, torch.bfloat16, Q.shape, device)
+
+    def _list_args(self, lists, counts, batch, max_q_len, run, device):
+        """Pointers of the lists and counts, entries of a list."""
+        if max_q_len < 1 or run < 1:
+            raise ValueError("max_q_len and run: at least 1")
+        n = batch * -(-max_q_len // run)
+        if lists.dim() != 3 or lists.shape[:2] != (n, self.kv_heads):
+            raise ValueError(f"lists: expected [{n}][{self.kv_heads}][width], got {tuple(lists.shape)}")
+        return (_checked("lists", lists, torch.int32, lists.shape, device), _checked("counts", counts, torch.int32, (n, self.kv_heads), device),
+                lists.shape[2])
 
     # -- status, tuning, counters
     def skv_get_status(self, stream=None) -> int:

@@ -2,6 +2,7 @@
 // owner-only page allocator's bookkeeping, and kernel launches.  Host code only.
 #include "../../include/skv.h"
 #include "skv_common.cuh"
+#include "skv_page_index.cuh"
 
 #include <math.h>
 #include <new>
@@ -19,7 +20,7 @@ namespace skv {
 cudaError_t ensure_dynamic_smem_fn(const void *kernel, size_t smem)
 {
     struct Granted { const void *kernel; int dev; int smem; };
-    static Granted table[128];
+    static Granted table[256];
     static int used = 0;
     static std::mutex lock;
     int dev = 0;
@@ -32,7 +33,7 @@ cudaError_t ensure_dynamic_smem_fn(const void *kernel, size_t smem)
     if (g && (int)smem <= g->smem) return cudaSuccess;
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    if (!g && used < 128) {
+    if (!g && used < 256) {
         g = &table[used++];
         g->kernel = kernel;
         g->dev = dev;
@@ -88,6 +89,7 @@ struct skv_cache {
     int prefill_variant = 0;         // 0 auto (tcgen05 where supported), 1 mma.sync kernel, 2 tcgen05 kernel
     uint8_t *prefill_scratch = nullptr;   // FP8 cache: room for one owner layer's pages as bf16 (caller's device memory)
     size_t prefill_scratch_bytes = 0;
+    uint8_t *page_index = nullptr;   // skv_set_page_index: the caller's device memory, index_layer_bytes per owner
     bool shape_is_default = true;    // until skv_set_decode_tuning is called: the CUDA-core kernel runs as 1 x 2 x 8
     int l2_keep_pct = 35;            // > 0: consecutive layers that read one owner walk it in opposite directions
     bool early_fetch = false;        // stand-alone attention calls fill their rings before waiting for the kernel before them
@@ -1257,7 +1259,201 @@ int prefill_over(skv_cache *c, int src, const void *Q, const int32_t *cu_q_lens,
 }
 }  // namespace
 
+// ---- attention over selected pages ------------------------------------------------
+
+namespace {
+// Rows of a sequence's lists, and what all three calls on lists ask of them.
+int check_runs(int batch, int max_q_len, int run, int G, int *per_seq)
+{
+    if (max_q_len <= 0 || run <= 0) return SKV_ERR_ARG;
+    if ((int64_t)(run < max_q_len ? run : max_q_len) * G > 128) return SKV_ERR_UNSUPPORTED;
+    const int64_t per = ((int64_t)max_q_len + run - 1) / run;
+    if (per * batch > 0x7FFFFFFF || (int64_t)batch * max_q_len > 0x7FFFFFFF) return SKV_ERR_UNSUPPORTED;
+    *per_seq = (int)per;
+    return SKV_OK;
+}
+
+void index_of(const skv_cache *c, int owner, int8_t *&codes, float *&scales)
+{
+    uint8_t *base = c->page_index + (size_t)c->slot[(size_t)owner] * (size_t)index_layer_bytes(c->max_pages, c->kv_heads, c->head_dim);
+    codes = reinterpret_cast<int8_t *>(base);
+    scales = reinterpret_cast<float *>(base + index_codes_bytes(c->max_pages, c->kv_heads, c->head_dim));
+}
+
+// A row at a time through the decode kernel: cu_q_lens null, a row per sequence
+int pages_by_rows(skv_cache *c, int src, const void *Q, const int32_t *cu_q_lens, const int32_t *page_table, const int32_t *seq_lens,
+                  const PageLists &lists, void *out, int batch, int max_q_len, int q_heads, int pt_stride, float scale, bool keep, void *stream)
+{
+    const int G = q_heads / c->kv_heads;
+    DecodeParams d;
+    memset(&d, 0, sizeof(d));
+    d.layer_base = c->layer_base(c->slot[(size_t)src]);
+    d.page_stride = (int64_t)c->page_bytes;
+    d.max_pages = c->max_pages;
+    d.Q = static_cast<const uint16_t *>(Q);
+    d.page_table = page_table;
+    d.seq_lens = seq_lens;
+    d.out = static_cast<uint16_t *>(out);
+    d.B = batch * max_q_len;
+    d.Hq = q_heads;
+    d.Hkv = c->kv_heads;
+    d.pt_stride = pt_stride;
+    d.scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)c->head_dim)) * 1.4426950408889634f;
+    d.cu_q = cu_q_lens;
+    d.max_q_len = max_q_len;
+    d.keep_pct = keep;
+    d.status = c->status_word();
+    const int kernel = c->fp8 ? 2 : c->tune.variant == 2 || (c->tune.variant == 0 && G > 1) ? 1 : 0;
+    if (launch_decode_pages(d, lists, c->head_dim, G, kernel, c->sm_count, c->tune.pdl != 0, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return SKV_ERR_CUDA;
+    }
+    c->launches += 1;
+    return SKV_OK;
+}
+}  // namespace
+
 extern "C" {
+
+int skv_page_index_bytes(const skv_cache *c, size_t *out_bytes)
+{
+    if (!c || !out_bytes) return SKV_ERR_ARG;
+    *out_bytes = (size_t)c->n_owners * (size_t)index_layer_bytes(c->max_pages, c->kv_heads, c->head_dim);
+    return SKV_OK;
+}
+
+int skv_set_page_index(skv_cache *c, void *device_memory, size_t bytes, void *stream)
+{
+    if (!c) return SKV_ERR_ARG;
+    if (device_memory) {
+        if (!c->pool || !aligned(device_memory, 256)) return SKV_ERR_ARG;
+        size_t need = 0;
+        skv_page_index_bytes(c, &need);
+        if (bytes < need) return SKV_ERR_NOMEM;
+        if (cudaMemsetAsync(device_memory, 0, need, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return SKV_ERR_CUDA;
+        }
+    }
+    c->page_index = static_cast<uint8_t *>(device_memory);
+    return SKV_OK;
+}
+
+int skv_index_pages(skv_cache *c, int layer, const int32_t *page_table, const int32_t *seq_lens, const int32_t *cu_q_lens, int batch,
+                    int max_q_len, int pt_stride, void *stream)
+{
+    if (!c || !c->pool) return SKV_ERR_ARG;
+    if (layer < 0 || layer >= c->n_layers) return SKV_ERR_LAYER;
+    if (c->slot[(size_t)layer] < 0) return SKV_OK;               // a layer that keeps no K,V has no index of its own
+    if (!c->page_index || !page_table || !seq_lens || batch <= 0 || max_q_len <= 0 || pt_stride <= 0) return SKV_ERR_ARG;
+    IndexParams p;
+    p.layer_base = c->layer_base(c->slot[(size_t)layer]);
+    p.page_stride = (int64_t)c->page_bytes;
+    p.max_pages = c->max_pages;
+    p.page_table = page_table;
+    p.seq_lens = seq_lens;
+    p.cu_q = cu_q_lens;
+    p.B = batch;
+    p.Hkv = c->kv_heads;
+    p.pt_stride = pt_stride;
+    p.max_q_len = cu_q_lens ? max_q_len : 1;
+    p.max_new_pages = (p.max_q_len - 1) / PAGE + 1;
+    if (p.max_new_pages > pt_stride) p.max_new_pages = pt_stride;
+    if ((int64_t)batch * p.max_new_pages * c->kv_heads > 0x7FFFFFFFll * 8) return SKV_ERR_UNSUPPORTED;       // grid limit
+    index_of(c, layer, p.codes, p.scales);
+    p.status = c->status_word();
+    if (launch_index_pages(p, c->head_dim, c->fp8, c->tune.pdl != 0, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return SKV_ERR_CUDA;
+    }
+    c->launches += 1;
+    return SKV_OK;
+}
+
+int skv_page_list_width(int top, int first_pages, int last_pages, int run, int *out_width)
+{
+    if (!out_width || top < 0 || first_pages < 0 || last_pages < 1 || run < 1) return SKV_ERR_ARG;
+    const int64_t w = (int64_t)top + first_pages + last_pages + ((int64_t)run + 14) / PAGE;
+    *out_width = w < 0x7FFFFFFF ? (int)w : 0x7FFFFFFF;
+    return SKV_OK;
+}
+
+int skv_select_pages(skv_cache *c, int layer, const void *Q, const int32_t *cu_q_lens, const int32_t *page_table, const int32_t *seq_lens,
+                     int32_t *lists, int32_t *counts, int batch, int max_q_len, int q_heads, int pt_stride, int run, int top,
+                     int first_pages, int last_pages, int list_stride, void *stream)
+{
+    const int rc = check_decode_args(c, layer, batch, q_heads);
+    if (rc) return rc;
+    if (!c->page_index || !Q || !page_table || !seq_lens || !lists || !counts || pt_stride <= 0 || !aligned(Q, 16)) return SKV_ERR_ARG;
+    if (!cu_q_lens && (max_q_len != 1 || run != 1)) return SKV_ERR_ARG;
+    int width = 0, per_seq = 0;
+    if (skv_page_list_width(top, first_pages, last_pages, run, &width)) return SKV_ERR_ARG;
+    if (list_stride < (width < pt_stride ? width : pt_stride)) return SKV_ERR_ARG;
+    const int rr = check_runs(batch, max_q_len, run, q_heads / c->kv_heads, &per_seq);
+    if (rr) return rr;
+    if (pt_stride > select_max_pages()) return SKV_ERR_UNSUPPORTED;
+    SelectParams p;
+    int8_t *codes;
+    float *scales;
+    index_of(c, c->r[(size_t)layer], codes, scales);
+    p.codes = codes;
+    p.scales = scales;
+    p.max_pages = c->max_pages;
+    p.Q = static_cast<const uint16_t *>(Q);
+    p.page_table = page_table;
+    p.seq_lens = seq_lens;
+    p.cu_q = cu_q_lens;
+    p.lists = lists;
+    p.counts = counts;
+    p.B = batch;
+    p.Hq = q_heads;
+    p.Hkv = c->kv_heads;
+    p.pt_stride = pt_stride;
+    p.max_q_len = max_q_len;
+    p.run = run;
+    p.per_seq = per_seq;
+    p.top = top;
+    p.first = first_pages;
+    p.last = last_pages;
+    p.stride = list_stride;
+    p.most = pt_stride;
+    p.status = c->status_word();
+    if (launch_select_pages(p, c->head_dim, c->sm_count, c->tune.pdl != 0, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return SKV_ERR_CUDA;
+    }
+    c->launches += 1;
+    return SKV_OK;
+}
+
+int skv_decode_attn_pages(skv_cache *c, int layer, const void *Q, const int32_t *page_table, const int32_t *seq_lens, const int32_t *lists,
+                          const int32_t *counts, void *out, int batch, int q_heads, int pt_stride, int list_stride, float scale, void *stream)
+{
+    const int rc = check_decode_args(c, layer, batch, q_heads);
+    if (rc) return rc;
+    if (!Q || !page_table || !seq_lens || !lists || !counts || !out || pt_stride <= 0 || list_stride <= 0) return SKV_ERR_ARG;
+    if (!aligned(Q, 16) || !aligned(out, 8)) return SKV_ERR_ARG;
+    const PageLists l = {lists, counts, list_stride, 1, 1};
+    // as over a window: a call whose pages fit in a third of L2 leaves them there for the next layer if that reads them too
+    const int64_t width = list_stride < pt_stride ? list_stride : pt_stride;
+    const bool keep = c->l2_keep_pct > 0 && c->walk_keep[(size_t)layer] && width * batch * (int64_t)c->page_bytes <= (int64_t)(c->l2_bytes / 3);
+    return pages_by_rows(c, c->r[(size_t)layer], Q, nullptr, page_table, seq_lens, l, out, batch, 1, q_heads, pt_stride, scale, keep, stream);
+}
+
+int skv_prefill_attn_pages(skv_cache *c, int layer, const void *Q, const int32_t *cu_q_lens, const int32_t *page_table, const int32_t *seq_lens,
+                           const int32_t *lists, const int32_t *counts, void *out, int batch, int max_q_len, int q_heads, int pt_stride,
+                           int run, int list_stride, float scale, void *stream)
+{
+    const int rc = check_decode_args(c, layer, batch, q_heads);
+    if (rc) return rc;
+    if (!Q || !cu_q_lens || !page_table || !seq_lens || !lists || !counts || !out || pt_stride <= 0 || list_stride <= 0) return SKV_ERR_ARG;
+    if (!aligned(Q, 16) || !aligned(out, 8)) return SKV_ERR_ARG;
+    int per_seq = 0;
+    const int rr = check_runs(batch, max_q_len, run, q_heads / c->kv_heads, &per_seq);
+    if (rr) return rr;
+    const PageLists l = {lists, counts, list_stride, run, per_seq};
+    return pages_by_rows(c, c->r[(size_t)layer], Q, cu_q_lens, page_table, seq_lens, l, out, batch, max_q_len, q_heads, pt_stride, scale, true, stream);
+}
 
 // ---- whole decode step from host buffers -------------------------------------
 namespace {

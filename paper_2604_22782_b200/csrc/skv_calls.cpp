@@ -1,5 +1,6 @@
 // Argument marshalling of the serving step's entry points (skv_rope_append, skv_plan_step, skv_plan_release,
-// skv_decode_attn_window, skv_prefill_attn_window) as a CPython extension: reads the tensors' types, shapes, devices and
+// skv_decode_attn_window, skv_prefill_attn_window, skv_index_pages, skv_select_pages, skv_decode_attn_pages,
+// skv_prefill_attn_pages) as a CPython extension: reads the tensors' types, shapes, devices and
 // pointers directly and calls the C entry point, whose address binding.py hands over.  These calls run for a few
 // microseconds on the GPU, and asking the same of the tensors from Python, then passing 15 to 20 arguments through ctypes, takes 7
 // to 9 on the host.
@@ -21,6 +22,10 @@ decltype(&skv_plan_step) plan_step_entry;
 decltype(&skv_plan_release) plan_release_entry;
 decltype(&skv_decode_attn_window) decode_window_entry;
 decltype(&skv_prefill_attn_window) prefill_window_entry;
+decltype(&skv_index_pages) index_pages_entry;
+decltype(&skv_select_pages) select_pages_entry;
+decltype(&skv_decode_attn_pages) decode_pages_entry;
+decltype(&skv_prefill_attn_pages) prefill_pages_entry;
 
 // The arguments of one call, in order; `ok` turns false at the first that is not plain.
 struct Args {
@@ -84,6 +89,10 @@ struct Args {
         device = THPVariable_Unpack(pool).get_device();
         if (device < 0 || device != c10::cuda::current_device()) ok = false;
         else stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream();
+    }
+    const at::Tensor *dense_or_none(at::ScalarType type, int dims)
+    {
+        return i < n && a[i] == Py_None ? (++i, nullptr) : dense(type, dims);
     }
     bool end()                         // the last argument: the caller's stream
     {
@@ -222,19 +231,100 @@ PyObject *plan_release(PyObject *, PyObject *const *a, Py_ssize_t n)
                      ptr<int32_t>(pages), (int)pages->size(0), ptr<int32_t>(n_free), ptr<int32_t>(free_out), x.stream);
 }
 
-// connect(address, ...): the entry points of the loaded library, in the order of the declarations above
+// lists [batch * ceil(most / run)][heads][entries] and counts [...][heads]
+bool lists_fit(const at::Tensor *lists, const at::Tensor *counts, int64_t batch, int most, int run, int heads)
+{
+    if (most < 1 || run < 1) return false;
+    const int64_t n = batch * (((int64_t)most + run - 1) / run);
+    return lists->size(0) == n && lists->size(1) == heads && counts->size(0) == n && counts->size(1) == heads;
+}
+
+// (cache, pool, layer, page_table, seq_lens, cu_q_lens, max_q_len, stream)
+PyObject *index_pages(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Args x{a, n};
+    x.begin();
+    const int layer = x.integer();
+    const at::Tensor *table = x.dense(at::kInt, 2), *lens = x.dense(at::kInt, 1), *cu = x.dense_or_none(at::kInt, 1);
+    const int most = x.integer();
+    if (!x.end() || table->size(0) != lens->size(0) || (cu && cu->size(0) != lens->size(0) + 1)) Py_RETURN_NONE;
+    return status_of(index_pages_entry, x.cache, layer, ptr<int32_t>(table), ptr<int32_t>(lens), cu ? ptr<int32_t>(cu) : nullptr, (int)lens->size(0), most,
+                     (int)table->size(1), x.stream);
+}
+
+// (cache, pool, head_dim, kv_heads, layer, Q, cu_q_lens, page_table, seq_lens, lists, counts, max_q_len, run, top, first, last, stream)
+PyObject *select_pages(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Args x{a, n};
+    x.begin();
+    const int head_dim = x.integer(), kv_heads = x.integer(), layer = x.integer();
+    const at::Tensor *q = x.dense(at::kBFloat16, 3), *cu = x.dense_or_none(at::kInt, 1), *table = x.dense(at::kInt, 2), *lens = x.dense(at::kInt, 1),
+                     *lists = x.dense(at::kInt, 3), *counts = x.dense(at::kInt, 2);
+    const int most = x.integer(), run = x.integer(), top = x.integer(), first = x.integer(), last = x.integer();
+    if (!x.end()) Py_RETURN_NONE;
+    const int64_t batch = lens->size(0);
+    if (q->size(2) != head_dim || table->size(0) != batch || (cu ? cu->size(0) != batch + 1 : q->size(0) != batch) ||
+        !lists_fit(lists, counts, batch, most, run, kv_heads))
+        Py_RETURN_NONE;
+    return status_of(select_pages_entry, x.cache, layer, ptr<void>(q), cu ? ptr<int32_t>(cu) : nullptr, ptr<int32_t>(table), ptr<int32_t>(lens), ptr<int32_t>(lists),
+                     ptr<int32_t>(counts), (int)batch, most, (int)q->size(1), (int)table->size(1), run, top, first, last, (int)lists->size(2), x.stream);
+}
+
+// (cache, pool, head_dim, kv_heads, layer, Q, page_table, seq_lens, lists, counts, out, scale, stream)
+PyObject *decode_attn_pages(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Args x{a, n};
+    x.begin();
+    const int head_dim = x.integer(), kv_heads = x.integer(), layer = x.integer();
+    const at::Tensor *q = x.dense(at::kBFloat16, 3), *table = x.dense(at::kInt, 2), *lens = x.dense(at::kInt, 1), *lists = x.dense(at::kInt, 3),
+                     *counts = x.dense(at::kInt, 2), *out = x.dense(at::kBFloat16, 3);
+    const float scale = x.real();
+    if (!x.end()) Py_RETURN_NONE;
+    const int64_t batch = lens->size(0);
+    if (q->size(0) != batch || q->size(2) != head_dim || out->sizes() != q->sizes() || table->size(0) != batch || !lists_fit(lists, counts, batch, 1, 1, kv_heads))
+        Py_RETURN_NONE;
+    return status_of(decode_pages_entry, x.cache, layer, ptr<void>(q), ptr<int32_t>(table), ptr<int32_t>(lens), ptr<int32_t>(lists), ptr<int32_t>(counts), ptr<void>(out),
+                     (int)batch, (int)q->size(1), (int)table->size(1), (int)lists->size(2), scale, x.stream);
+}
+
+// (cache, pool, head_dim, kv_heads, layer, Q, cu_q_lens, page_table, seq_lens, lists, counts, out, max_q_len, run, scale, stream)
+PyObject *prefill_attn_pages(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Args x{a, n};
+    x.begin();
+    const int head_dim = x.integer(), kv_heads = x.integer(), layer = x.integer();
+    const at::Tensor *q = x.dense(at::kBFloat16, 3), *cu = x.dense(at::kInt, 1), *table = x.dense(at::kInt, 2), *lens = x.dense(at::kInt, 1),
+                     *lists = x.dense(at::kInt, 3), *counts = x.dense(at::kInt, 2), *out = x.dense(at::kBFloat16, 3);
+    const int most = x.integer(), run = x.integer();
+    const float scale = x.real();
+    if (!x.end()) Py_RETURN_NONE;
+    const int64_t batch = lens->size(0);
+    if (q->size(2) != head_dim || out->sizes() != q->sizes() || table->size(0) != batch || cu->size(0) != batch + 1 ||
+        !lists_fit(lists, counts, batch, most, run, kv_heads))
+        Py_RETURN_NONE;
+    return status_of(prefill_pages_entry, x.cache, layer, ptr<void>(q), ptr<int32_t>(cu), ptr<int32_t>(table), ptr<int32_t>(lens), ptr<int32_t>(lists), ptr<int32_t>(counts),
+                     ptr<void>(out), (int)batch, most, (int)q->size(1), (int)table->size(1), run, (int)lists->size(2), scale, x.stream);
+}
+
+// connect(address, ...), connect_pages(address, ...): the entry points of the loaded library, in the order of the declarations above
+bool addresses(PyObject *const *a, Py_ssize_t n, Py_ssize_t want, void **p, const char *refusal)
+{
+    if (n != want) {
+        PyErr_SetString(PyExc_TypeError, refusal);
+        return false;
+    }
+    for (int i = 0; i < want; ++i)
+        if (!(p[i] = PyLong_AsVoidPtr(a[i]))) {
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "connect: a null address");
+            return false;
+        }
+    return true;
+}
+
 PyObject *connect(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     void *p[6];
-    if (n != 6) {
-        PyErr_SetString(PyExc_TypeError, "connect: six addresses");
-        return nullptr;
-    }
-    for (int i = 0; i < 6; ++i)
-        if (!(p[i] = PyLong_AsVoidPtr(a[i]))) {
-            if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "connect: a null address");
-            return nullptr;
-        }
+    if (!addresses(a, n, 6, p, "connect: six addresses")) return nullptr;
     is_owner = reinterpret_cast<decltype(is_owner)>(p[0]);
     rope_append_entry = reinterpret_cast<decltype(rope_append_entry)>(p[1]);
     plan_step_entry = reinterpret_cast<decltype(plan_step_entry)>(p[2]);
@@ -244,8 +334,21 @@ PyObject *connect(PyObject *, PyObject *const *a, Py_ssize_t n)
     Py_RETURN_NONE;
 }
 
+PyObject *connect_pages(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    void *p[4];
+    if (!addresses(a, n, 4, p, "connect_pages: four addresses")) return nullptr;
+    index_pages_entry = reinterpret_cast<decltype(index_pages_entry)>(p[0]);
+    select_pages_entry = reinterpret_cast<decltype(select_pages_entry)>(p[1]);
+    decode_pages_entry = reinterpret_cast<decltype(decode_pages_entry)>(p[2]);
+    prefill_pages_entry = reinterpret_cast<decltype(prefill_pages_entry)>(p[3]);
+    Py_RETURN_NONE;
+}
+
 #define METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(declining<f>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"connect", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(connect)), METH_FASTCALL, nullptr},
+                         {"connect_pages", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(connect_pages)), METH_FASTCALL, nullptr},
+                         METHOD(index_pages), METHOD(select_pages), METHOD(decode_attn_pages), METHOD(prefill_attn_pages),
                          METHOD(decode_attn_window), METHOD(prefill_attn_window), METHOD(rope_append), METHOD(plan_step),
                          METHOD(plan_release), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
