@@ -1452,7 +1452,35 @@ int skv_prefill_attn_pages(skv_cache *c, int layer, const void *Q, const int32_t
     const int rr = check_runs(batch, max_q_len, run, q_heads / c->kv_heads, &per_seq);
     if (rr) return rr;
     const PageLists l = {lists, counts, list_stride, run, per_seq};
-    return pages_by_rows(c, c->r[(size_t)layer], Q, cu_q_lens, page_table, seq_lens, l, out, batch, max_q_len, q_heads, pt_stride, scale, true, stream);
+    const int src = c->r[(size_t)layer];
+    const bool can_umma = !c->fp8 && aligned(out, 16) && prefill_pages_smem_bytes(c->head_dim) <= (size_t)c->max_smem_optin;
+    const bool few_rows = max_q_len == 1;
+    if (c->prefill_variant == 2 && !can_umma) return SKV_ERR_UNSUPPORTED;
+    if (can_umma && (c->prefill_variant == 2 || (c->prefill_variant == 0 && !few_rows))) {
+        PrefillParams p;
+        memset(&p, 0, sizeof(p));
+        p.layer_base = c->layer_base(c->slot[(size_t)src]);
+        p.page_stride = (int64_t)c->page_bytes;
+        p.max_pages = c->max_pages;
+        p.Q = static_cast<const uint16_t *>(Q);
+        p.out = static_cast<uint16_t *>(out);
+        p.cu_q = cu_q_lens;
+        p.page_table = page_table;
+        p.seq_lens = seq_lens;
+        p.B = batch;
+        p.Hq = q_heads;
+        p.Hkv = c->kv_heads;
+        p.pt_stride = pt_stride;
+        p.scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)c->head_dim)) * 1.4426950408889634f;
+        p.status = c->status_word();
+        if (launch_prefill_pages(p, l, c->head_dim, q_heads / c->kv_heads, max_q_len, c->tune.pdl != 0, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return SKV_ERR_CUDA;
+        }
+        c->launches += 1;
+        return SKV_OK;
+    }
+    return pages_by_rows(c, src, Q, cu_q_lens, page_table, seq_lens, l, out, batch, max_q_len, q_heads, pt_stride, scale, true, stream);
 }
 
 // ---- whole decode step from host buffers -------------------------------------

@@ -324,26 +324,31 @@ def chunk_runs(lens, new, most, run):
     return got
 
 
-@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("fp8,variant", [(False, 1), (False, 2), (True, 0)])
 @pytest.mark.parametrize("hq,hkv,d,run", CHUNKS)
-def test_chunks_over_listed_pages(hq, hkv, d, run, fp8):
+def test_chunks_over_listed_pages(hq, hkv, d, run, fp8, variant):
+    """A row at a time and a tile at a time."""
     lens, new = [0, 1, 40, 300, 1201, 2000, 129], [0, 1, 40, 77, 150, 1, 0]
     p = Paged(lens, hkv, d, fp8, seed=run)
+    p.cache.skv_set_prefill_variant(variant)
     q = p.rows(sum(new), hq)
     runs = chunk_runs(lens, new, 150, run)
     lists, counts = some_lists(random.Random(run), [(r[2][-1] // 16 + 1 if r[2] else 0) for r in runs], hkv, 30, keep_last=False)
-    out = torch.full(q.shape, float("nan"), dtype=torch.bfloat16, device="cuda")
+    held = torch.full((len(q) + run, hq, d), 7.0, dtype=torch.bfloat16, device="cuda")          # rows behind the last stay as they are
+    out = held[:len(q)]
     cu = i32([sum(new[:b]) for b in range(len(new) + 1)])
     p.cache.skv_prefill_attn_pages(1, q.cuda(), cu, p.table_dev, p.lens_dev, lists.cuda(), counts.cuda(), out, 150, run=run)
     check_rows(p, q, out, lists, counts, runs)
-    assert p.cache.skv_get_status() == 0
+    assert p.cache.skv_get_status() == 0 and bool((held[len(q):] == 7.0).all())
 
 
-def test_hidden_tokens_and_unlisted_pages_may_hold_anything():
+@pytest.mark.parametrize("variant", [1, 2])
+def test_hidden_tokens_and_unlisted_pages_may_hold_anything(variant):
     """NaN behind a row's position and in pages that are not listed; page-table entries that are not listed are not read."""
     lens, new = [1000, 333], [20, 7]
     for d, hkv, hq in ((128, 2, 8), (64, 2, 6), (128, 4, 4)):
         p = Paged(lens, hkv, d, seed=d)
+        p.cache.skv_set_prefill_variant(variant)
         q = p.rows(27, hq)
         runs = chunk_runs(lens, new, 20, 4)
         rng = random.Random(d)
