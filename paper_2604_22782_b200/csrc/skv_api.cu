@@ -1453,7 +1453,7 @@ int skv_prefill_attn_pages(skv_cache *c, int layer, const void *Q, const int32_t
     if (rr) return rr;
     const PageLists l = {lists, counts, list_stride, run, per_seq};
     const int src = c->r[(size_t)layer];
-    const bool can_umma = !c->fp8 && aligned(out, 16) && prefill_pages_smem_bytes(c->head_dim) <= (size_t)c->max_smem_optin;
+    const bool can_umma = aligned(out, 16) && prefill_pages_smem_bytes(c->head_dim, c->fp8) <= (size_t)c->max_smem_optin;
     const bool few_rows = max_q_len == 1;
     if (c->prefill_variant == 2 && !can_umma) return SKV_ERR_UNSUPPORTED;
     if (can_umma && (c->prefill_variant == 2 || (c->prefill_variant == 0 && !few_rows))) {
@@ -1473,7 +1473,7 @@ int skv_prefill_attn_pages(skv_cache *c, int layer, const void *Q, const int32_t
         p.pt_stride = pt_stride;
         p.scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)c->head_dim)) * 1.4426950408889634f;
         p.status = c->status_word();
-        if (launch_prefill_pages(p, l, c->head_dim, q_heads / c->kv_heads, max_q_len, c->tune.pdl != 0, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+        if (launch_prefill_pages(p, l, c->head_dim, q_heads / c->kv_heads, max_q_len, c->fp8, c->tune.pdl != 0, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
             (void)cudaGetLastError();
             return SKV_ERR_CUDA;
         }

@@ -62,8 +62,8 @@ cudaError_t launch_select_pages(const SelectParams &p, int D, int sm_count, bool
 // decode attention over listed pages (skv_decode_pages.cu); kernel as in launch_decode_splitk.  p.cu_q: rows of chunks, a row as a
 // sequence of its own (p.B = sequences * p.max_q_len)
 cudaError_t launch_decode_pages(const DecodeParams &p, const PageLists &l, int D, int G, int kernel, int sm_count, bool pdl, cudaStream_t s);
-// chunk attention over listed pages on the tensor cores (skv_prefill_pages.cu): bf16 pages, min(run, max_q_len) * G <= 128
-size_t prefill_pages_smem_bytes(int D);
-cudaError_t launch_prefill_pages(const PrefillParams &p, const PageLists &l, int D, int G, int max_q_len, bool pdl, cudaStream_t s);
+// chunk attention over listed pages on the tensor cores (skv_prefill_pages.cu): min(run, max_q_len) * G <= 128
+size_t prefill_pages_smem_bytes(int D, bool fp8);
+cudaError_t launch_prefill_pages(const PrefillParams &p, const PageLists &l, int D, int G, int max_q_len, bool fp8, bool pdl, cudaStream_t s);
 
 }  // namespace skv

@@ -3,12 +3,15 @@
 //
 // An item is a list: (sequence, run of rows, kv head), one tile of 128 query rows, row r = token r / G, head r % G.  Lists of
 // neighbouring tiles differ, so tiles share no K and V read (as the windowed kernel's two do) and a CTA has one item.  Two CTAs
-// share an SM, 256 threads, 98 KB and 256 columns of tensor memory each: while one's softmax works the other's instructions do,
-// and what an item's beginning and end leave idle the other CTA uses.  Eight warps:
-//   warps 0-3  fetch the queries, then softmax: thread = row (TMEM lane)
+// share an SM, 256 threads, about 100 KB and 256 columns of tensor memory each: while one's softmax works the other's instructions
+// do, and what an item's beginning and end leave idle the other CTA uses.  Keys go in blocks of 64, 4 listed pages.
+// Warps 0-3 fetch the queries, then softmax: thread = row (TMEM lane).  The other four, on bf16 pages:
 //   warp 4     issues the scores Q K^T,  warp 5  the outputs P V
-//   warp 6     copies K and V of the key blocks (64 keys = 4 listed pages); the entries' page ids are had 32 at a time
+//   warp 6     copies K and V of the key blocks; the entries' page ids are had 32 at a time
 //   warp 7     zeroes the V rows of tokens that no row of the item sees, whatever they hold
+// On FP8 pages the codes are turned into bf16, which holds every one of them exactly, on the way into the operands, and the tokens'
+// scales are applied in fp32 to the scores and to the probabilities:
+//   warps 4, 6  convert K, 4 issues Q K^T, 6 copies;  warps 5, 7  convert V (tokens that no row sees: zero), 5 issues P V, 7 copies
 // Operand layouts, softmax and waits are those of skv_prefill_window.cu.  Runs of one sequence and head are neighbours in the grid:
 // their lists have pages in common, which are then in L2.
 #include "skv_page_index.cuh"
@@ -31,37 +34,106 @@ constexpr int COL_O = 2 * KEYS;       // scores at columns 0 and 64, output from
 constexpr int TMEM_COLS = 256;
 constexpr int NO_PAGE = 0x07FFFFFF;   // no row sees a token of it
 
-__host__ __device__ constexpr int stages_of(int D) { return D == 128 ? 2 : 4; }
+// Shared memory (from a 1024-byte boundary on).  bf16: Q [D/64][128 rows][128 B] | K ring [8 groups][D/8 chunks][8 keys][16 B] | V ring
+// [4 pages][V half].  FP8: Q | K tile (as a stage of the K ring) | V tile [4 pages][2 halves of 8 tokens][D dims][16 B] | K ring: codes of 4
+// pages, their K and V scales | V ring: codes | scales of 4 blocks [K scale x log2(e) / sqrt(d) | V scale][64].  Then barriers and words.
+template <int D, bool FP8>
+struct Layout {
+    static constexpr int STAGES = D == 128 ? 2 : 4;                  // bf16: of the K ring and of the V ring
+    static constexpr int K_STAGES = FP8 ? 3 : STAGES, V_STAGES = FP8 ? 2 : STAGES;
+    static constexpr int Q_BYTES = ROWS * D * 2, TILE = KEYS * D * 2;
+    static constexpr int K_STAGE = FP8 ? KEYS * D + KB * 2 * PAGE * 4 : TILE, V_STAGE = FP8 ? KEYS * D : TILE;
+    static constexpr int K_RING = Q_BYTES + (FP8 ? 2 * TILE : 0), V_RING = K_RING + K_STAGES * K_STAGE;
+    static constexpr int SCALES = V_RING + V_STAGES * V_STAGE, BARS = SCALES + (FP8 ? 4 * 2 * KEYS * 4 : 0);
+    static constexpr int N_BARS = 2 * K_STAGES + 2 * V_STAGES + (FP8 ? 4 : V_STAGES) + 3 * 2 + 1;
+    static constexpr int WORDS = BARS + 8 * N_BARS + (8 * N_BARS & 8);
+    static constexpr int BYTES = 1024 + WORDS + 48;
+};
 
-// Dynamic shared memory: Q [D/64][128 rows][128 B] | K ring [8 groups][D/8 chunks][8 keys][16 B] | V ring [4 pages][V half] | barriers | words
-template <int D>
-constexpr size_t smem_bytes_of() { return 1024 + (size_t)ROWS * D * 2 + 2 * stages_of(D) * (size_t)KEYS * D * 2 + 5 * 8 * stages_of(D) + 3 * 16 + 8 + 32; }
+// four E4M3 codes -> four bf16: the bits of exponent and mantissa moved into place are the value times 2^-120
+__device__ __forceinline__ void e4m3x4_to_bf16(uint32_t w, uint32_t &r0, uint32_t &r1)
+{
+    const uint32_t hi = ((w >> 4) & 0x07070707u) | (w & 0x80808080u), lo = (w << 4) & 0xF0F0F0F0u;
+    r0 = __byte_perm(lo, hi, 0x5140);
+    r1 = __byte_perm(lo, hi, 0x7362);
+    asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(r0) : "r"(0x7B807B80u));
+    asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(r1) : "r"(0x7B807B80u));
+}
 
-template <int D>
+// 16 codes -> two times 8 bf16; a code of NaN is NaN
+__device__ __forceinline__ void convert16(const uint4 &w, uint4 &a, uint4 &b)
+{
+    e4m3x4_to_bf16(w.x, a.x, a.y);
+    e4m3x4_to_bf16(w.y, a.z, a.w);
+    e4m3x4_to_bf16(w.z, b.x, b.y);
+    e4m3x4_to_bf16(w.w, b.z, b.w);
+    const uint32_t mag = 0x7F7F7F7Fu, one = 0x01010101u;             // bit 7 of a byte's magnitude + 1: it was 0x7F
+    const uint32_t n[4] = {(w.x & mag) + one, (w.y & mag) + one, (w.z & mag) + one, (w.w & mag) + one};
+    if ((n[0] | n[1] | n[2] | n[3]) & 0x80808080u) {
+        uint32_t *r[8] = {&a.x, &a.y, &a.z, &a.w, &b.x, &b.y, &b.z, &b.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t f = n[i / 2] >> (16 * (i & 1));
+            if (f & 0x80u) *r[i] |= 0x7FFFu;
+            if (f & 0x8000u) *r[i] |= 0x7FFF0000u;
+        }
+    }
+}
+
+__device__ __forceinline__ uint4 ld_shared(uint32_t a)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void st_shared(uint32_t a, const uint4 &v)
+{
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+// the tokens of page `page` (NO_PAGE: none) up to position pos
+__device__ __forceinline__ uint32_t bits_up_to(int pos, int page)
+{
+    const int left = pos + 1 - page * PAGE;
+    return (1u << (left < 0 ? 0 : left < PAGE ? left : PAGE)) - 1;
+}
+
+template <int D, bool FP8>
 __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_constant__ PrefillParams p, const __grid_constant__ PageLists l,
                                                                       const __grid_constant__ CUtensorMap k_map, int G, int max_q_len)
 {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
-    constexpr int BLOCK = block_bytes(D), HALF = half_bytes(D), CH = D / 8, STAGES = stages_of(D);
-    constexpr int Q_BYTES = ROWS * D * 2, STAGE = KEYS * D * 2;
-    constexpr uint32_t IDESC_QK = instr_desc(ROWS, KEYS, false), IDESC_PV = instr_desc(ROWS, D, true);
+    using L = Layout<D, FP8>;
+    constexpr int BLOCK = FP8 ? fp8_block_bytes(D) : block_bytes(D), HALF = half_bytes(D), CH = D / 8, KS = L::K_STAGES, VS = L::V_STAGES;
+    constexpr uint32_t IDESC_QK = instr_desc(ROWS, KEYS, false), IDESC_PV = instr_desc(ROWS, D, !FP8);
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(FULL, tid >> 5, 0);      // (known to be the same for the warp)
     const uint32_t base = smem_u32(smem_raw);
     const uint32_t pad = (1024u - (base & 1023u)) & 1023u;
-    const uint32_t q_smem = base + pad, k_ring = q_smem + Q_BYTES, v_ring = k_ring + STAGES * STAGE, bars = v_ring + STAGES * STAGE;
-    const uint32_t k_full = bars, v_full = k_full + 8 * STAGES, v_landed = v_full + 8 * STAGES, k_empty = v_landed + 8 * STAGES, v_empty = k_empty + 8 * STAGES;
-    const uint32_t s_ready = v_empty + 8 * STAGES, p_ready = s_ready + 16, pv_done = p_ready + 16, q_full = pv_done + 16;
-    uint8_t *words = smem_raw + pad + Q_BYTES + 2 * STAGES * STAGE + 5 * 8 * STAGES + 3 * 16 + 8;
+    const uint32_t q_smem = base + pad, k_tile = q_smem + L::Q_BYTES, v_tile = k_tile + L::TILE, k_ring = q_smem + L::K_RING, v_ring = q_smem + L::V_RING,
+                   scale_ring = q_smem + L::SCALES;
+    const uint32_t k_full = q_smem + L::BARS, k_empty = k_full + 8 * KS, v_full = k_empty + 8 * KS, v_empty = v_full + 8 * VS;
+    // bf16: a V stage with tokens that nobody sees has landed; FP8: a tile is complete, its instructions are done with it
+    const uint32_t v_landed = v_empty + 8 * VS, k_ready = v_landed, v_ready = k_ready + 8, k_free = v_ready + 8, v_free = k_free + 8;
+    const uint32_t s_ready = v_landed + (FP8 ? 32 : 8 * VS), p_ready = s_ready + 16, pv_done = p_ready + 16, q_full = pv_done + 16;
+    uint8_t *words = smem_raw + pad + L::WORDS;
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(words), *gave_up = tmem_slot + 1;
     volatile int32_t *item = reinterpret_cast<volatile int32_t *>(words + 8);      // rows, first position, tokens of the sequence, first row, entries
 
     if (tid == 0) {
-        for (int i = 0; i < STAGES; ++i) {
+        for (int i = 0; i < KS; ++i) {
             mbar_init(k_full + 8 * i, 1);
+            mbar_init(k_empty + 8 * i, FP8 ? 2 : 1);
+        }
+        for (int i = 0; i < VS; ++i) {
             mbar_init(v_full + 8 * i, 1);
-            mbar_init(v_landed + 8 * i, 1);
-            mbar_init(k_empty + 8 * i, 1);
-            mbar_init(v_empty + 8 * i, 1);
+            mbar_init(v_empty + 8 * i, FP8 ? 2 : 1);
+            if (!FP8) mbar_init(v_landed + 8 * i, 1);
+        }
+        if (FP8) {
+            mbar_init(k_ready, 2);
+            mbar_init(v_ready, 2);
+            mbar_init(k_free, 1);
+            mbar_init(v_free, 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(s_ready + 8 * i, 1);
@@ -121,9 +193,22 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
     const int blocks = (listed + KB - 1) / KB;
     const int32_t *entries = l.lists + list_no * l.stride, *table = p.page_table + (int64_t)b * p.pt_stride;
     const uint32_t tmem = *tmem_slot;
+    // a listed page's number, NO_PAGE where it is none of the sequence's
+    auto page_at = [&](int i) {
+        const int page = i < listed ? __ldg(entries + i) : NO_PAGE;
+        return page >= 0 && page < pages ? page : NO_PAGE;
+    };
+    // physical page of entry i; where there is none, one whose content is not looked at
+    auto id_at = [&](int i) {
+        if (i >= listed) return 0;
+        const int page = page_at(i), id = page != NO_PAGE ? __ldg(table + page) : -1;
+        if (id >= 0 && (int64_t)id < p.max_pages) return id;
+        atomicOr(p.status, STATUS_BOUNDS);
+        return 0;
+    };
 
     if (warp < 4) {
-        more_registers<208>();
+        more_registers<200>();
         // =================== queries ===================
         {
             // 8 lanes a row of 128 bytes; rows that the item does not have are zero
@@ -137,7 +222,7 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
                     if (token < rows)
                         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (uint32_t)(half * ROWS * 128)), "l"(src + half * 64) : "memory");
                     else
-                        asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(dst + (uint32_t)(half * ROWS * 128)), "r"(0u) : "memory");
+                        st_shared(dst + (uint32_t)(half * ROWS * 128), make_uint4(0, 0, 0, 0));
                 }
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
@@ -153,15 +238,11 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
         const int pos = row_ok ? p0 + token : 0x7FFFFFF0;
         const uint64_t scale2 = pair_of(p.scale_log2, p.scale_log2);
         float m_used = -INFINITY, l_sum = 0.f;
-        auto entry = [&](int i) {                          // a listed page's number
-            const int page = i < listed ? __ldg(entries + i) : NO_PAGE;
-            return page >= 0 && page < pages ? page : NO_PAGE;
-        };
-        int page32 = entry(lane), next32 = entry(32 + lane);           // lane: entry 8 k + lane
+        int page32 = page_at(lane), next32 = page_at(32 + lane);       // lane: entry 8 k + lane
         for (int kb = 0; kb < blocks; ++kb) {
             if (kb > 0 && (kb & 7) == 0) {
                 page32 = next32;
-                next32 = entry((kb + 8) * KB + lane);
+                next32 = page_at((kb + 8) * KB + lane);
             }
             int page[KB];
             bool clear = true;
@@ -172,21 +253,28 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
             }
             const int buf = kb & 1, bar = 8 * buf;
             const uint32_t phase = (uint32_t)((kb >> 1) & 1), scores = lane_base + (uint32_t)(buf * KEYS);
+            const uint32_t scales = scale_ring + (uint32_t)((kb & 3) * 2 * KEYS * 4);
             wait(s_ready + bar, phase, gave_up);
             tc_fence_after();
             uint32_t raw[2][32];
 #pragma unroll
             for (int i = 0; i < 2; ++i) tmem_ld32(scores + 32 * i, raw[i]);
             tmem_wait_ld();
+            if (FP8) {
+                // scores in units of log2, before anything is hidden: a hidden token's scale may be anything
+#pragma unroll
+                for (int c = 0; c < KEYS; c += 4) {
+                    const uint4 s = ld_shared(scales + 4 * c);
+                    raw[c / 32][c % 32] = __float_as_uint(__uint_as_float(raw[c / 32][c % 32]) * __uint_as_float(s.x));
+                    raw[c / 32][c % 32 + 1] = __float_as_uint(__uint_as_float(raw[c / 32][c % 32 + 1]) * __uint_as_float(s.y));
+                    raw[c / 32][c % 32 + 2] = __float_as_uint(__uint_as_float(raw[c / 32][c % 32 + 2]) * __uint_as_float(s.z));
+                    raw[c / 32][c % 32 + 3] = __float_as_uint(__uint_as_float(raw[c / 32][c % 32 + 3]) * __uint_as_float(s.w));
+                }
+            }
             if (!clear) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    uint32_t bits = 0;
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const int left = pos + 1 - page[2 * i + j] * PAGE;
-                        bits |= ((1u << (left < 0 ? 0 : left < PAGE ? left : PAGE)) - 1) << (PAGE * j);
-                    }
+                    const uint32_t bits = bits_up_to(pos, page[2 * i]) | bits_up_to(pos, page[2 * i + 1]) << PAGE;
 #pragma unroll
                     for (int c = 0; c < 32; ++c)
                         if (!((bits >> c) & 1u)) raw[i][c] = 0xFF800000u;      // -inf
@@ -202,7 +290,7 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
 #pragma unroll
                 for (int c = 0; c < 32; ++c) {
                     const float s0 = __uint_as_float(raw[c >> 4][(2 * c) & 31]), s1 = __uint_as_float(raw[c >> 4][(2 * c + 1) & 31]);
-                    const uint64_t x = fma2(pair_of(s0, s1), scale2, neg2);
+                    const uint64_t x = FP8 ? add2(pair_of(s0, s1), neg2) : fma2(pair_of(s0, s1), scale2, neg2);
                     float e0, e1;
                     if (c % BY_FMA == BY_FMA - 1) {
                         exp2_by_fma(x, e0, e1);
@@ -213,9 +301,15 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
                     }
                     mx4[c & 3] = fmaxf(mx4[c & 3], fmaxf(s0, s1));
                     sum2[c & 1] = add2(sum2[c & 1], pair_of(e0, e1));
+                    if (FP8) {
+                        float v0, v1;
+                        asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v0), "=f"(v1) : "r"(scales + (uint32_t)(4 * (KEYS + 2 * c))));
+                        e0 *= v0;
+                        e1 *= v1;
+                    }
                     pk[c] = pack_bf16x2(e0, e1);
                 }
-                const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * p.scale_log2;      // the scale is positive
+                const float top = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])), mx = FP8 ? top : top * p.scale_log2;      // the scale is positive
                 const bool move = mx > m_used + RESCALE_STEP;      // also true for the first key that the row sees
                 if (!__any_sync(FULL, move)) {
                     float s0, s1;
@@ -273,94 +367,202 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
             }
         }
     } else {
-        fewer_registers<48>();
-        if (warp < 6) {
+        fewer_registers<56>();
+        const bool leader = elect_one(), values = (warp & 1) != 0;
+        const uint32_t output = tmem + COL_O;
+        const uint64_t q_desc = swizzled_desc(q_smem);
+        // scores of block kb from the K at k_desc / output of block kb from the V at v_desc, whose pages and halves of 8 tokens are
+        // `half` bytes apart and whose 8-dim groups are `group` bytes: by one lane of a warp that has waited for its operands
+        auto issue_scores = [&](int kb, uint64_t k_desc) {
+            const uint32_t scores = tmem + (uint32_t)((kb & 1) * KEYS);
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks)
+                umma_ss(scores, q_desc + (uint64_t)(((ks >> 2) * ROWS * 128 + (ks & 3) * 32) >> 4), k_desc + (uint64_t)((ks * 2 * 128) >> 4), IDESC_QK, ks > 0);
+            tc_commit(s_ready + 8 * (kb & 1));
+        };
+        auto issue_output = [&](int kb, uint64_t v_desc) {
+            const uint32_t scores = tmem + (uint32_t)((kb & 1) * KEYS);
+            const int np = listed - kb * KB;
+#pragma unroll
+            for (int j = 0; j < KB; ++j)
+                if (j < np) umma_ts(output, scores + (uint32_t)(8 * j), v_desc + (uint64_t)((j * HALF) >> 4), IDESC_PV, j > 0 || kb > 0 ? 1u : 0u);
+            tc_commit(pv_done + 8 * (kb & 1));
+        };
+        if (FP8) {
+            // =================== conversion: 64 lanes for K, 64 for V; 4 and 5 issue, 6 and 7 copy ===================
+            const bool second = warp >= 6;
+            const int stages = values ? VS : KS, me = lane + (second ? 32 : 0);
+            const uint32_t ring = values ? v_ring : k_ring, stage_bytes = values ? L::V_STAGE : L::K_STAGE, tile = values ? v_tile : k_tile;
+            const uint32_t full = values ? v_full : k_full, empty = values ? v_empty : k_empty, ready = values ? v_ready : k_ready, free = values ? v_free : k_free;
+            const uint64_t desc = values ? smem_desc(tile, D * 16, 128) : smem_desc(tile, 128, CH * 128);
+            // copies (the second warp): lane 4 (kb % 8) + j has entry j of block kb
+            int id = 0, next_id = 0;
+            auto copy = [&](int kb) {
+                if (kb >= blocks) return;
+                if (kb > 0 && (kb & 7) == 0) {
+                    id = next_id;
+                    next_id = id_at((kb + 8) * KB + lane);
+                }
+                const int st = kb % stages, np = listed - kb * KB < KB ? listed - kb * KB : KB, j = lane - (kb & 7) * KB;
+                if (kb >= stages) wait(empty + 8 * st, (uint32_t)((kb / stages - 1) & 1), gave_up);
+                if (lane == 0) mbar_expect_tx(full + 8 * st, (uint32_t)(np * (values ? PAGE * D : PAGE * D + 2 * PAGE * 4)));
+                __syncwarp();
+                if (j < 0 || j >= np) return;
+                const uint8_t *src = p.layer_base + (int64_t)id * p.page_stride + (int64_t)h * BLOCK;
+                const uint32_t dst = ring + (uint32_t)st * stage_bytes;
+                bulk_copy_g2s(dst + (uint32_t)(j * PAGE * D), src + (values ? fp8_v_off(D) : 0), PAGE * D, full + 8 * st);
+                if (!values) bulk_copy_g2s(dst + (uint32_t)(KEYS * D + j * 2 * PAGE * 4), src + fp8_ks_off(D), 2 * PAGE * 4, full + 8 * st);
+            };
+            if (second) {
+                id = id_at(lane);
+                next_id = id_at(32 + lane);
+                for (int kb = 0; kb < stages - 1; ++kb) copy(kb);
+            }
+            int page32 = page_at(lane), next32 = page_at(32 + lane);
+            if (warp == 4) wait(q_full, 0, gave_up);
+            for (int kb = 0; kb < blocks; ++kb) {
+                if (second) copy(kb + stages - 1);
+                if (kb > 0 && (kb & 7) == 0) {
+                    page32 = next32;
+                    next32 = page_at((kb + 8) * KB + lane);
+                }
+                const int st = kb % stages, np = listed - kb * KB < KB ? listed - kb * KB : KB;
+                const uint32_t from = ring + (uint32_t)st * stage_bytes;
+                // tokens that some row sees, of this lane's entry of the block
+                const uint32_t seen = bits_up_to(p1, page32);
+                wait(full + 8 * st, (uint32_t)((kb / stages) & 1), gave_up);
+                if (kb > 0) wait(free, (uint32_t)((kb - 1) & 1), gave_up);
+                if (!values) {
+                    // this lane's token: K scale into units of log2, V scale (0 where no row sees it)
+                    const uint32_t bits = __shfl_sync(FULL, seen, (kb & 7) * KB + me / PAGE);
+                    float ks = 0.f, vs = 0.f;
+                    if (me / PAGE < np && (bits >> (me % PAGE) & 1u)) {
+                        const uint32_t a = from + (uint32_t)(KEYS * D + (me / PAGE * 2 * PAGE + me % PAGE) * 4);
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ks) : "r"(a) : "memory");
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(vs) : "r"(a + PAGE * 4) : "memory");
+                    }
+                    const uint32_t to = scale_ring + (uint32_t)(((kb & 3) * 2 * KEYS + me) * 4);
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(ks * p.scale_log2) : "memory");
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + KEYS * 4), "f"(vs) : "memory");
+                    // unit: 16 dims of a token
+#pragma unroll 2
+                    for (int u = me; u < np * PAGE * (D / 16); u += 64) {
+                        const int group = u / (D / 2), c = u / 8 % (D / 16), t = u & 7;
+                        uint4 x, y;
+                        convert16(ld_shared(from + (uint32_t)(u * 16)), x, y);
+                        st_shared(tile + (uint32_t)(((group * CH + 2 * c) * 8 + t) * 16), x);
+                        st_shared(tile + (uint32_t)(((group * CH + 2 * c + 1) * 8 + t) * 16), y);
+                    }
+                } else {
+                    // unit: a dim of a page, 16 tokens
+#pragma unroll 2
+                    for (int u = me; u < np * D; u += 64) {
+                        const int j = u / D, dim = u % D;
+                        const uint32_t bits = __shfl_sync(FULL, seen, (kb & 7) * KB + j);
+                        uint4 w = ld_shared(from + (uint32_t)(u * 16)), x, y;
+                        if (bits != 0xFFFFu) {
+                            uint32_t *words4[4] = {&w.x, &w.y, &w.z, &w.w};
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const uint32_t f = bits >> (4 * k) & 0xFu;
+                                *words4[k] &= ((f & 1u) | (f & 2u) << 7 | (f & 4u) << 14 | (f & 8u) << 21) * 0xFFu;
+                            }
+                        }
+                        convert16(w, x, y);
+                        st_shared(tile + (uint32_t)(j * HALF + dim * 16), x);
+                        st_shared(tile + (uint32_t)(j * HALF + (D + dim) * 16), y);
+                    }
+                }
+                fence_proxy_async();                   // the tensor core reads the tile through the async proxy
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(empty + 8 * st);
+                    mbar_arrive(ready);
+                }
+                if (second) continue;
+                wait(ready, (uint32_t)(kb & 1), gave_up);
+                if (!values) {
+                    if (kb >= 2) wait(pv_done + 8 * (kb & 1), (uint32_t)((kb / 2 - 1) & 1), gave_up);       // the buffer: P V two blocks back is over
+                    tc_fence_after();
+                    if (leader) {
+                        issue_scores(kb, desc);
+                        tc_commit(free);
+                    }
+                } else {
+                    wait(p_ready + 8 * (kb & 1), (uint32_t)((kb >> 1) & 1), gave_up);
+                    tc_fence_after();
+                    if (leader) {
+                        issue_output(kb, desc);
+                        tc_commit(free);
+                    }
+                }
+                __syncwarp();
+            }
+            // the last commit arrives, and the last copies (waited for above, but for a failure: then it is not known which are still in
+            // flight, and they are given time), while there is somewhere to arrive
+            wait(free, (uint32_t)((blocks - 1) & 1), gave_up);
+            if (second && *gave_up) {
+                const uint64_t t = global_timer_ns();
+                while (global_timer_ns() - t < 1000000ull) __nanosleep(1000);
+            }
+        } else if (warp < 6) {
             // =================== tensor-core issue: the whole warp walks along, one lane issues ===================
-            const bool leader = elect_one(), values = warp == 5;
-            const uint32_t output = tmem + COL_O;
-            const uint64_t q_desc = swizzled_desc(q_smem);
             const uint64_t ring_desc = values ? smem_desc(v_ring, 128, PAGE * 16) : smem_desc(k_ring, 128, CH * 128);
             const uint32_t full = values ? v_full : k_full, empty = values ? v_empty : k_empty;
             if (!values) wait(q_full, 0, gave_up);
             for (int kb = 0; kb < blocks; ++kb) {
-                const uint32_t st = (uint32_t)kb & (STAGES - 1), parity = (uint32_t)(kb / STAGES) & 1u;
-                const uint32_t buf = (uint32_t)kb & 1u, turn = (uint32_t)(kb >> 1), bar = 8 * buf, scores = tmem + buf * KEYS;
-                const uint64_t desc = ring_desc + (uint64_t)(st * (STAGE >> 4));
-                wait(full + 8 * st, parity, gave_up);
+                const uint32_t st = (uint32_t)kb & (KS - 1), bar = 8 * ((uint32_t)kb & 1u), turn = (uint32_t)(kb >> 1);
+                const uint64_t desc = ring_desc + (uint64_t)(st * (L::TILE >> 4));
+                wait(full + 8 * st, (uint32_t)(kb / KS) & 1u, gave_up);
                 if (!values) {
                     if (kb >= 2) wait(pv_done + bar, (turn - 1) & 1u, gave_up);        // the buffer: P V two blocks back is over
                     tc_fence_after();
-                    if (leader) {
-#pragma unroll
-                        for (int ks = 0; ks < D / 16; ++ks)
-                            umma_ss(scores, q_desc + (uint64_t)(((ks >> 2) * ROWS * 128 + (ks & 3) * 32) >> 4), desc + (uint64_t)((ks * 2 * 128) >> 4), IDESC_QK, ks > 0);
-                        tc_commit(s_ready + bar);
-                        tc_commit(empty + 8 * st);
-                    }
+                    if (leader) issue_scores(kb, desc);
                 } else {
                     wait(p_ready + bar, turn & 1u, gave_up);
                     tc_fence_after();
-                    if (leader) {
-                        const int np = listed - kb * KB;
-#pragma unroll
-                        for (int j = 0; j < KB; ++j)
-                            if (j < np)
-                                umma_ts(output, scores + (uint32_t)(8 * j), desc + (uint64_t)((j * HALF) >> 4), IDESC_PV, j > 0 || kb > 0 ? 1u : 0u);
-                        tc_commit(pv_done + bar);
-                        tc_commit(empty + 8 * st);
-                    }
+                    if (leader) issue_output(kb, desc);
                 }
+                if (leader) tc_commit(empty + 8 * st);
                 __syncwarp();
             }
             // the last commits arrive while the barriers are still there
-            for (int j = blocks > STAGES ? blocks - STAGES : 0; j < blocks; ++j) wait(empty + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1), gave_up);
+            for (int j = blocks > KS ? blocks - KS : 0; j < blocks; ++j) wait(empty + 8 * (j & (KS - 1)), (uint32_t)((j / KS) & 1), gave_up);
         } else if (warp == 6) {
             // =================== copies of K and V ===================
             if (lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
             // lane: entry 8 k + lane; a page no row sees a token of is some page's copy, whose V is zeroed
-            auto entry = [&](int i, int &id, bool &whole) {
-                id = 0;
-                whole = true;
-                if (i >= listed) return;
-                const int page = __ldg(entries + i);
-                whole = page >= 0 && page < pages && page * PAGE + PAGE - 1 <= p1;
-                if (page >= 0 && page < pages) id = __ldg(table + page);
-                if (page < 0 || page >= pages || id < 0 || (int64_t)id >= p.max_pages) {
-                    atomicOr(p.status, STATUS_BOUNDS);
-                    id = 0;
-                }
-            };
-            int id, next_id;
-            bool whole, next_whole;
-            entry(lane, id, whole);
-            entry(32 + lane, next_id, next_whole);
+            auto whole_at = [&](int i) { return i >= listed || bits_up_to(p1, page_at(i)) == 0xFFFFu; };
+            int id = id_at(lane), next_id = id_at(32 + lane);
+            bool whole = whole_at(lane), next_whole = whole_at(32 + lane);
             for (int kb = 0; kb < blocks; ++kb) {
                 if (kb > 0 && (kb & 7) == 0) {
                     id = next_id;
                     whole = next_whole;
-                    entry((kb + 8) * KB + lane, next_id, next_whole);
+                    next_id = id_at((kb + 8) * KB + lane);
+                    next_whole = whole_at((kb + 8) * KB + lane);
                 }
-                const int st = kb & (STAGES - 1), np = listed - kb * KB < KB ? listed - kb * KB : KB, j = lane - (kb & 7) * KB;
-                const uint32_t again = (uint32_t)((kb / STAGES - 1) & 1);
+                const int st = kb & (KS - 1), np = listed - kb * KB < KB ? listed - kb * KB : KB, j = lane - (kb & 7) * KB;
+                const uint32_t again = (uint32_t)((kb / KS - 1) & 1);
                 const bool mine = j >= 0 && j < np;
                 // a block with tokens that no row sees passes through the hands of warp 7 first
                 const bool partial = __any_sync(FULL, mine && !whole);
                 const uint32_t v_bar = (partial ? v_landed : v_full) + 8 * st;
-                if (kb >= STAGES) wait(k_empty + 8 * st, again, gave_up);
+                if (kb >= KS) wait(k_empty + 8 * st, again, gave_up);
                 if (lane == 0) mbar_expect_tx(k_full + 8 * st, (uint32_t)(np * HALF));
                 __syncwarp();
-                if (mine) tensor_copy_k(k_ring + (uint32_t)(st * STAGE + j * HALF), &k_map, h, id, k_full + 8 * st);
-                if (kb >= STAGES) wait(v_empty + 8 * st, again, gave_up);
+                if (mine) tensor_copy_k(k_ring + (uint32_t)(st * L::TILE + j * HALF), &k_map, h, id, k_full + 8 * st);
+                if (kb >= KS) wait(v_empty + 8 * st, again, gave_up);
                 if (lane == 0) mbar_expect_tx(v_bar, (uint32_t)(np * HALF));
                 __syncwarp();
                 if (mine)
-                    bulk_copy_g2s(v_ring + (uint32_t)(st * STAGE + j * HALF), p.layer_base + (int64_t)id * p.page_stride + (int64_t)h * BLOCK + HALF, HALF, v_bar);
+                    bulk_copy_g2s(v_ring + (uint32_t)(st * L::TILE + j * HALF), p.layer_base + (int64_t)id * p.page_stride + (int64_t)h * BLOCK + HALF, HALF, v_bar);
             }
             // leave only when every copy has landed (normally long the case; after a failure it is not known which barrier one
             // still in flight will come through, and it is given time)
-            for (int j = blocks > STAGES ? blocks - STAGES : 0; j < blocks; ++j) {
-                wait(k_full + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1), gave_up);
-                wait(v_full + 8 * (j & (STAGES - 1)), (uint32_t)((j / STAGES) & 1), gave_up);
+            for (int j = blocks > KS ? blocks - KS : 0; j < blocks; ++j) {
+                wait(k_full + 8 * (j & (KS - 1)), (uint32_t)((j / KS) & 1), gave_up);
+                wait(v_full + 8 * (j & (KS - 1)), (uint32_t)((j / KS) & 1), gave_up);
             }
             if (*gave_up) {
                 const uint64_t t = global_timer_ns();
@@ -369,18 +571,11 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
         } else {
             // =================== V rows that no row of the item sees ===================
             uint32_t landed = 0;                       // bit per ring stage: parity of the blocks that came through v_landed
-            auto tokens = [&](int i) -> uint32_t {     // of entry i, those that some row sees
-                if (i >= listed) return 0xFFFFu;
-                const int page = __ldg(entries + i);
-                if (page < 0 || page >= pages) return 0;
-                const int left = p1 + 1 - page * PAGE;
-                return (1u << (left < 0 ? 0 : left < PAGE ? left : PAGE)) - 1;
-            };
             for (int kb0 = 0; kb0 < blocks; kb0 += 8) {
-                const uint32_t bits = tokens(kb0 * KB + lane);
+                const uint32_t bits = kb0 * KB + lane < listed ? bits_up_to(p1, page_at(kb0 * KB + lane)) : 0xFFFFu;
                 unsigned todo = __ballot_sync(FULL, bits != 0xFFFFu);
                 while (todo) {                         // (few have any: the last page of a list)
-                    const int x = __ffs(todo) - 1, kb = kb0 + x / KB, st = kb & (STAGES - 1);
+                    const int x = __ffs(todo) - 1, kb = kb0 + x / KB, st = kb & (KS - 1);
                     const unsigned block = todo & (((1u << KB) - 1) << (x / KB * KB));
                     wait(v_landed + 8 * st, (landed >> st) & 1u, gave_up);
                     landed ^= 1u << st;
@@ -389,7 +584,7 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
                         const uint32_t set = __shfl_sync(FULL, bits, y);
                         for (int i = lane; i < CH * PAGE; i += 32)
                             if (!((set >> (i & (PAGE - 1))) & 1u))
-                                asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(v_ring + (uint32_t)(st * STAGE + (y & (KB - 1)) * HALF + i * 16)), "r"(0u) : "memory");
+                                st_shared(v_ring + (uint32_t)(st * L::TILE + (y & (KB - 1)) * HALF + i * 16), make_uint4(0, 0, 0, 0));
                     }
                     fence_proxy_async();
                     __syncwarp();
@@ -409,15 +604,15 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
     }
 }
 
-template <int D>
+template <int D, bool FP8>
 cudaError_t launch_t(const PrefillParams &p, const PageLists &l, int G, int max_q_len, bool pdl, cudaStream_t s)
 {
     const int64_t ctas = (int64_t)p.B * l.per_seq * p.Hkv;
     if (ctas > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
-    CUtensorMap k_map;
-    if (!encode_k_map(&k_map, p.layer_base, p.page_stride, p.max_pages, p.Hkv, D)) return cudaErrorNotSupported;
-    auto kern = prefill_pages_kernel<D>;
-    const size_t smem = smem_bytes_of<D>();
+    CUtensorMap k_map = {};
+    if (!FP8 && !encode_k_map(&k_map, p.layer_base, p.page_stride, p.max_pages, p.Hkv, D)) return cudaErrorNotSupported;
+    auto kern = prefill_pages_kernel<D, FP8>;
+    const size_t smem = Layout<D, FP8>::BYTES;
     const cudaError_t e = ensure_dynamic_smem(kern, smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
@@ -435,12 +630,16 @@ cudaError_t launch_t(const PrefillParams &p, const PageLists &l, int G, int max_
 
 }  // namespace
 
-size_t prefill_pages_smem_bytes(int D) { return D == 128 ? smem_bytes_of<128>() : D == 64 ? smem_bytes_of<64>() : 0; }
-
-cudaError_t launch_prefill_pages(const PrefillParams &p, const PageLists &l, int D, int G, int max_q_len, bool pdl, cudaStream_t s)
+size_t prefill_pages_smem_bytes(int D, bool fp8)
 {
-    if (D == 128) return launch_t<128>(p, l, G, max_q_len, pdl, s);
-    if (D == 64) return launch_t<64>(p, l, G, max_q_len, pdl, s);
+    if (D == 128) return fp8 ? Layout<128, true>::BYTES : Layout<128, false>::BYTES;
+    return D == 64 ? (fp8 ? Layout<64, true>::BYTES : Layout<64, false>::BYTES) : 0;
+}
+
+cudaError_t launch_prefill_pages(const PrefillParams &p, const PageLists &l, int D, int G, int max_q_len, bool fp8, bool pdl, cudaStream_t s)
+{
+    if (D == 128) return fp8 ? launch_t<128, true>(p, l, G, max_q_len, pdl, s) : launch_t<128, false>(p, l, G, max_q_len, pdl, s);
+    if (D == 64) return fp8 ? launch_t<64, true>(p, l, G, max_q_len, pdl, s) : launch_t<64, false>(p, l, G, max_q_len, pdl, s);
     return cudaErrorInvalidValue;
 }
 
