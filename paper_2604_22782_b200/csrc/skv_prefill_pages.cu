@@ -9,8 +9,10 @@
 //   warp 4     issues the scores Q K^T,  warp 5  the outputs P V
 //   warp 6     copies K and V of the key blocks; the entries' page ids are had 32 at a time
 //   warp 7     zeroes the V rows of tokens that no row of the item sees, whatever they hold
-// On FP8 pages the codes are turned into bf16, which holds every one of them exactly, on the way into the operands, and the tokens'
-// scales are applied in fp32 to the scores and to the probabilities:
+// On FP8 pages the codes are turned into f16, which holds every one of them exactly, on the way into the operands.  Queries are f16
+// too, times a power of two that brings a row's largest to [1, 2): exact but for elements 2^-14 of that and less.  The tokens' scales
+// are applied in fp32, K's to the scores and V's to the probabilities, which are taken relative to c, the power of two at or above every
+// V scale that the row has seen, so that they fit f16 whatever the scales:
 //   warps 4, 6  convert K, 4 issues Q K^T, 6 copies;  warps 5, 7  convert V (tokens that no row sees: zero), 5 issues P V, 7 copies
 // Operand layouts, softmax and waits are those of skv_prefill_window.cu.  Runs of one sequence and head are neighbours in the grid:
 // their lists have pages in common, which are then in L2.
@@ -36,48 +38,37 @@ constexpr int NO_PAGE = 0x07FFFFFF;   // no row sees a token of it
 
 // Shared memory (from a 1024-byte boundary on).  bf16: Q [D/64][128 rows][128 B] | K ring [8 groups][D/8 chunks][8 keys][16 B] | V ring
 // [4 pages][V half].  FP8: Q | K tile (as a stage of the K ring) | V tile [4 pages][2 halves of 8 tokens][D dims][16 B] | K ring: codes of 4
-// pages, their K and V scales | V ring: codes | scales of 4 blocks [K scale x log2(e) / sqrt(d) | V scale][64].  Then barriers and words.
+// pages, their K and V scales | V ring: codes | scales of 4 blocks: K scale x log2(e) / sqrt(d) [64] | V scale [64] |
+// the largest V scale of each half.  Then barriers and words.
 template <int D, bool FP8>
 struct Layout {
     static constexpr int STAGES = D == 128 ? 2 : 4;                  // bf16: of the K ring and of the V ring
+    static constexpr int SCALE_STAGE = (2 * KEYS + 4) * 4;
     static constexpr int K_STAGES = FP8 ? 3 : STAGES, V_STAGES = FP8 ? 2 : STAGES;
     static constexpr int Q_BYTES = ROWS * D * 2, TILE = KEYS * D * 2;
     static constexpr int K_STAGE = FP8 ? KEYS * D + KB * 2 * PAGE * 4 : TILE, V_STAGE = FP8 ? KEYS * D : TILE;
     static constexpr int K_RING = Q_BYTES + (FP8 ? 2 * TILE : 0), V_RING = K_RING + K_STAGES * K_STAGE;
-    static constexpr int SCALES = V_RING + V_STAGES * V_STAGE, BARS = SCALES + (FP8 ? 4 * 2 * KEYS * 4 : 0);
+    static constexpr int SCALES = V_RING + V_STAGES * V_STAGE, BARS = SCALES + (FP8 ? 4 * SCALE_STAGE : 0);
     static constexpr int N_BARS = 2 * K_STAGES + 2 * V_STAGES + (FP8 ? 4 : V_STAGES) + 3 * 2 + 1;
     static constexpr int WORDS = BARS + 8 * N_BARS + (8 * N_BARS & 8);
     static constexpr int BYTES = 1024 + WORDS + 48;
 };
 
-// four E4M3 codes -> four bf16: the bits of exponent and mantissa moved into place are the value times 2^-120
-__device__ __forceinline__ void e4m3x4_to_bf16(uint32_t w, uint32_t &r0, uint32_t &r1)
-{
-    const uint32_t hi = ((w >> 4) & 0x07070707u) | (w & 0x80808080u), lo = (w << 4) & 0xF0F0F0F0u;
-    r0 = __byte_perm(lo, hi, 0x5140);
-    r1 = __byte_perm(lo, hi, 0x7362);
-    asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(r0) : "r"(0x7B807B80u));
-    asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(r1) : "r"(0x7B807B80u));
-}
-
-// 16 codes -> two times 8 bf16; a code of NaN is NaN
+// 16 E4M3 codes -> two times 8 f16 (exact)
 __device__ __forceinline__ void convert16(const uint4 &w, uint4 &a, uint4 &b)
 {
-    e4m3x4_to_bf16(w.x, a.x, a.y);
-    e4m3x4_to_bf16(w.y, a.z, a.w);
-    e4m3x4_to_bf16(w.z, b.x, b.y);
-    e4m3x4_to_bf16(w.w, b.z, b.w);
-    const uint32_t mag = 0x7F7F7F7Fu, one = 0x01010101u;             // bit 7 of a byte's magnitude + 1: it was 0x7F
-    const uint32_t n[4] = {(w.x & mag) + one, (w.y & mag) + one, (w.z & mag) + one, (w.w & mag) + one};
-    if ((n[0] | n[1] | n[2] | n[3]) & 0x80808080u) {
-        uint32_t *r[8] = {&a.x, &a.y, &a.z, &a.w, &b.x, &b.y, &b.z, &b.w};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t f = n[i / 2] >> (16 * (i & 1));
-            if (f & 0x80u) *r[i] |= 0x7FFFu;
-            if (f & 0x8000u) *r[i] |= 0x7FFF0000u;
-        }
-    }
+    e4m3x4_to_f16x2(w.x, a.x, a.y);
+    e4m3x4_to_f16x2(w.y, a.z, a.w);
+    e4m3x4_to_f16x2(w.z, b.x, b.y);
+    e4m3x4_to_f16x2(w.w, b.z, b.w);
+}
+
+// exponent of the power of two at or above x >= 0, at least LEAST_C: a probability of up to 2^8 over c stays far from fp32's end
+constexpr int LEAST_C = -100;
+__device__ __forceinline__ float ceil_log2(float x)
+{
+    const int e = (int)((__float_as_uint(x) + 0x007FFFFFu) >> 23) - 127;
+    return (float)(e < LEAST_C ? LEAST_C : e);
 }
 
 __device__ __forceinline__ uint4 ld_shared(uint32_t a)
@@ -105,7 +96,8 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     using L = Layout<D, FP8>;
     constexpr int BLOCK = FP8 ? fp8_block_bytes(D) : block_bytes(D), HALF = half_bytes(D), CH = D / 8, KS = L::K_STAGES, VS = L::V_STAGES;
-    constexpr uint32_t IDESC_QK = instr_desc(ROWS, KEYS, false), IDESC_PV = instr_desc(ROWS, D, !FP8);
+    constexpr uint32_t F16 = FP8 ? (1u << 7) | (1u << 10) : 0u;              // the operands' type bits: bf16, or neither
+    constexpr uint32_t IDESC_QK = instr_desc(ROWS, KEYS, false) & ~F16, IDESC_PV = instr_desc(ROWS, D, !FP8) & ~F16;
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(FULL, tid >> 5, 0);      // (known to be the same for the warp)
     const uint32_t base = smem_u32(smem_raw);
     const uint32_t pad = (1024u - (base & 1023u)) & 1023u;
@@ -178,8 +170,11 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const int rows = item[0], p0 = item[1], p1 = p0 + rows - 1, pages = (item[2] + PAGE - 1) / PAGE, listed = item[4];
-    const int64_t first_row = item[3];
+    // (by a shuffle: then they are known to be the same for the warp, and what is worked out from them stays in uniform registers, from
+    // which the tensor core's instructions take their operands)
+    auto shared = [&](int i) { return __shfl_sync(FULL, item[i], 0); };
+    const int rows = shared(0), p0 = shared(1), p1 = p0 + rows - 1, pages = (shared(2) + PAGE - 1) / PAGE, listed = shared(4);
+    const int64_t first_row = shared(3);
     const uint16_t *q_rows = p.Q + (first_row * p.Hq + (int64_t)h * G) * D;
     uint16_t *out_rows = p.out + (first_row * p.Hq + (int64_t)h * G) * D;
     if (rows <= 0) return;
@@ -192,7 +187,7 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
     }
     const int blocks = (listed + KB - 1) / KB;
     const int32_t *entries = l.lists + list_no * l.stride, *table = p.page_table + (int64_t)b * p.pt_stride;
-    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem = __shfl_sync(FULL, *tmem_slot, 0);
     // a listed page's number, NO_PAGE where it is none of the sequence's
     auto page_at = [&](int i) {
         const int page = i < listed ? __ldg(entries + i) : NO_PAGE;
@@ -210,19 +205,47 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
     if (warp < 4) {
         more_registers<200>();
         // =================== queries ===================
+        float row_scale = 0.f;                             // FP8: the power of two that was taken out of this thread's row
         {
-            // 8 lanes a row of 128 bytes; rows that the item does not have are zero
+            // 8 lanes a row of 128 bytes, a warp its 32 rows; rows that the item does not have are zero
             const int c = lane & 7;
-            for (int row = warp * 4 + (lane >> 3); row < ROWS; row += 16) {
-                const int token = row / G;
+#pragma unroll 1
+            for (int i = 0; i < 8; ++i) {
+                const int row = warp * 32 + i * 4 + (lane >> 3), token = row / G;
                 const uint16_t *src = q_rows + ((int64_t)token * p.Hq + row - token * G) * D + c * 8;
                 const uint32_t dst = q_smem + (uint32_t)(row * 128 + ((c ^ (row & 7)) * 16));
+                if constexpr (FP8) {
+                    uint4 w[D / 64];
+                    uint32_t top = 0;
 #pragma unroll
-                for (int half = 0; half < D / 64; ++half) {
-                    if (token < rows)
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (uint32_t)(half * ROWS * 128)), "l"(src + half * 64) : "memory");
-                    else
-                        st_shared(dst + (uint32_t)(half * ROWS * 128), make_uint4(0, 0, 0, 0));
+                    for (int half = 0; half < D / 64; ++half) {
+                        w[half] = token < rows ? __ldg(reinterpret_cast<const uint4 *>(src + half * 64)) : make_uint4(0, 0, 0, 0);
+                        const uint32_t x[4] = {w[half].x, w[half].y, w[half].z, w[half].w};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) top = max(top, max(x[k] & 0x7FFFu, x[k] >> 16 & 0x7FFFu));
+                    }
+#pragma unroll
+                    for (int x = 1; x < 8; x <<= 1) top = max(top, __shfl_xor_sync(FULL, top, x));
+                    const int e = min(max((int)(top >> 7) - 127, -126), 126);            // (both powers are normal numbers)
+                    const float out = __int_as_float((127 - e) << 23), in = __int_as_float((127 + e) << 23);
+#pragma unroll
+                    for (int half = 0; half < D / 64; ++half) {
+                        const uint32_t x[4] = {w[half].x, w[half].y, w[half].z, w[half].w};
+                        uint32_t y[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) y[k] = pack_f16x2(bf16_lo(x[k]) * out, bf16_hi(x[k]) * out);
+                        st_shared(dst + (uint32_t)(half * ROWS * 128), make_uint4(y[0], y[1], y[2], y[3]));
+                    }
+                    const float theirs = __shfl_sync(FULL, in, (lane & 3) * 8);
+                    if (lane >> 2 == i) row_scale = theirs;
+                } else {
+#pragma unroll
+                    for (int half = 0; half < D / 64; ++half) {
+                        if (token < rows)
+                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (uint32_t)(half * ROWS * 128)), "l"(src + half * 64) : "memory");
+                        else
+                            st_shared(dst + (uint32_t)(half * ROWS * 128), make_uint4(0, 0, 0, 0));
+                    }
                 }
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
@@ -236,8 +259,9 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
         const int token = tid / G, g = tid - token * G;
         const bool row_ok = token < rows;
         const int pos = row_ok ? p0 + token : 0x7FFFFFF0;
-        const uint64_t scale2 = pair_of(p.scale_log2, p.scale_log2);
-        float m_used = -INFINITY, l_sum = 0.f;
+        const float scale = FP8 ? row_scale : p.scale_log2;       // of what the loop below takes for scores (FP8: K's scales times the rest are in them)
+        const uint64_t scale2 = pair_of(scale, scale);
+        float m_used = -INFINITY, l_sum = 0.f, c_used = LEAST_C;    // c_used: log2 c
         int page32 = page_at(lane), next32 = page_at(32 + lane);       // lane: entry 8 k + lane
         for (int kb = 0; kb < blocks; ++kb) {
             if (kb > 0 && (kb & 7) == 0) {
@@ -253,15 +277,16 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
             }
             const int buf = kb & 1, bar = 8 * buf;
             const uint32_t phase = (uint32_t)((kb >> 1) & 1), scores = lane_base + (uint32_t)(buf * KEYS);
-            const uint32_t scales = scale_ring + (uint32_t)((kb & 3) * 2 * KEYS * 4);
+            const uint32_t scales = scale_ring + (uint32_t)((kb & 3) * L::SCALE_STAGE);
             wait(s_ready + bar, phase, gave_up);
             tc_fence_after();
             uint32_t raw[2][32];
 #pragma unroll
             for (int i = 0; i < 2; ++i) tmem_ld32(scores + 32 * i, raw[i]);
             tmem_wait_ld();
+            float c_block = 0.f;
             if (FP8) {
-                // scores in units of log2, before anything is hidden: a hidden token's scale may be anything
+                // before anything is hidden: a hidden token's scale may be anything
 #pragma unroll
                 for (int c = 0; c < KEYS; c += 4) {
                     const uint4 s = ld_shared(scales + 4 * c);
@@ -270,6 +295,9 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
                     raw[c / 32][c % 32 + 2] = __float_as_uint(__uint_as_float(raw[c / 32][c % 32 + 2]) * __uint_as_float(s.z));
                     raw[c / 32][c % 32 + 3] = __float_as_uint(__uint_as_float(raw[c / 32][c % 32 + 3]) * __uint_as_float(s.w));
                 }
+                float v0, v1;
+                asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v0), "=f"(v1) : "r"(scales + 2 * KEYS * 4));
+                c_block = fmaxf(v0, v1);
             }
             if (!clear) {
 #pragma unroll
@@ -279,10 +307,19 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
                     for (int c = 0; c < 32; ++c)
                         if (!((bits >> c) & 1u)) raw[i][c] = 0xFF800000u;      // -inf
                 }
+                if (FP8) {                                 // the largest V scale of what this row sees
+                    c_block = 0.f;
+                    for (int c = 0; c < KEYS; ++c) {
+                        float v;
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(scales + (uint32_t)(4 * (KEYS + c))));
+                        if (bits_up_to(pos, __shfl_sync(FULL, page32, (kb & 7) * KB + c / PAGE)) >> (c % PAGE) & 1u) c_block = fmaxf(c_block, v);
+                    }
+                }
             }
+            const float c_now = FP8 ? fmaxf(c_used, ceil_log2(c_block)) : 0.f;
             // Against the reference as it stands; again if the block's maximum turns out to have run away from it.
             for (;;) {
-                const float neg_m = m_used == -INFINITY ? 0.f : -m_used;
+                const float neg_m = (m_used == -INFINITY ? 0.f : -m_used) - (FP8 ? c_used : 0.f);
                 const uint64_t neg2 = pair_of(neg_m, neg_m);
                 uint64_t sum2[2] = {0ull, 0ull};
                 float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -290,7 +327,7 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
 #pragma unroll
                 for (int c = 0; c < 32; ++c) {
                     const float s0 = __uint_as_float(raw[c >> 4][(2 * c) & 31]), s1 = __uint_as_float(raw[c >> 4][(2 * c + 1) & 31]);
-                    const uint64_t x = FP8 ? add2(pair_of(s0, s1), neg2) : fma2(pair_of(s0, s1), scale2, neg2);
+                    const uint64_t x = fma2(pair_of(s0, s1), scale2, neg2);
                     float e0, e1;
                     if (c % BY_FMA == BY_FMA - 1) {
                         exp2_by_fma(x, e0, e1);
@@ -307,10 +344,11 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
                         e0 *= v0;
                         e1 *= v1;
                     }
-                    pk[c] = pack_bf16x2(e0, e1);
+                    pk[c] = FP8 ? pack_f16x2(e0, e1) : pack_bf16x2(e0, e1);
                 }
-                const float top = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])), mx = FP8 ? top : top * p.scale_log2;      // the scale is positive
-                const bool move = mx > m_used + RESCALE_STEP;      // also true for the first key that the row sees
+                const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * scale;      // the scale is positive
+                const bool higher = mx > m_used + RESCALE_STEP;    // also true for the first key that the row sees
+                const bool move = higher || (FP8 && c_now > c_used);
                 if (!__any_sync(FULL, move)) {
                     float s0, s1;
                     halves(add2(sum2[0], sum2[1]), s0, s1);
@@ -318,8 +356,12 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
                     tmem_st32(scores, pk);                         // P over the first half of its scores
                     break;
                 }
-                const float alpha = move ? ex2(m_used - mx) : 1.f;         // 0 when m_used = -inf
-                if (move) m_used = mx;
+                float alpha = higher ? ex2(m_used - mx) : 1.f;             // 0 when m_used = -inf
+                if (higher) m_used = mx;
+                if (FP8) {
+                    alpha *= ex2(c_used - c_now);
+                    c_used = c_now;
+                }
                 l_sum *= alpha;
                 if (kb > 0) {
                     // O has to hold all blocks so far (P V two blocks back is over: these scores were issued after it)
@@ -441,36 +483,52 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
                         asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ks) : "r"(a) : "memory");
                         asm volatile("ld.shared.f32 %0, [%1];" : "=f"(vs) : "r"(a + PAGE * 4) : "memory");
                     }
-                    const uint32_t to = scale_ring + (uint32_t)(((kb & 3) * 2 * KEYS + me) * 4);
+                    const uint32_t stage = scale_ring + (uint32_t)((kb & 3) * L::SCALE_STAGE), to = stage + (uint32_t)(me * 4);
+                    const uint32_t most = __reduce_max_sync(FULL, __float_as_uint(vs));          // (0 or more; the bits of a NaN are above all)
+                    if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(stage + (uint32_t)(2 * KEYS * 4 + (second ? 4 : 0))), "r"(most) : "memory");
                     asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(ks * p.scale_log2) : "memory");
                     asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + KEYS * 4), "f"(vs) : "memory");
-                    // unit: 16 dims of a token
-#pragma unroll 2
-                    for (int u = me; u < np * PAGE * (D / 16); u += 64) {
-                        const int group = u / (D / 2), c = u / 8 % (D / 16), t = u & 7;
-                        uint4 x, y;
-                        convert16(ld_shared(from + (uint32_t)(u * 16)), x, y);
-                        st_shared(tile + (uint32_t)(((group * CH + 2 * c) * 8 + t) * 16), x);
-                        st_shared(tile + (uint32_t)(((group * CH + 2 * c + 1) * 8 + t) * 16), y);
+                    // unit: 16 dims of a token; the units of a page are read together
+#pragma unroll 1
+                    for (int u0 = me; u0 < np * D; u0 += 2 * D) {
+                        uint4 w[D / 32];
+#pragma unroll
+                        for (int i = 0; i < D / 32; ++i) w[i] = ld_shared(from + (uint32_t)((u0 + 64 * i) * 16));
+#pragma unroll
+                        for (int i = 0; i < D / 32; ++i) {
+                            const int u = u0 + 64 * i, group = u / (D / 2), c = u / 8 % (D / 16), t = u & 7;
+                            uint4 x, y;
+                            convert16(w[i], x, y);
+                            st_shared(tile + (uint32_t)(((group * CH + 2 * c) * 8 + t) * 16), x);
+                            st_shared(tile + (uint32_t)(((group * CH + 2 * c + 1) * 8 + t) * 16), y);
+                        }
                     }
                 } else {
                     // unit: a dim of a page, 16 tokens
-#pragma unroll 2
-                    for (int u = me; u < np * D; u += 64) {
-                        const int j = u / D, dim = u % D;
-                        const uint32_t bits = __shfl_sync(FULL, seen, (kb & 7) * KB + j);
-                        uint4 w = ld_shared(from + (uint32_t)(u * 16)), x, y;
-                        if (bits != 0xFFFFu) {
-                            uint32_t *words4[4] = {&w.x, &w.y, &w.z, &w.w};
+                    const bool partial = __any_sync(FULL, seen != 0xFFFFu && lane >> 2 == (kb & 7));
+#pragma unroll 1
+                    for (int u0 = me; u0 < np * D; u0 += 2 * D) {
+                        uint4 w[D / 32];
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                const uint32_t f = bits >> (4 * k) & 0xFu;
-                                *words4[k] &= ((f & 1u) | (f & 2u) << 7 | (f & 4u) << 14 | (f & 8u) << 21) * 0xFFu;
+                        for (int i = 0; i < D / 32; ++i) w[i] = ld_shared(from + (uint32_t)((u0 + 64 * i) * 16));
+                        if (partial)
+#pragma unroll
+                            for (int i = 0; i < D / 32; ++i) {
+                                const uint32_t bits = __shfl_sync(FULL, seen, (kb & 7) * KB + (u0 + 64 * i) / D);
+                                auto keep = [&](int k) {
+                                    const uint32_t f = bits >> (4 * k) & 0xFu;
+                                    return ((f & 1u) | (f & 2u) << 7 | (f & 4u) << 14 | (f & 8u) << 21) * 0xFFu;
+                                };
+                                w[i] = make_uint4(w[i].x & keep(0), w[i].y & keep(1), w[i].z & keep(2), w[i].w & keep(3));
                             }
+#pragma unroll
+                        for (int i = 0; i < D / 32; ++i) {
+                            const int u = u0 + 64 * i, j = u / D, dim = u % D;
+                            uint4 x, y;
+                            convert16(w[i], x, y);
+                            st_shared(tile + (uint32_t)(j * HALF + dim * 16), x);
+                            st_shared(tile + (uint32_t)(j * HALF + (D + dim) * 16), y);
                         }
-                        convert16(w, x, y);
-                        st_shared(tile + (uint32_t)(j * HALF + dim * 16), x);
-                        st_shared(tile + (uint32_t)(j * HALF + (D + dim) * 16), y);
                     }
                 }
                 fence_proxy_async();                   // the tensor core reads the tile through the async proxy

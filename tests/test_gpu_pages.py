@@ -32,14 +32,11 @@ def i32(x):
     return torch.tensor(x, dtype=torch.int32, device="cuda")
 
 
-def check(got, want, what, tile=None):
-    """On FP8 pages a row at a time has queries and probabilities rounded to f16.  A tile at a time has neither: the codes are
-    exact in bf16, as the queries are, the tokens' scales multiply fp32 scores (one more rounding, of 2^-24, to the 128 sums'), and a
-    probability times its V scale is rounded to bf16, so that what is said of bf16 pages holds.  tile None: either."""
+def check(got, want, what):
+    """serving_reference's bounds.  A tile at a time on FP8 pages: queries are f16 times a power of two (2^-25 of the row's largest
+    element at most), probabilities times V scale over c are f16, as they are where a row is taken at a time."""
     out, size, reach, n, fp8, v_max = want
-    tol = ref.attention_tolerance(out, size, reach, n, fp8 and not tile, v_max)
-    if fp8 and tile is None:
-        tol = torch.maximum(tol, ref.attention_tolerance(out, size, reach, n, False, v_max))
+    tol = ref.attention_tolerance(out, size, reach, n, fp8, v_max)
     err = (got.double().cpu() - out).abs()
     assert bool((err <= tol).all()), f"{what}: {(err / tol.clamp(min=1e-30)).max().item():.2f} of what rounding allows"
 
@@ -261,7 +258,7 @@ def some_lists(rng, page_counts, hkv, width, keep_last=True):
     return lists, counts
 
 
-def check_rows(p, q, out, lists, counts, rows_of, scale=None, tile=False):
+def check_rows(p, q, out, lists, counts, rows_of, scale=None):
     """rows_of[i] = (sequence, first row of q, positions) of list i."""
     hkv = lists.shape[1]
     group = q.shape[1] // hkv
@@ -270,7 +267,7 @@ def check_rows(p, q, out, lists, counts, rows_of, scale=None, tile=False):
             mine = slice(row, row + len(pos)), slice(h * group, (h + 1) * group)
             want = pages.attention(q[mine], p.k[b][:, h], p.v[b][:, h], torch.tensor(pos), lists[i, h, :counts[i, h]].tolist(), scale)
             v_max = float(p.v[b].double().abs().max()) if p.lens[b] else 0.0
-            check(out[mine], want + (16 * int(counts[i, h]), p.fp8, v_max), f"list {i} head {h}", tile)
+            check(out[mine], want + (16 * int(counts[i, h]), p.fp8, v_max), f"list {i} head {h}")
 
 
 @pytest.mark.parametrize("fp8", [False, True])
@@ -344,7 +341,7 @@ def test_chunks_over_listed_pages(hq, hkv, d, run, fp8, variant):
     out = held[:len(q)]
     cu = i32([sum(new[:b]) for b in range(len(new) + 1)])
     p.cache.skv_prefill_attn_pages(1, q.cuda(), cu, p.table_dev, p.lens_dev, lists.cuda(), counts.cuda(), out, 150, run=run)
-    check_rows(p, q, out, lists, counts, runs, tile=variant == 2)
+    check_rows(p, q, out, lists, counts, runs)
     assert p.cache.skv_get_status() == 0 and bool((held[len(q):] == 7.0).all())
 
 
@@ -414,7 +411,7 @@ def test_fp8_codes_of_every_value(hq, hkv, d, run, variant):
         p.cache.skv_prefill_attn_pages(0, q.cuda(), i32([0, a]), p.table_dev, p.lens_dev, lists.cuda(), counts.cuda(), out, a, run=run)
         assert p.cache.skv_get_status() == 0
     attend()
-    check_rows(p, q, out, lists, counts, runs, tile=variant == 2)
+    check_rows(p, q, out, lists, counts, runs)
     k[n - 3, 0, 5] = v[n - 2, 1, 7] = math.nan
     p.cache.skv_append(0, k[n - 3:].cuda(), v[n - 3:].cuda(), slots[n - 3:])
     attend()
@@ -422,6 +419,41 @@ def test_fp8_codes_of_every_value(hq, hkv, d, run, variant):
     group = hq // hkv
     assert bool(nan[a - 3:, :group].all()) and not bool(nan[:a - 3, :group].any())
     assert bool(nan[a - 2:, group:2 * group, 7].all()) and not bool(nan[:a - 16, group:].any())
+
+
+@pytest.mark.parametrize("variant", [1, 2])
+@pytest.mark.parametrize("d,hkv,hq", [(128, 2, 8), (64, 2, 6)])
+def test_fp8_value_scales_far_apart(d, hkv, hq, variant):
+    """V rows of zeros, V growing by 2^12 from page to page of a list and falling again, and a huge one that earlier rows must not see."""
+    n, a, run = 288, 8, 8
+    p = Paged([n], hkv, d, True, seed=d)
+    p.cache.skv_set_prefill_variant(variant)
+    v = torch.randn(n, hkv, d, generator=p.g)
+    for j, e in enumerate([None, -60, -48, -36, -24, -12, 0, 12, 24, 30, 12, 0, -12, -36, None, 0, 0, 0]):
+        v[16 * j:16 * j + 16] *= 0.0 if e is None else 2.0 ** e
+    v[n - 1] *= 2.0 ** 60
+    v = v.bfloat16()
+    slots = ref.slots_of(p.table, 0, torch.arange(n)).cuda()
+    k = p.k[0].bfloat16()
+    p.cache.skv_append(0, k.cuda(), v.cuda(), slots)
+    codes, scales = [torch.empty(n, hkv, d, dtype=torch.uint8, device="cuda") for _ in range(2)], [torch.empty(n, hkv, device="cuda") for _ in range(2)]
+    p.cache.skv_gather_fp8(0, slots, *codes, *scales)
+    p.k, p.v = ([(c.view(torch.float8_e4m3fn).double() * x.double()[..., None]).cpu()] for c, x in zip(codes, scales))
+    q = p.rows(a, hq)
+    runs = chunk_runs([n], [a], a, run)
+    for pages_listed in ([0, 14], list(range(9)), [8, 7, 1, 0], list(range(18)), [0, 14, 17], [13, 1, 2, 17]):
+        lists = torch.tensor(pages_listed, dtype=torch.int32).expand(1, hkv, -1).contiguous()
+        counts = torch.full((1, hkv), len(pages_listed), dtype=torch.int32)
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
+        p.cache.skv_prefill_attn_pages(0, q.cuda(), i32([0, a]), p.table_dev, p.lens_dev, lists.cuda(), counts.cuda(), out, a, run=run)
+        for i in range(a):                                    # row by row: what a row does not see has no part in its bound
+            there = [t for j in pages_listed for t in range(16 * j, 16 * j + 16) if t <= n - a + i]
+            v_max = float(p.v[0][there].abs().max())
+            for h in range(hkv):
+                mine = slice(i, i + 1), slice(h * hq // hkv, (h + 1) * hq // hkv)
+                want = pages.attention(q[mine], p.k[0][:, h], p.v[0][:, h], torch.tensor([n - a + i]), pages_listed)
+                check(out[mine], want + (len(there), True, v_max), f"pages {pages_listed} row {i} head {h}")
+    assert p.cache.skv_get_status() == 0 and len(runs) == 1
 
 
 @pytest.mark.parametrize("fp8", [False, True])
@@ -530,7 +562,7 @@ def test_a_layer_of_prompt_and_steps(hq, hkv, d, fp8):
                     mine = q.cpu()[row:row + len(pos), h * group:(h + 1) * group]
                     want = pages.page_list(pages.scores(mine, c, s) if full else [], pos[0], pos[-1], top, first_pages, last_pages)
                 assert lists[i, h, :counts[i, h]].tolist() == want
-        check_rows(p, q.cpu(), out, lists.cpu(), counts.cpu(), runs, tile=None)
+        check_rows(p, q.cpu(), out, lists.cpu(), counts.cpu(), runs)
 
     for new in (first, second):
         kk, vv, q = rows(new)
