@@ -3,9 +3,9 @@
 //
 // An item is a list: (sequence, run of rows, kv head), one tile of 128 query rows, row r = token r / G, head r % G.  Lists of
 // neighbouring tiles differ, so tiles share no K and V read (as the windowed kernel's two do) and a CTA has one item.  Two CTAs
-// share an SM, 256 threads, about 100 KB and 256 columns of tensor memory each: while one's softmax works the other's instructions
+// share an SM, 256 or 384 threads, about 100 KB and 256 columns of tensor memory each: while one's softmax works the other's instructions
 // do, and what an item's beginning and end leave idle the other CTA uses.  Keys go in blocks of 64, 4 listed pages.
-// Warps 0-3 fetch the queries, then softmax: thread = row (TMEM lane).  The other four, on bf16 pages:
+// Warps 0-3 fetch the queries, then softmax: thread = row (TMEM lane).  The others, on bf16 pages:
 //   warp 4     issues the scores Q K^T,  warp 5  the outputs P V
 //   warp 6     copies K and V of the key blocks; the entries' page ids are had 32 at a time
 //   warp 7     zeroes the V rows of tokens that no row of the item sees, whatever they hold
@@ -13,7 +13,7 @@
 // too, times a power of two that brings a row's largest to [1, 2): exact but for elements 2^-14 of that and less.  The tokens' scales
 // are applied in fp32, K's to the scores and V's to the probabilities, which are taken relative to c, the power of two at or above every
 // V scale that the row has seen, so that they fit f16 whatever the scales:
-//   warps 4, 6  convert K, 4 issues Q K^T, 6 copies;  warps 5, 7  convert V (tokens that no row sees: zero), 5 issues P V, 7 copies
+//   warps 4, 5  convert K,  warps 6, 7  V (tokens that no row sees: zero),  warp 8  issues Q K^T,  9  P V,  warps 10, 11  copy K and V
 // Operand layouts, softmax and waits are those of skv_prefill_window.cu.  Runs of one sequence and head are neighbours in the grid:
 // their lists have pages in common, which are then in L2.
 #include "skv_page_index.cuh"
@@ -31,7 +31,7 @@ constexpr unsigned FULL = 0xFFFFFFFFu;
 constexpr int ROWS = 128;             // query rows of an item
 constexpr int KB = 4;                 // pages of a key block
 constexpr int KEYS = KB * PAGE;
-constexpr int THREADS = 256;
+__host__ __device__ constexpr int threads_of(bool fp8) { return fp8 ? 384 : 256; }
 constexpr int COL_O = 2 * KEYS;       // scores at columns 0 and 64, output from 128 on
 constexpr int TMEM_COLS = 256;
 constexpr int NO_PAGE = 0x07FFFFFF;   // no row sees a token of it
@@ -90,11 +90,12 @@ __device__ __forceinline__ uint32_t bits_up_to(int pos, int page)
 }
 
 template <int D, bool FP8>
-__global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_constant__ PrefillParams p, const __grid_constant__ PageLists l,
+__global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const __grid_constant__ PrefillParams p, const __grid_constant__ PageLists l,
                                                                       const __grid_constant__ CUtensorMap k_map, int G, int max_q_len)
 {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     using L = Layout<D, FP8>;
+    constexpr int THREADS = threads_of(FP8);
     constexpr int BLOCK = FP8 ? fp8_block_bytes(D) : block_bytes(D), HALF = half_bytes(D), CH = D / 8, KS = L::K_STAGES, VS = L::V_STAGES;
     constexpr uint32_t F16 = FP8 ? (1u << 7) | (1u << 10) : 0u;              // the operands' type bits: bf16, or neither
     constexpr uint32_t IDESC_QK = instr_desc(ROWS, KEYS, false) & ~F16, IDESC_PV = instr_desc(ROWS, D, !FP8) & ~F16;
@@ -203,7 +204,7 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
     };
 
     if (warp < 4) {
-        more_registers<200>();
+        more_registers<FP8 ? 160 : 200>();
         // =================== queries ===================
         float row_scale = 0.f;                             // FP8: the power of two that was taken out of this thread's row
         {
@@ -409,8 +410,10 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
             }
         }
     } else {
-        fewer_registers<56>();
-        const bool leader = elect_one(), values = (warp & 1) != 0;
+        if (!FP8) fewer_registers<56>();
+        else if (warp < 8) fewer_registers<48>();
+        else fewer_registers<32>();
+        const bool leader = elect_one(), values = FP8 && warp < 8 ? warp >= 6 : (warp & 1) != 0;
         const uint32_t output = tmem + COL_O;
         const uint64_t q_desc = swizzled_desc(q_smem);
         // scores of block kb from the K at k_desc / output of block kb from the V at v_desc, whose pages and halves of 8 tokens are
@@ -431,137 +434,136 @@ __global__ void __launch_bounds__(THREADS, 2) prefill_pages_kernel(const __grid_
             tc_commit(pv_done + 8 * (kb & 1));
         };
         if (FP8) {
-            // =================== conversion: 64 lanes for K, 64 for V; 4 and 5 issue, 6 and 7 copy ===================
-            const bool second = warp >= 6;
-            const int stages = values ? VS : KS, me = lane + (second ? 32 : 0);
+            const int stages = values ? VS : KS;
             const uint32_t ring = values ? v_ring : k_ring, stage_bytes = values ? L::V_STAGE : L::K_STAGE, tile = values ? v_tile : k_tile;
             const uint32_t full = values ? v_full : k_full, empty = values ? v_empty : k_empty, ready = values ? v_ready : k_ready, free = values ? v_free : k_free;
-            const uint64_t desc = values ? smem_desc(tile, D * 16, 128) : smem_desc(tile, 128, CH * 128);
-            // copies (the second warp): lane 4 (kb % 8) + j has entry j of block kb
-            int id = 0, next_id = 0;
-            auto copy = [&](int kb) {
-                if (kb >= blocks) return;
-                if (kb > 0 && (kb & 7) == 0) {
-                    id = next_id;
-                    next_id = id_at((kb + 8) * KB + lane);
-                }
-                const int st = kb % stages, np = listed - kb * KB < KB ? listed - kb * KB : KB, j = lane - (kb & 7) * KB;
-                if (kb >= stages) wait(empty + 8 * st, (uint32_t)((kb / stages - 1) & 1), gave_up);
-                if (lane == 0) mbar_expect_tx(full + 8 * st, (uint32_t)(np * (values ? PAGE * D : PAGE * D + 2 * PAGE * 4)));
-                __syncwarp();
-                if (j < 0 || j >= np) return;
-                const uint8_t *src = p.layer_base + (int64_t)id * p.page_stride + (int64_t)h * BLOCK;
-                const uint32_t dst = ring + (uint32_t)st * stage_bytes;
-                bulk_copy_g2s(dst + (uint32_t)(j * PAGE * D), src + (values ? fp8_v_off(D) : 0), PAGE * D, full + 8 * st);
-                if (!values) bulk_copy_g2s(dst + (uint32_t)(KEYS * D + j * 2 * PAGE * 4), src + fp8_ks_off(D), 2 * PAGE * 4, full + 8 * st);
-            };
-            if (second) {
-                id = id_at(lane);
-                next_id = id_at(32 + lane);
-                for (int kb = 0; kb < stages - 1; ++kb) copy(kb);
-            }
-            int page32 = page_at(lane), next32 = page_at(32 + lane);
-            if (warp == 4) wait(q_full, 0, gave_up);
-            for (int kb = 0; kb < blocks; ++kb) {
-                if (second) copy(kb + stages - 1);
-                if (kb > 0 && (kb & 7) == 0) {
-                    page32 = next32;
-                    next32 = page_at((kb + 8) * KB + lane);
-                }
-                const int st = kb % stages, np = listed - kb * KB < KB ? listed - kb * KB : KB;
-                const uint32_t from = ring + (uint32_t)st * stage_bytes;
-                // tokens that some row sees, of this lane's entry of the block
-                const uint32_t seen = bits_up_to(p1, page32);
-                wait(full + 8 * st, (uint32_t)((kb / stages) & 1), gave_up);
-                if (kb > 0) wait(free, (uint32_t)((kb - 1) & 1), gave_up);
-                if (!values) {
-                    // this lane's token: K scale into units of log2, V scale (0 where no row sees it)
-                    const uint32_t bits = __shfl_sync(FULL, seen, (kb & 7) * KB + me / PAGE);
-                    float ks = 0.f, vs = 0.f;
-                    if (me / PAGE < np && (bits >> (me % PAGE) & 1u)) {
-                        const uint32_t a = from + (uint32_t)(KEYS * D + (me / PAGE * 2 * PAGE + me % PAGE) * 4);
-                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ks) : "r"(a) : "memory");
-                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(vs) : "r"(a + PAGE * 4) : "memory");
+            if (warp < 8) {
+                // =================== conversion: 64 lanes for K, 64 for V ===================
+                const bool second = (warp & 1) != 0;
+                const int me = lane + (second ? 32 : 0);
+                int page32 = page_at(lane), next32 = page_at(32 + lane);
+                for (int kb = 0; kb < blocks; ++kb) {
+                    if (kb > 0 && (kb & 7) == 0) {
+                        page32 = next32;
+                        next32 = page_at((kb + 8) * KB + lane);
                     }
-                    const uint32_t stage = scale_ring + (uint32_t)((kb & 3) * L::SCALE_STAGE), to = stage + (uint32_t)(me * 4);
-                    const uint32_t most = __reduce_max_sync(FULL, __float_as_uint(vs));          // (0 or more; the bits of a NaN are above all)
-                    if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(stage + (uint32_t)(2 * KEYS * 4 + (second ? 4 : 0))), "r"(most) : "memory");
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(ks * p.scale_log2) : "memory");
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + KEYS * 4), "f"(vs) : "memory");
-                    // unit: 16 dims of a token; the units of a page are read together
-#pragma unroll 1
-                    for (int u0 = me; u0 < np * D; u0 += 2 * D) {
-                        uint4 w[D / 32];
-#pragma unroll
-                        for (int i = 0; i < D / 32; ++i) w[i] = ld_shared(from + (uint32_t)((u0 + 64 * i) * 16));
-#pragma unroll
-                        for (int i = 0; i < D / 32; ++i) {
-                            const int u = u0 + 64 * i, group = u / (D / 2), c = u / 8 % (D / 16), t = u & 7;
-                            uint4 x, y;
-                            convert16(w[i], x, y);
-                            st_shared(tile + (uint32_t)(((group * CH + 2 * c) * 8 + t) * 16), x);
-                            st_shared(tile + (uint32_t)(((group * CH + 2 * c + 1) * 8 + t) * 16), y);
+                    const int st = kb % stages, np = listed - kb * KB < KB ? listed - kb * KB : KB;
+                    const uint32_t from = ring + (uint32_t)st * stage_bytes;
+                    // tokens that some row sees, of this lane's entry of the block
+                    const uint32_t seen = bits_up_to(p1, page32);
+                    wait(full + 8 * st, (uint32_t)((kb / stages) & 1), gave_up);
+                    if (kb > 0) wait(free, (uint32_t)((kb - 1) & 1), gave_up);
+                    if (!values) {
+                        // this lane's token: K scale into units of log2, V scale (0 where no row sees it)
+                        const uint32_t bits = __shfl_sync(FULL, seen, (kb & 7) * KB + me / PAGE);
+                        float ks = 0.f, vs = 0.f;
+                        if (me / PAGE < np && (bits >> (me % PAGE) & 1u)) {
+                            const uint32_t a = from + (uint32_t)(KEYS * D + (me / PAGE * 2 * PAGE + me % PAGE) * 4);
+                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ks) : "r"(a) : "memory");
+                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(vs) : "r"(a + PAGE * 4) : "memory");
                         }
-                    }
-                } else {
-                    // unit: a dim of a page, 16 tokens
-                    const bool partial = __any_sync(FULL, seen != 0xFFFFu && lane >> 2 == (kb & 7));
+                        const uint32_t stage = scale_ring + (uint32_t)((kb & 3) * L::SCALE_STAGE), to = stage + (uint32_t)(me * 4);
+                        const uint32_t most = __reduce_max_sync(FULL, __float_as_uint(vs));          // (0 or more; the bits of a NaN are above all)
+                        if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(stage + (uint32_t)(2 * KEYS * 4 + (second ? 4 : 0))), "r"(most) : "memory");
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(ks * p.scale_log2) : "memory");
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + KEYS * 4), "f"(vs) : "memory");
+                        // unit: 16 dims of a token; the units of a page are read together
 #pragma unroll 1
-                    for (int u0 = me; u0 < np * D; u0 += 2 * D) {
-                        uint4 w[D / 32];
+                        for (int u0 = me; u0 < np * D; u0 += D) {
+                            uint4 w[D / 64];
 #pragma unroll
-                        for (int i = 0; i < D / 32; ++i) w[i] = ld_shared(from + (uint32_t)((u0 + 64 * i) * 16));
-                        if (partial)
+                            for (int i = 0; i < D / 64; ++i) w[i] = ld_shared(from + (uint32_t)((u0 + 64 * i) * 16));
 #pragma unroll
-                            for (int i = 0; i < D / 32; ++i) {
-                                const uint32_t bits = __shfl_sync(FULL, seen, (kb & 7) * KB + (u0 + 64 * i) / D);
-                                auto keep = [&](int k) {
-                                    const uint32_t f = bits >> (4 * k) & 0xFu;
-                                    return ((f & 1u) | (f & 2u) << 7 | (f & 4u) << 14 | (f & 8u) << 21) * 0xFFu;
-                                };
-                                w[i] = make_uint4(w[i].x & keep(0), w[i].y & keep(1), w[i].z & keep(2), w[i].w & keep(3));
+                            for (int i = 0; i < D / 64; ++i) {
+                                const int u = u0 + 64 * i, group = u / (D / 2), c = u / 8 % (D / 16), t = u & 7;
+                                uint4 x, y;
+                                convert16(w[i], x, y);
+                                st_shared(tile + (uint32_t)(((group * CH + 2 * c) * 8 + t) * 16), x);
+                                st_shared(tile + (uint32_t)(((group * CH + 2 * c + 1) * 8 + t) * 16), y);
                             }
+                        }
+                    } else {
+                        // unit: a dim of a page, 16 tokens
+                        const bool partial = __any_sync(FULL, seen != 0xFFFFu && lane >> 2 == (kb & 7));
+#pragma unroll 1
+                        for (int u0 = me; u0 < np * D; u0 += D) {
+                            uint4 w[D / 64];
 #pragma unroll
-                        for (int i = 0; i < D / 32; ++i) {
-                            const int u = u0 + 64 * i, j = u / D, dim = u % D;
-                            uint4 x, y;
-                            convert16(w[i], x, y);
-                            st_shared(tile + (uint32_t)(j * HALF + dim * 16), x);
-                            st_shared(tile + (uint32_t)(j * HALF + (D + dim) * 16), y);
+                            for (int i = 0; i < D / 64; ++i) w[i] = ld_shared(from + (uint32_t)((u0 + 64 * i) * 16));
+                            if (partial)
+#pragma unroll
+                                for (int i = 0; i < D / 64; ++i) {
+                                    const uint32_t bits = __shfl_sync(FULL, seen, (kb & 7) * KB + (u0 + 64 * i) / D);
+                                    auto keep = [&](int k) {
+                                        const uint32_t f = bits >> (4 * k) & 0xFu;
+                                        return ((f & 1u) | (f & 2u) << 7 | (f & 4u) << 14 | (f & 8u) << 21) * 0xFFu;
+                                    };
+                                    w[i] = make_uint4(w[i].x & keep(0), w[i].y & keep(1), w[i].z & keep(2), w[i].w & keep(3));
+                                }
+#pragma unroll
+                            for (int i = 0; i < D / 64; ++i) {
+                                const int u = u0 + 64 * i, j = u / D, dim = u % D;
+                                uint4 x, y;
+                                convert16(w[i], x, y);
+                                st_shared(tile + (uint32_t)(j * HALF + dim * 16), x);
+                                st_shared(tile + (uint32_t)(j * HALF + (D + dim) * 16), y);
+                            }
                         }
                     }
-                }
-                fence_proxy_async();                   // the tensor core reads the tile through the async proxy
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(empty + 8 * st);
-                    mbar_arrive(ready);
-                }
-                if (second) continue;
-                wait(ready, (uint32_t)(kb & 1), gave_up);
-                if (!values) {
-                    if (kb >= 2) wait(pv_done + 8 * (kb & 1), (uint32_t)((kb / 2 - 1) & 1), gave_up);       // the buffer: P V two blocks back is over
-                    tc_fence_after();
-                    if (leader) {
-                        issue_scores(kb, desc);
-                        tc_commit(free);
-                    }
-                } else {
-                    wait(p_ready + 8 * (kb & 1), (uint32_t)((kb >> 1) & 1), gave_up);
-                    tc_fence_after();
-                    if (leader) {
-                        issue_output(kb, desc);
-                        tc_commit(free);
+                    fence_proxy_async();               // the tensor core reads the tile through the async proxy
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(ready);
+                        mbar_arrive(empty + 8 * st);
                     }
                 }
-                __syncwarp();
-            }
-            // the last commit arrives, and the last copies (waited for above, but for a failure: then it is not known which are still in
-            // flight, and they are given time), while there is somewhere to arrive
-            wait(free, (uint32_t)((blocks - 1) & 1), gave_up);
-            if (second && *gave_up) {
-                const uint64_t t = global_timer_ns();
-                while (global_timer_ns() - t < 1000000ull) __nanosleep(1000);
+            } else if (warp < 10) {
+                // =================== tensor-core issue: the whole warp walks along, one lane issues ===================
+                const uint64_t desc = values ? smem_desc(tile, D * 16, 128) : smem_desc(tile, 128, CH * 128);
+                if (!values) wait(q_full, 0, gave_up);
+                for (int kb = 0; kb < blocks; ++kb) {
+                    const uint32_t bar = 8 * ((uint32_t)kb & 1u), turn = (uint32_t)(kb >> 1);
+                    if (!values) {
+                        if (kb >= 2) wait(pv_done + bar, (turn - 1) & 1u, gave_up);        // the buffer: P V two blocks back is over
+                        wait(ready, (uint32_t)(kb & 1), gave_up);
+                        tc_fence_after();
+                        if (leader) issue_scores(kb, desc);
+                    } else {
+                        wait(ready, (uint32_t)(kb & 1), gave_up);
+                        wait(p_ready + bar, turn & 1u, gave_up);
+                        tc_fence_after();
+                        if (leader) issue_output(kb, desc);
+                    }
+                    if (leader) tc_commit(free);
+                    __syncwarp();
+                }
+                wait(free, (uint32_t)((blocks - 1) & 1), gave_up);       // the last commit arrives while the barriers are still there
+            } else {
+                // =================== copies ===================
+                int id = id_at(lane), next_id = id_at(32 + lane);        // lane 4 (kb % 8) + j has entry j of block kb
+                for (int kb = 0; kb < blocks; ++kb) {
+                    if (kb > 0 && (kb & 7) == 0) {
+                        id = next_id;
+                        next_id = id_at((kb + 8) * KB + lane);
+                    }
+                    const int st = kb % stages, np = listed - kb * KB < KB ? listed - kb * KB : KB, j = lane - (kb & 7) * KB;
+                    if (kb >= stages) wait(empty + 8 * st, (uint32_t)((kb / stages - 1) & 1), gave_up);
+                    if (lane == 0) mbar_expect_tx(full + 8 * st, (uint32_t)(np * (values ? PAGE * D : PAGE * D + 2 * PAGE * 4)));
+                    __syncwarp();
+                    if (j >= 0 && j < np) {
+                        const uint8_t *src = p.layer_base + (int64_t)id * p.page_stride + (int64_t)h * BLOCK;
+                        const uint32_t dst = ring + (uint32_t)st * stage_bytes;
+                        bulk_copy_g2s(dst + (uint32_t)(j * PAGE * D), src + (values ? fp8_v_off(D) : 0), PAGE * D, full + 8 * st);
+                        if (!values) bulk_copy_g2s(dst + (uint32_t)(KEYS * D + j * 2 * PAGE * 4), src + fp8_ks_off(D), 2 * PAGE * 4, full + 8 * st);
+                    }
+                    __syncwarp();
+                }
+                // leave only when every copy has landed (as on bf16 pages)
+                for (int j = blocks > stages ? blocks - stages : 0; j < blocks; ++j) wait(full + 8 * (j % stages), (uint32_t)((j / stages) & 1), gave_up);
+                if (*gave_up) {
+                    const uint64_t t = global_timer_ns();
+                    while (global_timer_ns() - t < 1000000ull) __nanosleep(1000);
+                }
             }
         } else if (warp < 6) {
             // =================== tensor-core issue: the whole warp walks along, one lane issues ===================
@@ -675,7 +677,7 @@ cudaError_t launch_t(const PrefillParams &p, const PageLists &l, int G, int max_
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ctas);
-    cfg.blockDim = dim3(THREADS);
+    cfg.blockDim = dim3(threads_of(FP8));
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
