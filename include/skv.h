@@ -538,8 +538,8 @@ int skv_page_list_width(int top, int first_pages, int last_pages, int run, int *
  *   counts     device int32 [batch * ceil(max_q_len / run)][kv_heads]; 0 for a run that a
  *              sequence has no rows for
  *   list_stride  at least the smaller of skv_page_list_width and pt_stride
- * min(run, max_q_len) * q_heads / kv_heads may be 128 at most, pt_stride 45056
- * (SKV_ERR_UNSUPPORTED).  A sequence that does not fit raises SKV_ERR_BOUNDS and gets
+ * min(run, max_q_len) * q_heads / kv_heads may be 128 at most, pt_stride 45056, or 28672
+ * where that product is above 16 (SKV_ERR_UNSUPPORTED).  A sequence that does not fit raises SKV_ERR_BOUNDS and gets
  * empty lists, or without cu_q_lens is cut to pt_stride pages; so does a page id out of
  * range (the page is scored as page 0).  One launch.  Errors as skv_decode_attn, and
  * SKV_ERR_ARG without an index. */

@@ -1391,7 +1391,7 @@ int skv_select_pages(skv_cache *c, int layer, const void *Q, const int32_t *cu_q
     if (list_stride < (width < pt_stride ? width : pt_stride)) return SKV_ERR_ARG;
     const int rr = check_runs(batch, max_q_len, run, q_heads / c->kv_heads, &per_seq);
     if (rr) return rr;
-    if (pt_stride > select_max_pages()) return SKV_ERR_UNSUPPORTED;
+    if (pt_stride > select_max_pages((run < max_q_len ? run : max_q_len) * (q_heads / c->kv_heads))) return SKV_ERR_UNSUPPORTED;
     SelectParams p;
     int8_t *codes;
     float *scales;

@@ -57,7 +57,7 @@ struct PageLists {
 };
 
 cudaError_t launch_index_pages(const IndexParams &p, int D, bool fp8, bool pdl, cudaStream_t s);
-int select_max_pages();         // of a sequence
+int select_max_pages(int columns);      // of a sequence; columns: min(run, max_q_len) * G
 cudaError_t launch_select_pages(const SelectParams &p, int D, int sm_count, bool pdl, cudaStream_t s);
 // decode attention over listed pages (skv_decode_pages.cu); kernel as in launch_decode_splitk.  p.cu_q: rows of chunks, a row as a
 // sequence of its own (p.B = sequences * p.max_q_len)

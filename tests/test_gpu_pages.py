@@ -205,6 +205,12 @@ def test_selection_in_long_caches(batch):
     for top in (100, 1999):
         lists, counts = p.select(q, top, 1, 8)
         p.check(q, lists, counts, top, 1, 8)
+    if batch == 3:                                            # many columns
+        new = [20, 9, 31]
+        q = torch.randn(sum(new), 4, 64, generator=p.g).bfloat16()
+        for run in (9, 31):
+            lists, counts = p.select(q, 300, 2, 3, new, 31, run)
+            p.check(q, lists, counts, 300, 2, 3, new, 31, run)
 
 
 def test_selection_with_unusual_queries():
