@@ -16,6 +16,16 @@ __host__ __device__ inline int64_t index_layer_bytes(int64_t max_pages, int Hkv,
     return index_codes_bytes(max_pages, Hkv, D) + (max_pages * Hkv * 4 + 255) / 256 * 256;
 }
 
+// Rows of a run, of which `left` are there.  As an instruction of its own: written as a comparison, the lesser of the two came out as
+// run in kernels that take it from a __grid_constant__ parameter (nvcc 12.9.86, whole kernels only, not where the value was also printed), and
+// rows behind the last were read and written.
+__device__ __forceinline__ int rows_of_run(int left, int run)
+{
+    int r;
+    asm volatile("min.s32 %0, %1, %2;" : "=r"(r) : "r"(left), "r"(run));
+    return r;
+}
+
 struct IndexParams {
     const uint8_t *layer_base;  // first page of the owner layer
     int64_t page_stride;

@@ -140,16 +140,15 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
     pdl_wait();
     const int pair = (int)blockIdx.x / l.per_seq, r = (int)blockIdx.x - pair * l.per_seq, b = pair / p.Hkv, h = pair - b * p.Hkv;
     const int64_t list_no = ((int64_t)b * l.per_seq + r) * p.Hkv + h;
-    // The item, worked out by one warp and handed over in shared memory.  (Worked out by every thread for itself, the lesser of run and
-    // the rows that are left came out as run in code compiled by nvcc 12.9.86, though not where it was also printed.)
+    // The item, worked out by one warp and handed over in shared memory.
     if (warp == 4) {
         const int q_begin = __ldg(p.cu_q + b), q_len = __ldg(p.cu_q + b + 1) - q_begin, n = __ldg(p.seq_lens + b);
-        const int64_t at = (int64_t)r * l.run;                           // the run's first row
+        const int at = r * l.run;                                        // the run's first row (below max_q_len, since r < per_seq)
         int rows = 0, listed = 0;
         if (q_begin < 0 || q_len < 0 || q_len > n || q_len > max_q_len || (int64_t)n > (int64_t)p.pt_stride * PAGE) {
             if (r == 0 && h == 0 && lane == 0) atomicOr(p.status, STATUS_BOUNDS);
         } else if (at < q_len) {
-            rows = q_len - (int)at < l.run ? q_len - (int)at : l.run;
+            rows = rows_of_run(q_len - at, l.run);
             listed = __ldg(l.counts + list_no);
             if (listed > l.stride) {
                 listed = l.stride;
@@ -158,9 +157,9 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
         }
         if (lane == 0) {
             item[0] = rows;
-            item[1] = n - q_len + (int)at;
+            item[1] = n - q_len + at;
             item[2] = n;
-            item[3] = q_begin + (int)at;
+            item[3] = q_begin + at;
             item[4] = listed;
         }
         if (rows > 0 && listed > 0) {

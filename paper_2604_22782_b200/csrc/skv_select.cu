@@ -30,10 +30,9 @@ using chunk::swizzled_desc;
 constexpr unsigned FULL = 0xFFFFFFFFu;
 constexpr int WARPS = 8, THREADS = WARPS * 32;
 constexpr int BINS = 2048;
-constexpr int HELD = 8;                // scores of a segment that a thread keeps in registers: THREADS * HELD pages of it
 constexpr int FEW = 16;                // columns up to which mma.sync does
 constexpr int MAX_PAGES = 45056, MAX_PAGES_MANY = 28672;      // of a sequence: the scores of a segment are in one CTA's shared memory
-constexpr int WORDS = 256;             // of shared memory that choose() has for itself
+constexpr int WORDS = 96;              // of shared memory, for choose() and what comes before it
 
 // D(16x8, s32) += A(16x32, s8, row) * B(32x8, s8, col)
 __device__ __forceinline__ void mma_s8_16832(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
@@ -69,11 +68,11 @@ __device__ __forceinline__ Run run_of(const SelectParams &p, int list, bool repo
             if (report && i == 0) atomicOr(p.status, STATUS_BOUNDS);
             return r;
         }
-        const int64_t at = (int64_t)i * p.run;
+        const int at = i * p.run;              // (below max_q_len, since i < per_seq)
         if (at >= len) return r;
-        r.row = first + (int)at;
-        r.rows = len - (int)at < p.run ? len - (int)at : p.run;
-        pos = n - len + (int)at;
+        r.row = first + at;
+        r.rows = rows_of_run(len - at, p.run);
+        pos = n - len + at;
     } else {
         if (n <= 0) return r;
         if ((int64_t)n > (int64_t)p.pt_stride * PAGE) {
@@ -103,7 +102,10 @@ __device__ __forceinline__ void list_all(const SelectParams &p, int seg, const R
 
 __device__ __forceinline__ void sync_threads() { asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory"); }
 
-// 8 dims of a row in steps: [max(c, 0)] and [min(c, 0)], a byte each; an element that is not finite counts as 0
+// (What runs once in a CTA is kept small below, loops rolled: straight code that is new to the SM comes in at some 10 cycles an
+// instruction, and made the queries' codes take 10000 cycles, choose() 8000.)
+
+// the largest of a piece of 8 dims; an element that is not finite counts as 0
 __device__ __forceinline__ uint32_t magnitude(uint32_t bits) { return bits >= 0x7F80u ? 0u : bits; }
 __device__ __forceinline__ uint32_t largest(const uint4 &w)
 {
@@ -113,19 +115,28 @@ __device__ __forceinline__ uint32_t largest(const uint4 &w)
     for (int k = 0; k < 4; ++k) top = max(top, max(magnitude(x[k] & 0x7FFFu), magnitude(x[k] >> 16 & 0x7FFFu)));
     return top;
 }
+// two dims in steps, in the low bytes: x * inv is 127 and a rounding at most, or x was not finite
+__device__ __forceinline__ uint32_t step_of(float x, float inv)
+{
+    const float y = __fmul_rn(x, inv);
+    return __float_as_uint(__fadd_rn(fabsf(y) < 128.f ? y : 0.f, 12582912.f));      // 1.5 * 2^23: the nearest whole number is in the low bits
+}
+// 8 dims of a row in steps: [max(c, 0)] and [min(c, 0)], a byte each
 __device__ __forceinline__ void steps_of(const uint4 &w, float inv, uint2 &up, uint2 &down)
 {
     const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-    uint32_t u[2] = {0, 0}, d[2] = {0, 0};
+    uint32_t c[2];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const uint32_t bits = (k & 1) ? x[k / 2] >> 16 : x[k / 2] & 0xFFFFu;
-        const int c = magnitude(bits & 0x7FFFu) ? __float2int_rn(__uint_as_float(bits << 16) * inv) : 0;
-        u[k / 4] |= ((uint32_t)max(c, 0) & 0xFFu) << (8 * (k & 3));
-        d[k / 4] |= ((uint32_t)min(c, 0) & 0xFFu) << (8 * (k & 3));
+    for (int k = 0; k < 2; ++k) {
+        const uint32_t lo = __byte_perm(step_of(bf16_lo(x[2 * k]), inv), step_of(bf16_hi(x[2 * k]), inv), 0x0040);
+        const uint32_t hi = __byte_perm(step_of(bf16_lo(x[2 * k + 1]), inv), step_of(bf16_hi(x[2 * k + 1]), inv), 0x0040);
+        c[k] = __byte_perm(lo, hi, 0x5410);
     }
-    up = make_uint2(u[0], u[1]);
-    down = make_uint2(d[0], d[1]);
+    uint32_t sign0, sign1;                     // every byte's sign, all over it
+    asm("prmt.b32 %0, %1, 0, 0xba98;" : "=r"(sign0) : "r"(c[0]));
+    asm("prmt.b32 %0, %1, 0, 0xba98;" : "=r"(sign1) : "r"(c[1]));
+    up = make_uint2(c[0] & ~sign0, c[1] & ~sign1);
+    down = make_uint2(c[0] & sign0, c[1] & sign1);
 }
 // 127 / a for the largest element's bits in words[0 .. WARPS) (one of each warp's threads), which all THREADS have written
 __device__ __forceinline__ float steps_per_unit(const uint32_t *words, int lane)
@@ -134,83 +145,85 @@ __device__ __forceinline__ float steps_per_unit(const uint32_t *words, int lane)
     return amax < INDEX_TINY ? 0.f : __fdiv_rn(127.f, amax);
 }
 
-// By THREADS threads: the list of a run whose scores' numbers are keys[0 .. run.scored), more than p.top of them.
-// bins [BINS] and words [WORDS] are its own.
-__device__ void choose(const SelectParams &p, int seg, const Run &run, const uint32_t *keys, uint32_t *bins, uint32_t *words, int tid)
+// The least and the largest of a segment's numbers, as they are written: one for each of lo_hi[0], lo_hi[1] of the first CTA
+__device__ __forceinline__ void note_range(uint32_t lo_hi, uint32_t lo, uint32_t hi, int lane)
 {
-    const int lane = tid & 31, warp = tid >> 5, n = p.top > 0 ? run.scored : 0;
-    int32_t *out = p.lists + (int64_t)seg * p.stride;
-    // (a page that is not there: 0, below every score's number, which is 0x007FFFFF at least)
-    uint32_t held[HELD];
-    uint32_t lo = 0xFFFFFFFFu, hi = 0;
-#pragma unroll
-    for (int j = 0; j < HELD; ++j) {
-        held[j] = j * THREADS + tid < n ? keys[j * THREADS + tid] : 0u;
-        lo = min(lo, held[j] - 1);             // (0 wraps to the top)
-        hi = max(hi, held[j]);
-    }
-    for (int i = HELD * THREADS + tid; i < n; i += THREADS) {
-        lo = min(lo, keys[i] - 1);
-        hi = max(hi, keys[i]);
-    }
     lo = __reduce_min_sync(FULL, lo);
     hi = __reduce_max_sync(FULL, hi);
     if (lane == 0) {
-        words[warp] = lo;
-        words[WARPS + warp] = hi;
+        asm volatile("red.relaxed.cluster.shared::cluster.min.u32 [%0], %1;" ::"r"(lo_hi), "r"(lo) : "memory");
+        asm volatile("red.relaxed.cluster.shared::cluster.max.u32 [%0], %1;" ::"r"(lo_hi + 4), "r"(hi) : "memory");
     }
-    for (int i = tid; i < BINS / 4; i += THREADS) reinterpret_cast<uint4 *>(bins)[i] = make_uint4(0, 0, 0, 0);
-    if (tid == 0) words[48] = 0;
-    sync_threads();
-    lo = __reduce_min_sync(FULL, words[lane & (WARPS - 1)]) + 1;
-    hi = __reduce_max_sync(FULL, words[WARPS + (lane & (WARPS - 1))]);
+}
+
+// By THREADS threads: the list of a run whose scores' numbers are keys[0 .. run.scored), more than p.top of them, the least and the largest
+// in words[0] and words[1].  keys and bins [BINS] are aligned to 16 bytes (keys may be read up to 7 past the end); bins and
+// words [2 .. WORDS) are its own.  A thread has 8 pages in a row, a round of the threads 2048; where there is one round they stay in registers.
+__device__ __forceinline__ void choose(const SelectParams &p, int seg, const Run &run, const uint32_t *keys, uint32_t *bins, uint32_t *words, int tid)
+{
+    constexpr int MINE = 8, ROUND = THREADS * MINE;
+    const int lane = tid & 31, warp = tid >> 5, n = p.top > 0 ? run.scored : 0;
+    int32_t *out = p.lists + (int64_t)seg * p.stride;
+    uint32_t k[MINE];
+    auto load = [&](int r0) {                  // (0 where there is none, which is below every score's number)
+        const int i = r0 + tid * MINE;
+        uint4 u = make_uint4(0, 0, 0, 0), v = u;
+        if (i < n) {
+            u = *reinterpret_cast<const uint4 *>(keys + i);
+            v = *reinterpret_cast<const uint4 *>(keys + i + 4);
+        }
+        const uint32_t x[MINE] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int m = 0; m < MINE; ++m) k[m] = i + m < n ? x[m] : 0u;
+    };
+    uint32_t lo = words[0], hi = words[1];
     // everything above `limit` is taken, and the first `ties` that equal it
     uint32_t limit = 0xFFFFFFFFu;              // (no score's number: that of NaN)
     int need = p.top, ties = 0;
     int shift = 32 - __clz((int)(hi - lo));    // 2^shift > hi - lo
     shift = shift > 11 ? shift - 11 : 0;
+    load(0);
     while (need > 0) {
+#pragma unroll 1
+        for (int i = tid; i < BINS / 4; i += THREADS) reinterpret_cast<uint4 *>(bins)[i] = make_uint4(0, 0, 0, 0);
+        if (tid == 0) words[2] = 0;
+        sync_threads();
+#pragma unroll 1
+        for (int r0 = 0; r0 < n; r0 += ROUND) {
+            if (n > ROUND) load(r0);
 #pragma unroll
-        for (int j = 0; j < HELD; ++j)
-            if (held[j] >= lo && held[j] <= hi) atomicAdd(&bins[(held[j] - lo) >> shift], 1u);
-        for (int i = HELD * THREADS + tid; i < n; i += THREADS) {
-            const uint32_t k = keys[i];
-            if (k >= lo && k <= hi) atomicAdd(&bins[(k - lo) >> shift], 1u);
+            for (int m = 0; m < MINE; ++m)
+                if (k[m] >= lo && k[m] <= hi) atomicAdd(&bins[(k[m] - lo) >> shift], 1u);
         }
         sync_threads();
         // bins from the top: the one where the count passes `need`
-        uint32_t mine[BINS / THREADS], sum = 0;
         const int from = BINS - (tid + 1) * (BINS / THREADS);          // thread 0 has the highest bins
-#pragma unroll
-        for (int i = 0; i < BINS / THREADS; i += 4) {
-            const uint4 w = *reinterpret_cast<const uint4 *>(bins + from + i);
-            mine[i] = w.x;
-            mine[i + 1] = w.y;
-            mine[i + 2] = w.z;
-            mine[i + 3] = w.w;
-            sum += w.x + w.y + w.z + w.w;
-        }
+        static_assert(BINS / THREADS == 8, "two loads a thread");
+        const uint4 u = *reinterpret_cast<const uint4 *>(bins + from), v = *reinterpret_cast<const uint4 *>(bins + from + 4);
+        const uint32_t sum = u.x + u.y + u.z + u.w + v.x + v.y + v.z + v.w;
         uint32_t above = sum;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const uint32_t u = __shfl_up_sync(FULL, above, d);
-            if (lane >= d) above += u;
+            const uint32_t o = __shfl_up_sync(FULL, above, d);
+            if (lane >= d) above += o;
         }
         if (lane == 31) words[16 + warp] = above;
         sync_threads();
-        for (int w = 0; w < warp; ++w) above += words[16 + w];
-        above -= sum;                          // in the bins above this thread's
+        uint32_t others = lane < warp ? words[16 + lane] : 0u;
+        others = __reduce_add_sync(FULL, others);
+        above += others - sum;                 // in the bins above this thread's
         if (above < (uint32_t)need && (uint32_t)need <= above + sum) {
+            const uint32_t mine[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
             bool found = false;
 #pragma unroll
-            for (int i = BINS / THREADS - 1; i >= 0; --i) {
+            for (int i = 7; i >= 0; --i) {
                 if (!found && (uint32_t)need <= above + mine[i]) {
                     found = true;
                     words[24] = (uint32_t)(from + i);
                     words[25] = above;
                     words[26] = mine[i];
                 }
-                if (!found) above += mine[i];
+                above += mine[i];
             }
         }
         sync_threads();
@@ -218,7 +231,7 @@ __device__ void choose(const SelectParams &p, int seg, const Run &run, const uin
         lo += bin << shift;
         need -= (int)higher;
         if ((uint32_t)need == in_bin) {        // the bin as a whole
-            limit = lo - 1;
+            limit = lo - 1;                    // (a score's number is 0x007FFFFF at least)
             break;
         }
         if (shift == 0) {                      // scores that are equal
@@ -229,71 +242,64 @@ __device__ void choose(const SelectParams &p, int seg, const Run &run, const uin
         hi = lo + ((1u << shift) - 1);
         if (in_bin <= 32) {
             // a warp's worth: its need-th largest by comparison.  (Which of equal ones is whose does not matter here: limit and ties do.)
-            auto note = [&](uint32_t k) {
-                if (k >= lo && k <= hi) words[64 + atomicAdd(&words[48], 1u)] = k;
-            };
+#pragma unroll 1
+            for (int r0 = 0; r0 < n; r0 += ROUND) {
+                if (n > ROUND) load(r0);
 #pragma unroll
-            for (int j = 0; j < HELD; ++j) note(held[j]);
-            for (int i = HELD * THREADS + tid; i < n; i += THREADS) note(keys[i]);
-            sync_threads();
-            const uint32_t k = lane < (int)in_bin ? words[64 + lane] : 0u;
-            int higher_ones = 0, equal_before = 0;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                const uint32_t o = __shfl_sync(FULL, k, i);
-                higher_ones += o > k;
-                equal_before += o == k && i < lane;
+                for (int m = 0; m < MINE; ++m)
+                    if (k[m] >= lo && k[m] <= hi) words[32 + atomicAdd(&words[2], 1u)] = k[m];
             }
-            const unsigned at = __ballot_sync(FULL, k != 0u && higher_ones + equal_before == need - 1);
-            const int who = __ffs(at) - 1;
-            limit = __shfl_sync(FULL, k, who);
+            sync_threads();
+            const uint32_t c = lane < (int)in_bin ? words[32 + lane] : 0u;
+            int higher_ones = 0, equal_before = 0;
+#pragma unroll 1
+            for (int i = 0; i < (int)in_bin; ++i) {
+                const uint32_t o = __shfl_sync(FULL, c, i);
+                higher_ones += o > c;
+                equal_before += o == c && i < lane;
+            }
+            const int who = __ffs(__ballot_sync(FULL, c != 0u && higher_ones + equal_before == need - 1)) - 1;
+            limit = __shfl_sync(FULL, c, who);
             ties = need - __shfl_sync(FULL, higher_ones, who);
             break;
         }
-        sync_threads();
-        for (int i = tid; i < BINS / 4; i += THREADS) reinterpret_cast<uint4 *>(bins)[i] = make_uint4(0, 0, 0, 0);
-        sync_threads();
         shift = shift > 11 ? shift - 11 : 0;
     }
-    // ---- the list, ascending: 32 pages a warp at a time, their places from the counts of those before them ----
-    const unsigned lower = (1u << lane) - 1;
-    int taken = 0, same = 0;                   // of the pages before the round; those that equal the limit
-    for (int i0 = 0; i0 < n; i0 += HELD * THREADS) {
-        unsigned gt[HELD], eq[HELD];
+    // ---- the list, ascending ----
+    int taken = 0, same = 0;                   // of the rounds before; those that equal the limit
+#pragma unroll 1
+    for (int r0 = 0; r0 < n; r0 += ROUND) {
+        if (n > ROUND) load(r0);
+        uint32_t mine = 0;                     // above the limit | << 16 equal to it (at most 2048 of each in a round)
 #pragma unroll
-        for (int j = 0; j < HELD; ++j) {
-            if (i0 > 0) {
-                const int i = i0 + j * THREADS + tid;
-                held[j] = i < n ? keys[i] : 0u;
-            }
-            gt[j] = __ballot_sync(FULL, held[j] > limit);
-            eq[j] = __ballot_sync(FULL, held[j] == limit);
-            if (lane == 0) words[128 + j * WARPS + warp] = (uint32_t)(__popc(gt[j]) | __popc(eq[j]) << 16);
-        }
-        sync_threads();
-        // two counts a lane, in order
-        const uint32_t c0 = words[128 + 2 * lane], c1 = words[128 + 2 * lane + 1];
-        uint32_t sum = c0 + c1;                // (both halves at once: at most 2048 in each)
+        for (int m = 0; m < MINE; ++m) mine += (k[m] > limit ? 1u : 0u) + (k[m] == limit ? 0x10000u : 0u);
+        uint32_t before = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const uint32_t u = __shfl_up_sync(FULL, sum, d);
-            if (lane >= d) sum += u;
+            const uint32_t o = __shfl_up_sync(FULL, before, d);
+            if (lane >= d) before += o;
         }
-        const uint32_t all = __shfl_sync(FULL, sum, 31), before0 = sum - c0 - c1, before1 = sum - c1;
+        if (lane == 31) words[64 + warp] = before;
+        sync_threads();
+        const uint32_t w = lane < WARPS ? words[64 + lane] : 0u;
+        const uint32_t all = __reduce_add_sync(FULL, w), others = __reduce_add_sync(FULL, lane < warp ? w : 0u);
+        before += others - mine;
+        int place = taken + (int)(before & 0xFFFFu), equal = same + (int)(before >> 16);
+        if (mine)
 #pragma unroll
-        for (int j = 0; j < HELD; ++j) {
-            const int x = j * WARPS + warp;
-            const uint32_t b0 = __shfl_sync(FULL, before0, x / 2), b1 = __shfl_sync(FULL, before1, x / 2), before = x & 1 ? b1 : b0;
-            const int eq_before = same + (int)(before >> 16) + __popc(eq[j] & lower);
-            if (held[j] > limit || (held[j] == limit && eq_before < ties))
-                out[run.first + taken + (int)(before & 0xFFFFu) + __popc(gt[j] & lower) + (eq_before < ties ? eq_before : ties)] = run.first + i0 + j * THREADS + tid;
-        }
+            for (int m = 0; m < MINE; ++m) {
+                if (k[m] > limit || (k[m] == limit && equal < ties)) out[run.first + place + (equal < ties ? equal : ties)] = run.first + r0 + tid * MINE + m;
+                place += k[m] > limit;
+                equal += k[m] == limit;
+            }
         taken += (int)(all & 0xFFFFu);
         same += (int)(all >> 16);
-        if (i0 + HELD * THREADS < n) sync_threads();
+        if (r0 + ROUND < n) sync_threads();
     }
     const int tail = run.first + p.top, total = tail + run.end - run.last;
+#pragma unroll 1
     for (int i = tid; i < run.first; i += THREADS) out[i] = i;
+#pragma unroll 1
     for (int i = tail + tid; i < p.stride; i += THREADS) out[i] = i < total ? run.last + i - tail : -1;
     if (tid == 0) p.counts[seg] = total;
 }
@@ -303,10 +309,10 @@ __device__ void choose(const SelectParams &p, int seg, const Run &run, const uin
 template <int D>
 __host__ __device__ constexpr int code_row() { return 2 * D + 64; }        // (two rows that a load touches at once are not in the same banks)
 template <int D>
-size_t few_smem_bytes(int most, int nt) { return (size_t)((most + 3) & ~3) * 4 + BINS * 4 + (size_t)nt * 8 * code_row<D>() + WORDS * 4; }
+size_t few_smem_bytes(int most, int nt) { return (size_t)((most + 7) & ~7) * 4 + BINS * 4 + (size_t)nt * 8 * code_row<D>() + WORDS * 4; }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(THREADS, 3) select_few_kernel(SelectParams p, int G)
+__global__ void __launch_bounds__(THREADS, 3) select_few_kernel(const __grid_constant__ SelectParams p, int G)
 {
     extern __shared__ __align__(16) uint8_t smem_raw[];
     constexpr int J = 2 * D / 64;              // pieces of 64 bytes of an entry
@@ -316,9 +322,13 @@ __global__ void __launch_bounds__(THREADS, 3) select_few_kernel(SelectParams p, 
     uint32_t rank, ranks;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ranks));
-    uint32_t *keys = reinterpret_cast<uint32_t *>(smem_raw), *bins = keys + ((p.most + 3) & ~3);
+    uint32_t *keys = reinterpret_cast<uint32_t *>(smem_raw), *bins = keys + ((p.most + 7) & ~7);
     uint8_t *q_codes = reinterpret_cast<uint8_t *>(bins + BINS);
     uint32_t *words = reinterpret_cast<uint32_t *>(q_codes + NT * 8 * ROW);
+    if (tid == 0) {
+        words[0] = 0xFFFFFFFFu;
+        words[1] = 0;
+    }
     pdl_wait();
     pdl_trigger();
     if (ranks > 1) cluster_arrive();           // (the first CTA has to be there before anyone writes to it)
@@ -376,9 +386,9 @@ __global__ void __launch_bounds__(THREADS, 3) select_few_kernel(SelectParams p, 
 #pragma unroll
         for (int m = 0; m < MINE; ++m) top = max(top, largest(w[m]));
         top = __reduce_max_sync(FULL, top);
-        if (lane == 0) words[warp] = top;
+        if (lane == 0) words[4 + warp] = top;
         __syncthreads();
-        const float inv = steps_per_unit(words, lane);
+        const float inv = steps_per_unit(words + 4, lane);
 #pragma unroll
         for (int m = 0; m < MINE; ++m) {
             const int i = tid + m * THREADS, col = i / (D / 8), piece = i % (D / 8);
@@ -395,6 +405,7 @@ __global__ void __launch_bounds__(THREADS, 3) select_few_kernel(SelectParams p, 
         uint32_t to;                           // the first CTA's scores
         asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(to) : "r"(smem_u32(keys)));
         const uint8_t *mine = q_codes + g * ROW + tig * 16;
+        uint32_t least = 0xFFFFFFFFu, most = 0;
         for (; t < t_to; t += WARPS) {
             int best0 = -0x7FFFFFFF, best1 = -0x7FFFFFFF;
 #pragma unroll
@@ -420,9 +431,16 @@ __global__ void __launch_bounds__(THREADS, 3) select_few_kernel(SelectParams p, 
                 best1 = max(best1, __shfl_xor_sync(FULL, best1, x));
             }
             const int i = t * 16 + g + 8 * tig;
-            if (tig < 2 && i < run.scored)
-                asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to + 4u * (uint32_t)i), "r"(key_of(tig ? best1 : best0, my_scale)) : "memory");
+            if (tig < 2 && i < run.scored) {
+                const uint32_t key = key_of(tig ? best1 : best0, my_scale);
+                least = min(least, key);
+                most = max(most, key);
+                asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to + 4u * (uint32_t)i), "r"(key) : "memory");
+            }
         }
+        uint32_t range;
+        asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(range) : "r"(smem_u32(words)));
+        note_range(range, least, most, lane);
     } else if (ranks > 1) {
         cluster_wait();
     }
@@ -440,7 +458,7 @@ __global__ void __launch_bounds__(THREADS, 3) select_few_kernel(SelectParams p, 
 // ---- many columns ----------------------------------------------------------------------------------------------------
 constexpr int TILE = 128;              // pages of a tile
 constexpr int MANY_THREADS = THREADS + 32;
-constexpr int A_STAGES = 2;
+constexpr int A_STAGES = 4;            // of the ring of pages' codes; a stage is 128 bytes of each page of a tile
 
 __device__ __forceinline__ void umma_i8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
 {
@@ -451,30 +469,29 @@ __device__ __forceinline__ void umma_i8(uint32_t d_tmem, uint64_t a_desc, uint64
         : "memory");
 }
 
-// Shared memory from a 1024-byte boundary on: pages' codes [A_STAGES][2 D / 128][128 pages][128 B] in the 128-byte swizzle (the bins, once
-// all scores are there) | columns' codes [2 D / 128][N][128 B], the same | scores [most] | words [WORDS] | barriers
+// Shared memory from a 1024-byte boundary on: pages' codes [A_STAGES][128 pages][128 B] in the 128-byte swizzle (the bins, once all scores
+// are there) | columns' codes [2 D / 128][N][128 B], the same | scores [most] | words [WORDS] | barriers
+constexpr int STAGE = TILE * 128;
 template <int D>
-__host__ __device__ constexpr int a_stage_bytes() { return TILE * 2 * D; }
-template <int D>
-size_t many_smem_bytes(int most, int N) { return 1024 + A_STAGES * (size_t)a_stage_bytes<D>() + (size_t)N * 2 * D + (size_t)((most + 3) & ~3) * 4 + WORDS * 4 + 64; }
+size_t many_smem_bytes(int most, int N) { return 1024 + A_STAGES * (size_t)STAGE + (size_t)N * 2 * D + (size_t)((most + 7) & ~7) * 4 + WORDS * 4 + 128; }
 
 // Nine warps.  0-3: thread = page of a tile (TMEM lane), the largest of its columns;  4-7: fetch the pages' codes;  8: issues.
 template <int D>
 __global__ void __launch_bounds__(MANY_THREADS, 2) select_many_kernel(const __grid_constant__ SelectParams p, int G, int N, int tmem_cols)
 {
     extern __shared__ __align__(1024) uint8_t smem_many[];
-    constexpr int ROW = 2 * D, ATOMS = ROW / 128, STAGE = a_stage_bytes<D>();
+    constexpr int ROW = 2 * D, ATOMS = ROW / 128;
     constexpr int PIECES = D / 8;              // of 8 dims, of a column
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(FULL, tid >> 5, 0);
     const uint32_t base = smem_u32(smem_many);
     const uint32_t pad = (1024u - (base & 1023u)) & 1023u;
     const uint32_t a_smem = base + pad, b_smem = a_smem + A_STAGES * STAGE;
     uint8_t *behind = smem_many + pad + A_STAGES * STAGE + (size_t)N * ROW;
-    uint32_t *bins = reinterpret_cast<uint32_t *>(smem_many + pad), *keys = reinterpret_cast<uint32_t *>(behind), *words = keys + ((p.most + 3) & ~3);
+    uint32_t *bins = reinterpret_cast<uint32_t *>(smem_many + pad), *keys = reinterpret_cast<uint32_t *>(behind), *words = keys + ((p.most + 7) & ~7);
     const uint32_t bars = smem_u32(words + WORDS), full = bars, empty = full + 8 * A_STAGES, sums = empty + 8 * A_STAGES, taken = sums + 16;
-    static_assert(BINS * 4 <= A_STAGES * a_stage_bytes<D>(), "the bins fit");
-    volatile uint32_t *gave_up = words + 200, *tmem_slot = words + 201;
-    volatile int *shared = reinterpret_cast<volatile int *>(words + 202);
+    static_assert(BINS * 4 <= A_STAGES * STAGE, "the bins fit");
+    volatile uint32_t *gave_up = words + 80, *tmem_slot = words + 81;
+    volatile int *shared = reinterpret_cast<volatile int *>(words + 82);
     if (tid == 0) {
         for (int i = 0; i < A_STAGES; ++i) {
             mbar_init(full + 8 * i, 128);
@@ -485,6 +502,9 @@ __global__ void __launch_bounds__(MANY_THREADS, 2) select_many_kernel(const __gr
             mbar_init(taken + 8 * i, 4);
         }
         *gave_up = 0;
+        words[0] = 0xFFFFFFFFu;
+        words[1] = 0;
+        words[9] = words[10] = words[11] = 0;
         fence_barrier_init();
     }
     pdl_wait();
@@ -538,58 +558,67 @@ __global__ void __launch_bounds__(MANY_THREADS, 2) select_many_kernel(const __gr
             int ids[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) ids[i] = id_of(r0 + 16 * i);
-            auto landed = [&](int tile) {      // (the tensor core reads through the async proxy)
-                fence_proxy_async();
-                mbar_arrive(full + 8 * (tile & (A_STAGES - 1)));
-            };
+            const int8_t *codes = p.codes + (int64_t)h * ROW + c * 16;
+            const int64_t page_bytes = (int64_t)p.Hkv * ROW;
+            const uint32_t to = a_smem + (uint32_t)(r0 * 128 + ((c ^ (r0 & 7)) * 16));       // (rows 16 apart have the same place in the swizzle)
+            int use = 0;                       // stages filled so far
             for (int tile = 0; tile < tiles; ++tile) {
-                const int st = tile & (A_STAGES - 1);
-                if (tile >= A_STAGES) chunk::wait(empty + 8 * st, (uint32_t)((tile / A_STAGES - 1) & 1), gave_up);
+                const int8_t *src[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int row = r0 + 16 * i;
-                    const int8_t *src = p.codes + ((int64_t)ids[i] * p.Hkv + h) * ROW + c * 16;
-                    const uint32_t dst = a_smem + (uint32_t)(st * STAGE + row * 128 + ((c ^ (row & 7)) * 16));
-#pragma unroll
-                    for (int a = 0; a < ATOMS; ++a)
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (uint32_t)(a * TILE * 128)), "l"(src + a * 128) : "memory");
-                }
-                asm volatile("cp.async.commit_group;" ::: "memory");
+                for (int i = 0; i < 8; ++i) src[i] = codes + ids[i] * page_bytes;
                 if (tile + 1 < tiles)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) ids[i] = id_of((tile + 1) * TILE + r0 + 16 * i);
-                if (tile > 0) {
-                    asm volatile("cp.async.wait_group 1;" ::: "memory");
-                    landed(tile - 1);
+#pragma unroll
+                for (int a = 0; a < ATOMS; ++a, ++use) {
+                    const int st = use & (A_STAGES - 1);
+                    if (use >= A_STAGES) chunk::wait(empty + 8 * st, (uint32_t)((use / A_STAGES - 1) & 1), gave_up);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + (uint32_t)(st * STAGE + i * 16 * 128)), "l"(src[i] + a * 128) : "memory");
+                    // the barrier hears of it when they are there; whoever issues the products sees to the proxies
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full + 8 * st) : "memory");
                 }
             }
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
-            landed(tiles - 1);
+            asm volatile("cp.async.wait_all;" ::: "memory");
         }
         // ---- the queries' codes, by warps 0 to 3 and 8; columns that are left over repeat the first ----
         if (warp < 4 || warp == 8) {
             const int me = warp < 4 ? tid : 128 + lane, cols = run.rows * G;
             const uint16_t *q = p.Q + ((int64_t)run.row * p.Hq + (int64_t)h * G) * D;
-            auto piece_of = [&](int i) {
-                const int col = i / PIECES < cols ? i / PIECES : 0, row = col / G;
-                return __ldg(reinterpret_cast<const uint4 *>(q + ((int64_t)row * p.Hq + (col - row * G)) * D + i % PIECES * 8));
+            // 160 threads: a thread has the same piece of every 160 / PIECES-th column
+            constexpr int STEP = 160 / PIECES, AT_ONCE = (128 + STEP - 1) / STEP <= 7 ? (128 + STEP - 1) / STEP : 7;
+            const int piece = me % PIECES, c0 = me / PIECES;
+            const uint32_t by_G = 65535u / (uint32_t)G + 1u;         // col / G = col by_G >> 16 for the columns there are
+            auto piece_of = [&](int col) {
+                const int x = col < cols ? col : 0, row = (int)((uint32_t)x * by_G >> 16);
+                return __ldg(reinterpret_cast<const uint4 *>(q + ((int64_t)row * p.Hq + (x - row * G)) * D + piece * 8));
             };
             uint32_t top = 0;
-#pragma unroll 4
-            for (int i = me; i < cols * PIECES; i += 160) top = max(top, largest(piece_of(i)));
+#pragma unroll 1
+            for (int col = c0; col < cols; col += AT_ONCE * STEP) {
+                uint4 w[AT_ONCE];
+#pragma unroll
+                for (int m = 0; m < AT_ONCE; ++m) w[m] = piece_of(col + STEP * m);     // (past the last column: the first again)
+#pragma unroll
+                for (int m = 0; m < AT_ONCE; ++m) top = max(top, largest(w[m]));
+            }
             top = __reduce_max_sync(FULL, top);
-            if (lane == 0) words[warp < 4 ? warp : 4] = top;
-            if (tid < 3) words[5 + tid] = 0;
+            if (lane == 0) words[warp < 4 ? 4 + warp : 8] = top;
             asm volatile("bar.sync 2, 160;" ::: "memory");
-            const float inv = steps_per_unit(words, lane);
-#pragma unroll 4
-            for (int i = me; i < N * PIECES; i += 160) {
-                const int col = i / PIECES, piece = i % PIECES;
+            const float inv = steps_per_unit(words + 4, lane);
+            auto chunk_at = [&](int byte) { return (uint32_t)(byte / 128 * N * 128 + byte % 128 / 16 * 16); };
+            const uint32_t up_at = chunk_at(piece * 8), down_at = chunk_at(D + piece * 8), half = (uint32_t)(piece & 1) * 8;
+            uint4 next = piece_of(c0);
+#pragma unroll 1
+            for (int col = c0; col < N; col += STEP) {
+                const uint4 w = next;
+                next = piece_of(col + STEP);
                 uint2 up, down;
-                steps_of(piece_of(i), inv, up, down);
-                auto at = [&](int byte) { return b_smem + (uint32_t)(byte / 128 * N * 128 + col * 128 + (((byte % 128 / 16) ^ (col & 7)) * 16) + byte % 16); };
-                asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(at(piece * 8)), "r"(up.x), "r"(up.y) : "memory");
-                asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(at(D + piece * 8)), "r"(down.x), "r"(down.y) : "memory");
+                steps_of(w, inv, up, down);
+                const uint32_t to = b_smem + (uint32_t)(col * 128) + half, turn = (uint32_t)(col & 7) * 16;
+                asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(to + (up_at ^ turn)), "r"(up.x), "r"(up.y) : "memory");
+                asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(to + (down_at ^ turn)), "r"(down.x), "r"(down.y) : "memory");
             }
             fence_proxy_async();
             asm volatile("bar.sync 2, 160;" ::: "memory");
@@ -600,54 +629,76 @@ __global__ void __launch_bounds__(MANY_THREADS, 2) select_many_kernel(const __gr
             const uint32_t idesc = (2u << 4) /* s32 */ | (1u << 7) | (1u << 10) /* s8 by s8 */ | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
             const uint64_t a_desc = swizzled_desc(a_smem), b_desc = swizzled_desc(b_smem);
             const uint64_t b_atom = (uint64_t)((N * 128) >> 4);
+            int use = 0;
             for (int tile = 0; tile < tiles; ++tile) {
-                const int st = tile & (A_STAGES - 1), buf = tile & 1;
-                chunk::wait(full + 8 * st, (uint32_t)((tile / A_STAGES) & 1), gave_up);
+                const int buf = tile & 1;
                 if (tile >= 2) chunk::wait(taken + 8 * buf, (uint32_t)((tile / 2 - 1) & 1), gave_up);
-                tc5::tc_fence_after();
-                if (leader) {
 #pragma unroll
-                    for (int ks = 0; ks < ROW / 32; ++ks)
-                        umma_i8(tmem + (uint32_t)(buf * N), a_desc + (uint64_t)((st * STAGE + (ks >> 2) * TILE * 128 + (ks & 3) * 32) >> 4),
-                                b_desc + (uint64_t)(ks >> 2) * b_atom + (uint64_t)(((ks & 3) * 32) >> 4), idesc, ks > 0);
-                    tc5::tc_commit(sums + 8 * buf);
-                    tc5::tc_commit(empty + 8 * st);
+                for (int a = 0; a < ATOMS; ++a, ++use) {
+                    const int st = use & (A_STAGES - 1);
+                    chunk::wait(full + 8 * st, (uint32_t)((use / A_STAGES) & 1), gave_up);
+                    fence_proxy_async();       // (the codes came through the generic proxy)
+                    tc5::tc_fence_after();
+                    if (leader) {
+#pragma unroll
+                        for (int ks = 0; ks < 4; ++ks)
+                            umma_i8(tmem + (uint32_t)(buf * N), a_desc + (uint64_t)((st * STAGE + ks * 32) >> 4), b_desc + (uint64_t)a * b_atom + (uint64_t)((ks * 32) >> 4),
+                                    idesc, a > 0 || ks > 0);
+                        tc5::tc_commit(empty + 8 * st);
+                        if (a == ATOMS - 1) tc5::tc_commit(sums + 8 * buf);
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
             }
-            for (int j = tiles > A_STAGES ? tiles - A_STAGES : 0; j < tiles; ++j)      // the last commits arrive while the barriers are still there
+            for (int j = use > A_STAGES ? use - A_STAGES : 0; j < use; ++j)            // the last commits arrive while the barriers are still there
                 chunk::wait(empty + 8 * (j & (A_STAGES - 1)), (uint32_t)((j / A_STAGES) & 1), gave_up);
         } else if (warp < 4) {
             // ---- scores ----
             const uint32_t mine = tmem + ((uint32_t)(warp * 32) << 16);
-            float scale = __ldg(p.scales + (int64_t)id_of(tid) * p.Hkv + h);
+            // (a page's scale is asked for a tile ahead, its id two)
+            auto raw_id = [&](int i) { return __ldg(table + (i < run.scored ? i : run.scored - 1)); };
+            auto scale_of = [&](int id) { return __ldg(p.scales + (int64_t)(id >= 0 && (int64_t)id < p.max_pages ? id : 0) * p.Hkv + h); };
+            int id = raw_id(tid + TILE);
+            float scale = scale_of(raw_id(tid));
+            uint32_t least = 0xFFFFFFFFu, most = 0;
+#pragma unroll 1
             for (int tile = 0; tile < tiles; ++tile) {
                 const int buf = tile & 1, i = tile * TILE + tid;
-                const float next = tile + 1 < tiles ? __ldg(p.scales + (int64_t)id_of(i + TILE) * p.Hkv + h) : 0.f;
+                const float next = scale_of(id);
+                id = raw_id(i + 2 * TILE);
                 chunk::wait(sums + 8 * buf, (uint32_t)((tile >> 1) & 1), gave_up);
                 tc5::tc_fence_after();
-                int best[4] = {-0x7FFFFFFF, -0x7FFFFFFF, -0x7FFFFFFF, -0x7FFFFFFF};
+                int best[2] = {-0x7FFFFFFF, -0x7FFFFFFF};
                 int n = 0;
-                for (; n + 32 <= N; n += 32) {
-                    uint32_t v[32];
-                    tc5::tmem_ld32(mine + (uint32_t)(buf * N + n), v);
+#pragma unroll 1
+                for (; n + 64 <= N; n += 64) {
+                    uint32_t u[32], v[32];
+                    tc5::tmem_ld32(mine + (uint32_t)(buf * N + n), u);
+                    tc5::tmem_ld32(mine + (uint32_t)(buf * N + n + 32), v);
                     tc5::tmem_wait_ld();
 #pragma unroll
-                    for (int x = 0; x < 32; ++x) best[x & 3] = max(best[x & 3], (int)v[x]);
+                    for (int x = 0; x < 32; ++x) best[x & 1] = max(best[x & 1], max((int)u[x], (int)v[x]));
                 }
-                if (n < N) {
+#pragma unroll 1
+                for (; n < N; n += 16) {
                     uint32_t v[16];
                     tc5::tmem_ld16(mine + (uint32_t)(buf * N + n), v);
                     tc5::tmem_wait_ld();
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) best[x & 3] = max(best[x & 3], (int)v[x]);
+                    for (int x = 0; x < 16; ++x) best[x & 1] = max(best[x & 1], (int)v[x]);
                 }
                 tc5::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(taken + 8 * buf);
-                if (i < run.scored) keys[i] = key_of(max(max(best[0], best[1]), max(best[2], best[3])), scale);
+                if (i < run.scored) {
+                    const uint32_t key = key_of(max(best[0], best[1]), scale);
+                    least = min(least, key);
+                    most = max(most, key);
+                    keys[i] = key;
+                }
                 scale = next;
             }
+            note_range(smem_u32(words), least, most, lane);
         }
         tc5::tc_fence_before();
         __syncthreads();
