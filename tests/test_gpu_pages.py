@@ -185,7 +185,8 @@ def test_selection_for_one_row_each(hq, hkv, d, top, first, last, kind):
     p.check(q, lists, counts, top, first, last)
 
 
-@pytest.mark.parametrize("hq,hkv,d,run", [(8, 2, 128, 32), (8, 2, 128, 5), (4, 4, 128, 128), (8, 1, 128, 16), (6, 2, 64, 42), (6, 2, 64, 1), (4, 4, 64, 33), (16, 2, 64, 2)])
+@pytest.mark.parametrize("hq,hkv,d,run", [(8, 2, 128, 32), (8, 2, 128, 5), (8, 2, 128, 4), (6, 2, 128, 2), (4, 4, 128, 128), (4, 4, 128, 7), (8, 1, 128, 16), (6, 2, 64, 42), (6, 2, 64, 1),
+                                          (6, 2, 64, 4), (4, 4, 64, 33), (16, 2, 64, 2)])
 @pytest.mark.parametrize("kind", ["drawn", "ties", "wild"])
 def test_selection_for_runs(hq, hkv, d, run, kind):
     lens, new = [0, 1, 40, 300, 1201, 2000], [0, 1, 40, 77, 150, 1]
@@ -194,6 +195,17 @@ def test_selection_for_runs(hq, hkv, d, run, kind):
     for top, first, last in ((9, 1, 2), (40, 0, 1), (0, 1, 4)):
         lists, counts = p.select(q, top, first, last, new, 150, run)
         p.check(q, lists, counts, top, first, last, new, 150, run)
+
+
+@pytest.mark.parametrize("batch", [75, 250, 260])
+def test_selection_of_many_sequences(batch):
+    """More segments than SMs, with lengths all over, equal ones among them: longest first, and beyond 256 as they come."""
+    lens = [(37 * b * b + 11 * b) % 900 for b in range(batch)]
+    lens[3], lens[batch // 2], lens[batch - 1] = 0, lens[1], 900
+    p = Indexed(lens, 2, 64, seed=batch)
+    q = torch.randn(batch, 4, 64, generator=p.g).bfloat16()
+    lists, counts = p.select(q, 9, 1, 2)
+    p.check(q, lists, counts, 9, 1, 2)
 
 
 @pytest.mark.parametrize("batch", [1, 3, 40])
