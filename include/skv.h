@@ -504,8 +504,7 @@ int skv_set_page_index(skv_cache *cache, void *device_memory, size_t bytes, void
  *   max_q_len   host bound on the new tokens of a sequence
  * A sequence whose a, n or page ids do not fit raises SKV_ERR_BOUNDS in the device
  * status and is left out (of a bad page id, that page).  One launch.  Errors:
- * SKV_ERR_ARG (also: no index), SKV_ERR_LAYER, SKV_ERR_UNSUPPORTED (more than 2^34
- * pages of kv heads), SKV_ERR_CUDA. */
+ * SKV_ERR_ARG (also: no index), SKV_ERR_LAYER, SKV_ERR_CUDA. */
 int skv_index_pages(skv_cache *cache, int layer, const int32_t *page_table, const int32_t *seq_lens,
                     const int32_t *cu_q_lens, int batch, int max_q_len, int pt_stride, void *stream);
 

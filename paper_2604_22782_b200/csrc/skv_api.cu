@@ -1359,10 +1359,9 @@ int skv_index_pages(skv_cache *c, int layer, const int32_t *page_table, const in
     p.max_q_len = cu_q_lens ? max_q_len : 1;
     p.max_new_pages = (p.max_q_len - 1) / PAGE + 1;
     if (p.max_new_pages > pt_stride) p.max_new_pages = pt_stride;
-    if ((int64_t)batch * p.max_new_pages * c->kv_heads > 0x7FFFFFFFll * 8) return SKV_ERR_UNSUPPORTED;       // grid limit
     index_of(c, layer, p.codes, p.scales);
     p.status = c->status_word();
-    if (launch_index_pages(p, c->head_dim, c->fp8, c->tune.pdl != 0, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+    if (launch_index_pages(p, c->head_dim, c->fp8, c->sm_count, c->tune.pdl != 0, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
         (void)cudaGetLastError();
         return SKV_ERR_CUDA;
     }
@@ -1454,7 +1453,12 @@ int skv_prefill_attn_pages(skv_cache *c, int layer, const void *Q, const int32_t
     const PageLists l = {lists, counts, list_stride, run, per_seq};
     const int src = c->r[(size_t)layer];
     const bool can_umma = aligned(out, 16) && prefill_pages_smem_bytes(c->head_dim, c->fp8) <= (size_t)c->max_smem_optin;
-    const bool few_rows = max_q_len == 1;
+    // Few rows, or lists of a row each: a row at a time through the decode kernel.  That reads K and V once per row instead of once per list, but
+    // spreads rows and pages over the GPU, where a list is a chain of blocks of 0.75 us on one CTA.  (us, rows / tiles, 8 kv heads of 4, by row heads: bf16
+    // pages, lists of 117 pages, 16 8.0 / 22.8, 64 14.2 / 22.9, 128 20.2 / 23.2, 256 32.9 / 23.8; of 53 pages, 128 11.7 / 13.3, 256 17.5 / 13.8.
+    // FP8 pages, 117 pages, 128 20.3 / 38.3, 256 31.1 / 39.1, 512 59.5 / 38.9; 64 sequences of two rows 113 / 107.)
+    const int per_list = run < max_q_len ? run : max_q_len;
+    const bool few_rows = per_list == 1 || (int64_t)batch * max_q_len * c->kv_heads * c->head_dim <= (c->fp8 ? 320 : 160) * 128;
     if (c->prefill_variant == 2 && !can_umma) return SKV_ERR_UNSUPPORTED;
     if (can_umma && (c->prefill_variant == 2 || (c->prefill_variant == 0 && !few_rows))) {
         PrefillParams p;

@@ -66,7 +66,7 @@ struct PageLists {
     int run, per_seq;
 };
 
-cudaError_t launch_index_pages(const IndexParams &p, int D, bool fp8, bool pdl, cudaStream_t s);
+cudaError_t launch_index_pages(const IndexParams &p, int D, bool fp8, int sm_count, bool pdl, cudaStream_t s);
 int select_max_pages(int columns);      // of a sequence; columns: min(run, max_q_len) * G
 cudaError_t launch_select_pages(const SelectParams &p, int D, int sm_count, bool pdl, cudaStream_t s);
 // decode attention over listed pages (skv_decode_pages.cu); kernel as in launch_decode_splitk.  p.cu_q: rows of chunks, a row as a

@@ -82,6 +82,21 @@ def test_index_of_one_token_each(fp8):
     assert p.cache.skv_get_status() == 0
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+def test_index_with_room_for_many_more_tokens(fp8):
+    """A bound on the new tokens far above what there are, so that a CTA goes through its items in several rounds."""
+    lens = [700, 0, 33, 1000, 64]
+    p = Paged(lens, 3, 64, fp8, seed=7)
+    p.k = [k.float() for k in p.k]
+    _, [(codes, scales)] = index_of(p.cache)
+    table = torch.full((5, 9000), -1, dtype=torch.int32)
+    table[:, :p.table.shape[1]] = p.table
+    cu = [sum(lens[:b]) for b in range(6)]
+    p.cache.skv_index_pages(0, table.cuda(), p.lens_dev, cu_q_lens=i32(cu), max_q_len=144000)
+    check_index(p, codes, scales, [0] * 5, [n // 16 for n in lens])
+    assert p.cache.skv_get_status() == 0
+
+
 def test_index_of_unusual_keys():
     """Zeros, next to nothing, one large value, the largest finite ones, infinities, NaN: head by head."""
     import paper_2604_22782_b200 as skv
