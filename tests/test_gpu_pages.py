@@ -346,6 +346,37 @@ def test_decode_launch_shapes(batch, fp8):
     assert torch.equal(out, again)
 
 
+@pytest.mark.parametrize("batch,fp8", [(60, False), (112, False), (240, False), (112, True), (240, True)])
+def test_decode_of_more_segments_than_sms(batch, fp8):
+    """A segment to a CTA of four warps, or to two, and three or four of these to an SM; lists of a few pages to many."""
+    lens = [1300 if b % 7 == 0 else 5 + 61 * b % 900 for b in range(batch)]
+    p = Paged(lens, 2, 128, fp8, seed=batch)
+    q = p.rows(batch, 8)
+    lists, counts = some_lists(random.Random(batch), [-(-n // 16) for n in lens], 2, 80)
+    out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
+    p.cache.skv_decode_attn_pages(0, q.cuda(), p.table_dev, p.lens_dev, lists.cuda(), counts.cuda(), out)
+    check_rows(p, q, out, lists, counts, [(b, b, [n - 1]) for b, n in enumerate(lens)])
+    assert p.cache.skv_get_status() == 0
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_a_page_listed_twice_counts_twice(fp8):
+    p = Paged([100, 333], 2, 128, fp8, seed=4)
+    lists = torch.tensor([[[2, 2, 6], [6, 0, 6]], [[20, 3, 20], [7, 7, 7]]], dtype=torch.int32)
+    counts = torch.full((2, 2), 3, dtype=torch.int32)
+    q = p.rows(2, 8)
+    out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
+    p.cache.skv_decode_attn_pages(0, q.cuda(), p.table_dev, p.lens_dev, lists.cuda(), counts.cuda(), out)
+    check_rows(p, q, out, lists, counts, [(0, 0, [99]), (1, 1, [332])])
+    rows = p.rows(2 * 32, 8)
+    runs = [(b, 32 * b, list(range(n - 32, n))) for b, n in enumerate(p.lens)]
+    for variant in (1, 2):
+        p.cache.skv_set_prefill_variant(variant)
+        out = torch.empty(rows.shape, dtype=torch.bfloat16, device="cuda")
+        p.cache.skv_prefill_attn_pages(0, rows.cuda(), i32([0, 32, 64]), p.table_dev, p.lens_dev, lists.cuda(), counts.cuda(), out, 32, run=32)
+        check_rows(p, rows, out, lists, counts, runs)
+
+
 CHUNKS = [(8, 2, 128, 32), (8, 2, 128, 3), (4, 4, 128, 128), (8, 1, 128, 16), (6, 2, 64, 42), (6, 2, 128, 1), (4, 4, 64, 33), (16, 2, 64, 7), (8, 2, 64, 32)]
 
 
@@ -685,3 +716,122 @@ def test_two_streams_at_once():
         lists, counts, out = (x.cpu() for x in got[i][0])
         check_rows(p, q[i].cpu(), out, lists, counts, [(b, b, [2999]) for b in range(4)])
     assert p.cache.skv_get_status() == 0
+
+
+def test_two_captured_layers_replayed_at_once():
+    """No workspace: graphs of the same cache and the same rows may run at the same time."""
+    p = Paged([2000, 700], 2, 128, seed=9)
+    index_of(p.cache)
+    p.cache.skv_index_pages(0, p.table_dev, p.lens_dev, cu_q_lens=i32([0, 2000, 2700]), max_q_len=2000)
+    q, cu = p.rows(2 * 300, 8).cuda(), i32([0, 300, 600])
+    graphs, results, streams = [], [], [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        g = torch.cuda.CUDAGraph()
+        lists, counts = torch.empty(2 * 19, 2, 24, dtype=torch.int32, device="cuda"), torch.empty(2 * 19, 2, dtype=torch.int32, device="cuda")
+        out = torch.empty_like(q)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g, stream=s):
+            p.cache.skv_select_pages(0, q, p.table_dev, p.lens_dev, lists, counts, 20, cu_q_lens=cu, max_q_len=300, run=16)
+            p.cache.skv_prefill_attn_pages(0, q, cu, p.table_dev, p.lens_dev, lists, counts, out, 300, run=16)
+        graphs.append(g)
+        results.append((lists, counts, out))
+    for _ in range(5):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*results)) and p.cache.skv_get_status() == 0
+    lists, counts, out = (x.cpu() for x in results[0])
+    check_rows(p, q.cpu(), out, lists, counts, chunk_runs(p.lens, [300, 300], 300, 16))
+
+
+def test_both_ways_into_the_library_agree():
+    """Plain calls go through the extension; a whole-numbered scale or a given stream through the checked one."""
+    p = Paged([500, 90], 2, 128, seed=2)
+    index_of(p.cache)
+    cu, width = i32([0, 40, 80]), 9
+    p.cache.skv_index_pages(0, p.table_dev, p.lens_dev, cu, 500)
+    q, one = p.rows(80, 8).cuda(), p.rows(2, 8).cuda()
+    got = []
+    for scale, stream in ((1.0, None), (1, torch.cuda.current_stream())):
+        lists, counts = torch.empty(2 * 5, 2, width, dtype=torch.int32, device="cuda"), torch.empty(2 * 5, 2, dtype=torch.int32, device="cuda")
+        few, few_counts = torch.empty(2, 2, width, dtype=torch.int32, device="cuda"), torch.empty(2, 2, dtype=torch.int32, device="cuda")
+        out, row = torch.empty_like(q), torch.empty_like(one)
+        before = p.cache.skv_launch_count()
+        p.cache.skv_index_pages(0, p.table_dev, p.lens_dev, stream=stream)
+        p.cache.skv_index_pages(1, p.table_dev, p.lens_dev, stream=stream)       # (not an owner: nothing to do)
+        p.cache.skv_select_pages(1, q, p.table_dev, p.lens_dev, lists, counts, 5, 1, 2, cu, 40, 8, stream=stream)
+        p.cache.skv_select_pages(1, one, p.table_dev, p.lens_dev, few, few_counts, 5, stream=stream)
+        p.cache.skv_prefill_attn_pages(1, q, cu, p.table_dev, p.lens_dev, lists, counts, out, 40, 8, scale, stream=stream)
+        p.cache.skv_decode_attn_pages(1, one, p.table_dev, p.lens_dev, few, few_counts, row, scale, stream=stream)
+        assert p.cache.skv_launch_count() == before + 5
+        got.append((lists, counts, few, few_counts, out, row))
+    assert all(torch.equal(a, b) for a, b in zip(*got)) and p.cache.skv_get_status() == 0
+
+
+def test_refusals():
+    import paper_2604_22782_b200 as skv
+    from paper_2604_22782_b200.binding import SKV_ERR_ARG, SKV_ERR_LAYER, SKV_ERR_NOMEM, SKV_ERR_UNSUPPORTED, SkvError
+    p = Paged([200, 60], 2, 64, seed=1)
+    c, table, lens, cu = p.cache, p.table_dev, p.lens_dev, i32([0, 3, 6])
+    one, q = p.rows(2, 4).cuda(), p.rows(6, 4).cuda()
+    lists, counts = torch.empty(2, 2, 5, dtype=torch.int32, device="cuda"), torch.empty(2, 2, dtype=torch.int32, device="cuda")
+    out, rows = torch.empty_like(one), torch.empty_like(q)
+
+    def refused(status, call):
+        with pytest.raises(SkvError) as e:
+            call()
+        assert e.value.status == status
+
+    def select(layer=0, q=one, top=3, first=1, last=1, lists=lists, counts=counts, table=table, **more):
+        return lambda: c.skv_select_pages(layer, q, table, lens, lists, counts, top, first, last, **more)
+
+    def decode(layer=0, q=one, out=out, lists=lists, counts=counts):
+        return lambda: c.skv_decode_attn_pages(layer, q, table, lens, lists, counts, out)
+
+    def prefill(layer=0, q=q, out=rows, lists=lists, counts=counts, most=3, run=3):
+        return lambda: c.skv_prefill_attn_pages(layer, q, cu, table, lens, lists, counts, out, most, run)
+
+    before = c.skv_launch_count()
+    refused(SKV_ERR_ARG, lambda: c.skv_index_pages(0, table, lens))                  # no index yet
+    refused(SKV_ERR_ARG, select())
+    need = c.skv_page_index_bytes()
+    memory = torch.empty(need + 256, dtype=torch.uint8, device="cuda")
+    refused(SKV_ERR_NOMEM, lambda: c.skv_set_page_index(memory[:need - 1]))
+    refused(SKV_ERR_ARG, lambda: c.skv_set_page_index(memory[8:]))
+    c.skv_set_page_index(memory)
+    refused(SKV_ERR_ARG, lambda: c.skv_index_pages(0, table, lens, cu, 0))
+    for call in (lambda: c.skv_index_pages(2, table, lens), select(layer=2), select(layer=-1), decode(layer=2), prefill(layer=-1)):
+        refused(SKV_ERR_LAYER, call)
+    refused(SKV_ERR_ARG, select(top=-1))
+    refused(SKV_ERR_ARG, select(first=-1))
+    refused(SKV_ERR_ARG, select(last=0))
+    refused(SKV_ERR_ARG, select(top=4))                                              # lists of five entries
+    refused(SKV_ERR_ARG, select(q=q[:2], max_q_len=3, run=3))                        # rows without offsets
+    odd = torch.empty(2 * 4 * 64 + 1, dtype=torch.bfloat16, device="cuda")[1:].view(2, 4, 64)
+    three = torch.empty(2, 3, 64, dtype=torch.bfloat16, device="cuda")
+    refused(SKV_ERR_ARG, select(q=odd))
+    refused(SKV_ERR_ARG, decode(q=odd))
+    refused(SKV_ERR_ARG, decode(out=odd))
+    refused(SKV_ERR_UNSUPPORTED, select(q=three))
+    refused(SKV_ERR_UNSUPPORTED, decode(q=three, out=torch.empty_like(three)))
+    refused(SKV_ERR_UNSUPPORTED, prefill(most=65, run=65))                           # 65 rows of two heads
+    refused(SKV_ERR_UNSUPPORTED, select(cu_q_lens=cu, max_q_len=65, run=65, lists=torch.empty(2, 2, 9, dtype=torch.int32, device="cuda")))
+    long = torch.zeros(2, 45057, dtype=torch.int32, device="cuda")
+    refused(SKV_ERR_UNSUPPORTED, select(table=long))
+    refused(SKV_ERR_UNSUPPORTED, select(table=long[:, :28673].contiguous(), cu_q_lens=cu, max_q_len=16, run=16, lists=torch.empty(2, 2, 6, dtype=torch.int32, device="cuda")))
+    shifted = torch.empty(6 * 4 * 64 + 4, dtype=torch.bfloat16, device="cuda")[4:].view(6, 4, 64)
+    c.skv_set_prefill_variant(2)
+    refused(SKV_ERR_UNSUPPORTED, prefill(out=shifted))                               # the tile kernel writes 16 bytes at a time
+    c.skv_set_prefill_variant(0)
+    for call in (select(lists=lists.long()), select(lists=lists[:1]), select(counts=counts[:, :1]), select(q=one.half()), select(q=one[:1]), select(run=0),
+                 select(lists=lists.transpose(0, 1)), decode(lists=lists[:, :, ::2]), decode(out=rows), decode(counts=counts.cpu()), decode(q=one[..., :32]),
+                 prefill(lists=lists[:1]), prefill(out=out), prefill(run=1), prefill(most=0), prefill(counts=counts.long()),
+                 lambda: c.skv_index_pages(0, table[0], lens), lambda: c.skv_index_pages(0, table, lens.long()), lambda: c.skv_index_pages(0, table, lens, cu[:2]),
+                 lambda: c.skv_set_page_index(memory.int())):
+        with pytest.raises((ValueError, TypeError)):
+            call()
+    assert c.skv_launch_count() == before and c.skv_get_status() == 0
+    c.skv_set_page_index(None)
+    refused(SKV_ERR_ARG, select())
+    assert skv.skv_page_list_width(3, 1, 1) == 5
