@@ -9,11 +9,12 @@
 //   warp 4     issues the scores Q K^T,  warp 5  the outputs P V
 //   warp 6     copies K and V of the key blocks; the entries' page ids are had 32 at a time
 //   warp 7     zeroes the V rows of tokens that no row of the item sees, whatever they hold
-// On FP8 pages the codes are turned into f16, which holds every one of them exactly, on the way into the operands.  Queries are f16
-// too, times a power of two that brings a row's largest to [1, 2): exact but for elements 2^-14 of that and less.  The tokens' scales
-// are applied in fp32, K's to the scores and V's to the probabilities, which are taken relative to c, the power of two at or above every
-// V scale that the row has seen, so that they fit f16 whatever the scales:
-//   warps 4, 5  convert K,  warps 6, 7  V (tokens that no row sees: zero),  warp 8  issues Q K^T,  9  P V,  warps 10, 11  copy K and V
+// On FP8 pages K's codes are the scores' operand as they are.  A query is the sum of two E4M3 numbers, times a power of two that brings a
+// row's largest to [128, 256): the nearest, and the nearest to what that leaves, which hold bf16's 8 bits exactly, but for elements below
+// 2^-9 of the largest, which may be off by 2^-17 of it.  V's codes are turned into f16, which holds every one of them exactly, on the way
+// into the operand.  The tokens' scales are applied in fp32, K's to the scores and V's to the probabilities, which are taken relative to c,
+// the power of two at or above every V scale that the row has seen, so that they fit f16 whatever the scales:
+//   warps 4-7  convert V (tokens that no row sees: zero),  warp 8  scales, issues Q K^T,  9  P V,  warps 10, 11  copy K and V
 // Operand layouts, softmax and waits are those of skv_prefill_window.cu.  Runs of one sequence and head are neighbours in the grid:
 // their lists have pages in common, which are then in L2.
 #include "skv_page_index.cuh"
@@ -37,9 +38,9 @@ constexpr int TMEM_COLS = 256;
 constexpr int NO_PAGE = 0x07FFFFFF;   // no row sees a token of it
 
 // Shared memory (from a 1024-byte boundary on).  bf16: Q [D/64][128 rows][128 B] | K ring [8 groups][D/8 chunks][8 keys][16 B] | V ring
-// [4 pages][V half].  FP8: Q | K tile (as a stage of the K ring) | V tile [4 pages][2 halves of 8 tokens][D dims][16 B] | K ring: codes of 4
-// pages, their K and V scales | V ring: codes | scales of 4 blocks: K scale x log2(e) / sqrt(d) [64] | V scale [64] |
-// the largest V scale of each half.  Then barriers and words.
+// [4 pages][V half].  FP8: Q [128 rows][two terms][D dims], D = 128 the terms one after the other | two V tiles [4 pages][2 halves of
+// 8 tokens][D dims][16 B] | K ring: codes of 4 pages [8 groups][D/16 chunks][8 keys][16 B], their K and V scales | V ring: codes | scales of
+// 4 blocks: K scale x log2(e) / sqrt(d) [64] | V scale [64] | the largest V scale.  Then barriers and words.
 template <int D, bool FP8>
 struct Layout {
     static constexpr int STAGES = D == 128 ? 2 : 4;                  // bf16: of the K ring and of the V ring
@@ -49,7 +50,7 @@ struct Layout {
     static constexpr int K_STAGE = FP8 ? KEYS * D + KB * 2 * PAGE * 4 : TILE, V_STAGE = FP8 ? KEYS * D : TILE;
     static constexpr int K_RING = Q_BYTES + (FP8 ? 2 * TILE : 0), V_RING = K_RING + K_STAGES * K_STAGE;
     static constexpr int SCALES = V_RING + V_STAGES * V_STAGE, BARS = SCALES + (FP8 ? 4 * SCALE_STAGE : 0);
-    static constexpr int N_BARS = 2 * K_STAGES + 2 * V_STAGES + (FP8 ? 4 : V_STAGES) + 3 * 2 + 1;
+    static constexpr int N_BARS = 2 * K_STAGES + 2 * V_STAGES + (FP8 ? 2 : V_STAGES) + 3 * 2 + 1;
     static constexpr int WORDS = BARS + 8 * N_BARS + (8 * N_BARS & 8);
     static constexpr int BYTES = 1024 + WORDS + 48;
 };
@@ -61,6 +62,13 @@ __device__ __forceinline__ void convert16(const uint4 &w, uint4 &a, uint4 &b)
     e4m3x4_to_f16x2(w.y, a.z, a.w);
     e4m3x4_to_f16x2(w.z, b.x, b.y);
     e4m3x4_to_f16x2(w.w, b.z, b.w);
+}
+
+__device__ __forceinline__ float2 f16x2_to_f32x2(uint32_t w)
+{
+    float2 f;
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}" : "=f"(f.x), "=f"(f.y) : "r"(w));
+    return f;
 }
 
 // exponent of the power of two at or above x >= 0, at least LEAST_C: a probability of up to 2^8 over c stays far from fp32's end
@@ -97,17 +105,17 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
     using L = Layout<D, FP8>;
     constexpr int THREADS = threads_of(FP8);
     constexpr int BLOCK = FP8 ? fp8_block_bytes(D) : block_bytes(D), HALF = half_bytes(D), CH = D / 8, KS = L::K_STAGES, VS = L::V_STAGES;
-    constexpr uint32_t F16 = FP8 ? (1u << 7) | (1u << 10) : 0u;              // the operands' type bits: bf16, or neither
-    constexpr uint32_t IDESC_QK = instr_desc(ROWS, KEYS, false) & ~F16, IDESC_PV = instr_desc(ROWS, D, !FP8) & ~F16;
+    constexpr uint32_t F16 = FP8 ? (1u << 7) | (1u << 10) : 0u;              // the operands' type bits of P V: bf16, or neither
+    constexpr uint32_t IDESC_QK = FP8 ? instr_desc_e4m3(ROWS, KEYS) : instr_desc(ROWS, KEYS, false), IDESC_PV = instr_desc(ROWS, D, !FP8) & ~F16;
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(FULL, tid >> 5, 0);      // (known to be the same for the warp)
     const uint32_t base = smem_u32(smem_raw);
     const uint32_t pad = (1024u - (base & 1023u)) & 1023u;
-    const uint32_t q_smem = base + pad, k_tile = q_smem + L::Q_BYTES, v_tile = k_tile + L::TILE, k_ring = q_smem + L::K_RING, v_ring = q_smem + L::V_RING,
+    const uint32_t q_smem = base + pad, v_tiles = q_smem + L::Q_BYTES, k_ring = q_smem + L::K_RING, v_ring = q_smem + L::V_RING,
                    scale_ring = q_smem + L::SCALES;
     const uint32_t k_full = q_smem + L::BARS, k_empty = k_full + 8 * KS, v_full = k_empty + 8 * KS, v_empty = v_full + 8 * VS;
-    // bf16: a V stage with tokens that nobody sees has landed; FP8: a tile is complete, its instructions are done with it
-    const uint32_t v_landed = v_empty + 8 * VS, k_ready = v_landed, v_ready = k_ready + 8, k_free = v_ready + 8, v_free = k_free + 8;
-    const uint32_t s_ready = v_landed + (FP8 ? 32 : 8 * VS), p_ready = s_ready + 16, pv_done = p_ready + 16, q_full = pv_done + 16;
+    // bf16: a V stage with tokens that nobody sees has landed; FP8: a V tile is complete
+    const uint32_t v_landed = v_empty + 8 * VS, v_ready = v_landed;
+    const uint32_t s_ready = v_landed + 8 * (FP8 ? 2 : VS), p_ready = s_ready + 16, pv_done = p_ready + 16, q_full = pv_done + 16;
     uint8_t *words = smem_raw + pad + L::WORDS;
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(words), *gave_up = tmem_slot + 1;
     volatile int32_t *item = reinterpret_cast<volatile int32_t *>(words + 8);      // rows, first position, tokens of the sequence, first row, entries
@@ -115,21 +123,16 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
     if (tid == 0) {
         for (int i = 0; i < KS; ++i) {
             mbar_init(k_full + 8 * i, 1);
-            mbar_init(k_empty + 8 * i, FP8 ? 2 : 1);
+            mbar_init(k_empty + 8 * i, 1);
         }
         for (int i = 0; i < VS; ++i) {
             mbar_init(v_full + 8 * i, 1);
-            mbar_init(v_empty + 8 * i, FP8 ? 2 : 1);
+            mbar_init(v_empty + 8 * i, FP8 ? 4 : 1);
             if (!FP8) mbar_init(v_landed + 8 * i, 1);
         }
-        if (FP8) {
-            mbar_init(k_ready, 2);
-            mbar_init(v_ready, 2);
-            mbar_init(k_free, 1);
-            mbar_init(v_free, 1);
-        }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(s_ready + 8 * i, 1);
+            if (FP8) mbar_init(v_ready + 8 * i, 4);
+            mbar_init(s_ready + 8 * i, FP8 ? 2 : 1);                         // (FP8: the block's scales are there too)
             mbar_init(p_ready + 8 * i, 4);
             mbar_init(pv_done + 8 * i, 1);
         }
@@ -226,15 +229,30 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
                     }
 #pragma unroll
                     for (int x = 1; x < 8; x <<= 1) top = max(top, __shfl_xor_sync(FULL, top, x));
-                    const int e = min(max((int)(top >> 7) - 127, -126), 126);            // (both powers are normal numbers)
+                    // the row's largest comes to [128, 256); both powers are normal numbers
+                    const int e = min(max((int)(top >> 7) - 127, -119), 127) - 7;
                     const float out = __int_as_float((127 - e) << 23), in = __int_as_float((127 + e) << 23);
 #pragma unroll
                     for (int half = 0; half < D / 64; ++half) {
                         const uint32_t x[4] = {w[half].x, w[half].y, w[half].z, w[half].w};
-                        uint32_t y[4];
+                        uint32_t term[2][2];                             // 8 dims each
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) y[k] = pack_f16x2(bf16_lo(x[k]) * out, bf16_hi(x[k]) * out);
-                        st_shared(dst + (uint32_t)(half * ROWS * 128), make_uint4(y[0], y[1], y[2], y[3]));
+                        for (int k = 0; k < 2; ++k) {
+                            float v[4] = {bf16_lo(x[2 * k]) * out, bf16_hi(x[2 * k]) * out, bf16_lo(x[2 * k + 1]) * out, bf16_hi(x[2 * k + 1]) * out};
+#pragma unroll
+                            for (int n = 0; n < 4; ++n) v[n] += v[n] - v[n];             // what is not finite becomes NaN
+                            term[0][k] = pack_e4m3x2(v[0], v[1]) | pack_e4m3x2(v[2], v[3]) << 16;
+                            uint32_t a, b;
+                            e4m3x4_to_f16x2(term[0][k], a, b);
+                            const float2 f = f16x2_to_f32x2(a), g2 = f16x2_to_f32x2(b);
+                            term[1][k] = pack_e4m3x2(v[0] - f.x, v[1] - f.y) | pack_e4m3x2(v[2] - g2.x, v[3] - g2.y) << 16;
+                        }
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) {
+                            const int col = t * D + half * 64 + c * 8;   // byte of the row's two terms, in tiles of 128
+                            asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(q_smem + (uint32_t)((col >> 7) * ROWS * 128 + row * 128 + (((col >> 4 & 7) ^ (row & 7)) * 16) + (col & 8))),
+                                         "r"(term[t][0]), "r"(term[t][1]) : "memory");
+                        }
                     }
                     const float theirs = __shfl_sync(FULL, in, (lane & 3) * 8);
                     if (lane >> 2 == i) row_scale = theirs;
@@ -295,9 +313,7 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
                     raw[c / 32][c % 32 + 2] = __float_as_uint(__uint_as_float(raw[c / 32][c % 32 + 2]) * __uint_as_float(s.z));
                     raw[c / 32][c % 32 + 3] = __float_as_uint(__uint_as_float(raw[c / 32][c % 32 + 3]) * __uint_as_float(s.w));
                 }
-                float v0, v1;
-                asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v0), "=f"(v1) : "r"(scales + 2 * KEYS * 4));
-                c_block = fmaxf(v0, v1);
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(c_block) : "r"(scales + 2 * KEYS * 4));
             }
             if (!clear) {
 #pragma unroll
@@ -324,6 +340,7 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
                 uint64_t sum2[2] = {0ull, 0ull};
                 float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                 uint32_t pk[32];
+                uint4 vs = make_uint4(0, 0, 0, 0);                     // FP8: V scales of 4 tokens
 #pragma unroll
                 for (int c = 0; c < 32; ++c) {
                     const float s0 = __uint_as_float(raw[c >> 4][(2 * c) & 31]), s1 = __uint_as_float(raw[c >> 4][(2 * c + 1) & 31]);
@@ -339,10 +356,9 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
                     mx4[c & 3] = fmaxf(mx4[c & 3], fmaxf(s0, s1));
                     sum2[c & 1] = add2(sum2[c & 1], pair_of(e0, e1));
                     if (FP8) {
-                        float v0, v1;
-                        asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v0), "=f"(v1) : "r"(scales + (uint32_t)(4 * (KEYS + 2 * c))));
-                        e0 *= v0;
-                        e1 *= v1;
+                        if (c % 2 == 0) vs = ld_shared(scales + (uint32_t)(4 * (KEYS + 2 * c)));
+                        e0 *= __uint_as_float(c % 2 == 0 ? vs.x : vs.z);
+                        e1 *= __uint_as_float(c % 2 == 0 ? vs.y : vs.w);
                     }
                     pk[c] = FP8 ? pack_f16x2(e0, e1) : pack_bf16x2(e0, e1);
                 }
@@ -410,18 +426,28 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
         }
     } else {
         if (!FP8) fewer_registers<56>();
-        else if (warp < 8) fewer_registers<48>();
-        else fewer_registers<32>();
-        const bool leader = elect_one(), values = FP8 && warp < 8 ? warp >= 6 : (warp & 1) != 0;
+        else fewer_registers<40>();
+        const bool leader = elect_one(), values = (warp & 1) != 0;
         const uint32_t output = tmem + COL_O;
         const uint64_t q_desc = swizzled_desc(q_smem);
         // scores of block kb from the K at k_desc / output of block kb from the V at v_desc, whose pages and halves of 8 tokens are
         // `half` bytes apart and whose 8-dim groups are `group` bytes: by one lane of a warp that has waited for its operands
         auto issue_scores = [&](int kb, uint64_t k_desc) {
             const uint32_t scores = tmem + (uint32_t)((kb & 1) * KEYS);
+            if constexpr (FP8) {                       // both terms of the queries on the codes as they are, 32 dims at a time
 #pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks)
-                umma_ss(scores, q_desc + (uint64_t)(((ks >> 2) * ROWS * 128 + (ks & 3) * 32) >> 4), k_desc + (uint64_t)((ks * 2 * 128) >> 4), IDESC_QK, ks > 0);
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int ks = 0; ks < D / 32; ++ks) {
+                        const int col = t * D + ks * 32;
+                        umma_ss_f8(scores, q_desc + (uint64_t)(((col >> 7) * ROWS * 128 + (col & 127)) >> 4), k_desc + (uint64_t)((ks * 2 * 128) >> 4), IDESC_QK,
+                                   t > 0 || ks > 0);
+                    }
+            } else {
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks)
+                    umma_ss(scores, q_desc + (uint64_t)(((ks >> 2) * ROWS * 128 + (ks & 3) * 32) >> 4), k_desc + (uint64_t)((ks * 2 * 128) >> 4), IDESC_QK, ks > 0);
+            }
             tc_commit(s_ready + 8 * (kb & 1));
         };
         auto issue_output = [&](int kb, uint64_t v_desc) {
@@ -433,112 +459,115 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
             tc_commit(pv_done + 8 * (kb & 1));
         };
         if (FP8) {
-            const int stages = values ? VS : KS;
-            const uint32_t ring = values ? v_ring : k_ring, stage_bytes = values ? L::V_STAGE : L::K_STAGE, tile = values ? v_tile : k_tile;
-            const uint32_t full = values ? v_full : k_full, empty = values ? v_empty : k_empty, ready = values ? v_ready : k_ready, free = values ? v_free : k_free;
             if (warp < 8) {
-                // =================== conversion: 64 lanes for K, 64 for V ===================
-                const bool second = (warp & 1) != 0;
-                const int me = lane + (second ? 32 : 0);
+                // =================== conversion of V ===================
+                const int me = tid - 128;
                 int page32 = page_at(lane), next32 = page_at(32 + lane);
                 for (int kb = 0; kb < blocks; ++kb) {
                     if (kb > 0 && (kb & 7) == 0) {
                         page32 = next32;
                         next32 = page_at((kb + 8) * KB + lane);
                     }
-                    const int st = kb % stages, np = listed - kb * KB < KB ? listed - kb * KB : KB;
-                    const uint32_t from = ring + (uint32_t)st * stage_bytes;
+                    const int st = kb % VS, np = listed - kb * KB < KB ? listed - kb * KB : KB;
+                    const uint32_t from = v_ring + (uint32_t)(st * L::V_STAGE), tile = v_tiles + (uint32_t)((kb & 1) * L::TILE);
                     // tokens that some row sees, of this lane's entry of the block
                     const uint32_t seen = bits_up_to(p1, page32);
-                    wait(full + 8 * st, (uint32_t)((kb / stages) & 1), gave_up);
-                    if (kb > 0) wait(free, (uint32_t)((kb - 1) & 1), gave_up);
-                    if (!values) {
-                        // this lane's token: K scale into units of log2, V scale (0 where no row sees it)
-                        const uint32_t bits = __shfl_sync(FULL, seen, (kb & 7) * KB + me / PAGE);
-                        float ks = 0.f, vs = 0.f;
-                        if (me / PAGE < np && (bits >> (me % PAGE) & 1u)) {
-                            const uint32_t a = from + (uint32_t)(KEYS * D + (me / PAGE * 2 * PAGE + me % PAGE) * 4);
-                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ks) : "r"(a) : "memory");
-                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(vs) : "r"(a + PAGE * 4) : "memory");
-                        }
-                        const uint32_t stage = scale_ring + (uint32_t)((kb & 3) * L::SCALE_STAGE), to = stage + (uint32_t)(me * 4);
-                        const uint32_t most = __reduce_max_sync(FULL, __float_as_uint(vs));          // (0 or more; the bits of a NaN are above all)
-                        if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(stage + (uint32_t)(2 * KEYS * 4 + (second ? 4 : 0))), "r"(most) : "memory");
-                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(ks * p.scale_log2) : "memory");
-                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + KEYS * 4), "f"(vs) : "memory");
-                        // unit: 16 dims of a token; the units of a page are read together
+                    const bool partial = __any_sync(FULL, seen != 0xFFFFu && lane >> 2 == (kb & 7));
+                    wait(v_full + 8 * st, (uint32_t)((kb / VS) & 1), gave_up);
+                    if (kb >= 2) wait(pv_done + 8 * (kb & 1), (uint32_t)(((kb >> 1) - 1) & 1), gave_up);       // the tile: P V two blocks back is over
+                    // unit: a dim of a page, 16 tokens (a warp's units are of one page)
 #pragma unroll 1
-                        for (int u0 = me; u0 < np * D; u0 += D) {
-                            uint4 w[D / 64];
+                    for (int u0 = me; u0 < np * D; u0 += 256) {
+                        uint4 w[2];
 #pragma unroll
-                            for (int i = 0; i < D / 64; ++i) w[i] = ld_shared(from + (uint32_t)((u0 + 64 * i) * 16));
+                        for (int i = 0; i < 2; ++i)
+                            if (u0 + 128 * i < np * D) w[i] = ld_shared(from + (uint32_t)((u0 + 128 * i) * 16));
 #pragma unroll
-                            for (int i = 0; i < D / 64; ++i) {
-                                const int u = u0 + 64 * i, group = u / (D / 2), c = u / 8 % (D / 16), t = u & 7;
-                                uint4 x, y;
-                                convert16(w[i], x, y);
-                                st_shared(tile + (uint32_t)(((group * CH + 2 * c) * 8 + t) * 16), x);
-                                st_shared(tile + (uint32_t)(((group * CH + 2 * c + 1) * 8 + t) * 16), y);
+                        for (int i = 0; i < 2; ++i) {
+                            const int u = u0 + 128 * i, j = u / D, dim = u % D;
+                            if (u >= np * D) break;
+                            if (partial) {
+                                const uint32_t bits = __shfl_sync(FULL, seen, (kb & 7) * KB + j);
+                                auto keep = [&](int k) {
+                                    const uint32_t f = bits >> (4 * k) & 0xFu;
+                                    return ((f & 1u) | (f & 2u) << 7 | (f & 4u) << 14 | (f & 8u) << 21) * 0xFFu;
+                                };
+                                w[i] = make_uint4(w[i].x & keep(0), w[i].y & keep(1), w[i].z & keep(2), w[i].w & keep(3));
                             }
-                        }
-                    } else {
-                        // unit: a dim of a page, 16 tokens
-                        const bool partial = __any_sync(FULL, seen != 0xFFFFu && lane >> 2 == (kb & 7));
-#pragma unroll 1
-                        for (int u0 = me; u0 < np * D; u0 += D) {
-                            uint4 w[D / 64];
-#pragma unroll
-                            for (int i = 0; i < D / 64; ++i) w[i] = ld_shared(from + (uint32_t)((u0 + 64 * i) * 16));
-                            if (partial)
-#pragma unroll
-                                for (int i = 0; i < D / 64; ++i) {
-                                    const uint32_t bits = __shfl_sync(FULL, seen, (kb & 7) * KB + (u0 + 64 * i) / D);
-                                    auto keep = [&](int k) {
-                                        const uint32_t f = bits >> (4 * k) & 0xFu;
-                                        return ((f & 1u) | (f & 2u) << 7 | (f & 4u) << 14 | (f & 8u) << 21) * 0xFFu;
-                                    };
-                                    w[i] = make_uint4(w[i].x & keep(0), w[i].y & keep(1), w[i].z & keep(2), w[i].w & keep(3));
-                                }
-#pragma unroll
-                            for (int i = 0; i < D / 64; ++i) {
-                                const int u = u0 + 64 * i, j = u / D, dim = u % D;
-                                uint4 x, y;
-                                convert16(w[i], x, y);
-                                st_shared(tile + (uint32_t)(j * HALF + dim * 16), x);
-                                st_shared(tile + (uint32_t)(j * HALF + (D + dim) * 16), y);
-                            }
+                            uint4 x, y;
+                            convert16(w[i], x, y);
+                            st_shared(tile + (uint32_t)(j * HALF + dim * 16), x);
+                            st_shared(tile + (uint32_t)(j * HALF + (D + dim) * 16), y);
                         }
                     }
                     fence_proxy_async();               // the tensor core reads the tile through the async proxy
                     __syncwarp();
                     if (lane == 0) {
-                        mbar_arrive(ready);
-                        mbar_arrive(empty + 8 * st);
+                        mbar_arrive(v_ready + 8 * (kb & 1));
+                        mbar_arrive(v_empty + 8 * st);
                     }
                 }
-            } else if (warp < 10) {
-                // =================== tensor-core issue: the whole warp walks along, one lane issues ===================
-                const uint64_t desc = values ? smem_desc(tile, D * 16, 128) : smem_desc(tile, 128, CH * 128);
-                if (!values) wait(q_full, 0, gave_up);
+            } else if (warp == 8) {
+                // =================== scales, and scores from the codes as they are ===================
+                const uint64_t ring_desc = smem_desc(k_ring, 128, 8 * D);
+                int page32 = page_at(lane), next32 = page_at(32 + lane);
+                wait(q_full, 0, gave_up);
                 for (int kb = 0; kb < blocks; ++kb) {
-                    const uint32_t bar = 8 * ((uint32_t)kb & 1u), turn = (uint32_t)(kb >> 1);
-                    if (!values) {
-                        if (kb >= 2) wait(pv_done + bar, (turn - 1) & 1u, gave_up);        // the buffer: P V two blocks back is over
-                        wait(ready, (uint32_t)(kb & 1), gave_up);
-                        tc_fence_after();
-                        if (leader) issue_scores(kb, desc);
-                    } else {
-                        wait(ready, (uint32_t)(kb & 1), gave_up);
-                        wait(p_ready + bar, turn & 1u, gave_up);
-                        tc_fence_after();
-                        if (leader) issue_output(kb, desc);
+                    if (kb > 0 && (kb & 7) == 0) {
+                        page32 = next32;
+                        next32 = page_at((kb + 8) * KB + lane);
                     }
-                    if (leader) tc_commit(free);
+                    const int st = kb % KS, np = listed - kb * KB < KB ? listed - kb * KB : KB;
+                    const uint32_t bar = 8 * ((uint32_t)kb & 1u), seen = bits_up_to(p1, page32);
+                    // (this slot's last scales were those of four blocks back, whose P V was over when the block before this was issued)
+                    const uint32_t from = k_ring + (uint32_t)(st * L::K_STAGE + KEYS * D), slot = scale_ring + (uint32_t)((kb & 3) * L::SCALE_STAGE);
+                    wait(k_full + 8 * st, (uint32_t)((kb / KS) & 1), gave_up);
+                    uint32_t most = 0;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        // a token's K scale into units of log2, V scale (0 where no row sees it)
+                        const int x = lane + 32 * i, j = x / PAGE, t = x % PAGE;
+                        const uint32_t bits = __shfl_sync(FULL, seen, (kb & 7) * KB + j);
+                        float ks = 0.f, vs = 0.f;
+                        if (j < np && (bits >> t & 1u)) {
+                            const uint32_t a = from + (uint32_t)((j * 2 * PAGE + t) * 4);
+                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ks) : "r"(a) : "memory");
+                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(vs) : "r"(a + PAGE * 4) : "memory");
+                        }
+                        most = max(most, __float_as_uint(vs));           // (0 or more; the bits of a NaN are above all)
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(slot + (uint32_t)(x * 4)), "f"(ks * p.scale_log2) : "memory");
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(slot + (uint32_t)((KEYS + x) * 4)), "f"(vs) : "memory");
+                    }
+                    most = __reduce_max_sync(FULL, most);
+                    if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(slot + (uint32_t)(2 * KEYS * 4)), "r"(most) : "memory");
+                    __syncwarp();
+                    if (kb >= 2) wait(pv_done + bar, (uint32_t)(((kb >> 1) - 1) & 1), gave_up);        // the buffer: P V two blocks back is over
+                    tc_fence_after();
+                    if (leader) {
+                        mbar_arrive(s_ready + bar);
+                        issue_scores(kb, ring_desc + (uint64_t)((st * L::K_STAGE) >> 4));
+                        tc_commit(k_empty + 8 * st);
+                    }
                     __syncwarp();
                 }
-                wait(free, (uint32_t)((blocks - 1) & 1), gave_up);       // the last commit arrives while the barriers are still there
+                // the last commits arrive while the barriers are still there
+                for (int j = blocks > KS ? blocks - KS : 0; j < blocks; ++j) wait(k_empty + 8 * (j % KS), (uint32_t)((j / KS) & 1), gave_up);
+            } else if (warp == 9) {
+                // =================== outputs ===================
+                const uint64_t desc = smem_desc(v_tiles, D * 16, 128);
+                for (int kb = 0; kb < blocks; ++kb) {
+                    const uint32_t bar = 8 * ((uint32_t)kb & 1u), turn = (uint32_t)(kb >> 1);
+                    wait(v_ready + bar, turn & 1u, gave_up);
+                    wait(p_ready + bar, turn & 1u, gave_up);
+                    tc_fence_after();
+                    if (leader) issue_output(kb, desc + (uint64_t)(((kb & 1) * L::TILE) >> 4));
+                    __syncwarp();
+                }
             } else {
-                // =================== copies ===================
+                // =================== copies: K and the scales, or V ===================
+                const int stages = values ? VS : KS;
+                const uint32_t ring = values ? v_ring : k_ring, stage_bytes = values ? L::V_STAGE : L::K_STAGE, full = values ? v_full : k_full,
+                               empty = values ? v_empty : k_empty;
                 int id = id_at(lane), next_id = id_at(32 + lane);        // lane 4 (kb % 8) + j has entry j of block kb
                 for (int kb = 0; kb < blocks; ++kb) {
                     if (kb > 0 && (kb & 7) == 0) {
