@@ -1453,12 +1453,18 @@ int skv_prefill_attn_pages(skv_cache *c, int layer, const void *Q, const int32_t
     const PageLists l = {lists, counts, list_stride, run, per_seq};
     const int src = c->r[(size_t)layer];
     const bool can_umma = aligned(out, 16) && prefill_pages_smem_bytes(c->head_dim, c->fp8) <= (size_t)c->max_smem_optin;
-    // Few rows, or lists of a row each: a row at a time through the decode kernel.  That reads K and V once per row instead of once per list, but
-    // spreads rows and pages over the GPU, where a list is a chain of blocks of 0.75 us on one CTA.  (us, rows / tiles, 8 kv heads of 4, by row heads: bf16
-    // pages, lists of 117 pages, 16 8.0 / 22.8, 64 14.2 / 22.9, 128 20.2 / 23.2, 256 32.9 / 23.8; of 53 pages, 128 11.7 / 13.3, 256 17.5 / 13.8.
-    // FP8 pages, 117 pages, 128 20.3 / 38.3, 256 31.1 / 39.1, 512 59.5 / 38.9; 64 sequences of two rows 113 / 107.)
-    const int per_list = run < max_q_len ? run : max_q_len;
-    const bool few_rows = per_list == 1 || (int64_t)batch * max_q_len * c->kv_heads * c->head_dim <= (c->fp8 ? 320 : 160) * 128;
+    // Lists of a row each, or few rows: a row at a time through the decode kernel.  That reads K and V once per row instead of once per
+    // list, but begins sooner and spreads over the GPU as it likes.  What either takes, in us, for `pages` of a list: by rows the pages read, of
+    // which 1150 pass in a us (FP8 1300); by tiles the longest chain of an SM, 0.19 a page.  (Rows / tiles, 8 kv heads of 4, row heads x pages,
+    // measured: bf16 pages 16 x 21 6.1 / 9.1, 256 x 21 9.2 / 9.7, 512 x 21 16.8 / 9.7, 64 x 53 9.9 / 10.7, 128 x 53 11.9 / 10.7, 32 x 117 10.1 / 11.0,
+    // 64 x 117 14.2 / 11.2, 512 x 117 58 / 13.5; 64 sequences of two rows and 117 pages 104 / 86.  FP8 pages 512 x 21 12.9 / 13.5, 128 x 53 11.3 / 14.3,
+    // 256 x 53 16.6 / 14.6, 64 x 117 13.1 / 14.8, 128 x 117 18.1 / 14.9; the 64 sequences 84 / 96.)
+    const int per_list = run < max_q_len ? run : max_q_len, most = list_stride < pt_stride ? list_stride : pt_stride;
+    const int64_t items = (int64_t)batch * per_seq * c->kv_heads;
+    const int parts = prefill_pages_parts(items, most, c->sm_count);
+    const double by_rows = 5.5 + (double)batch * max_q_len * c->kv_heads * most / (c->fp8 ? 1300 : 1150);
+    const double by_tiles = (c->fp8 ? 12 : 8.5) + 0.19 * ((most + parts - 1) / parts) * (double)((items * parts + c->sm_count - 1) / c->sm_count);
+    const bool few_rows = per_list == 1 || by_rows <= by_tiles;
     if (c->prefill_variant == 2 && !can_umma) return SKV_ERR_UNSUPPORTED;
     if (can_umma && (c->prefill_variant == 2 || (c->prefill_variant == 0 && !few_rows))) {
         PrefillParams p;
@@ -1477,7 +1483,7 @@ int skv_prefill_attn_pages(skv_cache *c, int layer, const void *Q, const int32_t
         p.pt_stride = pt_stride;
         p.scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)c->head_dim)) * 1.4426950408889634f;
         p.status = c->status_word();
-        if (launch_prefill_pages(p, l, c->head_dim, q_heads / c->kv_heads, max_q_len, c->fp8, c->tune.pdl != 0, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
+        if (launch_prefill_pages(p, l, c->head_dim, q_heads / c->kv_heads, max_q_len, c->fp8, c->sm_count, c->tune.pdl != 0, static_cast<cudaStream_t>(stream)) != cudaSuccess) {
             (void)cudaGetLastError();
             return SKV_ERR_CUDA;
         }

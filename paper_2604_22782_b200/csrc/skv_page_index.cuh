@@ -74,6 +74,7 @@ cudaError_t launch_select_pages(const SelectParams &p, int D, int sm_count, bool
 cudaError_t launch_decode_pages(const DecodeParams &p, const PageLists &l, int D, int G, int kernel, int sm_count, bool pdl, cudaStream_t s);
 // chunk attention over listed pages on the tensor cores (skv_prefill_pages.cu): min(run, max_q_len) * G <= 128
 size_t prefill_pages_smem_bytes(int D, bool fp8);
-cudaError_t launch_prefill_pages(const PrefillParams &p, const PageLists &l, int D, int G, int max_q_len, bool fp8, bool pdl, cudaStream_t s);
+int prefill_pages_parts(int64_t lists, int pages, int sm_count);         // CTAs that share a list
+cudaError_t launch_prefill_pages(const PrefillParams &p, const PageLists &l, int D, int G, int max_q_len, bool fp8, int sm_count, bool pdl, cudaStream_t s);
 
 }  // namespace skv

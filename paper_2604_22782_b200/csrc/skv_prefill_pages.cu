@@ -15,10 +15,13 @@
 // into the operand.  The tokens' scales are applied in fp32, K's to the scores and V's to the probabilities, which are taken relative to c,
 // the power of two at or above every V scale that the row has seen, so that they fit f16 whatever the scales:
 //   warps 4-7  convert V (tokens that no row sees: zero),  warp 8  scales, issues Q K^T,  9  P V,  warps 10, 11  copy K and V
+// Few lists leave SMs without one: then a cluster of CTAs shares a list, each has a part of its blocks, and their unnormalised outputs, with
+// each row's reference and sum, are joined through shared memory, every CTA some of the dims (prefill_pages_parts has the figures).
 // Operand layouts, softmax and waits are those of skv_prefill_window.cu.  Runs of one sequence and head are neighbours in the grid:
 // their lists have pages in common, which are then in L2.
 #include "skv_page_index.cuh"
 #include "skv_prefill_parts.cuh"
+#include "skv_segment.cuh"
 #include "skv_tcgen05.cuh"
 
 namespace skv {
@@ -35,6 +38,7 @@ constexpr int KEYS = KB * PAGE;
 __host__ __device__ constexpr int threads_of(bool fp8) { return fp8 ? 384 : 256; }
 constexpr int COL_O = 2 * KEYS;       // scores at columns 0 and 64, output from 128 on
 constexpr int TMEM_COLS = 256;
+constexpr int MAX_PARTS = 8;          // CTAs that may share a list
 constexpr int NO_PAGE = 0x07FFFFFF;   // no row sees a token of it
 
 // Shared memory (from a 1024-byte boundary on).  bf16: Q [D/64][128 rows][128 B] | K ring [8 groups][D/8 chunks][8 keys][16 B] | V ring
@@ -54,6 +58,19 @@ struct Layout {
     static constexpr int WORDS = BARS + 8 * N_BARS + (8 * N_BARS & 8);
     static constexpr int BYTES = 1024 + WORDS + 48;
 };
+
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 
 // 16 E4M3 codes -> two times 8 f16 (exact)
 __device__ __forceinline__ void convert16(const uint4 &w, uint4 &a, uint4 &b)
@@ -88,6 +105,64 @@ __device__ __forceinline__ uint4 ld_shared(uint32_t a)
 __device__ __forceinline__ void st_shared(uint32_t a, const uint4 &v)
 {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+// zeros where it is not there
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t a, bool there)
+{
+    float4 v;
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.f32 %0, 0f00000000;\n\tmov.f32 %1, %0;\n\tmov.f32 %2, %0;\n\tmov.f32 %3, %0;\n\t"
+                 "@p ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];\n\t}" : "=&f"(v.x), "=&f"(v.y), "=&f"(v.z), "=&f"(v.w) : "r"(a), "r"((int)there) : "memory");
+    return v;
+}
+
+// Groups [first, last) of 8 dims of this thread's row from the parts of up to N CTAs, U groups at a time.  `mine`: the row's O in this CTA's shared
+// memory, `sum` its reference and sum.
+template <int N, int U>
+__device__ __forceinline__ void join_parts(uint32_t mine, uint32_t sum, int parts, int first, int last, bool row_ok, uint16_t *dst)
+{
+    float w[N], top = -INFINITY, total = 0.f;
+    float2 ml[N];
+#pragma unroll
+    for (int c = 0; c < N; ++c) ml[c] = ld_cluster_f2(at_rank(sum, (uint32_t)(c < parts ? c : 0)));
+#pragma unroll
+    for (int c = 0; c < N; ++c)
+        if (c < parts) top = fmaxf(top, ml[c].x);
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+        w[c] = c >= parts ? 0.f : ml[c].x == top ? 1.f : ex2(ml[c].x - top);       // (1 too where all are -inf: nothing seen, or only NaN)
+        total = fmaf(w[c], c < parts ? ml[c].y : 0.f, total);
+    }
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll 1
+    for (int u0 = first; u0 < last; u0 += U) {
+        float4 x[U][N][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int c = 0; c < N; ++c)
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+                    x[u][c][half] = ld_cluster_f4(at_rank(mine, (uint32_t)(c < parts ? c : 0)) + (uint32_t)((2 * (u0 + u) + half) * ROWS * 16), c < parts && u0 + u < last);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            uint32_t y[4];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int c = 0; c < N; ++c) {
+                    a.x = fmaf(w[c], x[u][c][half].x, a.x);
+                    a.y = fmaf(w[c], x[u][c][half].y, a.y);
+                    a.z = fmaf(w[c], x[u][c][half].z, a.z);
+                    a.w = fmaf(w[c], x[u][c][half].w, a.w);
+                }
+                y[2 * half] = pack_bf16x2(a.x * inv, a.y * inv);
+                y[2 * half + 1] = pack_bf16x2(a.z * inv, a.w * inv);
+            }
+            if (row_ok && u0 + u < last) *reinterpret_cast<uint4 *>(dst + 8 * (u0 + u)) = make_uint4(y[0], y[1], y[2], y[3]);
+        }
+    }
 }
 
 // the tokens of page `page` (NO_PAGE: none) up to position pos
@@ -141,7 +216,10 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
         fence_barrier_init();
     }
     pdl_wait();
-    const int pair = (int)blockIdx.x / l.per_seq, r = (int)blockIdx.x - pair * l.per_seq, b = pair / p.Hkv, h = pair - b * p.Hkv;
+    uint32_t rank, ranks;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ranks));
+    const int index = (int)(blockIdx.x / ranks), pair = index / l.per_seq, r = index - pair * l.per_seq, b = pair / p.Hkv, h = pair - b * p.Hkv;
     const int64_t list_no = ((int64_t)b * l.per_seq + r) * p.Hkv + h;
     // The item, worked out by one warp and handed over in shared memory.
     if (warp == 4) {
@@ -158,16 +236,16 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
                 if (lane == 0) atomicOr(p.status, STATUS_BOUNDS);
             }
         }
+        if (rows > 0 && ((int64_t)listed + KEYS / PAGE - 1) / KB > (int64_t)rank) {
+            tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), TMEM_COLS);
+            tmem_relinquish();
+        }
         if (lane == 0) {
             item[0] = rows;
             item[1] = n - q_len + at;
             item[2] = n;
             item[3] = q_begin + at;
             item[4] = listed;
-        }
-        if (rows > 0 && listed > 0) {
-            tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), TMEM_COLS);
-            tmem_relinquish();
         }
     }
     tc_fence_before();
@@ -176,20 +254,30 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
     // (by a shuffle: then they are known to be the same for the warp, and what is worked out from them stays in uniform registers, from
     // which the tensor core's instructions take their operands)
     auto shared = [&](int i) { return __shfl_sync(FULL, item[i], 0); };
-    const int rows = shared(0), p0 = shared(1), p1 = p0 + rows - 1, pages = (shared(2) + PAGE - 1) / PAGE, listed = shared(4);
+    const int rows = shared(0), p0 = shared(1), p1 = p0 + rows - 1, pages = (shared(2) + PAGE - 1) / PAGE, all_listed = shared(4);
     const int64_t first_row = shared(3);
     const uint16_t *q_rows = p.Q + (first_row * p.Hq + (int64_t)h * G) * D;
     uint16_t *out_rows = p.out + (first_row * p.Hq + (int64_t)h * G) * D;
-    if (rows <= 0) return;
-    if (listed <= 0) {
-        for (int i = tid; i < rows * G * (D / 4); i += THREADS) {
+    if (rows <= 0) return;                     // (the whole cluster, here and where nothing is listed)
+    if (all_listed <= 0) {
+        for (int i = tid + (int)rank * THREADS; i < rows * G * (D / 4); i += THREADS * (int)ranks) {
             const int row = i / (D / 4), token = row / G;
             *reinterpret_cast<uint2 *>(out_rows + ((int64_t)token * p.Hq + row - token * G) * D + i % (D / 4) * 4) = make_uint2(0, 0);
         }
         return;
     }
-    const int blocks = (listed + KB - 1) / KB;
-    const int32_t *entries = l.lists + list_no * l.stride, *table = p.page_table + (int64_t)b * p.pt_stride;
+    // Each of the cluster's CTAs has a part of the list's blocks; where there are fewer of these than CTAs, the last ones have none.
+    const int all_blocks = (all_listed + KB - 1) / KB, parts = all_blocks < (int)ranks ? all_blocks : (int)ranks;
+    if ((int)rank >= parts) {
+        for (int i = 0; i < 2; ++i) {
+            cluster_arrive();
+            cluster_wait();
+        }
+        return;
+    }
+    const int from = (int)((int64_t)all_blocks * rank / parts), blocks = (int)((int64_t)all_blocks * (rank + 1) / parts) - from;
+    const int listed = all_listed - from * KB < blocks * KB ? all_listed - from * KB : blocks * KB;
+    const int32_t *entries = l.lists + list_no * l.stride + (int64_t)from * KB, *table = p.page_table + (int64_t)b * p.pt_stride;
     const uint32_t tmem = __shfl_sync(FULL, *tmem_slot, 0);
     // a listed page's number, NO_PAGE where it is none of the sequence's
     auto page_at = [&](int i) {
@@ -217,18 +305,34 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
                 const int row = warp * 32 + i * 4 + (lane >> 3), token = row / G;
                 const uint16_t *src = q_rows + ((int64_t)token * p.Hq + row - token * G) * D + c * 8;
                 const uint32_t dst = q_smem + (uint32_t)(row * 128 + ((c ^ (row & 7)) * 16));
-                if constexpr (FP8) {
+#pragma unroll
+                for (int half = 0; half < D / 64; ++half) {
+                    if (token < rows)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (uint32_t)(half * ROWS * 128)), "l"(src + half * 64) : "memory");
+                    else
+                        st_shared(dst + (uint32_t)(half * ROWS * 128), make_uint4(0, 0, 0, 0));
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            if constexpr (FP8) {
+                // a row's two terms take the place of its bf16 values
+#pragma unroll 1
+                for (int i = 0; i < 8; ++i) {
+                    const int row = warp * 32 + i * 4 + (lane >> 3);
+                    const uint32_t at = q_smem + (uint32_t)(row * 128);
                     uint4 w[D / 64];
                     uint32_t top = 0;
 #pragma unroll
                     for (int half = 0; half < D / 64; ++half) {
-                        w[half] = token < rows ? __ldg(reinterpret_cast<const uint4 *>(src + half * 64)) : make_uint4(0, 0, 0, 0);
+                        w[half] = ld_shared(at + (uint32_t)(half * ROWS * 128 + (c ^ (row & 7)) * 16));
                         const uint32_t x[4] = {w[half].x, w[half].y, w[half].z, w[half].w};
 #pragma unroll
                         for (int k = 0; k < 4; ++k) top = max(top, max(x[k] & 0x7FFFu, x[k] >> 16 & 0x7FFFu));
                     }
 #pragma unroll
                     for (int x = 1; x < 8; x <<= 1) top = max(top, __shfl_xor_sync(FULL, top, x));
+                    __syncwarp();                          // every lane has its part of the row
                     // the row's largest comes to [128, 256); both powers are normal numbers
                     const int e = min(max((int)(top >> 7) - 127, -119), 127) - 7;
                     const float out = __int_as_float((127 - e) << 23), in = __int_as_float((127 + e) << 23);
@@ -244,30 +348,20 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
                             term[0][k] = pack_e4m3x2(v[0], v[1]) | pack_e4m3x2(v[2], v[3]) << 16;
                             uint32_t a, b;
                             e4m3x4_to_f16x2(term[0][k], a, b);
-                            const float2 f = f16x2_to_f32x2(a), g2 = f16x2_to_f32x2(b);
-                            term[1][k] = pack_e4m3x2(v[0] - f.x, v[1] - f.y) | pack_e4m3x2(v[2] - g2.x, v[3] - g2.y) << 16;
+                            const float2 f = f16x2_to_f32x2(a), g = f16x2_to_f32x2(b);
+                            term[1][k] = pack_e4m3x2(v[0] - f.x, v[1] - f.y) | pack_e4m3x2(v[2] - g.x, v[3] - g.y) << 16;
                         }
 #pragma unroll
                         for (int t = 0; t < 2; ++t) {
                             const int col = t * D + half * 64 + c * 8;   // byte of the row's two terms, in tiles of 128
-                            asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(q_smem + (uint32_t)((col >> 7) * ROWS * 128 + row * 128 + (((col >> 4 & 7) ^ (row & 7)) * 16) + (col & 8))),
+                            asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(at + (uint32_t)((col >> 7) * ROWS * 128 + (((col >> 4 & 7) ^ (row & 7)) * 16) + (col & 8))),
                                          "r"(term[t][0]), "r"(term[t][1]) : "memory");
                         }
                     }
                     const float theirs = __shfl_sync(FULL, in, (lane & 3) * 8);
                     if (lane >> 2 == i) row_scale = theirs;
-                } else {
-#pragma unroll
-                    for (int half = 0; half < D / 64; ++half) {
-                        if (token < rows)
-                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (uint32_t)(half * ROWS * 128)), "l"(src + half * 64) : "memory");
-                        else
-                            st_shared(dst + (uint32_t)(half * ROWS * 128), make_uint4(0, 0, 0, 0));
-                    }
                 }
             }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
             fence_proxy_async();                           // the tensor core reads them through the async proxy
             __syncwarp();
             if (lane == 0) mbar_arrive(q_full);
@@ -308,10 +402,15 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
 #pragma unroll
                 for (int c = 0; c < KEYS; c += 4) {
                     const uint4 s = ld_shared(scales + 4 * c);
-                    raw[c / 32][c % 32] = __float_as_uint(__uint_as_float(raw[c / 32][c % 32]) * __uint_as_float(s.x));
-                    raw[c / 32][c % 32 + 1] = __float_as_uint(__uint_as_float(raw[c / 32][c % 32 + 1]) * __uint_as_float(s.y));
-                    raw[c / 32][c % 32 + 2] = __float_as_uint(__uint_as_float(raw[c / 32][c % 32 + 2]) * __uint_as_float(s.z));
-                    raw[c / 32][c % 32 + 3] = __float_as_uint(__uint_as_float(raw[c / 32][c % 32 + 3]) * __uint_as_float(s.w));
+                    const uint32_t f[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+                    for (int k = 0; k < 4; k += 2) {
+                        uint32_t &a = raw[c / 32][c % 32 + k], &b = raw[c / 32][c % 32 + k + 1];
+                        float x, y;
+                        halves(mul2(pair_of(__uint_as_float(a), __uint_as_float(b)), pair_of(__uint_as_float(f[k]), __uint_as_float(f[k + 1]))), x, y);
+                        a = __float_as_uint(x);
+                        b = __float_as_uint(y);
+                    }
                 }
                 asm volatile("ld.shared.f32 %0, [%1];" : "=f"(c_block) : "r"(scales + 2 * KEYS * 4));
             }
@@ -353,12 +452,11 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
                         e0 = ex2(e0);
                         e1 = ex2(e1);
                     }
-                    mx4[c & 3] = fmaxf(mx4[c & 3], fmaxf(s0, s1));
+                    mx4[c & 3] = max3(mx4[c & 3], s0, s1);
                     sum2[c & 1] = add2(sum2[c & 1], pair_of(e0, e1));
                     if (FP8) {
                         if (c % 2 == 0) vs = ld_shared(scales + (uint32_t)(4 * (KEYS + 2 * c)));
-                        e0 *= __uint_as_float(c % 2 == 0 ? vs.x : vs.z);
-                        e1 *= __uint_as_float(c % 2 == 0 ? vs.y : vs.w);
+                        halves(mul2(pair_of(e0, e1), pair_of(__uint_as_float(c % 2 == 0 ? vs.x : vs.z), __uint_as_float(c % 2 == 0 ? vs.y : vs.w))), e0, e1);
                     }
                     pk[c] = FP8 ? pack_f16x2(e0, e1) : pack_bf16x2(e0, e1);
                 }
@@ -401,28 +499,53 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
         }
         wait(pv_done + 8 * ((blocks - 1) & 1), (uint32_t)(((blocks - 1) >> 1) & 1), gave_up);
         tc_fence_after();
-        const float inv = l_sum == 0.f ? 0.f : 1.f / l_sum;                // (a row that sees nothing)
-        uint32_t packed[D / 2];
+        if (ranks == 1) {
+            const float inv = l_sum == 0.f ? 0.f : 1.f / l_sum;                // (a row that sees nothing)
+            uint32_t packed[D / 2];
 #pragma unroll
-        for (int q = 0; q < D / 32; ++q) {
-            uint32_t ov[32];
-            tmem_ld32(output + 32 * q, ov);
-            tmem_wait_ld();
+            for (int q = 0; q < D / 32; ++q) {
+                uint32_t ov[32];
+                tmem_ld32(output + 32 * q, ov);
+                tmem_wait_ld();
 #pragma unroll
-            for (int c = 0; c < 16; ++c) packed[16 * q + c] = pack_bf16x2(__uint_as_float(ov[2 * c]) * inv, __uint_as_float(ov[2 * c + 1]) * inv);
-        }
-        if (row_ok) {
-            uint16_t *dst = out_rows + ((int64_t)token * p.Hq + g) * D;
-            if ((reinterpret_cast<uintptr_t>(p.out) & 31) == 0) {          // whole sectors: half as many, and none written twice
-#pragma unroll
-                for (int c = 0; c < D / 2; c += 8)
-                    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + 2 * c), "r"(packed[c]), "r"(packed[c + 1]),
-                                 "r"(packed[c + 2]), "r"(packed[c + 3]), "r"(packed[c + 4]), "r"(packed[c + 5]), "r"(packed[c + 6]), "r"(packed[c + 7]) : "memory");
-            } else {
-#pragma unroll
-                for (int c = 0; c < D / 2; c += 4)
-                    *reinterpret_cast<uint4 *>(dst + 2 * c) = make_uint4(packed[c], packed[c + 1], packed[c + 2], packed[c + 3]);
+                for (int c = 0; c < 16; ++c) packed[16 * q + c] = pack_bf16x2(__uint_as_float(ov[2 * c]) * inv, __uint_as_float(ov[2 * c + 1]) * inv);
             }
+            if (row_ok) {
+                uint16_t *dst = out_rows + ((int64_t)token * p.Hq + g) * D;
+                if ((reinterpret_cast<uintptr_t>(p.out) & 31) == 0) {          // whole sectors: half as many, and none written twice
+#pragma unroll
+                    for (int c = 0; c < D / 2; c += 8)
+                        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + 2 * c), "r"(packed[c]), "r"(packed[c + 1]),
+                                     "r"(packed[c + 2]), "r"(packed[c + 3]), "r"(packed[c + 4]), "r"(packed[c + 5]), "r"(packed[c + 6]), "r"(packed[c + 7]) : "memory");
+                } else {
+#pragma unroll
+                    for (int c = 0; c < D / 2; c += 4)
+                        *reinterpret_cast<uint4 *>(dst + 2 * c) = make_uint4(packed[c], packed[c + 1], packed[c + 2], packed[c + 3]);
+                }
+            }
+        } else {
+            // O [D/4 groups][128 rows][4], then each row's reference and sum, to where the operands were; every CTA joins some of the dims
+            const uint32_t mine = q_smem + (uint32_t)(tid * 16), sums = q_smem + ROWS * D * 4;
+#pragma unroll
+            for (int q = 0; q < D / 32; ++q) {
+                uint32_t ov[32];
+                tmem_ld32(output + 32 * q, ov);
+                tmem_wait_ld();
+#pragma unroll
+                for (int c = 0; c < 8; ++c) st_shared(mine + (uint32_t)((8 * q + c) * ROWS * 16), make_uint4(ov[4 * c], ov[4 * c + 1], ov[4 * c + 2], ov[4 * c + 3]));
+            }
+            asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(sums + (uint32_t)(tid * 8)), "f"(m_used + (FP8 ? c_used : 0.f)), "f"(l_sum) : "memory");
+            __syncwarp();
+            cluster_arrive();                      // this part is complete ...
+            cluster_wait();                        // ... and so is everybody's
+            uint16_t *dst = out_rows + ((int64_t)token * p.Hq + g) * D;
+            const int first = D / 8 * (int)rank / parts, last = D / 8 * ((int)rank + 1) / parts;       // groups of 8 dims
+            if (parts <= 2) join_parts<2, 4>(mine, sums + (uint32_t)(tid * 8), parts, first, last, row_ok, dst);
+            else if (parts <= 4) join_parts<4, 2>(mine, sums + (uint32_t)(tid * 8), parts, first, last, row_ok, dst);
+            else join_parts<MAX_PARTS, 1>(mine, sums + (uint32_t)(tid * 8), parts, first, last, row_ok, dst);
+            __syncwarp();
+            cluster_arrive();                      // nobody leaves while its part is being read
+            cluster_wait();
         }
     } else {
         if (!FP8) fewer_registers<56>();
@@ -682,6 +805,13 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
             }
         }
     }
+    if (ranks > 1 && warp >= 4) {              // (the softmax warps have been there)
+        __syncwarp();
+        for (int i = 0; i < 2; ++i) {
+            cluster_arrive();
+            cluster_wait();
+        }
+    }
     // ---- common exit ----
     tc_fence_before();
     __syncthreads();
@@ -693,10 +823,11 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
 }
 
 template <int D, bool FP8>
-cudaError_t launch_t(const PrefillParams &p, const PageLists &l, int G, int max_q_len, bool pdl, cudaStream_t s)
+cudaError_t launch_t(const PrefillParams &p, const PageLists &l, int G, int max_q_len, int sm_count, bool pdl, cudaStream_t s)
 {
     const int64_t ctas = (int64_t)p.B * l.per_seq * p.Hkv;
-    if (ctas > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
+    const int ranks = prefill_pages_parts(ctas, l.stride < p.pt_stride ? l.stride : p.pt_stride, sm_count);
+    if (ctas * ranks > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
     CUtensorMap k_map = {};
     if (!FP8 && !encode_k_map(&k_map, p.layer_base, p.page_stride, p.max_pages, p.Hkv, D)) return cudaErrorNotSupported;
     auto kern = prefill_pages_kernel<D, FP8>;
@@ -704,19 +835,49 @@ cudaError_t launch_t(const PrefillParams &p, const PageLists &l, int G, int max_
     const cudaError_t e = ensure_dynamic_smem(kern, smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.gridDim = dim3((unsigned)(ctas * ranks));
     cfg.blockDim = dim3(threads_of(FP8));
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchAttribute attr[2];
+    int n = 0;
+    if (ranks > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = (unsigned)ranks;
+        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (pdl) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
     cfg.attrs = attr;
-    cfg.numAttrs = pdl ? 1 : 0;
+    cfg.numAttrs = n;
     return cudaLaunchKernelEx(&cfg, kern, p, l, k_map, G, max_q_len);
 }
 
 }  // namespace
+
+// CTAs to a list.  A list is a chain of blocks, 0.6 us each on bf16 pages and 0.9 on FP8, and few lists leave SMs without one; what a part
+// costs besides is its beginning and the joining, 5 us.  (us by CTAs to a list, 1 / 2 / 4 / 8, lists of 8 and of 32 blocks, bf16:
+//     8 lists  10.8 10.4  9.6  9.6   25.6 17.6 13.3 11.5        64 lists  11.4 11.1 13.2 26.4   31.3 22.0 20.1 33.4
+//    16        11.0 10.6  9.8 12.2   25.9 17.9 13.6 14.8       128        11.9 14.7 24.2 48.4   34.1 30.0 39.2 63.4
+//    32        11.1 10.6 10.2 14.8   26.5 18.5 14.2 17.7       192        16.3 24.5 35.8 71.8   42.0 48.7 56.5 92.3
+//  FP8, 32 lists 17.5 15.8 14.9 18.9, 40.5 27.5 20.7 23.2; 128 lists 18.4 21.1 33.9 62.5, 44.0 40.5 54.1 85.0.)  So: powers of two, of two
+// blocks a part while there is an SM for each, of eight where two share one; 8 CTAs only with two SMs for each, as clusters share a GPC.
+int prefill_pages_parts(int64_t lists, int pages, int sm_count)
+{
+    const int blocks = (pages + KB - 1) / KB;
+    int r = 1;
+    for (int next = 2; next <= MAX_PARTS; next *= 2) {
+        const int64_t ctas = lists * next;
+        const bool alone = ctas <= (next == 8 ? sm_count / 2 : sm_count);
+        if (alone ? blocks < 2 * next : next == 8 || ctas > 2 * sm_count || blocks < 8 * next) break;
+        r = next;
+    }
+    return r;
+}
 
 size_t prefill_pages_smem_bytes(int D, bool fp8)
 {
@@ -724,10 +885,10 @@ size_t prefill_pages_smem_bytes(int D, bool fp8)
     return D == 64 ? (fp8 ? Layout<64, true>::BYTES : Layout<64, false>::BYTES) : 0;
 }
 
-cudaError_t launch_prefill_pages(const PrefillParams &p, const PageLists &l, int D, int G, int max_q_len, bool fp8, bool pdl, cudaStream_t s)
+cudaError_t launch_prefill_pages(const PrefillParams &p, const PageLists &l, int D, int G, int max_q_len, bool fp8, int sm_count, bool pdl, cudaStream_t s)
 {
-    if (D == 128) return fp8 ? launch_t<128, true>(p, l, G, max_q_len, pdl, s) : launch_t<128, false>(p, l, G, max_q_len, pdl, s);
-    if (D == 64) return fp8 ? launch_t<64, true>(p, l, G, max_q_len, pdl, s) : launch_t<64, false>(p, l, G, max_q_len, pdl, s);
+    if (D == 128) return fp8 ? launch_t<128, true>(p, l, G, max_q_len, sm_count, pdl, s) : launch_t<128, false>(p, l, G, max_q_len, sm_count, pdl, s);
+    if (D == 64) return fp8 ? launch_t<64, true>(p, l, G, max_q_len, sm_count, pdl, s) : launch_t<64, false>(p, l, G, max_q_len, sm_count, pdl, s);
     return cudaErrorInvalidValue;
 }
 

@@ -33,8 +33,9 @@ def i32(x):
 
 
 def check(got, want, what):
-    """serving_reference's bounds.  A tile at a time on FP8 pages: queries are f16 times a power of two (2^-25 of the row's largest
-    element at most), probabilities times V scale over c are f16, as they are where a row is taken at a time."""
+    """serving_reference's bounds.  A tile at a time on FP8 pages: queries are two E4M3 terms times a power of two (exact, but for elements
+    below 2^-9 of the row's largest: 2^-17 of that at most), probabilities times V scale over c are f16, as they are where a row is taken at
+    a time."""
     out, size, reach, n, fp8, v_max = want
     tol = ref.attention_tolerance(out, size, reach, n, fp8, v_max)
     err = (got.double().cpu() - out).abs()
@@ -407,6 +408,39 @@ def test_chunks_over_listed_pages(hq, hkv, d, run, fp8, variant):
     p.cache.skv_prefill_attn_pages(1, q.cuda(), cu, p.table_dev, p.lens_dev, lists.cuda(), counts.cuda(), out, 150, run=run)
     check_rows(p, q, out, lists, counts, runs)
     assert p.cache.skv_get_status() == 0 and bool((held[len(q):] == 7.0).all())
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (6, 2, 64)])
+@pytest.mark.parametrize("width,batch", [(7, 1), (20, 1), (60, 9), (200, 1), (200, 9), (200, 30)])
+def test_few_lists_in_parts(hq, hkv, d, width, batch, fp8):
+    """Two, four or eight CTAs to a list, of which some have no block of it, or none that a row sees a token of."""
+    from paper_2604_22782_b200.binding import SKV_ERR_BOUNDS
+    lens = [3600 - 31 * b for b in range(batch)]
+    p = Paged(lens, hkv, d, fp8, seed=width)
+    p.cache.skv_set_prefill_variant(2)
+    q = p.rows(30 * batch, hq)
+    q[7, 1, 3] = math.nan
+    runs = chunk_runs(lens, [30] * batch, 30, 30)
+    lists, counts = some_lists(random.Random(width), [-(-n // 16) for n in lens], hkv, width)
+    counts[0, 1] = 1
+    lists[batch - 1, 0, :5], counts[batch - 1, 0] = lens[-1] // 16 - 1 + torch.tensor([0, 1, 1, 1, 1], dtype=torch.int32), 5      # first rows see only the first of them
+    out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
+    args = 0, q.cuda(), i32(range(0, 30 * batch + 1, 30)), p.table_dev, p.lens_dev, lists.cuda(), counts.cuda()
+    p.cache.skv_prefill_attn_pages(*args, out, 30, 30)
+    again = torch.empty_like(out)
+    p.cache.skv_prefill_attn_pages(*args, again, 30, 30)
+    assert torch.equal(out.view(torch.int16), again.view(torch.int16))
+    # (where the last page is full the one behind it, listed here, is none of the sequence's: left out, and reported)
+    assert p.cache.skv_get_status() == (SKV_ERR_BOUNDS if lens[-1] % 16 == 0 else 0)
+    want = torch.zeros(q.shape[:2], dtype=torch.bool)
+    want[7, 1] = any(16 * page <= runs[0][2][7] for page in lists[0, 0, :counts[0, 0]].tolist())      # (one that sees nothing gives zeros)
+    out = out.cpu()
+    assert torch.equal(torch.isnan(out).all(-1), want) and torch.equal(torch.isnan(out).any(-1), want)
+    q[7, 1] = 0.0
+    p.cache.skv_prefill_attn_pages(0, q.cuda(), *args[2:], again, 30, 30)
+    out[7, 1] = again[7, 1].cpu()                             # (that row from a call without the NaN)
+    check_rows(p, q, out, lists, counts, runs)
 
 
 @pytest.mark.parametrize("variant", [1, 2])
