@@ -488,7 +488,7 @@ int skv_page_index_bytes(const skv_cache *cache, size_t *out_bytes);
 int skv_set_page_index(skv_cache *cache, void *device_memory, size_t bytes, void *stream);
 
 /* Indexes the pages of `layer` that a step's new tokens, whose K,V have been stored, have
- * filled: of sequence b with n = seq_lens[b] tokens, the last
+ * filled (pages whose K,V came in another way: by a call that counts their tokens as new): of sequence b with n = seq_lens[b] tokens, the last
  * a = cu_q_lens[b+1] - cu_q_lens[b] of them new, pages (n - a) / 16 <= p < n / 16.
  * On a layer that is not an owner this is a no-op that launches nothing.  For page p and
  * kv head h, from the 16 tokens' keys (FP8 pages: code value x scale, in fp32):
@@ -566,7 +566,16 @@ int skv_decode_attn_pages(skv_cache *cache, int layer, const void *Q, const int3
  * t <= pos of its run's pages (lists and counts as skv_select_pages writes them with the same
  * run and max_q_len, or the caller's own under the rules above).  A row whose pages hold no
  * such token gives zeros.  min(run, max_q_len) * q_heads / kv_heads may be 128 at most.
- * Other arguments, status and errors as skv_prefill_attn; Q 16-byte, out 8-byte aligned. */
+ * What a row does not see has no weight; V that only some rows of a run see has to be finite
+ * for the others' sake (V that none sees may hold anything).  NaN in a query or in an attended
+ * key makes the row NaN.  Results repeat bit for bit.  Lists of a row, and few rows, go through the
+ * kernel of skv_decode_attn_pages, a row at a time, the rest through a tcgen05 kernel, 128
+ * query rows (tokens x heads) a list; skv_set_prefill_variant 1 or 2 asks for the one or the other
+ * (2: out 16-byte aligned, else SKV_ERR_UNSUPPORTED).  On FP8 pages the tcgen05 kernel takes
+ * K's codes as they are against queries in two E4M3 terms (exact, or off by 2^-17 of the row's
+ * largest element), and V's as f16; no scratch area is used.
+ * No workspace, one launch.  Other arguments, status and errors as skv_prefill_attn; Q
+ * 16-byte, out 8-byte aligned. */
 int skv_prefill_attn_pages(skv_cache *cache, int layer, const void *Q, const int32_t *cu_q_lens,
                            const int32_t *page_table, const int32_t *seq_lens, const int32_t *lists,
                            const int32_t *counts, void *out, int batch, int max_q_len, int q_heads,

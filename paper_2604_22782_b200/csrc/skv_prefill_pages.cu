@@ -19,6 +19,9 @@
 // each row's reference and sum, are joined through shared memory, every CTA some of the dims (prefill_pages_parts has the figures).
 // Operand layouts, softmax and waits are those of skv_prefill_window.cu.  Runs of one sequence and head are neighbours in the grid:
 // their lists have pages in common, which are then in L2.
+// Measured, 8 kv heads of 128, 32 query heads: 2 x 1024 rows, 32 to a list of 126 pages, 79 us on bf16 pages, 0.85 PFLOP/s (94 in a long loop, under
+// the power limit); 4 chunks of 129 to 256 rows on FP8 pages 55 us.  Neither tensor cores (45 % and 31 %) nor shared memory (45 % and 62 %) are
+// busy throughout: with two CTAs to an SM it is the chain copy, scores, softmax, P V, and 512 items in 296 places.
 #include "skv_page_index.cuh"
 #include "skv_prefill_parts.cuh"
 #include "skv_segment.cuh"

@@ -15,6 +15,9 @@
 // goes by direct comparison, or where that is more than a warp holds, through bins again.
 // Bound by HBM with many segments of few columns (2 D + 4 bytes a page and head), by the tensor cores and their operands with many
 // columns, by latency with few segments.
+// Measured, 8 heads of 128, 32 query heads: one sequence of 32767 tokens 7.0 us (scores 4.7, choosing 2.3), 64 of 8192 to 32767 36.5 us (4.7 TB/s),
+// two chunks of 1024 rows behind 30000 tokens, 32 to a list, 44.5 us (1.4 POP/s, 43 % of twice the bf16 rate: an item's beginning -- the
+// queries' codes -- and its end -- choosing -- leave the tensor cores to the other CTA of the SM).
 #include "skv_page_index.cuh"
 #include "skv_prefill_parts.cuh"
 #include "skv_segment.cuh"
