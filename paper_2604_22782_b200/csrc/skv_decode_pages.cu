@@ -384,16 +384,26 @@ cudaError_t launch_t(const DecodeParams &p, const PageLists &l, int G, int sm_co
         const int64_t n = segments * ways, slots = (int64_t)per_sm * sm_count;
         return (double)n / (double)((n + slots - 1) / slots * slots);
     };
-    if (f.ranks == 1 && f.warps == 4) {
-        // FP8 pages: four CTAs to an SM with a stage less, where three would leave more empty.  (us, 256 pages, three / four: 384 segments 72 / 81,
-        // 512 131 / 95, 768 142 / 168, 1024 208 / 186.)
-        if (State::PAGES == 2) {
-            if (filled(1, 4) > filled(1, 3)) f.stages = 1;
+    if (State::PAGES == 2) {
+        // FP8 pages of 128 dims are bound by issue and by the chain of a warp's steps, so warps count for more than bytes under way: as many ranks as
+        // leave all CTAs resident at once, three to an SM with two stages or, over long lists, three and a half with one (clusters of 4 and 8 share a
+        // GPC: 576 CTAs in fours do not fit 592 places, 45 us for 34); and of two to a segment a CTA of 8 warps.  (us, 256 pages, shape_of / these: 48
+        // segments 20.5 / 16.9, 64 22.0 / 19.4, 96 33.9 / 25.3, 128 34.2 / 30.5, 192 59.2 / 41.4, 256 60.0 / 51.1; 26 pages: 16 segments 8.3 / 7.1,
+        // 48 8.6 / 7.4, 256 12.2 / 11.3, but 128 8.2 / 9.4, where shape_of has as many warps.  Of 64 dims: 32 segments 9.7 / 10.2, 256 33.6 / 35.8.)
+        int r = 1;
+        for (int next = 2; D == 128 && next <= 8; next *= 2) {
+            const int64_t ctas = segments * next;
+            if (ctas <= 3 * (int64_t)sm_count ? most < 3 * next : next == 2 ? ctas > 4 * (int64_t)sm_count || most < 16 : 2 * ctas > 7 * (int64_t)sm_count || most < 128) break;
+            r = next;
+        }
+        if (4 * r > f.warps * f.ranks) f = segments * r <= 3 * (int64_t)sm_count ? Shape{4, 2, r} : r == 2 ? Shape{8, 1, 1} : Shape{4, 1, r};
+        // And with a CTA to a segment, four to an SM with a stage less, where three would leave more empty.  (us, 256 pages, three / four: 384 segments
+        // 72 / 81, 512 131 / 95, 768 142 / 168, 1024 208 / 186.)
+        if (f.ranks == 1 && f.warps == 4 && filled(1, 4) > filled(1, 3)) f.stages = 1;
+    } else if (f.ranks == 1 && f.warps == 4 && filled(2, 3) > 1.25 * filled(1, 3) && most >= 64) {
         // bf16 pages: a cluster of two to a segment, where that fills a quarter more.  (One / two: 512 segments, 128 pages 99.8 / 91.9, 256 pages
         // 195 / 169; 384 segments 67.4 / 68.2; 768 120 / 127; 1024 165 / 163.)
-        } else if (filled(2, 3) > 1.25 * filled(1, 3) && most >= 64) {
-            f.ranks = 2;
-        }
+        f.ranks = 2;
     }
     if (segments * f.ranks > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
     const size_t smem = 128 + (size_t)f.warps * f.stages * UNIT + (size_t)part_floats(G, D) * 4 + (size_t)f.warps * f.stages * 8;

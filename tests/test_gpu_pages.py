@@ -332,7 +332,7 @@ def test_decode_variants_and_scale(variant):
 
 
 @pytest.mark.parametrize("fp8", [False, True])
-@pytest.mark.parametrize("batch", [1, 2, 5, 30, 150])
+@pytest.mark.parametrize("batch", [1, 2, 5, 10, 30, 60, 150])
 def test_decode_launch_shapes(batch, fp8):
     """One segment to many: clusters of every size, long lists, warps without pages."""
     lens = [6000 if b == 0 else 200 + 37 * b % 1000 for b in range(batch)]
