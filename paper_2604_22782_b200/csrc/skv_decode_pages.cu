@@ -6,7 +6,7 @@
 // of a cluster of CTAs, as over a window (skv_decode_window.cu): the warps take the listed pages in turn through
 // rings of bulk copies of their own and the states are joined in shared memory.  Two loads stand between a warp and its first
 // page, the list's entry and the page table's: a lane has them done for a page of its own, for 32 pages ahead.
-// Measured, 8 kv heads of 128, 32 query heads: one sequence, 128 pages 7.9 us (launch, count, entry, page id, copies, cluster exchange); 32 sequences
+// Measured, 8 kv heads of 128, 32 query heads: one sequence, 128 pages 7.7 us (launch, count, entry, page id, copies, cluster exchange); 32 sequences
 // 44 us, 6.1 TB/s; 128 sequences of 256 FP8 pages 185 us, 6.0 TB/s.
 #include "skv_decode_states.cuh"
 #include "skv_page_index.cuh"
@@ -218,11 +218,14 @@ __global__ void __launch_bounds__(NW * 32, ctas_per_sm<State>(NW)) decode_pages_
     pdl_wait();
     if (EARLY) pdl_trigger();
     const int seg = (int)(blockIdx.x / ranks), slot = seg / p.Hkv, h = seg - slot * p.Hkv;
-    int b = slot, row = slot, list = slot, n;  // sequence, row of Q and out, list, tokens up to the row's own
+    // sequence, which of its rows, list; row of Q and out, tokens up to the row's own
+    const int b = CHUNK ? slot / p.max_q_len : slot, i = CHUNK ? slot - b * p.max_q_len : 0, list = CHUNK ? b * l.per_seq + i / l.run : slot;
+    int row = slot, n;
     int pages;                                 // of the sequence
+    const int64_t at = (int64_t)list * p.Hkv + h;
+    const int length = __ldg(l.counts + at);   // (with the lengths: one trip for both)
     if (CHUNK) {                               // (every exit is the whole cluster's)
-        b = slot / p.max_q_len;
-        const int i = slot - b * p.max_q_len, first = __ldg(p.cu_q + b), q_len = __ldg(p.cu_q + b + 1) - first;
+        const int first = __ldg(p.cu_q + b), q_len = __ldg(p.cu_q + b + 1) - first;
         n = __ldg(p.seq_lens + b);
         if (first < 0 || q_len < 0 || q_len > n || q_len > p.max_q_len || (int64_t)n > (int64_t)p.pt_stride * PAGE) {
             if (i == 0 && h == 0 && rank == 0 && threadIdx.x == 0) atomicOr(p.status, STATUS_BOUNDS);
@@ -232,7 +235,6 @@ __global__ void __launch_bounds__(NW * 32, ctas_per_sm<State>(NW)) decode_pages_
         pages = (n + PAGE - 1) / PAGE;
         n -= q_len - 1 - i;
         row = first + i;
-        list = b * l.per_seq + i / l.run;
     } else {
         n = __ldg(p.seq_lens + b);
         n = n > 0 ? n : 0;
@@ -242,8 +244,7 @@ __global__ void __launch_bounds__(NW * 32, ctas_per_sm<State>(NW)) decode_pages_
         }
         pages = (n + PAGE - 1) / PAGE;
     }
-    const int64_t at = (int64_t)list * p.Hkv + h;
-    int listed = n > 0 ? __ldg(l.counts + at) : 0;
+    int listed = n > 0 ? length : 0;
     if (listed > l.stride) {
         listed = l.stride;
         if (rank == 0 && threadIdx.x == 0) atomicOr(p.status, STATUS_BOUNDS);
