@@ -17,10 +17,11 @@
 //   warps 4-7  convert V (tokens that no row sees: zero),  warp 8  scales, issues Q K^T,  9  P V,  warps 10, 11  copy K and V
 // Few lists leave SMs without one: then a cluster of CTAs shares a list, each has a part of its blocks, and their unnormalised outputs, with
 // each row's reference and sum, are joined through shared memory, every CTA some of the dims (prefill_pages_parts has the figures).
-// Operand layouts, softmax and waits are those of skv_prefill_window.cu.  Runs of one sequence and head are neighbours in the grid:
+// Operand layouts, softmax and waits are those of skv_prefill_window.cu, but for its exponentials on the FMA units: here the softmax waits for
+// issue, not for the exponential's unit (every eighth pair, as there: 79.9 / 55.4 us below, none 79.3 / 54.2, every other 59.3 on FP8).  Runs of one sequence and head are neighbours in the grid:
 // their lists have pages in common, which are then in L2.
 // Measured, 8 kv heads of 128, 32 query heads: 2 x 1024 rows, 32 to a list of 126 pages, 79 us on bf16 pages, 0.85 PFLOP/s (94 in a long loop, under
-// the power limit); 4 chunks of 129 to 256 rows on FP8 pages 55 us.  Neither tensor cores (45 % and 31 %) nor shared memory (45 % and 62 %) are
+// the power limit); 4 chunks of 129 to 256 rows on FP8 pages 54 us.  Neither tensor cores (45 % and 31 %) nor shared memory (45 % and 62 %) are
 // busy throughout: with two CTAs to an SM it is the chain copy, scores, softmax, P V, and 512 items in 296 places.
 #include "skv_page_index.cuh"
 #include "skv_prefill_parts.cuh"
@@ -448,13 +449,9 @@ __global__ void __launch_bounds__(threads_of(FP8), 2) prefill_pages_kernel(const
                     const float s0 = __uint_as_float(raw[c >> 4][(2 * c) & 31]), s1 = __uint_as_float(raw[c >> 4][(2 * c + 1) & 31]);
                     const uint64_t x = fma2(pair_of(s0, s1), scale2, neg2);
                     float e0, e1;
-                    if (c % BY_FMA == BY_FMA - 1) {
-                        exp2_by_fma(x, e0, e1);
-                    } else {
-                        halves(x, e0, e1);
-                        e0 = ex2(e0);
-                        e1 = ex2(e1);
-                    }
+                    halves(x, e0, e1);
+                    e0 = ex2(e0);
+                    e1 = ex2(e1);
                     mx4[c & 3] = max3(mx4[c & 3], s0, s1);
                     sum2[c & 1] = add2(sum2[c & 1], pair_of(e0, e1));
                     if (FP8) {

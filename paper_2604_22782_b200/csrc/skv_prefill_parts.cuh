@@ -10,7 +10,6 @@ namespace skv {
 namespace chunk {
 
 constexpr float RESCALE_STEP = 8.f;   // the softmax's reference maximum moves when it has grown by more than 2^8
-constexpr int BY_FMA = 8;             // every eighth pair of exponentials is computed on the FMA units
 
 __host__ __device__ constexpr uint32_t instr_desc(int M, int N, bool b_mn_major)
 {
@@ -77,33 +76,6 @@ __device__ __forceinline__ float ex2(float x)          // (fast_exp2 without its
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
-}
-
-// 2^x of a pair on the FMA units: x = n + f with n the nearest integer, a polynomial for 2^f on [-1/2, 1/2] (least largest
-// relative error, by Remez exchange: 2.7e-6 in fp32, a thousandth of the rounding to bf16 that follows), times 2^n.
-// x is clamped to -127, whose power of two has the bits of 0: a hidden key (x = -inf) gets exactly 0, as from ex2, and its V,
-// however large, does not show.
-__device__ __forceinline__ void exp2_by_fma(uint64_t x, float &lo, float &hi)
-{
-    const float magic = 12582912.f;                    // 1.5 * 2^23: x + magic has the nearest integer in its low bits
-    float x0, x1;
-    halves(x, x0, x1);
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(x0) : "f"(x0), "f"(-127.f));
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(x1) : "f"(x1), "f"(-127.f));
-    x = pair_of(x0, x1);
-    const uint64_t r = add2(x, pair_of(magic, magic));
-    const uint64_t n = add2(r, pair_of(-magic, -magic));
-    const uint64_t f = fma2(n, pair_of(-1.f, -1.f), x);
-    uint64_t y = pair_of(0.009570102207362652f, 0.009570102207362652f);
-    y = fma2(y, f, pair_of(0.05591785907745361f, 0.05591785907745361f));
-    y = fma2(y, f, pair_of(0.240247443318367f, 0.240247443318367f));
-    y = fma2(y, f, pair_of(0.6931217908859253f, 0.6931217908859253f));
-    y = fma2(y, f, pair_of(0.9999992847442627f, 0.9999992847442627f));
-    float r0, r1;
-    halves(r, r0, r1);
-    const uint64_t power = pair_of(__int_as_float((__float_as_int(r0) << 23) + 0x3F800000), __int_as_float((__float_as_int(r1) << 23) + 0x3F800000));
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(y), "l"(power));       // (a NaN stays one)
-    halves(y, lo, hi);
 }
 
 // one lane of the warp, the same one every time
