@@ -520,6 +520,35 @@ def test_fp8_codes_of_every_value(hq, hkv, d, run, variant):
 
 
 @pytest.mark.parametrize("variant", [1, 2])
+@pytest.mark.parametrize("hq,hkv,d,run", [(8, 2, 128, 16), (6, 2, 64, 5)])
+def test_fp8_queries_of_every_size(hq, hkv, d, run, variant):
+    """Rows of zeros, rows far apart in size and elements far apart within a row.  A query element may be off by 2^-17 of the row's largest at most
+    (serving_reference counts 2^-11 of every product): 2^-17 max|q| sum|k| on a score, twice that on what it weighs."""
+    n, a = 400, 2 * run
+    p = Paged([n], hkv, d, True, seed=d)
+    p.cache.skv_set_prefill_variant(variant)
+    q = p.rows(a, hq).float()
+    q *= torch.exp2(torch.randint(-14, 1, q.shape, generator=p.g).float())
+    q *= torch.exp2(torch.tensor([-110.0, -40.0, -3.0, 0.0, 2.0])[torch.randint(0, 5, (a, hq, 1), generator=p.g)])
+    q[3] = 0.0
+    q = q.bfloat16()
+    runs = chunk_runs([n], [a], a, run)
+    lists, counts = some_lists(random.Random(run), [n // 16] * 2, hkv, 20)
+    out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
+    p.cache.skv_prefill_attn_pages(0, q.cuda(), i32([0, a]), p.table_dev, p.lens_dev, lists.cuda(), counts.cuda(), out, a, run=run)
+    group = hq // hkv
+    for i, (b, row, pos) in enumerate(runs):
+        for h in range(hkv):
+            mine = slice(row, row + len(pos)), slice(h * group, (h + 1) * group)
+            want = pages.attention(q[mine], p.k[0][:, h], p.v[0][:, h], torch.tensor(pos), lists[i, h, :counts[i, h]].tolist())
+            tol = ref.attention_tolerance(*want, 16 * int(counts[i, h]), True, float(p.v[0].double().abs().max()))
+            far = q[mine].double().abs().amax(2, keepdim=True) * p.k[0][:, h].double().abs().sum(1).max() / math.sqrt(d)
+            err = (out[mine].double().cpu() - want[0]).abs()
+            assert bool((err <= tol + 2 * 2 ** -17 * far * want[1]).all())
+    assert p.cache.skv_get_status() == 0
+
+
+@pytest.mark.parametrize("variant", [1, 2])
 @pytest.mark.parametrize("d,hkv,hq", [(128, 2, 8), (64, 2, 6)])
 def test_fp8_value_scales_far_apart(d, hkv, hq, variant):
     """V rows of zeros, V growing by 2^12 from page to page of a list and falling again, and a huge one that earlier rows must not see."""
