@@ -54,6 +54,12 @@ uint64_t skv_test_rope_phase(double inv_freq);
  * where the stack has room for `room` pages only.  Host only. */
 int64_t skv_test_release_place(int64_t before, int have, int room);
 
+/* How decode attention over listed pages (listed 1) or over a window (0) is laid
+ * out: out[0..3] = warps of a CTA, stages of a warp, CTAs of a segment, CTAs that an
+ * SM's registers hold.  kernel: 0 CUDA cores, 1 tensor cores, 2 FP8 pages.  Host
+ * only.  Errors: SKV_ERR_ARG. */
+int skv_test_decode_shape(int listed, int head_dim, int kernel, int64_t segments, int64_t pages, int sm_count, int *out);
+
 #ifdef __cplusplus
 }
 #endif

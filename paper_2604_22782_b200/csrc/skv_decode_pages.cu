@@ -184,11 +184,13 @@ struct Fp8PairState {
 };
 
 // CTAs of NW warps whose registers an SM is to hold. bf16 pages: a cluster of 16 CTAs needs two of 8 warps an SM, as a
-// GPC may have fewer than 16 SMs; the CUDA cores' state of 128 dimensions is too large for that.
+// GPC may have fewer than 16 SMs; the CUDA cores' state of 128 dimensions is too large for that, and takes no such clusters.  Of 4 warps three,
+// which shape_of counts on.  (That state with two of 4 warps an SM: 16 segments of 128 pages 14.5 us, 9.0 with three; 12 of 512, which need
+// no more than two, 14.1 and 15.6.)
 template <class State>
 constexpr int ctas_per_sm(int warps)
 {
-    return State::PAGES == 2 ? 16 / warps : sizeof(State) > 400 ? 1 : warps == 8 ? 2 : 3;
+    return State::PAGES == 2 ? 16 / warps : warps == 8 ? wide_ctas<State>() : 3;
 }
 
 // Dynamic shared memory: rings [NW][ST] units of State::PAGES blocks | the CTA's state | barriers [NW][ST]
@@ -372,13 +374,11 @@ __global__ void __launch_bounds__(NW * 32, ctas_per_sm<State>(NW)) decode_pages_
     cluster_wait();
 }
 
-template <int D, class State, bool CHUNK>
-cudaError_t launch_t(const DecodeParams &p, const PageLists &l, int G, int sm_count, bool pdl, cudaStream_t s)
+// The shape of a call of `segments`, of at most `most` listed pages each
+template <int D, class State>
+Shape pages_shape(int64_t segments, int64_t most, int sm_count)
 {
-    const int64_t segments = (int64_t)p.B * p.Hkv;
-    constexpr int UNIT = State::PAGES * State::BLOCK;
-    const int64_t most = l.stride < p.pt_stride ? l.stride : p.pt_stride;
-    Shape f = shape_of(UNIT, segments, (most + State::PAGES - 1) / State::PAGES, sm_count);
+    Shape f = shape_of(State::PAGES * State::BLOCK, segments, (most + State::PAGES - 1) / State::PAGES, sm_count, wide_ctas<State>());
     // Segments are much of a size, so with a CTA each they come in waves, of which the last may be nearly empty.  What share of the slots
     // that `ways` to cut the segments fill, in waves of 4-warp CTAs:
     auto filled = [&](int ways, int per_sm) {
@@ -406,6 +406,15 @@ cudaError_t launch_t(const DecodeParams &p, const PageLists &l, int G, int sm_co
         // 195 / 169; 384 segments 67.4 / 68.2; 768 120 / 127; 1024 165 / 163.)
         f.ranks = 2;
     }
+    return f;
+}
+
+template <int D, class State, bool CHUNK>
+cudaError_t launch_t(const DecodeParams &p, const PageLists &l, int G, int sm_count, bool pdl, cudaStream_t s)
+{
+    const int64_t segments = (int64_t)p.B * p.Hkv;
+    constexpr int UNIT = State::PAGES * State::BLOCK;
+    const Shape f = pages_shape<D, State>(segments, l.stride < p.pt_stride ? l.stride : p.pt_stride, sm_count);
     if (segments * f.ranks > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
     const size_t smem = 128 + (size_t)f.warps * f.stages * UNIT + (size_t)part_floats(G, D) * 4 + (size_t)f.warps * f.stages * 8;
     const bool early = segments * f.ranks <= sm_count;       // (as over a window: the next launch may fill the SMs that this one leaves free)
@@ -460,5 +469,27 @@ cudaError_t launch_decode_pages(const DecodeParams &p, const PageLists &l, int D
     };
     return D == 128 ? go(std::integral_constant<int, 128>()) : D == 64 ? go(std::integral_constant<int, 64>()) : cudaErrorInvalidValue;
 }
+
+#ifdef SKV_TEST_HOOKS
+void decode_pages_shape(int D, int kernel, int64_t segments, int64_t pages, int sm_count, int *out)
+{
+    auto ask = [&](auto state, auto dim) {
+        using State = typename decltype(state)::type;
+        const Shape f = pages_shape<decltype(dim)::value, State>(segments, pages, sm_count);
+        out[0] = f.warps;
+        out[1] = f.stages;
+        out[2] = f.ranks;
+        out[3] = ctas_per_sm<State>(f.warps);
+    };
+    auto go = [&](auto dim) {
+        constexpr int N = decltype(dim)::value;
+        if (kernel == 2) ask(Type<Fp8PairState<N>>(), dim);
+        else if (kernel == 1) ask(Type<ByPage<TensorCoreState<N>>>(), dim);
+        else ask(Type<ByPage<CudaCoreState<N>>>(), dim);
+    };
+    if (D == 128) go(std::integral_constant<int, 128>());
+    else go(std::integral_constant<int, 64>());
+}
+#endif
 
 }  // namespace skv

@@ -158,7 +158,7 @@ cudaError_t launch_t(const DecodeParams &p, int G, int sm_count, bool pdl, cudaS
     const int64_t segments = (int64_t)p.B * p.Hkv;
     int64_t pages = ((int64_t)p.window + PAGE - 2) / PAGE + 1 + ((int64_t)p.sinks + PAGE - 1) / PAGE;      // of a segment, at most
     if (pages > p.pt_stride) pages = p.pt_stride;
-    const Shape f = shape_of(State::BLOCK, segments, pages, sm_count);
+    const Shape f = shape_of(State::BLOCK, segments, pages, sm_count, wide_ctas<State>());
     if (segments * f.ranks > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
     const size_t smem = 128 + (size_t)f.warps * f.stages * State::BLOCK + (size_t)(f.warps + 1) * part_floats(G, D) * 4 + (size_t)f.warps * f.stages * 8;
     // The next launch may be let in at once where there is an SM for every CTA; else it would fill what this one leaves
@@ -220,5 +220,21 @@ cudaError_t launch_decode_window(const DecodeParams &p, int D, int G, int kernel
     }
     return cudaErrorInvalidValue;
 }
+
+#ifdef SKV_TEST_HOOKS
+void decode_window_shape(int D, int kernel, int64_t segments, int64_t pages, int sm_count, int *out)
+{
+    auto ask = [&](auto state) {
+        using State = typename decltype(state)::type;
+        const Shape f = shape_of(State::BLOCK, segments, pages, sm_count, wide_ctas<State>());
+        out[0] = f.warps;
+        out[1] = f.stages;
+        out[2] = f.ranks;
+        out[3] = f.warps == 8 ? wide_ctas<State>() : 2;
+    };
+    if (D == 128) kernel == 2 ? ask(Type<Fp8State<128>>()) : kernel == 1 ? ask(Type<TensorCoreState<128>>()) : ask(Type<CudaCoreState<128>>());
+    else kernel == 2 ? ask(Type<Fp8State<64>>()) : kernel == 1 ? ask(Type<TensorCoreState<64>>()) : ask(Type<CudaCoreState<64>>());
+}
+#endif
 
 }  // namespace skv

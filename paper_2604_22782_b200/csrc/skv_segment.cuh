@@ -60,10 +60,15 @@ __device__ __forceinline__ void join_states(int n_states, int head, int e2, MlOf
     }
 }
 
+// CTAs of 8 warps of it that an SM's registers hold: two, but one of the CUDA cores' state of 128 dims (128 floats a thread for queries
+// and outputs alone).
+template <class State>
+constexpr int wide_ctas() { return sizeof(State) > 400 ? 1 : 2; }
+
 // How a call is laid out: warps per CTA, pages in flight per warp, CTAs per segment.
 struct Shape { int warps, stages, ranks; };
 
-// `block` bytes per page and kv head, `segments` of at most `pages` pages.  Measured (us; rows of the sweep: segments x
+// `block` bytes per page and kv head, `segments` of at most `pages` pages; `wide`: wide_ctas of the state.  Measured (us; rows of the sweep: segments x
 // pages at 8 KB blocks; W warps, S stages, R ranks):
 //       8 x   65   W8 S1 R16  5.7   W8 S2 R8  6.0   W4 S2 R16  5.8
 //       8 x  513   W8 S1 R16 11.1   W4 S2 R16 12.2
@@ -78,8 +83,10 @@ struct Shape { int warps, stages, ranks; };
 // SM, and 4 warps with two stages (three per SM) else, as many ranks as still leave all CTAs resident at once.  A cluster's CTAs
 // share a GPC, whose SMs are not a multiple of 8: of 8 CTAs with an SM each 15 clusters run at once, and the 16th doubles the time.
 // Blocks of half the size (FP8, head_dim 64) take 8 warps in the same space, and 16 ranks of them only with an SM for each
-// (16 segments x 257 pages: 11.5 us, in clusters of 8 7.8).  A rank has at least four pages.
-inline Shape shape_of(int block, int64_t segments, int64_t pages, int sm)
+// (16 segments x 257 pages: 11.5 us, in clusters of 8 7.8).  A rank has at least four pages.  Of 8 warps of which an SM holds one CTA, clusters
+// of 16 would need 16 free SMs of one GPC each (7 run at once here, and where no GPC has as many none): these take 4 warps (8 segments x 128
+// pages 7.6 us, 12.6 to 13.2 in clusters of 16 x 8 warps).
+inline Shape shape_of(int block, int64_t segments, int64_t pages, int sm, int wide)
 {
     Shape best = {block >= 8192 ? 4 : 8, 2, 1};
     auto ranks_up_to = [&](int64_t ctas, int most) {
@@ -89,7 +96,7 @@ inline Shape shape_of(int block, int64_t segments, int64_t pages, int sm)
     };
     best.ranks = ranks_up_to(2 * (int64_t)sm + sm / 4, block >= 8192 || 16 * segments <= sm ? MAX_RANKS : 8);
     if (block >= 8192) {
-        const int r = ranks_up_to(sm, MAX_RANKS);
+        const int r = ranks_up_to(sm, wide > 1 ? MAX_RANKS : 8);
         const int64_t room = r == 8 ? 3 * (int64_t)sm / 4 : r == 4 ? 7 * (int64_t)sm / 8 : sm;
         const bool fills = 4 * segments * r >= 3 * (int64_t)sm && segments * r <= room;
         if (fills) best = {8, r > 8 ? 1 : 2, r};             // (a cluster of 16 needs two CTAs to an SM: a GPC may not have 16 SMs)
@@ -98,5 +105,13 @@ inline Shape shape_of(int block, int64_t segments, int64_t pages, int sm)
     if (per_warp < best.stages) best.stages = 1;
     return best;
 }
+
+#ifdef SKV_TEST_HOOKS
+template <class T>
+struct Type { using type = T; };
+// {warps, stages, ranks, CTAs of it that an SM's registers hold} of a call; kernel as in launch_decode_splitk
+void decode_pages_shape(int D, int kernel, int64_t segments, int64_t pages, int sm_count, int *out);
+void decode_window_shape(int D, int kernel, int64_t segments, int64_t pages, int sm_count, int *out);
+#endif
 
 }  // namespace skv

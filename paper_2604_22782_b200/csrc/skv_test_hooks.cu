@@ -3,6 +3,7 @@
 #ifdef SKV_TEST_HOOKS
 #include "../../include/skv_test_hooks.h"
 #include "skv_common.cuh"
+#include "skv_segment.cuh"
 
 namespace {
 
@@ -90,5 +91,12 @@ extern "C" int64_t skv_test_release_place(int64_t before, int have, int room)
 {
     const uint32_t k = skv::release_next(skv::release_start(before, (uint32_t)room), have, (uint32_t)room);
     return k < (uint32_t)room ? (int64_t)k : -1;
+}
+
+extern "C" int skv_test_decode_shape(int listed, int head_dim, int kernel, int64_t segments, int64_t pages, int sm_count, int *out)
+{
+    if ((head_dim != 64 && head_dim != 128) || kernel < 0 || kernel > 2 || segments < 1 || pages < 1 || sm_count < 1 || !out) return SKV_ERR_ARG;
+    (listed ? skv::decode_pages_shape : skv::decode_window_shape)(head_dim, kernel, segments, pages, sm_count, out);
+    return SKV_OK;
 }
 #endif  // SKV_TEST_HOOKS
