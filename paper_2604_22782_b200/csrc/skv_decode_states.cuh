@@ -320,8 +320,9 @@ struct Fp8State {
         }
         amax = fmaxf(amax, __shfl_xor_sync(FULL, amax, 1));
         amax = fmaxf(amax, __shfl_xor_sync(FULL, amax, 2));
-        qmax = amax;
-        const float inv = amax > 0.f ? 1.f / amax : 0.f;
+        // (of a row whose largest is below 2^-126 that is taken for it: the reciprocal of 2^-128 is not finite)
+        qmax = amax > 0.f ? fmaxf(amax, 1.17549435e-38f) : 0.f;
+        const float inv = qmax > 0.f ? 1.f / qmax : 0.f;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             qa[ks][0] = pack_f16x2(q[4 * ks] * inv, q[4 * ks + 1] * inv);
