@@ -370,6 +370,9 @@ __global__ void __launch_bounds__(128, 2) prefill_fp8_kernel(PrefillParams p, in
         qmax_lo = fmaxf(qmax_lo, __shfl_xor_sync(FULL, qmax_lo, 2));
         qmax_hi = fmaxf(qmax_hi, __shfl_xor_sync(FULL, qmax_hi, 1));
         qmax_hi = fmaxf(qmax_hi, __shfl_xor_sync(FULL, qmax_hi, 2));
+        // (of a row whose largest is below 2^-126 that is taken for it: the reciprocal of 2^-128 is not finite)
+        qmax_lo = qmax_lo > 0.f ? fmaxf(qmax_lo, 1.17549435e-38f) : 0.f;
+        qmax_hi = qmax_hi > 0.f ? fmaxf(qmax_hi, 1.17549435e-38f) : 0.f;
         const float il = qmax_lo > 0.f ? 1.f / qmax_lo : 0.f, ih = qmax_hi > 0.f ? 1.f / qmax_hi : 0.f;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {

@@ -4,6 +4,8 @@ import random
 import pytest
 import torch
 
+import pages_reference as pages
+import serving_reference as ref
 from test_gpu_pages import check_rows, chunk_runs, i32, some_lists
 from test_gpu_window import Paged
 
@@ -55,4 +57,29 @@ def test_fp8_chunks_of_queries_next_to_nothing(hq, hkv, d, run, variant):
     out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
     p.cache.skv_prefill_attn_pages(0, q.cuda(), i32([0, a]), p.table_dev, p.lens_dev, lists.cuda(), counts.cuda(), out, a, run=run)
     check_rows(p, q, out, lists, counts, runs)
+    assert p.cache.skv_get_status() == 0
+
+
+@pytest.mark.parametrize("scratch", [False, True])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (6, 2, 64)])
+def test_fp8_prefill_of_queries_next_to_nothing(hq, hkv, d, scratch):
+    """Every page, and every page that a window reaches.  With a scratch area the values are rounded to bf16 there (2^-8 of each: 2^-8 sum w |v|) and
+    the probabilities are bf16; keys are as well, which scores next to nothing do not hear."""
+    n, a = 400, 40
+    p = Paged([n], hkv, d, True, seed=d)
+    if scratch:
+        p.cache.skv_set_prefill_scratch(torch.empty(p.cache.skv_prefill_scratch_bytes(), dtype=torch.uint8, device="cuda"))
+    q = tiny_queries(a, hq, d, p.g)
+    pos, group = torch.arange(n - a, n), hq // hkv
+    for window in (None, 100000):
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
+        if window is None:
+            p.cache.skv_prefill_attn(0, q.cuda(), i32([0, a]), p.table_dev, p.lens_dev, out, a)
+        else:
+            p.cache.skv_prefill_attn_window(0, q.cuda(), i32([0, a]), p.table_dev, p.lens_dev, out, a, window)
+        for h in range(hkv):
+            mine = slice(None), slice(h * group, (h + 1) * group)
+            want = pages.attention(q[mine], p.k[0][:, h], p.v[0][:, h], pos, list(range(n // 16)))
+            tol = ref.attention_tolerance(*want, n, not scratch, float(p.v[0].abs().max())) + (want[1] * 2 ** -8 if scratch else 0.0)
+            assert bool(((out[mine].double().cpu() - want[0]).abs() <= tol).all()), (window, h)
     assert p.cache.skv_get_status() == 0
