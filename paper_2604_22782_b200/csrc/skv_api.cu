@@ -1345,7 +1345,7 @@ int skv_index_pages(skv_cache *c, int layer, const int32_t *page_table, const in
     if (!c || !c->pool) return SKV_ERR_ARG;
     if (layer < 0 || layer >= c->n_layers) return SKV_ERR_LAYER;
     if (c->slot[(size_t)layer] < 0) return SKV_OK;               // a layer that keeps no K,V has no index of its own
-    if (!c->page_index || !page_table || !seq_lens || batch <= 0 || max_q_len <= 0 || pt_stride <= 0) return SKV_ERR_ARG;
+    if (!c->page_index || !page_table || !seq_lens || batch <= 0 || (cu_q_lens && max_q_len <= 0) || pt_stride <= 0) return SKV_ERR_ARG;
     IndexParams p;
     p.layer_base = c->layer_base(c->slot[(size_t)layer]);
     p.page_stride = (int64_t)c->page_bytes;
