@@ -573,7 +573,10 @@ int skv_decode_attn_pages(skv_cache *cache, int layer, const void *Q, const int3
  * query rows (tokens x heads) a list; skv_set_prefill_variant 1 or 2 asks for the one or the other
  * (2: out 16-byte aligned, else SKV_ERR_UNSUPPORTED).  On FP8 pages the tcgen05 kernel takes
  * K's codes as they are against queries in two E4M3 terms (exact, or off by 2^-17 of the row's
- * largest element), and V's as f16; no scratch area is used.
+ * largest element), and V's as f16; no scratch area is used.  The sums of weights times V are
+ * fp32, relative to a row's largest weight, as in every attention call: |V| times the tokens of
+ * a row's list has to stay below 2^120.  V rows on FP8 pages whose largest element is below 2^-91
+ * lose bits in that kernel: its probabilities times V's scale are held relative to 2^-100 or more.
  * No workspace, one launch.  Other arguments, status and errors as skv_prefill_attn; Q
  * 16-byte, out 8-byte aligned. */
 int skv_prefill_attn_pages(skv_cache *cache, int layer, const void *Q, const int32_t *cu_q_lens,
