@@ -6,6 +6,9 @@
 // of a cluster of CTAs, as over a window (skv_decode_window.cu): the warps take the listed pages in turn through
 // rings of bulk copies of their own and the states are joined in shared memory.  Two loads stand between a warp and its first
 // page, the list's entry and the page table's: a lane has them done for a page of its own, for 32 pages ahead.
+// Probabilities: fp32 on the CUDA cores; on the tensor cores, whose operands are of V's type, two bf16 terms, the second in the half of the instruction's
+// rows that the heads leave empty, at 0 to 2 % of the time (one term: 2^-8 of every weight, which showed beside the result's own rounding);
+// on FP8 pages f16 relative to a power of two, 2^-11 of a weight.
 // Measured, 8 kv heads of 128, 32 query heads: one sequence, 128 pages 7.7 us (launch, count, entry, page id, copies, cluster exchange); 32 sequences
 // 44 us, 6.1 TB/s; 128 sequences of 256 FP8 pages 185 us, 6.0 TB/s.
 #include "skv_decode_states.cuh"
@@ -464,7 +467,7 @@ cudaError_t launch_decode_pages(const DecodeParams &p, const PageLists &l, int D
     auto go = [&](auto dim) {
         constexpr int N = decltype(dim)::value;
         if (kernel == 2) return p.cu_q ? launch_t<N, Fp8PairState<N>, true>(p, l, G, sm_count, pdl, s) : launch_t<N, Fp8PairState<N>, false>(p, l, G, sm_count, pdl, s);
-        if (kernel == 1) return p.cu_q ? launch_t<N, ByPage<TensorCoreState<N>>, true>(p, l, G, sm_count, pdl, s) : launch_t<N, ByPage<TensorCoreState<N>>, false>(p, l, G, sm_count, pdl, s);
+        if (kernel == 1) return p.cu_q ? launch_t<N, ByPage<TensorCoreState<N, true>>, true>(p, l, G, sm_count, pdl, s) : launch_t<N, ByPage<TensorCoreState<N, true>>, false>(p, l, G, sm_count, pdl, s);
         return p.cu_q ? launch_t<N, ByPage<CudaCoreState<N>>, true>(p, l, G, sm_count, pdl, s) : launch_t<N, ByPage<CudaCoreState<N>>, false>(p, l, G, sm_count, pdl, s);
     };
     return D == 128 ? go(std::integral_constant<int, 128>()) : D == 64 ? go(std::integral_constant<int, 64>()) : cudaErrorInvalidValue;
@@ -484,7 +487,7 @@ void decode_pages_shape(int D, int kernel, int64_t segments, int64_t pages, int 
     auto go = [&](auto dim) {
         constexpr int N = decltype(dim)::value;
         if (kernel == 2) ask(Type<Fp8PairState<N>>(), dim);
-        else if (kernel == 1) ask(Type<ByPage<TensorCoreState<N>>>(), dim);
+        else if (kernel == 1) ask(Type<ByPage<TensorCoreState<N, true>>>(), dim);
         else ask(Type<ByPage<CudaCoreState<N>>>(), dim);
     };
     if (D == 128) go(std::integral_constant<int, 128>());

@@ -20,9 +20,10 @@ constexpr int WIN = 128;   // page ids a warp keeps in registers (4 per lane)
 // Per-warp compute state, tensor-core variant: the G query heads of one kv head
 // are rows of a 16-row A operand (rows >= G are zero), one page is 16 key
 // columns.  S = Q K^T  (m16 n16 k D) and  O += P V  (m16 n D k16) with
-// mma.m16n8k16; softmax runs on the accumulator fragment in fp32.
+// mma.m16n8k16; softmax runs on the accumulator fragment in fp32.  V is bf16, and both operands of the instruction are of one type: P is
+// rounded to bf16, or with FINE is the sum of two bf16 numbers (2^-17 of it is lost), of which the second takes the rows 8 .. 15.
 // ---------------------------------------------------------------------------
-template <int D>
+template <int D, bool FINE = false>
 struct TensorCoreState {
     static constexpr int BLOCK = block_bytes(D);   // bytes of one (page, kv head) block
     static constexpr int MAX_CTA_CONSUMERS = 8;    // consumer warps of the CTA-per-range kernel that the registers allow
@@ -108,6 +109,8 @@ struct TensorCoreState {
         l = l * alpha + ((p0 + p1) + (p2 + p3));
         m = m_new;
         const uint32_t pa0 = pack_bf16x2(p0, p1), pa2 = pack_bf16x2(p2, p3);
+        // (what bf16 does not hold of them; of infinity or NaN NaN)
+        const uint32_t pa1 = FINE ? pack_bf16x2(p0 - bf16_lo(pa0), p1 - bf16_hi(pa0)) : 0u, pa3 = FINE ? pack_bf16x2(p2 - bf16_lo(pa2), p3 - bf16_hi(pa2)) : 0u;
         // V fragments (transposed): matrices (chunk nd | nd+1) x (tokens 0-7 | 8-15)
         const uint32_t v_lane = sV + (uint32_t)(((lane >> 4) * PAGE + ((lane >> 3) & 1) * 8 + (lane & 7)) * 16);
 #pragma unroll
@@ -116,8 +119,12 @@ struct TensorCoreState {
             ldmatrix_x4_trans(v_lane + (uint32_t)(j * 2 * PAGE * 16), r0, r1, r2, r3);
             o[2 * j][0] *= alpha; o[2 * j][1] *= alpha;
             o[2 * j + 1][0] *= alpha; o[2 * j + 1][1] *= alpha;
-            mma_bf16_16816(o[2 * j], pa0, 0u, pa2, 0u, r0, r1);
-            mma_bf16_16816(o[2 * j + 1], pa0, 0u, pa2, 0u, r2, r3);
+            if (FINE) {
+                o[2 * j][2] *= alpha; o[2 * j][3] *= alpha;
+                o[2 * j + 1][2] *= alpha; o[2 * j + 1][3] *= alpha;
+            }
+            mma_bf16_16816(o[2 * j], pa0, pa1, pa2, pa3, r0, r1);
+            mma_bf16_16816(o[2 * j + 1], pa0, pa1, pa2, pa3, r2, r3);
         }
     }
 
@@ -130,7 +137,12 @@ struct TensorCoreState {
         if (g < G) {
             float *po = part_o + (slot * G + g) * D + 2 * tig;
 #pragma unroll
-            for (int i = 0; i < D / 8; ++i) *reinterpret_cast<float2 *>(po + 8 * i) = make_float2(o[i][0], o[i][1]);
+            for (int i = 0; i < D / 8; ++i) {
+                // (an infinite V: the second term has 0 times it, or both signs of it, and the first has what the sum is)
+                if (FINE && fabsf(o[i][2]) < INFINITY) o[i][0] += o[i][2];
+                if (FINE && fabsf(o[i][3]) < INFINITY) o[i][1] += o[i][3];
+                *reinterpret_cast<float2 *>(po + 8 * i) = make_float2(o[i][0], o[i][1]);
+            }
             if (tig == 0) *reinterpret_cast<float2 *>(part_ml + (slot * G + g) * 2) = make_float2(m, l);
         }
     }

@@ -15,6 +15,9 @@
 // into the operand.  The tokens' scales are applied in fp32, K's to the scores and V's to the probabilities, which are taken relative to c,
 // the power of two at or above every V scale that the row has seen, so that they fit f16 whatever the scales:
 //   warps 4-7  convert V (tokens that no row sees: zero),  warp 8  scales, issues Q K^T,  9  P V,  warps 10, 11  copy K and V
+// On bf16 pages probabilities are bf16, as both operands of the instruction are of V's type: 2^-8 of a weight at most, as in the other bf16 chunk
+// kernels.  (A second term for the rest, as skv_decode_pages.cu has it, is not free here: half as much again for the tensor cores, and five
+// instructions a pair for a softmax that waits for issue.)  Sums and references are fp32.
 // Few lists leave SMs without one: then a cluster of CTAs shares a list, each has a part of its blocks, and their unnormalised outputs, with
 // each row's reference and sum, are joined through shared memory, every CTA some of the dims (prefill_pages_parts has the figures).
 // Operand layouts, softmax and waits are those of skv_prefill_window.cu, but for its exponentials on the FMA units: here the softmax waits for
