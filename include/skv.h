@@ -527,8 +527,9 @@ int skv_page_list_width(int top, int first_pages, int last_pages, int run, int *
  *   score(p) = dot(p) * scale_p   (one fp32 product of a whole number below 2^24; scale
  *   +inf: +inf),
  * which is, up to the rounding to steps, the largest score that any key inside the page's bounds
- * could give any of the rows.  The lists do not depend on how the work is cut: they
- * repeat bit for bit.
+ * could give any of the rows.  (The step is the run's: rows and heads that are small beside its
+ * largest element have few steps, and less of a say.)  The lists do not depend on how the work is
+ * cut: they repeat bit for bit.
  *   Q          device bf16 [n_q][q_heads][head_dim], 16-byte aligned
  *   cu_q_lens  as in skv_prefill_attn; NULL: one row per sequence, at seq_lens[b] - 1
  *              (max_q_len and run must be 1; a length of 0 gives an empty list)
@@ -538,7 +539,8 @@ int skv_page_list_width(int top, int first_pages, int last_pages, int run, int *
  *              sequence has no rows for
  *   list_stride  at least the smaller of skv_page_list_width and pt_stride
  * min(run, max_q_len) * q_heads / kv_heads may be 128 at most, pt_stride 45056, or 28672
- * where that product is above 16 (SKV_ERR_UNSUPPORTED).  A sequence that does not fit raises SKV_ERR_BOUNDS and gets
+ * where that product is above 16 (SKV_ERR_UNSUPPORTED); shared memory is taken by pt_stride, so a
+ * table no wider than the sequences need is the quicker one (above 16, from 3968 entries on).  A sequence that does not fit raises SKV_ERR_BOUNDS and gets
  * empty lists, or without cu_q_lens is cut to pt_stride pages; so does a page id out of
  * range (the page is scored as page 0).  One launch.  Errors as skv_decode_attn, and
  * SKV_ERR_ARG without an index. */

@@ -1455,7 +1455,10 @@ int skv_prefill_attn_pages(skv_cache *c, int layer, const void *Q, const int32_t
     const bool can_umma = aligned(out, 16) && prefill_pages_smem_bytes(c->head_dim, c->fp8) <= (size_t)c->max_smem_optin;
     // Lists of a row each, or few rows: a row at a time through the decode kernel.  That reads K and V once per row instead of once per
     // list, but begins sooner and spreads over the GPU as it likes.  What either takes, in us, for `pages` of a list: by rows the pages read, of
-    // which 1150 pass in a us (FP8 1300); by tiles the longest chain of an SM, 0.19 a page.  (Rows / tiles, 8 kv heads of 4, row heads x pages,
+    // which 1150 pass in a us (FP8 1300); by tiles the longest chain of an SM, 0.19 a page.  The constants are those of 128 dims; of 64
+    // dims, of ragged chunks, whose rows count as max_q_len, and where an SM has two CTAs, whose chains overlap, both estimates are too long, by up to 1.9 times.
+    // Which is the lesser they still tell: of 140 calls (64 and 128 dims, 1 to 8 query heads a kv head, 1 to 1536 items, either type) 132 went the quicker way or
+    // one less than a tenth slower; the worst took 14.1 us for 10.6 (FP8 pages of 64 dims, 64 lists of 4 rows and 64 pages).  (Rows / tiles, 8 kv heads of 4, row heads x pages,
     // measured: bf16 pages 16 x 21 6.1 / 9.1, 256 x 21 9.2 / 9.7, 512 x 21 16.8 / 9.7, 64 x 53 9.9 / 10.7, 128 x 53 11.9 / 10.7, 32 x 117 10.1 / 11.0,
     // 64 x 117 14.2 / 11.2, 512 x 117 58 / 13.5; 64 sequences of two rows and 117 pages 104 / 86.  FP8 pages 512 x 21 12.9 / 13.5, 128 x 53 11.3 / 14.3,
     // 256 x 53 16.6 / 14.6, 64 x 117 13.1 / 14.8, 128 x 117 18.1 / 14.9; the 64 sequences 84 / 96.)

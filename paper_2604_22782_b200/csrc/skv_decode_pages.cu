@@ -9,8 +9,9 @@
 // Probabilities: fp32 on the CUDA cores; on the tensor cores, whose operands are of V's type, two bf16 terms, the second in the half of the instruction's
 // rows that the heads leave empty, at 0 to 2 % of the time (one term: 2^-8 of every weight, which showed beside the result's own rounding);
 // on FP8 pages f16 relative to a power of two, 2^-11 of a weight.
-// Measured, 8 kv heads of 128, 32 query heads: one sequence, 128 pages 7.7 us (launch, count, entry, page id, copies, cluster exchange); 32 sequences
-// 44 us, 6.1 TB/s; 128 sequences of 256 FP8 pages 185 us, 6.0 TB/s.
+// Measured, 8 kv heads of 128, 32 query heads: one sequence, 128 pages 7.5 us (launch, count, entry, page id, copies, cluster exchange); 32 sequences
+// 44.6 us, 6.0 TB/s; 128 sequences of 256 FP8 pages 185 us, 6.0 TB/s (198 in a long loop, at the clocks that the power limit leaves).
+// Registers: of 128 dims the 8-warp form has 128 and spills some 50 to 130 bytes, FP8 pages some 40 (two and four CTAs to an SM count for more).
 #include "skv_decode_states.cuh"
 #include "skv_page_index.cuh"
 #include "skv_segment.cuh"

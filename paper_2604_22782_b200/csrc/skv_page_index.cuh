@@ -18,7 +18,7 @@ __host__ __device__ inline int64_t index_layer_bytes(int64_t max_pages, int Hkv,
 
 // Rows of a run, of which `left` are there.  As an instruction of its own: written as a comparison, the lesser of the two came out as
 // run in kernels that take it from a __grid_constant__ parameter (nvcc 12.9.86, whole kernels only, not where the value was also printed), and
-// rows behind the last were read and written.
+// rows behind the last were read and written.  No small kernel shows it, so that its cause is not known; the tests' guard rows hold it down.
 __device__ __forceinline__ int rows_of_run(int left, int run)
 {
     int r;

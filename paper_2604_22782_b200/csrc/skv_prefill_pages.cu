@@ -23,8 +23,8 @@
 // Operand layouts, softmax and waits are those of skv_prefill_window.cu, but for its exponentials on the FMA units: here the softmax waits for
 // issue, not for the exponential's unit (every eighth pair, as there: 79.9 / 55.4 us below, none 79.3 / 54.2, every other 59.3 on FP8).  Runs of one sequence and head are neighbours in the grid:
 // their lists have pages in common, which are then in L2.
-// Measured, 8 kv heads of 128, 32 query heads: 2 x 1024 rows, 32 to a list of 126 pages, 79 us on bf16 pages, 0.85 PFLOP/s (96 in a long loop, under
-// the power limit); 4 chunks of 129 to 256 rows on FP8 pages 54 us.  Neither tensor cores (45 % and 31 %) nor shared memory (45 % and 62 %) are
+// Measured, 8 kv heads of 128, 32 query heads: 2 x 1024 rows, 32 to a list of 126 pages, 79 us on bf16 pages, 0.85 PFLOP/s, in short loops (90 to 96, 0.72,
+// in long ones, under the power limit); 4 chunks of 129 to 256 rows on FP8 pages 54 us.  Neither tensor cores (45 % and 31 %) nor shared memory (45 % and 62 %) are
 // busy throughout: with two CTAs to an SM it is the chain copy, scores, softmax, P V, and 512 items in 296 places.
 #include "skv_page_index.cuh"
 #include "skv_prefill_parts.cuh"

@@ -13,6 +13,8 @@
 // select_many_kernel, tcgen05 (kind i8), tiles of 128 pages against all columns, whose scores a thread per page reduces.
 // The CTA then finds the top-th largest score by counting into 2048 bins between lowest and highest; what lies in the bin where it is
 // goes by direct comparison, or where that is more than a warp holds, through bins again.
+// The scores' room in shared memory is that of the page table's width, not of the sequences: select_many_kernel's two CTAs fit an SM up to 3968 entries
+// at 128 columns of 128 dims, and one where a table is wider.
 // Bound by HBM with many segments of few columns (2 D + 4 bytes a page and head), by the tensor cores and their operands with many
 // columns, by latency with few segments.
 // Measured, 8 heads of 128, 32 query heads: one sequence of 32767 tokens 7.0 us (scores 4.7, choosing 2.3), 64 of 8192 to 32767 36.5 us (4.7 TB/s),
